@@ -54,6 +54,7 @@ enum {
     TIDAL_ERR_TIMEOUT = -5,       /* reserved: a bounded device-side wait expired (no kernel waits on another) */
     TIDAL_ERR_INDEX = -6,         /* device saw a token index or page id out of range */
     TIDAL_ERR_TOO_LARGE = -7,     /* tidal_sparse_attn_noalloc only: problem exceeds its fixed scratch */
+    TIDAL_ERR_PAGES = -9,         /* tidal_page_map: the request does not fit its arrays or the pool (nothing was changed) */
     TIDAL_ERR_INTERNAL = -8       /* a kernel found the host's launch plan inconsistent: a bug, results invalid */
 };
 
@@ -277,8 +278,89 @@ tidal_status_t tidal_sparse_attn_noalloc(const tidal_kv_t *kv, const void *q, co
                                          const int32_t *idx_count, int32_t k, int32_t num_index_heads,
                                          float *out, void *stream);
 
+/* ---- Paged caches filled on the device ------------------------------------------------------------ */
+
+/* Page tables and slot maps from request lengths, for a pool of pages of 16 positions. Every sequence goes from old_lens[b]
+ * to new_lens[b] cached tokens (device int32 [batch], batch <= 4096, each in 0 .. 16 * max_pages_per_seq <= 262144): one
+ * that grows takes pages, one that shrinks (new_lens[b] = 0: it has ended) gives its last ones back.
+ *   free_pages     device int32 [num_pages], a stack of free page ids whose first *num_free entries count. The pages given
+ *                  back are pushed in the order (sequence, logical page), then the growing sequences pop theirs in
+ *                  the same order, so a page given back can be taken again in the same call. A page must not be
+ *                  shared by two sequences when one of them gives it back.
+ *   num_free       device int32, read; num_free_out, device int32, receives the new count (may be the same word).
+ *   page_table     device int32 [batch, max_pages_per_seq]: entries P(old) .. P(new) - 1 of growing sequences are written
+ *                  (P(x) = ceil(x / 16)), no others.
+ *   slots          device int64 [max_tokens]: the new tokens of all sequences one after the other (sequence b's positions
+ *                  old_lens[b] .. new_lens[b] - 1), token at position p of sequence b at slot page * 16 + p % 16;
+ *                  entries behind the last token are -1, so that a write of max_tokens rows skips them.
+ *   positions      device int32 [max_tokens] or NULL: p of every token, -1 behind the last.
+ *   token_offsets  device int32 [batch + 1] or NULL: where each sequence's tokens start in slots; the total last.
+ * A request that cannot be met as a whole (a length out of range, more than max_tokens tokens, more pages than are free,
+ * *num_free outside 0 .. num_pages, a page id given back that is outside the pool, a stack that would pass num_pages)
+ * changes neither page_table nor free_pages: num_free_out receives *num_free, every slot and position is -1, every offset
+ * 0, and tidal_device_status reports TIDAL_ERR_PAGES. A page id outside the pool in a table or on the stack
+ * gives its tokens slot -1 and reports TIDAL_ERR_INDEX. No arrays may overlap (but the two counts). */
+tidal_status_t tidal_page_map(tidal_ctx_t *ctx, int32_t batch, const int32_t *old_lens, const int32_t *new_lens,
+                              int32_t *page_table, int32_t max_pages_per_seq, int32_t num_pages, int32_t *free_pages,
+                              const int32_t *num_free, int32_t *num_free_out, int32_t max_tokens, int64_t *slots,
+                              int32_t *positions, int32_t *token_offsets, void *stream);
+
+/* The rows of num_tokens tokens into one layer's cache, through a slot map: k_new, v_new device bf16, token t's rows
+ * [num_kv_heads, head_dim] contiguous at t * k_stride / t * v_stride elements (multiples of 8; the bases 16-byte aligned),
+ * so they may be slices of a fused projection's output. slots: device int64 [num_tokens]; paged caches: page * 16 + place
+ * (tidal_page_map), contiguous ones: sequence * max_ctx_len + position. -1 is skipped; any other slot outside
+ * the cache is skipped and reported as TIDAL_ERR_INDEX. If a slot is named twice, which of its rows stays is
+ * not specified. An FP8 cache receives E4M3 codes: x / k_scale[g] (fp32 quotient; v_scale for values) rounded to
+ * the nearest code, ties to even, saturated at +-448, NaN kept. The cache is WRITTEN although the descriptor declares it
+ * const; ctx_lens and page_table are not read. */
+tidal_status_t tidal_kv_write(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t num_tokens, const void *k_new, const void *v_new,
+                              int64_t k_stride, int64_t v_stride, const int64_t *slots, void *stream);
+
+/* ---- Block-sparse attention --------------------------------------------------------------------------
+ * A coarser and cheaper selection than tidal_select_attn: blocks of 16 consecutive positions (one page) are
+ * ranked by an upper bound of their logits, computed from 512 bytes per block and KV head instead of the
+ * block's keys, and attention reads the chosen blocks whole. Sequences of length 0 are allowed here: they choose no
+ * block and their output is zero. */
+
+/* Key bounds of blocks: for block i of sequence b and KV head g the channelwise least and greatest key over the cached
+ * positions of the block (positions at and beyond ctx_lens[b] do not count), as bf16 (exact; for an FP8 cache
+ * of the codes' values without the scale), NaN where a key is NaN.
+ *   bounds  device bf16, 16-byte aligned; contiguous caches [batch, num_kv_heads, bound_blocks, 2, head_dim] with
+ *           bound_blocks >= ceil(max_ctx_len / 16), paged ones one entry per physical page,
+ *           [bound_blocks, num_kv_heads, 2, head_dim] with bound_blocks >= num_pages; least keys first.
+ *   start_lens  device int32 [batch] or NULL: only blocks from start_lens[b] / 16 on are computed (the tokens before
+ *           start_lens[b] were there at the last call); NULL: all of them. Other blocks keep their bounds.
+ *   max_new host upper bound of ctx_lens[b] - start_lens[b], which sizes the launch (tokens beyond it may be left out);
+ *           0: not known. */
+tidal_status_t tidal_block_bounds(tidal_ctx_t *ctx, const tidal_kv_t *kv, const int32_t *start_lens, int32_t max_new,
+                                  void *bounds, int32_t bound_blocks, void *stream);
+
+/* The blocks to attend: per query head the score of a block is sum_c max(q_c lo_c, q_c hi_c), no less than q.k for
+ * any key k of the block; an index head's score is the sum over its member heads (with SHARED over an FP8 cache
+ * each KV head's part is multiplied by its k_scale, which must be positive). Chosen are the m' = min(m, ceil(ctx_lens[b] / 16))
+ * best, equal scores resolved toward the lower block, after the first keep_first and the last keep_last blocks, which count as better than
+ * any score (lower ones first if they are more than m). The set is the one that the scores in 64 bits give. Blocks
+ * with bounds that are not finite have an unspecified rank.
+ *   idx       int32 [batch, Hi, m]: block numbers in ascending order, padded with -1.
+ *   idx_count int32 [batch] or NULL: receives m'.
+ * m <= 16384. Scratch is the context's and may grow inside the call unless `stream` is being captured
+ * (TIDAL_ERR_NOMEM then; tidal_reserve provides it); graphs captured earlier stay valid. */
+tidal_status_t tidal_block_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const void *q, const void *bounds, int32_t bound_blocks,
+                                  int32_t m, int32_t granularity, int32_t keep_first, int32_t keep_last, int32_t *idx,
+                                  int32_t *idx_count, void *stream);
+
+/* Attention over the listed blocks: Eq. 1 restricted to the cached positions of the blocks listed for the query head's
+ * index head h * Hi / Hq, renormalised over them. -1 is padding; any other entry outside the sequence's blocks is skipped and
+ * reported as TIDAL_ERR_INDEX; a repeated block counts once per occurrence; any order. Only the first idx_count[b]
+ * entries are read when idx_count is given, else m. A head without a valid entry gets zeros. num_index_heads
+ * must be Hq, Hkv or 1. Output type as set by tidal_set_output_dtype; softmax weights enter the product with V
+ * with 16 bits or more, statistics and sums are fp32. tidal_set_attend_newest has no effect here (keep_last does that).
+ * Uses no scratch memory. */
+tidal_status_t tidal_block_attn(tidal_ctx_t *ctx, const tidal_kv_t *kv, const void *q, const int32_t *idx,
+                                const int32_t *idx_count, int32_t m, int32_t num_index_heads, float *out, void *stream);
+
 /* Waits for `stream`, then returns and clears the sticky device status word: TIDAL_OK,
- * TIDAL_ERR_INDEX, TIDAL_ERR_INTERNAL, or TIDAL_ERR_CUDA if the stream reports an error. */
+ * TIDAL_ERR_INDEX, TIDAL_ERR_PAGES, TIDAL_ERR_INTERNAL, or TIDAL_ERR_CUDA if the stream reports an error. */
 tidal_status_t tidal_device_status(tidal_ctx_t *ctx, void *stream);
 
 /* Kernels launched through this context since it was created. */

@@ -17,7 +17,7 @@ from . import build as _build
 
 OK = 0
 ERR_INVALID, ERR_UNSUPPORTED, ERR_NOMEM, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX = -1, -2, -3, -4, -5, -6
-ERR_TOO_LARGE, ERR_INTERNAL = -7, -8
+ERR_TOO_LARGE, ERR_INTERNAL, ERR_PAGES = -7, -8, -9
 KV_CONTIG, KV_PAGED = 0, 1
 KV_BF16, KV_FP8_E4M3 = 0, 1
 SEL_PER_QHEAD, SEL_PER_KVHEAD, SEL_SHARED = 0, 1, 2
@@ -29,7 +29,10 @@ EXPORTS = [
     "tidal_launch_count", "tidal_strerror", "tidal_sparse_attn_noalloc", "tidal_kv_append",
     "tidal_decode_step_append", "tidal_set_graphs", "tidal_set_output_dtype", "tidal_set_attend_newest",
     "tidal_set_layer_overlap", "tidal_reserve", "tidal_set_select_margin",
+    "tidal_page_map", "tidal_kv_write", "tidal_block_bounds", "tidal_block_select", "tidal_block_attn",
 ]
+
+BLOCK = 16               # positions per block of the block-sparse calls, and per page
 
 
 class tidal_kv_t(C.Structure):
@@ -104,6 +107,16 @@ def load() -> C.CDLL:
     L.tidal_decode_step.restype = I32
     L.tidal_decode_step_host.argtypes = [P, I32, P, KVP, P, P, I32, I32, P]
     L.tidal_decode_step_host.restype = I32
+    L.tidal_page_map.argtypes = [P, I32, P, P, P, I32, I32, P, P, P, I32, P, P, P, P]
+    L.tidal_page_map.restype = I32
+    L.tidal_kv_write.argtypes = [P, KVP, I32, P, P, I64, I64, P, P]
+    L.tidal_kv_write.restype = I32
+    L.tidal_block_bounds.argtypes = [P, KVP, P, I32, P, I32, P]
+    L.tidal_block_bounds.restype = I32
+    L.tidal_block_select.argtypes = [P, KVP, P, P, I32, I32, I32, I32, I32, P, P, P]
+    L.tidal_block_select.restype = I32
+    L.tidal_block_attn.argtypes = [P, KVP, P, P, P, I32, I32, P, P]
+    L.tidal_block_attn.restype = I32
     L.tidal_device_status.argtypes = [P, P]
     L.tidal_device_status.restype = I32
     L.tidal_launch_count.argtypes = [P]
@@ -119,7 +132,10 @@ def strerror(status: int) -> str:
 
 
 def kv_struct(layer) -> tidal_kv_t:
-    """Descriptor of one layer's cache from any object with LayerKV's fields."""
+    """Descriptor of one layer's cache from any object with LayerKV's fields. A descriptor is returned as it is, so
+    that a caller may build it once (and then keeps the tensors behind it alive)."""
+    if isinstance(layer, tidal_kv_t):
+        return layer
     s = tidal_kv_t()
     s.batch, s.num_q_heads, s.num_kv_heads, s.head_dim = (
         layer.batch, layer.num_q_heads, layer.num_kv_heads, layer.head_dim)
@@ -150,6 +166,30 @@ def _stream() -> int:
 def _check(status: int, what: str) -> None:
     if status != OK:
         raise TidalError(status, what)
+
+
+def _need(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, device: int, shape=None, contiguous: bool = True) -> int:
+    """Address of a tensor that a call reads or writes, after the checks that the C side cannot make (0 for None)."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype:
+        raise ValueError(f"{name}: {dtype} is wanted, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: a tensor on cuda:{device} is wanted, got one on {t.device}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(shape)} is wanted, got {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor is wanted")
+    return t.data_ptr()
+
+
+def block_bounds_shape(layer) -> tuple:
+    """Shape of the bf16 tensor of a cache's key bounds: one entry per physical page of a paged cache, one per 16
+    positions of each sequence of a contiguous one (for its max_ctx_len; a larger third dimension is fine)."""
+    s = kv_struct(layer)
+    if s.kv_layout == KV_PAGED:
+        return (s.num_pages, s.num_kv_heads, 2, s.head_dim)
+    return (s.batch, s.num_kv_heads, -(-s.max_ctx_len // BLOCK), 2, s.head_dim)
 
 
 def sparse_attn_noalloc(layer, q: torch.Tensor, idx: torch.Tensor, idx_count: Optional[torch.Tensor] = None,
@@ -322,6 +362,108 @@ class Tidal:
     def set_layer_overlap(self, enabled: bool) -> None:
         """Layers of a step may stream their inputs while the layer before them finishes (on by default)."""
         _check(self.lib.tidal_set_layer_overlap(self.ctx, 1 if enabled else 0), "tidal_set_layer_overlap")
+
+    # ---- paged caches filled on the device, block-sparse attention ------------------------------------------------
+
+    def _stream(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def page_map(self, old_lens: torch.Tensor, new_lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor,
+                 num_free: torch.Tensor, slots: torch.Tensor, num_free_out: Optional[torch.Tensor] = None,
+                 positions: Optional[torch.Tensor] = None, token_offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Grow and shrink sequences from old_lens to new_lens (int32 [B]): pages are taken from and given back to the
+        stack free_pages (int32 [num_pages], num_free (int32, one element) of them valid), page_table (int32 [B, width])
+        gets the new entries and slots (int64 [max_tokens]) every new token's place in the cache, -1 behind the
+        last. num_free_out receives the new count (default: num_free itself); positions (int32 [max_tokens])
+        and token_offsets (int32 [B + 1]) are optional outputs. Returns slots. A request that does not fit changes
+        nothing and shows in device_status() as ERR_PAGES."""
+        i32, dev = torch.int32, self.device
+        out = num_free if num_free_out is None else num_free_out
+        B, cap = old_lens.numel(), slots.numel()
+        if page_table.dim() != 2 or page_table.shape[0] != B:
+            raise ValueError(f"page_table: [{B}, pages] is wanted, got {tuple(page_table.shape)}")
+        if num_free.numel() != 1 or out.numel() != 1:
+            raise ValueError("num_free, num_free_out: one element is wanted")
+        _check(self.lib.tidal_page_map(
+            self.ctx, B, _need(old_lens, "old_lens", i32, dev), _need(new_lens, "new_lens", i32, dev, (B,)),
+            _need(page_table, "page_table", i32, dev), page_table.shape[1], free_pages.numel(),
+            _need(free_pages, "free_pages", i32, dev), _need(num_free, "num_free", i32, dev),
+            _need(out, "num_free_out", i32, dev), cap, _need(slots, "slots", torch.int64, dev),
+            _need(positions, "positions", i32, dev, (cap,)), _need(token_offsets, "token_offsets", i32, dev, (B + 1,)),
+            self._stream()), "tidal_page_map")
+        return slots
+
+    def kv_write(self, layer, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor) -> None:
+        """Write the rows of T tokens (bf16 [T, Hkv, d]; only the two inner dimensions have to be contiguous) at their slots
+        (int64 [T]; -1: skipped) of the layer's cache; an FP8 cache quantises them with its scales."""
+        s = kv_struct(layer)
+        T = slots.numel()
+        for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+            if t.shape != (T, s.num_kv_heads, s.head_dim):
+                raise ValueError(f"{name}: shape {(T, s.num_kv_heads, s.head_dim)} is wanted, got {tuple(t.shape)}")
+            if T and (t.stride(2) != 1 or (t.stride(1) != s.head_dim and s.num_kv_heads > 1)):
+                raise ValueError(f"{name}: the rows of a token have to be contiguous")
+        bf = torch.bfloat16
+        _check(self.lib.tidal_kv_write(
+            self.ctx, C.byref(s), T, _need(k_new, "k_new", bf, self.device, None, False),
+            _need(v_new, "v_new", bf, self.device, None, False), k_new.stride(0), v_new.stride(0),
+            _need(slots, "slots", torch.int64, self.device), self._stream()), "tidal_kv_write")
+
+    @staticmethod
+    def _bound_blocks(s: tidal_kv_t, bounds: torch.Tensor) -> int:
+        paged = s.kv_layout == KV_PAGED
+        blocks = bounds.shape[0 if paged else 2] if bounds.dim() == (4 if paged else 5) else -1
+        want = (blocks, s.num_kv_heads, 2, s.head_dim) if paged else (s.batch, s.num_kv_heads, blocks, 2, s.head_dim)
+        if bounds.shape != want:
+            raise ValueError(f"bounds: shape {want} is wanted, got {tuple(bounds.shape)}")
+        return blocks
+
+    def block_bounds(self, layer, bounds: Optional[torch.Tensor] = None, start_lens: Optional[torch.Tensor] = None,
+                     max_new: int = 0) -> torch.Tensor:
+        """Channelwise least and greatest key of every block of 16 positions (bf16, see block_bounds_shape): of all
+        blocks, or of those that hold positions from start_lens (int32 [B]) on. max_new: host bound of the tokens
+        that came since start_lens (0: not known)."""
+        s = kv_struct(layer)
+        if bounds is None:
+            bounds = torch.zeros(block_bounds_shape(s), dtype=torch.bfloat16, device=f"cuda:{self.device}")
+        _check(self.lib.tidal_block_bounds(
+            self.ctx, C.byref(s), _need(start_lens, "start_lens", torch.int32, self.device, (s.batch,)), max_new,
+            _need(bounds, "bounds", torch.bfloat16, self.device), self._bound_blocks(s, bounds), self._stream()),
+            "tidal_block_bounds")
+        return bounds
+
+    def block_select(self, layer, bounds: torch.Tensor, q: torch.Tensor, m: int, granularity: int = SEL_PER_QHEAD,
+                     keep_first: int = 0, keep_last: int = 0, idx: Optional[torch.Tensor] = None,
+                     idx_count: Optional[torch.Tensor] = None):
+        """The m blocks per index head with the largest upper bound of their logits, the first keep_first and the last
+        keep_last blocks among them. Returns (idx int32 [B, Hi, m] ascending and -1 padded, idx_count int32 [B])."""
+        s, dev = kv_struct(layer), self.device
+        hi = {SEL_PER_QHEAD: s.num_q_heads, SEL_PER_KVHEAD: s.num_kv_heads, SEL_SHARED: 1}.get(granularity, 1)
+        if idx is None:
+            idx = torch.empty(s.batch, hi, max(m, 1), dtype=torch.int32, device=q.device)
+        if idx_count is None:
+            idx_count = torch.empty(s.batch, dtype=torch.int32, device=q.device)
+        _check(self.lib.tidal_block_select(
+            self.ctx, C.byref(s), _need(q, "q", torch.bfloat16, dev, (s.batch, s.num_q_heads, s.head_dim)),
+            _need(bounds, "bounds", torch.bfloat16, dev), self._bound_blocks(s, bounds), m, granularity, keep_first,
+            keep_last, _need(idx, "idx", torch.int32, dev, (s.batch, hi, max(m, 1))),
+            _need(idx_count, "idx_count", torch.int32, dev, (s.batch,)), self._stream()), "tidal_block_select")
+        return idx, idx_count
+
+    def block_attn(self, layer, q: torch.Tensor, idx: torch.Tensor, idx_count: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention over the blocks listed in idx (int32 [B, Hi, m], block_select's or any other)."""
+        s, dev = kv_struct(layer), self.device
+        shape = (s.batch, s.num_q_heads, s.head_dim)
+        if out is None:
+            out = torch.empty(shape, dtype=self.out_dtype, device=q.device)
+        if idx.dim() != 3 or idx.shape[0] != s.batch:
+            raise ValueError(f"idx: [{s.batch}, Hi, m] is wanted, got {tuple(idx.shape)}")
+        _check(self.lib.tidal_block_attn(
+            self.ctx, C.byref(s), _need(q, "q", torch.bfloat16, dev, shape), _need(idx, "idx", torch.int32, dev),
+            _need(idx_count, "idx_count", torch.int32, dev, (s.batch,)), idx.shape[2], idx.shape[1],
+            _need(out, "out", self.out_dtype, dev, shape), self._stream()), "tidal_block_attn")
+        return out
 
     def device_status(self) -> int:
         return self.lib.tidal_device_status(self.ctx, _stream())

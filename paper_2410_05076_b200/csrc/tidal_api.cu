@@ -15,6 +15,8 @@
 #include <new>
 
 #include "attn_kernels.cuh"
+#include "block_kernels.cuh"
+#include "page_kernels.cuh"
 #include "split_select_kernels.cuh"
 #include "topk_kernels.cuh"
 
@@ -53,6 +55,12 @@ struct tidal_ctx {
     void* state = nullptr;
     int state_rows = 0;                         // capacity in (sequence, head) rows
     int* status = nullptr;                      // device word, sticky
+    // Scratch of the block selection. It grows by doubling, and what it outgrows is kept until the context goes:
+    // graphs that the caller captured may still name it.
+    void* blk_ws = nullptr;
+    size_t blk_ws_bytes = 0;
+    void* blk_old[64] = {};
+    int blk_old_count = 0;
     int out_bf16 = 0;                           // outputs are written as bf16 instead of fp32
     int attend_newest = 0;                      // sparse layers also attend the newest token (not in the paper)
     int cursor_set = 0;                         // which of the sets of pool cursors the last attention launch used
@@ -759,6 +767,115 @@ void remember_last(tidal_ctx* ctx) {
     ctx->last.launches = ctx->ran_launches;
 }
 
+// ---- block-sparse operators --------------------------------------------------------------------------
+// Scratch of a block selection: score rows, the largest bound of every chunk, and per index head the keys and blocks
+// of a candidate list that does not fit shared memory.
+struct BlockWs {
+    size_t scores, amax, wide, wide_blk, total;
+    long long stride;
+    int max_blocks, chunks;
+};
+
+BlockWs block_ws_layout(const tidal_kv_t* kv, int rows, int Hi) {
+    BlockWs w;
+    w.max_blocks = (kv->max_ctx_len + TILE - 1) / TILE;
+    w.stride = (long long)align_up((size_t)w.max_blocks, TB_PER);
+    w.chunks = (w.max_blocks + BS_BLOCKS - 1) / BS_BLOCKS;
+    const size_t B = (size_t)kv->batch;
+    size_t at = 0;
+    w.scores = at;   at += align_up(B * rows * w.stride * sizeof(float), 256);
+    w.amax = at;     at += align_up(B * kv->num_kv_heads * w.chunks * sizeof(float), 256);
+    w.wide = at;     at += align_up(B * Hi * w.max_blocks * sizeof(unsigned long long), 256);
+    w.wide_blk = at; at += align_up(B * Hi * w.max_blocks * sizeof(int), 256);
+    w.total = at;
+    return w;
+}
+
+// The context's device for the length of a call; the caller's own is current again afterwards.
+struct DeviceScope {
+    int before = -1;
+    bool ok = false;
+    explicit DeviceScope(int device) {
+        if (cudaGetDevice(&before) != cudaSuccess) { before = -1; cudaGetLastError(); return; }
+        ok = before == device || cudaSetDevice(device) == cudaSuccess;
+        if (before == device) before = -1;
+    }
+    ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
+};
+
+tidal_status_t ensure_block_ws(tidal_ctx* ctx, size_t bytes, const cudaStream_t* st) {
+    if (ctx->blk_ws_bytes >= bytes) return TIDAL_OK;
+    if (st) {                                   // nothing may be allocated into a capture
+        cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(*st, &cs) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
+        if (cs != cudaStreamCaptureStatusNone) return TIDAL_ERR_NOMEM;
+    }
+    if (ctx->blk_ws && ctx->blk_old_count == (int)(sizeof ctx->blk_old / sizeof ctx->blk_old[0])) return TIDAL_ERR_NOMEM;
+    const size_t want = std::max(bytes, 2 * ctx->blk_ws_bytes);
+    void* p = nullptr;
+    if (cudaMalloc(&p, want) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
+    if (ctx->blk_ws) ctx->blk_old[ctx->blk_old_count++] = ctx->blk_ws;
+    ctx->blk_ws = p;
+    ctx->blk_ws_bytes = want;
+    return TIDAL_OK;
+}
+
+constexpr int BA_MAX_CLUSTER = 16;
+
+bool prepare_block_kernels() {
+    auto wide = [](const void* k) {
+        return cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+    };
+    return wide((const void*)block_attn_kernel<false>) && wide((const void*)block_attn_kernel<true>) &&
+           cudaFuncSetAttribute(block_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ba_smem<false>()) == cudaSuccess &&
+           cudaFuncSetAttribute(block_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ba_smem<true>()) == cudaSuccess &&
+           cudaFuncSetAttribute(page_map_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (PM_MAX_BATCH + 1) * (int)sizeof(int)) == cudaSuccess;
+}
+
+void fill_block_cache(BlockCache& c, const tidal_ctx* ctx, const tidal_kv_t* kv, int bound_blocks) {
+    std::memset(&c, 0, sizeof c);
+    c.k = (const uint8_t*)kv->k; c.v = (const uint8_t*)kv->v;
+    c.stride_b = kv->stride_b; c.stride_pos = kv->stride_pos; c.stride_head = kv->stride_head; c.stride_page = kv->stride_page;
+    c.page_table = kv->page_table; c.max_pages = kv->max_pages_per_seq; c.num_pages = kv->num_pages;
+    c.paged = kv->kv_layout == TIDAL_KV_PAGED;
+    c.ctx_lens = kv->ctx_lens; c.max_ctx = kv->max_ctx_len;
+    c.max_blocks = (kv->max_ctx_len + TILE - 1) / TILE;
+    c.bound_blocks = bound_blocks;
+    c.batch = kv->batch; c.Hq = kv->num_q_heads; c.Hkv = kv->num_kv_heads; c.G = c.Hq / c.Hkv;
+    c.status = ctx->status;
+}
+
+// The bounds buffer must hold every block that the cache can name.
+tidal_status_t check_bounds(const tidal_kv_t* kv, const void* bounds, int32_t bound_blocks) {
+    if (!bounds || ((uintptr_t)bounds & 15)) return TIDAL_ERR_INVALID;
+    const int need = kv->kv_layout == TIDAL_KV_PAGED ? kv->num_pages : (kv->max_ctx_len + TILE - 1) / TILE;
+    return bound_blocks >= need ? TIDAL_OK : TIDAL_ERR_INVALID;
+}
+
+// Launch with programmatic stream serialization (the kernel waits first thing for the one before it) and, for cluster > 0,
+// with thread-block clusters of that size.
+template <typename P>
+tidal_status_t launch_block(tidal_ctx* ctx, void (*kernel)(P), const P& p, int grid, int threads, size_t smem, int cluster,
+                            cudaStream_t st) {
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(grid, 1, 1);
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 0 ? 2 : 1;
+    ctx->launches++;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess) return TIDAL_OK;
+    cudaGetLastError();
+    return TIDAL_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" {
@@ -801,6 +918,7 @@ tidal_status_t tidal_create(tidal_ctx_t** out, int device, size_t workspace_byte
     const bool topk_ok = cudaFuncSetAttribute(topk_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)topk_smem) == cudaSuccess;
     const size_t compact_smem = 2 * ((size_t)(MAX_CTX / 32) + 1) * sizeof(unsigned) + (size_t)COMPACT_LIST_SMEM * sizeof(uint2);
     const bool compact_ok = cudaFuncSetAttribute(topk_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)compact_smem) == cudaSuccess;
+    if (!prepare_block_kernels()) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     if (d0 <= 0 || d1 <= 0 || d2 < d1 || s0 <= 0 || s1 < s0 || e0 < d0 || e1 < d1 || e2 < s0 || !topk_ok || !compact_ok || !split_ok) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     ctx->dense_slots = std::min(d0, d1);
     ctx->sparse_slots = s0;
@@ -824,6 +942,8 @@ tidal_status_t tidal_destroy(tidal_ctx_t* ctx) {
     if (ctx->ev_fork) cudaEventDestroy(ctx->ev_fork);
     if (ctx->ev_join) cudaEventDestroy(ctx->ev_join);
     if (ctx->ws) cudaFree(ctx->ws);
+    if (ctx->blk_ws) cudaFree(ctx->blk_ws);
+    for (int i = 0; i < ctx->blk_old_count; ++i) cudaFree(ctx->blk_old[i]);
     if (ctx->state) cudaFree(ctx->state);
     if (ctx->status) cudaFree(ctx->status);
     delete ctx;
@@ -842,6 +962,8 @@ tidal_status_t tidal_reserve(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t k, 
     if (cudaSetDevice(ctx->device) != cudaSuccess) return TIDAL_ERR_CUDA;
     const tidal_status_t rs = ensure_side_stream(ctx);       // a later step's selection layers may use it
     if (rs != TIDAL_OK) return rs;
+    const tidal_status_t rb = ensure_block_ws(ctx, block_ws_layout(kv, kv->num_q_heads, kv->num_q_heads).total, nullptr);
+    if (rb != TIDAL_OK) return rb;
     return ensure_all(ctx, kv, ws_bytes_for(kv, k, num_layers_host));
 }
 
@@ -1207,9 +1329,142 @@ tidal_status_t tidal_device_status(tidal_ctx_t* ctx, void* stream) {
     if (cudaMemcpy(&word, ctx->status, sizeof word, cudaMemcpyDeviceToHost) != cudaSuccess) return TIDAL_ERR_CUDA;
     if (word != 0 && cudaMemset(ctx->status, 0, sizeof(int)) != cudaSuccess) return TIDAL_ERR_CUDA;
     if (word & STATUS_SPLIT_OVERFLOW) return TIDAL_ERR_INTERNAL;
+    if (word & STATUS_NO_PAGES) return TIDAL_ERR_PAGES;
     return word ? TIDAL_ERR_INDEX : TIDAL_OK;
 }
 
+
+// ---- paged caches filled on the device, block-sparse attention -------------------------------------------
+tidal_status_t tidal_page_map(tidal_ctx_t* ctx, int32_t batch, const int32_t* old_lens, const int32_t* new_lens,
+                              int32_t* page_table, int32_t max_pages_per_seq, int32_t num_pages, int32_t* free_pages,
+                              const int32_t* num_free, int32_t* num_free_out, int32_t max_tokens, int64_t* slots,
+                              int32_t* positions, int32_t* token_offsets, void* stream) {
+    if (!ctx || !old_lens || !new_lens || !page_table || !free_pages || !num_free || !num_free_out) return TIDAL_ERR_INVALID;
+    if (batch <= 0 || max_pages_per_seq <= 0 || num_pages <= 0 || max_tokens < 0 || (max_tokens > 0 && !slots)) return TIDAL_ERR_INVALID;
+    if (batch > PM_MAX_BATCH || (long long)max_pages_per_seq * TILE > MAX_CTX) return TIDAL_ERR_UNSUPPORTED;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    PageMapParams p;
+    std::memset(&p, 0, sizeof p);
+    p.batch = batch; p.max_pages = max_pages_per_seq; p.num_pages = num_pages; p.max_tokens = max_tokens;
+    p.old_lens = old_lens; p.new_lens = new_lens; p.page_table = page_table; p.free_pages = free_pages;
+    p.num_free = num_free; p.num_free_out = num_free_out;
+    p.slots = (long long*)slots; p.positions = positions; p.token_offsets = token_offsets; p.status = ctx->status;
+    const int cluster = max_tokens > 8 * PM_THREADS ? 8 : 1;
+    return launch_block(ctx, page_map_kernel, p, cluster, PM_THREADS, 3 * ((size_t)batch + 1) * sizeof(int), cluster, (cudaStream_t)stream);
+}
+
+tidal_status_t tidal_kv_write(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t num_tokens, const void* k_new, const void* v_new,
+                              int64_t k_stride, int64_t v_stride, const int64_t* slots, void* stream) {
+    if (!ctx || num_tokens < 0) return TIDAL_ERR_INVALID;
+    const tidal_status_t rc = check_kv(kv);
+    if (rc != TIDAL_OK) return rc;
+    if (num_tokens == 0) return TIDAL_OK;
+    if (!k_new || !v_new || !slots || (((uintptr_t)k_new | (uintptr_t)v_new) & 15)) return TIDAL_ERR_INVALID;
+    if (k_stride < 0 || v_stride < 0 || ((k_stride | v_stride) & 7)) return TIDAL_ERR_INVALID;
+    const long long units = (long long)num_tokens * kv->num_kv_heads;
+    const long long grid = (units + KW_UNITS * KW_WARPS - 1) / (KW_UNITS * KW_WARPS);
+    if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    KvWriteParams p;
+    std::memset(&p, 0, sizeof p);
+    p.k = (uint8_t*)const_cast<void*>(kv->k); p.v = (uint8_t*)const_cast<void*>(kv->v);
+    p.k_new = (const __nv_bfloat16*)k_new; p.v_new = (const __nv_bfloat16*)v_new;
+    p.k_stride = k_stride; p.v_stride = v_stride; p.slots = (const long long*)slots;
+    p.num_tokens = num_tokens; p.Hkv = kv->num_kv_heads; p.paged = kv->kv_layout == TIDAL_KV_PAGED; p.max_ctx = kv->max_ctx_len;
+    p.num_slots = p.paged ? (long long)kv->num_pages * TILE : (long long)kv->batch * kv->max_ctx_len;
+    p.stride_b = kv->stride_b; p.stride_pos = kv->stride_pos; p.stride_head = kv->stride_head; p.stride_page = kv->stride_page;
+    p.k_scale = kv->k_scale; p.v_scale = kv->v_scale; p.status = ctx->status;
+    return launch_block(ctx, kv->kv_dtype == TIDAL_KV_FP8_E4M3 ? kv_write_kernel<true> : kv_write_kernel<false>, p, (int)grid,
+                        KW_WARPS * 32, 0, 0, (cudaStream_t)stream);
+}
+
+tidal_status_t tidal_block_bounds(tidal_ctx_t* ctx, const tidal_kv_t* kv, const int32_t* start_lens, int32_t max_new, void* bounds,
+                                  int32_t bound_blocks, void* stream) {
+    if (!ctx || max_new < 0) return TIDAL_ERR_INVALID;
+    tidal_status_t rc = check_kv(kv);
+    if (rc != TIDAL_OK || (rc = check_bounds(kv, bounds, bound_blocks)) != TIDAL_OK) return rc;
+    BoundsParams p;
+    fill_block_cache(p.c, ctx, kv, bound_blocks);
+    p.start_lens = start_lens;
+    p.bounds = (__nv_bfloat16*)bounds;
+    // max_new tokens from `start` on lie in at most ceil((max_new - 1) / 16) + 1 blocks
+    p.blocks = p.c.max_blocks;
+    if (start_lens && max_new > 0) p.blocks = (int)std::min<long long>(p.blocks, ((long long)max_new - 1 + TILE - 1) / TILE + 1);
+    const long long grid = ((long long)kv->batch * kv->num_kv_heads * p.blocks + BB_WARPS - 1) / BB_WARPS;
+    if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    return launch_block(ctx, kv->kv_dtype == TIDAL_KV_FP8_E4M3 ? block_bounds_kernel<true> : block_bounds_kernel<false>, p, (int)grid,
+                        BB_WARPS * 32, 0, 0, (cudaStream_t)stream);
+}
+
+tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const void* q, const void* bounds, int32_t bound_blocks,
+                                  int32_t m, int32_t granularity, int32_t keep_first, int32_t keep_last, int32_t* idx,
+                                  int32_t* idx_count, void* stream) {
+    if (!ctx || !q || !idx || ((uintptr_t)q & 15) || m <= 0 || keep_first < 0 || keep_last < 0) return TIDAL_ERR_INVALID;
+    tidal_status_t rc = check_kv(kv);
+    if (rc != TIDAL_OK || (rc = check_bounds(kv, bounds, bound_blocks)) != TIDAL_OK) return rc;
+    const int Hi = hi_of(kv, granularity);
+    if (Hi <= 0 || m > MAX_CTX / TILE) return TIDAL_ERR_INVALID;
+    const bool per_qhead = granularity == TIDAL_SEL_PER_QHEAD;
+    const int rows = per_qhead ? kv->num_q_heads : kv->num_kv_heads;
+    const BlockWs w = block_ws_layout(kv, rows, Hi);
+    const long long grid = (long long)kv->batch * kv->num_kv_heads * w.chunks;
+    if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = ensure_block_ws(ctx, w.total, &st)) != TIDAL_OK) return rc;
+    char* ws = (char*)ctx->blk_ws;
+    ScoreParams s;
+    fill_block_cache(s.c, ctx, kv, bound_blocks);
+    s.q = (const __nv_bfloat16*)q;
+    s.bounds = (const __nv_bfloat16*)bounds;
+    // one KV head's factor changes no order: it matters only where several KV heads are added up
+    s.k_scale = kv->kv_dtype == TIDAL_KV_FP8_E4M3 && granularity == TIDAL_SEL_SHARED ? kv->k_scale : nullptr;
+    s.group_sum = !per_qhead;
+    s.scores = (float*)(ws + w.scores); s.stride = w.stride;
+    s.amax = (float*)(ws + w.amax); s.chunks = w.chunks;
+    if ((rc = launch_block(ctx, block_score_kernel, s, (int)grid, BS_WARPS * 32, 0, 0, st)) != TIDAL_OK) return rc;
+    TopBlocksParams t;
+    t.c = s.c; t.q = s.q; t.bounds = s.bounds; t.k_scale = s.k_scale;
+    t.scores = s.scores; t.stride = s.stride; t.amax = s.amax; t.chunks = s.chunks;
+    t.rows = rows; t.Hi = Hi; t.m = m; t.keep_first = keep_first; t.keep_last = keep_last;
+    t.idx = idx; t.idx_count = idx_count;
+    t.wide = (unsigned long long*)(ws + w.wide); t.wide_blk = (int*)(ws + w.wide_blk);
+    // 16 blocks per thread: up to 4096 blocks fit 256 threads, whose barriers and scans are shorter
+    if (w.max_blocks <= 256 * TB_PER) return launch_block(ctx, block_topk_kernel<256>, t, kv->batch * Hi, 256, 0, 0, st);
+    return launch_block(ctx, block_topk_kernel<1024>, t, kv->batch * Hi, 1024, 0, 0, st);
+}
+
+tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const void* q, const int32_t* idx, const int32_t* idx_count,
+                                int32_t m, int32_t num_index_heads, float* out, void* stream) {
+    if (!ctx || !q || !out || !idx || ((uintptr_t)q & 15) || m <= 0) return TIDAL_ERR_INVALID;
+    const tidal_status_t rc = check_kv(kv);
+    if (rc != TIDAL_OK) return rc;
+    const int Hi = num_index_heads;
+    if (Hi != kv->num_q_heads && Hi != kv->num_kv_heads && Hi != 1) return TIDAL_ERR_INVALID;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    BlockAttnParams p;
+    fill_block_cache(p.c, ctx, kv, 0);
+    p.q = (const __nv_bfloat16*)q;
+    p.out = out; p.out_bf16 = ctx->out_bf16;
+    p.idx = idx; p.idx_count = idx_count; p.m = m; p.Hi = Hi;
+    const float scale = kv->sm_scale > 0.f ? kv->sm_scale : 1.0f / std::sqrt((float)kv->head_dim);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3;
+    p.k_scale = fp8 ? kv->k_scale : nullptr;
+    p.v_scale = fp8 ? kv->v_scale : nullptr;
+    const int items = kv->batch * (Hi == kv->num_q_heads ? kv->num_q_heads : kv->num_kv_heads);
+    // clusters as large as two CTAs per SM allow, while every warp has two blocks or more
+    int cluster = 1;
+    while (cluster < BA_MAX_CLUSTER && (long long)items * cluster * 2 <= 2LL * ctx->sm_count && cluster * BA_WARPS * 2 <= m) cluster *= 2;
+    if (fp8) return launch_block(ctx, block_attn_kernel<true>, p, items * cluster, BA_WARPS * 32, ba_smem<true>(), cluster, (cudaStream_t)stream);
+    return launch_block(ctx, block_attn_kernel<false>, p, items * cluster, BA_WARPS * 32, ba_smem<false>(), cluster, (cudaStream_t)stream);
+}
 
 int64_t tidal_launch_count(const tidal_ctx_t* ctx) { return ctx ? ctx->launches : 0; }
 
@@ -1223,6 +1478,7 @@ const char* tidal_strerror(tidal_status_t s) {
         case TIDAL_ERR_TIMEOUT: return "device-side wait timed out";
         case TIDAL_ERR_INDEX: return "token index or page id out of range";
         case TIDAL_ERR_TOO_LARGE: return "problem exceeds the fixed scratch of the allocation-free entry point";
+        case TIDAL_ERR_PAGES: return "page map not built: lengths, tokens or pages beyond what the arrays and the pool hold";
         case TIDAL_ERR_INTERNAL: return "launch plan inconsistency detected on the device (results are invalid)";
         default: return "unknown status";
     }

@@ -1,8 +1,8 @@
 // Block-sparse decode attention: blocks of 16 positions (one page) ranked by an upper bound of their logits.
 //
 //   block_bounds_kernel  per block and KV head the channelwise least and greatest key (lo, hi), in bf16 (exact)
-//   block_score_kernel   s = sum_c max(q_c lo_c, q_c hi_c) >= q . k for every key k of the block
-//   block_topk_kernel    the m blocks with the largest s per index head, exactly, ties toward the lower block
+//   block_select_kernel  s = sum_c max(q_c lo_c, q_c hi_c) >= q . k for every key k of a block, and per index head the m
+//                        blocks with the largest s, exactly, ties toward the lower block
 //   block_attn_kernel    softmax attention over the cached positions of the listed blocks
 #pragma once
 
@@ -153,146 +153,46 @@ __global__ void __launch_bounds__(BB_WARPS * 32) block_bounds_kernel(const Bound
     }
 }
 
-// ---- block scores ----------------------------------------------------------------------------------------------
-// sum_c max(q_c lo_c, q_c hi_c) = q+ . hi + q- . lo with q+ = max(q, 0), q- = min(q, 0): two products, so one pair of
-// matrix instructions serves 16 blocks and the whole group of query heads. A warp takes 16 blocks x 512 bytes straight
-// into the registers that are its A fragments (the contraction index may be relabelled: lane (gid, tig) holds the
-// 16-byte pieces tig + 4 j of rows gid and gid + 8). Bound by memory; the result is an approximation in fp32 whose
-// error the ranking kernel bounds (see there) from the largest |bound| that each CTA finds on the way.
-struct ScoreParams {
-    BlockCache c;
-    const __nv_bfloat16* q;
-    const __nv_bfloat16* bounds;
-    const float* k_scale;                                   // factors of the KV heads where several of them are added up (or null)
-    int group_sum;                                          // one row per KV head: the sum of its query heads' scores
-    float* scores;                                          // [batch, Hq or Hkv, stride]
-    long long stride;
-    float* amax;                                            // [batch, Hkv, chunks] largest |bound| of the chunk
-    int chunks;
-};
-
-constexpr int BS_WARPS = 4;
-constexpr int BS_BLOCKS = BS_WARPS * 16;                    // blocks per CTA
-
-__global__ void __launch_bounds__(BS_WARPS * 32) block_score_kernel(const ScoreParams p) {
-    const BlockCache& c = p.c;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-    pdl_wait();
-    pdl_trigger();
-    const int pair = blockIdx.x / p.chunks, chunk = blockIdx.x - pair * p.chunks;
-    const int b = pair / c.Hkv, g = pair - b * c.Hkv;
-    const int nblk = (cached_len(c, b) + TILE - 1) / TILE;
-    const int first = chunk * BS_BLOCKS + warp * 16;
-    __shared__ float s_amax[BS_WARPS];
-    float amax = 0.f;
-    if (first < nblk) {
-        uint4 a[2][8];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int blk = first + gid + 8 * r;
-            bool on = blk < nblk;
-            int page = 0;
-            if (on && c.paged) {
-                page = __ldg(c.page_table + (long long)b * c.max_pages + blk);
-                if ((unsigned)page >= (unsigned)c.num_pages) { on = false; atomicOr(c.status, STATUS_BAD_PAGE); }
-            }
-            const uint4* src = reinterpret_cast<const uint4*>(p.bounds + bounds_row(c, b, on ? blk : 0, page, g) * BOUND_ELEMS) + tig;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) a[r][j] = on ? __ldg(src + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
-        }
-        float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
-        const uint4* qp = reinterpret_cast<const uint4*>(p.q + ((long long)b * c.Hq + g * c.G + min(gid, c.G - 1)) * HEAD_DIM) + tig;
-        uint32_t mx = 0u;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint4 q4 = __ldg(qp + 4 * j);
-            const uint32_t qw[4] = {q4.x, q4.y, q4.z, q4.w};
-            uint32_t neg[4], pos[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                neg[i] = gid < c.G ? bmin2(qw[i], 0u) : 0u;
-                pos[i] = gid < c.G ? bmax2(qw[i], 0u) : 0u;
-            }
-            const uint4 l0 = a[0][j], l1 = a[1][j], h0 = a[0][j + 4], h1 = a[1][j + 4];
-            mma_bf16_16816(s, l0.x, l1.x, l0.y, l1.y, neg[0], neg[1]);
-            mma_bf16_16816(s2, h0.x, h1.x, h0.y, h1.y, pos[0], pos[1]);
-            mma_bf16_16816(s, l0.z, l1.z, l0.w, l1.w, neg[2], neg[3]);
-            mma_bf16_16816(s2, h0.z, h1.z, h0.w, h1.w, pos[2], pos[3]);
-            const uint32_t all[16] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w, h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w};
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mx = bmax2(mx, all[i] & 0x7fff7fffu);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] += s2[i];
-        amax = fmaxf(__uint_as_float(mx << 16), __uint_as_float(mx & 0xffff0000u));
-        if ((mx & 0x7fffu) > 0x7f80u || (mx >> 16) > 0x7f80u) amax = INFINITY;      // not a number: no bound on the error
-        const int r0 = first + gid, r1 = r0 + 8;
-        if (p.group_sum) {
-            float x = s[0] + s[1], y = s[2] + s[3];
-            x += __shfl_xor_sync(0xffffffffu, x, 1); y += __shfl_xor_sync(0xffffffffu, y, 1);
-            x += __shfl_xor_sync(0xffffffffu, x, 2); y += __shfl_xor_sync(0xffffffffu, y, 2);
-            const float f = p.k_scale ? __ldg(p.k_scale + g) : 1.f;
-            float* row = p.scores + ((long long)b * c.Hkv + g) * p.stride;
-            if (tig == 0) {
-                if (r0 < nblk) row[r0] = x * f;
-                if (r1 < nblk) row[r1] = y * f;
-            }
-        } else {
-            float* row = p.scores + ((long long)b * c.Hq + g * c.G) * p.stride;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int col = 2 * tig + i;
-                if (col < c.G) {
-                    if (r0 < nblk) row[col * p.stride + r0] = s[i];
-                    if (r1 < nblk) row[col * p.stride + r1] = s[2 + i];
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int sh = 16; sh >= 1; sh >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, sh));
-    if (lane == 0) s_amax[warp] = amax;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        float m = s_amax[0];
-#pragma unroll
-        for (int w = 1; w < BS_WARPS; ++w) m = fmaxf(m, s_amax[w]);
-        p.amax[(long long)pair * p.chunks + chunk] = m;
-    }
-}
-
 // ---- the m best blocks -----------------------------------------------------------------------------------------
-// One CTA per (sequence, index head), sixteen scores per thread in registers. The set is the one that the scores in 64 bits
-// give. From the fp32 scores x, each within e of its true value, one histogram over the row's range gives the bin of the
-// need-th largest x, t say: a block with bin(x - 2e) > t is in for certain (x - 2e exceeds the need-th largest x,
-// whose true value exceeds no less than need true values by more than e), one with bin(x + 2e) < t is out for certain;
-// bin() is monotone, so rounding in it does no harm. What is left, a handful of blocks next to the border, is evaluated in 64 bits
-// from the bounds and ranked by (score, lower block first).
-//   e: a matrix instruction adds 16 exact products and an accumulator with an error of at most 2^-22 of the sum of their
-// magnitudes; at most 16 follow each other, the final additions (a group's heads, KV heads, their factors) add 2^-24
-// each: together below 2^-17 of sum_c |q_c| max|bound|, taken as 2^-16.
-// Rows whose scores or error bound are not finite, or whose range is empty, evaluate every block in 64 bits.
-struct TopBlocksParams {
+// One launch, no scratch memory. A thread-block cluster serves an item: a (sequence, KV head), or a sequence where all
+// heads share a set. Its CTAs score the item's blocks and push each score row (one per query head, or one
+// sum) into the shared memory of the CTA that owns the row; after one cluster barrier the owners rank their rows, one
+// per CTA, and the others leave.
+//
+// Scores. sum_c max(q_c lo_c, q_c hi_c) = q+ . hi + q- . lo with q+ = max(q, 0), q- = min(q, 0): two products, so 16 matrix
+// instructions serve 16 blocks and the whole group of query heads. A warp takes 16 blocks x 512 bytes straight into the
+// registers that are its A fragments (the contraction index may be relabelled: lane (gid, tig) holds the 16-byte
+// pieces tig + 4 j of rows gid and gid + 8). Bound by memory: 512 bytes per block and KV head.
+//
+// The set is the one that the scores in 64 bits give. Every instruction starts from zero and its results are added in fp32:
+// aligned to its largest product and cut at 2^-23 of that, 16 products lose at most 2^-19 of it, 16 instructions 2^-15;
+// the additions (16 per score, three over a group, one per KV head) lose 2^-24 of sum_c |q_c| max|bound| each. Call that e.
+// One histogram over the row's range gives the bin t of the need-th largest fp32 score x; a block with
+// bin(x - 2e) > t is in for certain (x - 2e exceeds the need-th largest x, so its true value exceeds all but
+// need - 1 others'), one with bin(x + 2e) < t is out; bin() is monotone, so rounding in it does no harm. What is left, a
+// few blocks, is ranked by x; if the gap at the border is not more than 2e, those within 2e of it are evaluated in 64 bits
+// and ranked by (score, lower block first). Rows that have no finite range or error bound, or too many blocks at
+// the border, are evaluated in 64 bits wherever undecided.
+struct SelectBlocksParams {
     BlockCache c;
     const __nv_bfloat16* q;
     const __nv_bfloat16* bounds;
-    const float* k_scale;                                   // as in ScoreParams
-    const float* scores;
-    long long stride;
-    const float* amax;
-    int chunks;
-    int rows, Hi;                                           // score rows per sequence, index heads
+    const float* k_scale;                                   // factors of the KV heads where several are added up (or null)
+    int mode;                                               // TIDAL_SEL_*: rows of an item are its query heads, or their sum
     int m, keep_first, keep_last;
+    int npad;                                               // blocks a score row has room for (a multiple of 32)
     int* idx;
     int* idx_count;
-    unsigned long long* wide;                               // [batch, Hi, max_blocks] keys in 64 bits where they do not fit shared memory
-    int* wide_blk;
 };
 
-constexpr int TB_BINS = 2048;
-constexpr int TB_PER = 16;                                  // blocks per thread
-constexpr int TB_CAND = 1024;                               // candidates kept in shared memory
-constexpr int TB_RANK = 192;                                // candidates ranked by counting
+constexpr int SB_BINS = 2048;
+constexpr int SB_CAND = 256;                                // border blocks ranked directly
+constexpr int SB_MAX_CLUSTER = 16;
+constexpr int SB_MAX_BLOCKS = 16384;
+constexpr int SB_QROW = HEAD_DIM + 8;                       // padded query row in shared memory (elements)
+constexpr int SB_RANGES = (SB_MAX_CLUSTER + 7) * 16;        // (rows of a CTA) x (CTAs) x (warps) at most
+// Dynamic shared memory: 8 bytes per block (the row being ranked, then its keys in 64 bits), 4 for every further row.
+__host__ __device__ constexpr size_t sb_smem(int npad, int rows_per_cta) { return (size_t)npad * (4 + 4 * (size_t)rows_per_cta); }
 
 // Larger double <=> larger key; not-a-number above everything, -0 as +0.
 __device__ __forceinline__ unsigned long long wide_key(double s) {
@@ -302,8 +202,25 @@ __device__ __forceinline__ unsigned long long wide_key(double s) {
     return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(cluster_addr(addr, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, int rank, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(cluster_addr(addr, rank)), "f"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory"); }
+
+// Exclusive prefix sum over the CTA. s_part must not be in use; it is free again after the next barrier.
 template <int NT>
-__device__ __forceinline__ int block_scan(int v, int* s_part, int& total) {        // exclusive prefix sum over the CTA
+__device__ __forceinline__ int cta_scan(int v, int* s_part) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int x = v;
 #pragma unroll
@@ -311,22 +228,14 @@ __device__ __forceinline__ int block_scan(int v, int* s_part, int& total) {     
         const int y = __shfl_up_sync(0xffffffffu, x, sh);
         if (lane >= sh) x += y;
     }
-    __syncthreads();                                        // s_part may still be read from the last call
     if (lane == 31) s_part[warp] = x;
     __syncthreads();
-    int w = lane < NT / 32 ? s_part[lane] : 0;
-#pragma unroll
-    for (int sh = 1; sh < 32; sh <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, w, sh);
-        if (lane >= sh) w += y;
-    }
-    total = __shfl_sync(0xffffffffu, w, NT / 32 - 1);
-    const int before = __shfl_sync(0xffffffffu, w, max(warp - 1, 0));
-    return x - v + (warp > 0 ? before : 0);
+    const int w = lane < warp && lane < NT / 32 ? s_part[lane] : 0;
+    return x - v + __reduce_add_sync(0xffffffffu, w);
 }
 
-// One candidate's score in 64 bits, by a warp: every lane four channels of each member head.
-__device__ __forceinline__ double wide_score(const TopBlocksParams& p, int b, int h0, int h1, int blk, int lane) {
+// One block's score in 64 bits for query heads h0 .. h1 - 1, by a warp: four channels per lane and head.
+__device__ __forceinline__ double wide_score(const SelectBlocksParams& p, int b, int h0, int h1, int blk, int lane) {
     const BlockCache& c = p.c;
     int page = 0;
     if (c.paged) {
@@ -337,23 +246,17 @@ __device__ __forceinline__ double wide_score(const TopBlocksParams& p, int b, in
     int h = h0;
     for (int g = h0 / c.G; h < h1; ++g) {
         const uint2* bp = reinterpret_cast<const uint2*>(p.bounds + bounds_row(c, b, blk, page, g) * BOUND_ELEMS) + lane;
-        const uint2 l2 = __ldg(bp), h2 = __ldg(bp + 32);
-        double lo[4], hi[4], part = 0.0;
-        const uint32_t lw[2] = {l2.x, l2.y}, hw[2] = {h2.x, h2.y};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            lo[2 * i] = __uint_as_float(lw[i] << 16); lo[2 * i + 1] = __uint_as_float(lw[i] & 0xffff0000u);
-            hi[2 * i] = __uint_as_float(hw[i] << 16); hi[2 * i + 1] = __uint_as_float(hw[i] & 0xffff0000u);
-        }
+        const uint2 lo = __ldg(bp), hi = __ldg(bp + 32);
+        double part = 0.0;
         for (; h < h1 && h < (g + 1) * c.G; ++h) {
-            const uint2 q2 = __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h) * HEAD_DIM) + lane);
-            const uint32_t qw[2] = {q2.x, q2.y};
+            const uint2 q = __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h) * HEAD_DIM) + lane);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const double q0 = __uint_as_float(qw[i] << 16), q1 = __uint_as_float(qw[i] & 0xffff0000u);
-                const double x0 = q0 * lo[2 * i], y0 = q0 * hi[2 * i], x1 = q1 * lo[2 * i + 1], y1 = q1 * hi[2 * i + 1];
-                part += (x0 > y0 || x0 != x0) ? x0 : y0;
-                part += (x1 > y1 || x1 != x1) ? x1 : y1;
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t qw = i & 2 ? q.y : q.x, lw = i & 2 ? lo.y : lo.x, hw = i & 2 ? hi.y : hi.x;
+                const uint32_t bw = (i & 1 ? qw : qw << 16) >> 31 ? lw : hw;      // a negative q takes the least key
+                const float qf = __uint_as_float(i & 1 ? qw & 0xffff0000u : qw << 16);
+                const float bf = __uint_as_float(i & 1 ? bw & 0xffff0000u : bw << 16);
+                part = fma((double)qf, (double)bf, part);
             }
         }
         acc += p.k_scale ? part * (double)__ldg(p.k_scale + g) : part;
@@ -363,212 +266,407 @@ __device__ __forceinline__ double wide_score(const TopBlocksParams& p, int b, in
     return acc;
 }
 
+// NT threads per CTA: 512 with an SM to themselves, for few items, whose streaming wants every SM and whose ranking is the
+// critical path; 256 twice on an SM, for batches, where one item's ranking hides behind another's stream.
 template <int NT>
-__global__ void __launch_bounds__(NT) block_topk_kernel(const TopBlocksParams p) {
-    const BlockCache& c = p.c;
+__global__ void __launch_bounds__(NT, NT == 512 ? 1 : 2) block_select_kernel(const SelectBlocksParams p) {
     constexpr int NW = NT / 32;
-    __shared__ unsigned s_hist[TB_BINS];
-    __shared__ unsigned long long s_key[TB_CAND];
-    __shared__ int s_blk[TB_CAND];
-    __shared__ unsigned s_take[NT * TB_PER / 32];           // candidates that made it, one bit per block
-    __shared__ unsigned s_tie[NT * TB_PER / 32];
-    __shared__ float s_red[3][NW];
-    __shared__ int s_part[NW];
-    __shared__ int s_bin;
+    constexpr int VECS = 8;                                 // groups of four scores per thread: rows of up to 32 NT blocks
+    const BlockCache& c = p.c;
+    extern __shared__ __align__(16) uint8_t sb_rows[];
+    __shared__ __align__(16) __nv_bfloat16 s_q[2][8][SB_QROW];        // q-, q+ of a group
+    __shared__ __align__(16) unsigned s_hist[SB_BINS];
+    __shared__ float s_min[SB_RANGES], s_max[SB_RANGES], s_amax[SB_MAX_CLUSTER * NW];
+    __shared__ float s_qpart[8];
+    __shared__ int s_part[2][NW];
+    __shared__ unsigned s_take[SB_MAX_BLOCKS / 32], s_cand[SB_MAX_BLOCKS / 32];      // one bit per block: in, undecided
+    __shared__ unsigned long long s_key[SB_CAND];
+    __shared__ float s_x[SB_CAND];
+    __shared__ int s_blk[SB_CAND];
     __shared__ unsigned s_digit[256];
     __shared__ unsigned long long s_prefix;
-    __shared__ int s_need;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int b = blockIdx.x / p.Hi, hi = blockIdx.x - b * p.Hi;
-#pragma unroll
-    for (int i = tid; i < TB_BINS; i += NT) s_hist[i] = 0;
-    if (tid < NT * TB_PER / 32) { s_take[tid] = 0; s_tie[tid] = 0; }
-    if (tid == 0) s_bin = 0;
+    __shared__ int s_ncand, s_winners, s_bin, s_left;
+    __shared__ float s_edge[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
+    int rank, size;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+    cluster_arrive();                                       // waited for before the first write to another CTA
+    const bool shared_set = p.mode == 2, per_qhead = p.mode == 0;
+    const int item = blockIdx.x / size;
+    const int b = shared_set ? item : item / c.Hkv, g0 = shared_set ? 0 : item - b * c.Hkv, g1 = shared_set ? c.Hkv : g0 + 1;
+    const int rows = per_qhead ? c.G : 1;
+    const int owners = min(rows, size);
+    for (int i = tid; i < SB_BINS; i += NT) s_hist[i] = 0;
+    if (tid == 0) { s_ncand = 0; s_winners = 0; }
     pdl_wait();
     pdl_trigger();
-    const int n = (cached_len(c, b) + TILE - 1) / TILE;
-    const int kk = min(p.m, n);
-    const int members = c.Hq / p.Hi, h0 = hi * members, h1 = h0 + members;
-    int* const out = p.idx + ((long long)b * p.Hi + hi) * p.m;
-    if (hi == 0 && tid == 0 && p.idx_count) p.idx_count[b] = kk;
-    for (int i = kk + tid; i < p.m; i += NT) out[i] = -1;
-    const int base = tid * TB_PER;
+    const int len = c.ctx_lens[b];
+    const uint32_t a_rows = smem_u32(sb_rows);
+    // row slot s of a CTA: the first one lies where its keys go later
+    auto row_at = [&](int slot) -> uint32_t { return slot == 0 ? 0u : (uint32_t)p.npad * (4u + 4u * slot); };
+    const int n = (max(min(len, c.max_ctx), 0) + TILE - 1) / TILE;
     // blocks that are kept whatever they score
     auto forced = [&](int blk) { return blk < p.keep_first || blk >= n - p.keep_last; };
-    const int nforced = min((long long)n, (long long)p.keep_first + p.keep_last);
-    unsigned mine = 0;                                      // bit i: block base + i is in
-    if (kk == n || nforced >= kk) {
-        // every block, or the first kk of the kept ones
-        int have = 0;
-        for (int i = 0; i < TB_PER; ++i) if (base + i < n && (kk == n || forced(base + i))) { mine |= 1u << i; ++have; }
-        int total;
-        const int before = block_scan<NT>(have, s_part, total);
-        int at = before;
-        for (int i = 0; i < TB_PER; ++i) if ((mine >> i) & 1u) { if (at < kk) out[at] = base + i; ++at; }
-        return;
-    }
-    const int need = kk - nforced;
 
-    float x[TB_PER];
-    unsigned there = 0;                                     // bit i: an unforced block of the row
-    {
-        const float* row = p.scores + (p.rows == p.Hi ? (long long)b * p.rows + hi : (long long)b * p.rows) * p.stride;
-        const int sum_rows = p.rows / p.Hi;
+    float amax = 0.f, mn[2] = {INFINITY, INFINITY}, mx[2] = {-INFINITY, -INFINITY};
+    bool first_write = true;
+    for (int g = g0; g < g1; ++g) {
+        if (g > g0) __syncthreads();
+        for (int i = tid; i < 8 * HEAD_DIM / 2; i += NT) {
+            const int h = i / (HEAD_DIM / 2), w = i % (HEAD_DIM / 2);
+            const uint32_t x = h < c.G ? __ldg(reinterpret_cast<const uint32_t*>(p.q + ((long long)b * c.Hq + g * c.G + h) * HEAD_DIM) + w) : 0u;
+            *reinterpret_cast<uint32_t*>(&s_q[0][h][2 * w]) = bmin2(x, 0u);
+            *reinterpret_cast<uint32_t*>(&s_q[1][h][2 * w]) = bmax2(x, 0u);
+        }
+        const float factor = p.k_scale ? __ldg(p.k_scale + g) : 1.f;
+        float gmax = 0.f;
+        bool staged = false;
+        for (int first = (rank * NW + warp) * 16; first < n; first += size * NW * 16) {
+            const int r0 = first + gid, r1 = r0 + 8;
+            bool on0 = r0 < n, on1 = r1 < n;
+            int pg0 = 0, pg1 = 0;
+            if (c.paged) {
+                const int* row = c.page_table + (long long)b * c.max_pages;
+                if (on0) pg0 = __ldg(row + r0);
+                if (on1) pg1 = __ldg(row + r1);
+                if ((unsigned)pg0 >= (unsigned)c.num_pages) { on0 = false; pg0 = 0; atomicOr(c.status, STATUS_BAD_PAGE); }
+                if ((unsigned)pg1 >= (unsigned)c.num_pages) { on1 = false; pg1 = 0; atomicOr(c.status, STATUS_BAD_PAGE); }
+            }
+            const uint4* src0 = reinterpret_cast<const uint4*>(p.bounds + bounds_row(c, b, on0 ? r0 : 0, pg0, g) * BOUND_ELEMS) + tig;
+            const uint4* src1 = reinterpret_cast<const uint4*>(p.bounds + bounds_row(c, b, on1 ? r1 : 0, pg1, g) * BOUND_ELEMS) + tig;
+            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+            uint4 x0[8], x1[8];
 #pragma unroll
-        for (int i = 0; i < TB_PER; i += 4) {
-            float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (base + i < n) {                             // rows are padded to 16 scores: whole vectors may be read
-                for (int r = 0; r < sum_rows; ++r) {
-                    const float4 u = __ldcg(reinterpret_cast<const float4*>(row + r * p.stride + base + i));
-                    t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
+            for (int j = 0; j < 8; ++j) {
+                x0[j] = on0 ? __ldg(src0 + 4 * j) : zero;
+                x1[j] = on1 ? __ldg(src1 + 4 * j) : zero;
+            }
+            if (!staged) { asm volatile("bar.sync 1, %0;\n" ::"n"(NT) : "memory"); staged = true; }      // s_q is there
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t top = 0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint4 q4 = *reinterpret_cast<const uint4*>(&s_q[j >> 2][gid][8 * (tig + 4 * (j & 3))]);
+                float d[4] = {0.f, 0.f, 0.f, 0.f}, e[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_bf16_16816(d, x0[j].x, x1[j].x, x0[j].y, x1[j].y, q4.x, q4.y);
+                mma_bf16_16816(e, x0[j].z, x1[j].z, x0[j].w, x1[j].w, q4.z, q4.w);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] += d[i] + e[i];
+                const uint32_t all[8] = {x0[j].x, x0[j].y, x0[j].z, x0[j].w, x1[j].x, x1[j].y, x1[j].z, x1[j].w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = bmax2(top, all[i] & 0x7fff7fffu);
+            }
+            gmax = fmaxf(gmax, fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u)));
+            if ((top & 0x7fffu) >= 0x7f80u || (top >> 16) >= 0x7f80u) gmax = INFINITY;    // no bound on the error
+            if (first_write) { cluster_wait(); first_write = false; }
+            const bool f0 = r0 < n && !forced(r0), f1 = r1 < n && !forced(r1);
+            auto range = [&](int i, float v, bool on) {
+                if (on) { mn[i] = fminf(mn[i], v); mx[i] = fmaxf(mx[i], fabsf(v) <= 3.4e38f ? v : INFINITY); }
+            };
+            if (per_qhead) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int col = 2 * tig + i;
+                    if (col < c.G) {
+                        const int owner = col % size;
+                        const uint32_t at = a_rows + row_at(col / size);
+                        if (r0 < n) st_cluster(at + 4 * r0, owner, s[i]);
+                        if (r1 < n) st_cluster(at + 4 * r1, owner, s[2 + i]);
+                        range(i, s[i], f0);
+                        range(i, s[2 + i], f1);
+                    }
+                }
+            } else {
+                float x = s[0] + s[1], y = s[2] + s[3];
+                x += __shfl_xor_sync(0xffffffffu, x, 1); y += __shfl_xor_sync(0xffffffffu, y, 1);
+                x += __shfl_xor_sync(0xffffffffu, x, 2); y += __shfl_xor_sync(0xffffffffu, y, 2);
+                if (tig == 0) {                             // (the same lane adds the next KV head's part)
+                    x *= factor; y *= factor;
+                    if (g > g0) {
+                        if (r0 < n) x += ld_cluster(a_rows + 4 * r0, 0);
+                        if (r1 < n) y += ld_cluster(a_rows + 4 * r1, 0);
+                    }
+                    if (r0 < n) st_cluster(a_rows + 4 * r0, 0, x);
+                    if (r1 < n) st_cluster(a_rows + 4 * r1, 0, y);
+                    if (g == g1 - 1) { range(0, x, f0); range(0, y, f1); }
                 }
             }
-            x[i] = t.x; x[i + 1] = t.y; x[i + 2] = t.z; x[i + 3] = t.w;
         }
+        if (!staged) asm volatile("bar.sync 1, %0;\n" ::"n"(NT) : "memory");
+        amax = fmaxf(amax, gmax * fabsf(factor));
+        // what e needs of the query: 2^-15 max|q| + (24 + Hkv) 2^-24 sum|q| per head (added up over the KV heads of a shared set)
+        if (rank < owners && warp < c.G) {
+            float sum = 0.f, big = 0.f;
 #pragma unroll
-        for (int i = 0; i < TB_PER; ++i) if (base + i < n && !forced(base + i)) there |= 1u << i;
-    }
-    // range of the scores, and the error bound
-    float mn = INFINITY, mx = -INFINITY, err = 0.f;
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < TB_PER; ++i) {
-        if ((there >> i) & 1u) {
-            mn = fminf(mn, x[i]); mx = fmaxf(mx, x[i]);
-            odd |= !(fabsf(x[i]) <= 3.4e38f);
-        }
-    }
-    {
-        // sum over member KV heads of factor * max|bound| * sum |q|
-        const int g0 = h0 / c.G, g1 = (h1 - 1) / c.G;
-        const int used = (n + BS_BLOCKS - 1) / BS_BLOCKS;
-        for (int g = g0 + warp; g <= g1; g += NW) {
-            float big = 0.f, l1 = 0.f;
-            for (int i = lane; i < used; i += 32) big = fmaxf(big, __ldcg(p.amax + ((long long)b * c.Hkv + g) * p.chunks + i));
-            for (int h = max(h0, g * c.G); h < min(h1, (g + 1) * c.G); ++h) {
-                const uint2 q2 = __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h) * HEAD_DIM) + lane);
-                l1 += fabsf(__uint_as_float(q2.x << 16)) + fabsf(__uint_as_float(q2.x & 0xffff0000u)) +
-                      fabsf(__uint_as_float(q2.y << 16)) + fabsf(__uint_as_float(q2.y & 0xffff0000u));
+            for (int i = 0; i < 4; ++i) {
+                const float v = __bfloat162float(s_q[1][warp][lane + 32 * i]) - __bfloat162float(s_q[0][warp][lane + 32 * i]);
+                sum += v;
+                big = fmaxf(big, v);
             }
 #pragma unroll
             for (int sh = 16; sh >= 1; sh >>= 1) {
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, sh));
-                l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
+                sum += __shfl_xor_sync(0xffffffffu, sum, sh);
             }
-            err += big * l1 * (p.k_scale ? fabsf(__ldg(p.k_scale + g)) : 1.f);
+            const float part = big * (1.f / 32768.f) + sum * (float)(24 + c.Hkv) * (1.f / 16777216.f);
+            if (lane == 0) s_qpart[warp] = g > g0 ? s_qpart[warp] + part : part;
+        }
+    }
+    if (first_write) cluster_wait();
+#pragma unroll
+    for (int sh = 16; sh >= 4; sh >>= 1) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            mn[i] = fminf(mn[i], __shfl_xor_sync(0xffffffffu, mn[i], sh));
+            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], sh));
         }
     }
 #pragma unroll
-    for (int sh = 16; sh >= 1; sh >>= 1) {
-        mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, sh));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, sh));
-    }
-    if (lane == 0) { s_red[0][warp] = mn; s_red[1][warp] = mx; s_red[2][warp] = err; }
-    odd = __syncthreads_or(odd);
-    mn = s_red[0][0]; mx = s_red[1][0]; err = s_red[2][0];
+    for (int sh = 16; sh >= 1; sh >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, sh));
+    if (gid == 0) {
 #pragma unroll
-    for (int w = 1; w < NW; ++w) { mn = fminf(mn, s_red[0][w]); mx = fmaxf(mx, s_red[1][w]); err += s_red[2][w]; }
-    const float two_e = err * (2.1f / 65536.f);
-    const float inv = (float)(TB_BINS - 1) / (mx - mn);
-    const bool all = odd || !(two_e <= 3.4e38f) || !(mx > mn) || !(inv <= 3.4e38f);
-    auto bin = [&](float v) { return max(0, min(TB_BINS - 1, __float2int_rd((v - mn) * inv))); };
+        for (int i = 0; i < 2; ++i) {
+            const int col = 2 * tig + i;
+            if (col < rows) {
+                const uint32_t at = 4 * (((col / size) * size + rank) * NW + warp);
+                st_cluster(smem_u32(s_min) + at, col % size, mn[i]);
+                st_cluster(smem_u32(s_max) + at, col % size, mx[i]);
+            }
+        }
+    }
+    if (lane < owners) st_cluster(smem_u32(s_amax) + 4 * (rank * NW + warp), lane, amax);
+    cluster_arrive();                                       // every score of the item is where it belongs ...
+    const int kk = min(p.m, n), words = (n + 31) / 32;
+    if (g0 == 0 && rank == 0 && tid == 0 && p.idx_count) p.idx_count[b] = kk;
+    const int nforced = (int)min((long long)n, (long long)p.keep_first + p.keep_last), need = kk - nforced;
+    const bool plain = need <= 0 || kk == n;               // every block, or the first kk of the kept ones
+    auto clear_bits = [&]() {
+        for (int w = tid; w < words; w += NT) {
+            auto span = [&](int from, int to) -> unsigned {        // bits of this word for blocks from .. to - 1
+                const int f = max(from - 32 * w, 0), t = min(to - 32 * w, 32);
+                return f < t ? (0xffffffffu >> (32 - (t - f))) << f : 0u;
+            };
+            s_take[w] = kk == n ? span(0, n) : span(0, min(p.keep_first, n)) | span(max(n - p.keep_last, 0), n);
+            s_cand[w] = 0;
+        }
+    };
+    clear_bits();
+    cluster_wait();                                         // ... and nobody touches another CTA's memory from here on
+    if (rank >= owners) return;
+    __syncthreads();
 
-    unsigned cand = there;
-    if (!all) {
-#pragma unroll
-        for (int i = 0; i < TB_PER; ++i) if ((there >> i) & 1u) atomicAdd(&s_hist[bin(x[i])], 1u);
-        __syncthreads();
-        // the bin of the need-th largest: counts from the top
-        constexpr int PER = TB_BINS / NT;
-        int cnt = 0;
-#pragma unroll
-        for (int u = 0; u < PER; ++u) cnt += s_hist[TB_BINS - 1 - (tid * PER + u)];
-        int total;
-        int above = block_scan<NT>(cnt, s_part, total);
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int h = s_hist[TB_BINS - 1 - (tid * PER + u)];
-            if (above < need && above + h >= need) s_bin = TB_BINS - 1 - (tid * PER + u);
-            above += h;
-        }
-        __syncthreads();
-        const int t = s_bin;
-#pragma unroll
-        for (int i = 0; i < TB_PER; ++i) {
-            if ((there >> i) & 1u) {
-                if (bin(x[i] - two_e) > t) { mine |= 1u << i; cand &= ~(1u << i); }
-                else if (bin(x[i] + two_e) < t) cand &= ~(1u << i);
-            }
-        }
-    }
-    int winners;
-    block_scan<NT>(__popc(mine), s_part, winners);
-    int ncand;
-    int at = block_scan<NT>(__popc(cand), s_part, ncand);
-    const int want = need - winners;                        // of the candidates; 0 <= want <= ncand
-    const bool spill = ncand > TB_CAND;
-    const long long wrow = ((long long)b * p.Hi + hi) * c.max_blocks;
-    unsigned long long* key = spill ? p.wide + wrow : s_key;
-    int* cblk = spill ? p.wide_blk + wrow : s_blk;
-    for (unsigned m = cand; m; m &= m - 1) cblk[at++] = base + __ffs(m) - 1;      // in ascending order
-    __syncthreads();
-    if (want > 0 && want < ncand) {
-        for (int i = warp; i < ncand; i += NW) {
-            const double s = wide_score(p, b, h0, h1, cblk[i], lane);
-            if (lane == 0) key[i] = wide_key(s);
-        }
-        __syncthreads();
-    }
-    auto take = [&](unsigned* bits, int blk) { atomicOr(&bits[blk >> 5], 1u << (blk & 31)); };
-    if (want >= ncand) {
-        for (int i = tid; i < ncand; i += NT) take(s_take, cblk[i]);
-    } else if (want > 0 && ncand <= TB_RANK) {
-        // a candidate's place is the number of candidates before it: larger, or equal and lower (the list ascends)
-        for (int i = tid; i < ncand; i += NT) {
-            const unsigned long long k = key[i];
-            int before = 0;
-            for (int j = 0; j < ncand; ++j) before += (key[j] > k) || (key[j] == k && j < i);
-            if (before < want) take(s_take, cblk[i]);
-        }
-    } else if (want > 0) {
-        // the want-th largest key, eight bits at a time from the top
-        if (tid == 0) { s_prefix = 0ull; s_need = want; }
-        for (int shift = 56; shift >= 0; shift -= 8) {
-            if (tid < 256) s_digit[tid] = 0;
-            __syncthreads();
-            const unsigned long long prefix = s_prefix;
-            for (int i = tid; i < ncand; i += NT) {
-                const unsigned long long k = key[i];
-                if (shift == 56 || (k >> (shift + 8)) == prefix) atomicAdd(&s_digit[(unsigned)(k >> shift) & 255u], 1u);
-            }
-            __syncthreads();
-            if (tid == 0) {
-                int left = s_need, d = 255;
-                while (d > 0 && (int)s_digit[d] < left) left -= s_digit[d--];
-                s_prefix = (prefix << 8) | (unsigned)d;
-                s_need = left;
-            }
+    for (int row = rank, slot = 0; row < rows; row += size, ++slot) {
+        const int h0 = per_qhead ? g0 * c.G + row : g0 * c.G, h1 = per_qhead ? h0 + 1 : g1 * c.G;
+        const int hi = per_qhead ? h0 : (shared_set ? 0 : g0), Hi = per_qhead ? c.Hq : (shared_set ? 1 : c.Hkv);
+        int* const out = p.idx + ((long long)b * Hi + hi) * p.m;
+        const float* const x = reinterpret_cast<const float*>(sb_rows + row_at(slot));
+        unsigned long long* const keys = reinterpret_cast<unsigned long long*>(sb_rows);
+        if (slot > 0) {
+            for (int i = tid; i < SB_BINS; i += NT) s_hist[i] = 0;
+            if (tid == 0) { s_ncand = 0; s_winners = 0; }
+            clear_bits();
             __syncthreads();
         }
-        const unsigned long long border = s_prefix;
-        const int ties = s_need;                            // how many of those equal to the border are in: the lowest
-        for (int i = tid; i < ncand; i += NT) {
-            if (key[i] > border) take(s_take, cblk[i]);
-            else if (key[i] == border) take(s_tie, cblk[i]);
-        }
-        __syncthreads();
-        const unsigned tie = (s_tie[base >> 5] >> (base & 31)) & 0xffffu;
-        int total;
-        int before = block_scan<NT>(__popc(tie), s_part, total);
-        for (unsigned m = tie; m; m &= m - 1) if (before++ < ties) mine |= m & (~m + 1u);
-    }
-    __syncthreads();
-    mine |= (s_take[base >> 5] >> (base & 31)) & 0xffffu;
+        for (int i = kk + tid; i < p.m; i += NT) out[i] = -1;
+        if (!plain) {
+            // ---- this thread's scores; range of the row and error bound, by every warp for itself ------------------
+            float v[VECS][4];
+            unsigned open = 0;                              // bit 4 j + u: v[j][u] is a block that may be chosen
 #pragma unroll
-    for (int i = 0; i < TB_PER; ++i) if (base + i < n && forced(base + i)) mine |= 1u << i;
-    int total;
-    int pos = block_scan<NT>(__popc(mine), s_part, total);
-    for (unsigned m = mine; m; m &= m - 1) out[pos++] = base + __ffs(m) - 1;
+            for (int j = 0; j < VECS; ++j) {
+                const int at = (j * NT + tid) * 4;
+                if (at < n) {                               // rows have room for a multiple of 32 blocks
+                    const float4 t = *reinterpret_cast<const float4*>(x + at);
+                    v[j][0] = t.x; v[j][1] = t.y; v[j][2] = t.z; v[j][3] = t.w;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) if (at + u < n && !forced(at + u)) open |= 1u << (4 * j + u);
+                }
+            }
+            float lo = INFINITY, hi_s = -INFINITY, big = 0.f, qsum = 0.f;
+            for (int i = lane; i < size * NW; i += 32) {
+                lo = fminf(lo, s_min[slot * size * NW + i]);
+                hi_s = fmaxf(hi_s, s_max[slot * size * NW + i]);
+                big = fmaxf(big, s_amax[i]);
+            }
+#pragma unroll
+            for (int sh = 16; sh >= 1; sh >>= 1) {
+                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, sh));
+                hi_s = fmaxf(hi_s, __shfl_xor_sync(0xffffffffu, hi_s, sh));
+                big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, sh));
+            }
+            if (per_qhead) qsum = s_qpart[row];
+            else for (int h = 0; h < c.G; ++h) qsum += s_qpart[h];
+            const float two_e = 2.01f * big * qsum, width = (hi_s - lo) / (float)(SB_BINS - 1);
+            const float inv = 1.f / width;
+            const bool all = !(hi_s <= 3.4e38f) || !(lo >= -3.4e38f) || !(two_e <= 3.4e38f) || !(width > 0.f) || !(inv <= 3.4e38f) || !(width <= 3.4e38f);
+            float sure = INFINITY, least = -INFINITY;       // above the first: in; below the second: out
+            if (!all) {
+#pragma unroll
+                for (int j = 0; j < VECS; ++j)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if ((open >> (4 * j + u)) & 1u)
+                            atomicAdd(&s_hist[max(0, min(SB_BINS - 1, __float2int_rd((v[j][u] - lo) * inv)))], 1u);
+                __syncthreads();
+                // the bin t of the need-th largest: counts from the top
+                constexpr int PER = SB_BINS / NT;
+                int h[PER], cnt = 0;
+#pragma unroll
+                for (int u = 0; u < PER; u += 4) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(&s_hist[SB_BINS - 4 - (tid * PER + u)]);
+                    h[u] = w.w; h[u + 1] = w.z; h[u + 2] = w.y; h[u + 3] = w.x;
+                    cnt += w.x + w.y + w.z + w.w;
+                }
+                int above = cta_scan<NT>(cnt, s_part[0]);
+#pragma unroll
+                for (int u = 0; u < PER; ++u) {
+                    if (above < need && above + h[u] >= need) s_bin = SB_BINS - 1 - (tid * PER + u);
+                    above += h[u];
+                }
+                __syncthreads();
+                // Edges of the bin, moved outwards by 2 e and by more than what the binning rounds: (v - lo) inv and lo + t width
+                // are each within a few 2^-24 of |lo| + |hi| in terms of v.
+                const int t = s_bin;
+                const float slack = two_e + (fabsf(lo) + fabsf(hi_s)) * (1.f / 1048576.f);
+                if (t < SB_BINS - 1) sure = lo + (float)(t + 1) * width + slack;
+                if (t > 0) least = lo + (float)t * width - slack;
+            }
+            // ---- in, out or undecided --------------------------------------------------------------------------------
+            int winners = 0;
+#pragma unroll
+            for (int j = 0; j < VECS; ++j) {
+                const int at = (j * NT + tid) * 4;
+                if (at < n) {
+                    unsigned in = 0, und = 0;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if ((open >> (4 * j + u)) & 1u) {
+                            if (!all && v[j][u] > sure) in |= 1u << u;
+                            else if (all || v[j][u] >= least) und |= 1u << u;
+                        }
+                    }
+                    if (in) { atomicOr(&s_take[at >> 5], in << (at & 31)); winners += __popc(in); }
+                    if (und) {
+                        atomicOr(&s_cand[at >> 5], und << (at & 31));
+                        int place = atomicAdd(&s_ncand, __popc(und));
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if ((und >> u) & 1u) {
+                                if (place < SB_CAND) { s_x[place] = v[j][u]; s_blk[place] = at + u; }
+                                ++place;
+                            }
+                    }
+                }
+            }
+            winners = __reduce_add_sync(0xffffffffu, winners);
+            if (lane == 0 && winners) atomicAdd(&s_winners, winners);
+            __syncthreads();
+            const int ncand = s_ncand, want = need - s_winners;        // 1 <= want <= ncand
+            auto take = [&](int blk) { atomicOr(&s_take[blk >> 5], 1u << (blk & 31)); };
+            if (want == ncand) {
+                for (int w = tid; w < words; w += NT) s_take[w] |= s_cand[w];
+            } else if (!all && ncand <= SB_CAND) {
+                // ranks by x; the want-th and the next
+                int place = 0;
+                if (tid < ncand) {
+                    const float mine = s_x[tid];
+                    const int blk = s_blk[tid];
+                    for (int j = 0; j < ncand; ++j) place += s_x[j] > mine || (s_x[j] == mine && s_blk[j] < blk);
+                    if (place == want - 1) s_edge[0] = mine;
+                    if (place == want) s_edge[1] = mine;
+                }
+                __syncthreads();
+                const float edge = s_edge[0];
+                if (edge - s_edge[1] > two_e) {
+                    if (tid < ncand && place < want) take(s_blk[tid]);
+                } else {
+                    // 64 bits for those within 2e of the border; the others are certain
+                    for (int i = warp; i < ncand; i += NW) {
+                        const float d = s_x[i] - edge;
+                        unsigned long long k = d > 0.f ? ~0ull : 0ull;
+                        if (fabsf(d) <= two_e) k = wide_key(wide_score(p, b, h0, h1, s_blk[i], lane));
+                        if (lane == 0) s_key[i] = k;
+                    }
+                    __syncthreads();
+                    if (tid < ncand) {
+                        const unsigned long long k = s_key[tid];
+                        const int blk = s_blk[tid];
+                        int before = 0;
+                        for (int j = 0; j < ncand; ++j) before += s_key[j] > k || (s_key[j] == k && s_blk[j] < blk);
+                        if (before < want) take(blk);
+                    }
+                }
+            } else {
+                // ---- all undecided blocks in 64 bits; the want-th largest key eight bits at a time from the top --------
+                // (the keys lie over the row, whose fp32 scores are not read any more)
+                for (int w = warp; w < words; w += NW)
+                    for (unsigned m = s_cand[w]; m; m &= m - 1) {
+                        const int blk = w * 32 + __ffs(m) - 1;
+                        const unsigned long long k = wide_key(wide_score(p, b, h0, h1, blk, lane));
+                        if (lane == 0) keys[blk] = k;
+                    }
+                if (tid == 0) { s_prefix = 0ull; s_left = want; }
+                for (int shift = 56; shift >= 0; shift -= 8) {
+                    if (tid < 256) s_digit[tid] = 0;
+                    __syncthreads();
+                    const unsigned long long prefix = s_prefix;
+                    for (int i = tid; i < n; i += NT) {
+                        if (!((s_cand[i >> 5] >> (i & 31)) & 1u)) continue;
+                        const unsigned long long k = keys[i];
+                        if (shift == 56 || (k >> (shift + 8)) == prefix) atomicAdd(&s_digit[(unsigned)(k >> shift) & 255u], 1u);
+                    }
+                    __syncthreads();
+                    if (tid == 0) {
+                        int left = s_left, d = 255;
+                        while (d > 0 && (int)s_digit[d] < left) left -= s_digit[d--];
+                        s_prefix = (prefix << 8) | (unsigned)d;
+                        s_left = left;
+                    }
+                    __syncthreads();
+                }
+                // larger ones are in, and as many of the equal ones as are wanted, the lower first
+                const unsigned long long border = s_prefix;
+                const int ties = s_left;
+                constexpr int WPT = SB_MAX_BLOCKS / 32 / NT;
+                unsigned in[WPT], equal[WPT];
+                int mine = 0;
+#pragma unroll
+                for (int u = 0; u < WPT; ++u) {
+                    const int w = tid * WPT + u;
+                    in[u] = equal[u] = 0;
+                    if (w < words)
+                        for (unsigned m = s_cand[w]; m; m &= m - 1) {
+                            const unsigned long long k = keys[w * 32 + __ffs(m) - 1];
+                            if (k > border) in[u] |= m & (~m + 1u);
+                            else if (k == border) equal[u] |= m & (~m + 1u);
+                        }
+                    mine += __popc(equal[u]);
+                }
+                int before = cta_scan<NT>(mine, s_part[0]);
+#pragma unroll
+                for (int u = 0; u < WPT; ++u) {
+                    for (unsigned m = equal[u]; m; m &= m - 1) if (before++ < ties) in[u] |= m & (~m + 1u);
+                    if (tid * WPT + u < words) s_take[tid * WPT + u] |= in[u];
+                }
+            }
+            __syncthreads();
+        }
+        // ---- the chosen blocks in ascending order --------------------------------------------------------------------
+        constexpr int WPT = SB_MAX_BLOCKS / 32 / NT;
+        unsigned bits[WPT];
+        int mine = 0;
+#pragma unroll
+        for (int u = 0; u < WPT; ++u) {
+            bits[u] = tid * WPT + u < words ? s_take[tid * WPT + u] : 0u;
+            mine += __popc(bits[u]);
+        }
+        int pos = cta_scan<NT>(mine, s_part[1]);
+#pragma unroll
+        for (int u = 0; u < WPT; ++u)
+            for (unsigned m = bits[u]; m && pos < kk; m &= m - 1) out[pos++] = (tid * WPT + u) * 32 + __ffs(m) - 1;
+        __syncthreads();                                    // the next row uses the same arrays
+    }
 }
 
 // ---- attention over listed blocks ------------------------------------------------------------------------------
@@ -715,17 +813,6 @@ __device__ __forceinline__ void consume_block8(uint32_t ks, uint32_t vs, const u
         mma_f16_16816(acc.o[2 * u + 1], x1, y1, x3, y3, ph0, ph1);
         mma_f16_16816(acc.o[2 * u + 1], x1, y1, x3, y3, pl0, pl1);
     }
-}
-
-__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
-    uint32_t a;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
 }
 
 constexpr int BA_WARPS = 4;
@@ -926,7 +1013,8 @@ __global__ void __launch_bounds__(BA_WARPS * 32, 2) block_attn_kernel(const Bloc
         }
     }
     if (size == 1) return;
-    cluster_barrier();
+    cluster_arrive();
+    cluster_wait();
     const uint32_t amo = smem_u32(&s_mo[0][0]), am = smem_u32(s_m), al = smem_u32(s_l);
     for (int e = rank * NW * 32 + threadIdx.x; e < ncols * HEAD_DIM; e += size * NW * 32) {
         const int col = e >> 7, d = e & 127;
@@ -944,7 +1032,8 @@ __global__ void __launch_bounds__(BA_WARPS * 32, 2) block_attn_kernel(const Bloc
         if (p.out_bf16) reinterpret_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(r);
         else reinterpret_cast<float*>(p.out)[at] = r;
     }
-    cluster_barrier();                                      // nobody leaves while its shared memory is read
+    cluster_arrive();
+    cluster_wait();                                         // nobody leaves while its shared memory is read
 }
 
 }  // namespace tidal

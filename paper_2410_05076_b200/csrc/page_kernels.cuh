@@ -2,7 +2,6 @@
 // the rows of many tokens written through a slot map (kv_write_kernel).
 #pragma once
 
-#include <cooperative_groups.h>
 #include <cuda_fp8.h>
 
 #include "attn_kernels.cuh"
@@ -19,11 +18,13 @@ enum { STATUS_NO_PAGES = 8 };            // page_map: the request cannot be met,
 // push, which is free_pages[.] below F and the (. - F)-th page given back from F on. So every page is known from three
 // prefix sums over the sequences and nothing has to be moved before it is read.
 //
-// One launch of one thread-block cluster: every CTA computes the prefix sums and the checks for itself (a few
-// thousand lengths), the cluster's barrier separates all reads of what is written in place (num_free, the stack's upper
-// part) from the writes, and tables and slots are then dealt out over the cluster's threads.
-constexpr int PM_THREADS = 1024;
+// One launch. Every CTA computes the prefix sums and the checks for itself (a few thousand lengths, all in 32 bits: at most
+// 4096 x 262144 tokens) and takes its share of the pages and tokens. What is written in place does not meet
+// what is read: the stack is read below F and written from F on, a table is read below P(old) and for shrinking
+// sequences, and written from P(old) on for growing ones. The one word that may be both is num_free: the last CTA to have read it
+// writes it (an arrival count, nobody waits).
 constexpr int PM_PER = 4;                                   // sequences per thread
+constexpr int PM_THREADS = 1024, PM_THREADS_SMALL = 256;
 constexpr int PM_MAX_BATCH = PM_THREADS * PM_PER;
 
 struct PageMapParams {
@@ -38,6 +39,7 @@ struct PageMapParams {
     int* positions;
     int* token_offsets;
     int* status;
+    int* arrivals;                       // zero between launches
 };
 
 // The sequence that element `i` of a packed list belongs to: the last one that starts at or before it.
@@ -50,23 +52,20 @@ __device__ __forceinline__ int owner_of(const int* starts, int batch, int i) {
     return lo;
 }
 
-__global__ void __launch_bounds__(PM_THREADS) page_map_kernel(const PageMapParams p) {
-    namespace cg = cooperative_groups;
-    cg::cluster_group cluster = cg::this_cluster();
+template <int NT>
+__global__ void __launch_bounds__(NT) page_map_kernel(const PageMapParams p) {
     extern __shared__ int pm_smem[];
     int* s_tok = pm_smem;                                   // [batch + 1] prefix sums
     int* s_grow = s_tok + p.batch + 1;
     int* s_rel = s_grow + p.batch + 1;
-    __shared__ long long s_part[3][PM_THREADS / 32];
-    __shared__ int s_bad;
+    __shared__ int s_part[3][NT / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) s_bad = 0;
     pdl_wait();
     pdl_trigger();
-    __syncthreads();
 
-    const long long limit = (long long)p.max_pages * TILE;
-    long long v[PM_PER][3], sum[3] = {0, 0, 0};
+    const int F = *p.num_free;
+    const int limit = p.max_pages * TILE;                   // at most 262144
+    int v[PM_PER][3], sum[3] = {0, 0, 0};
     bool bad = false;
 #pragma unroll
     for (int u = 0; u < PM_PER; ++u) {
@@ -84,95 +83,98 @@ __global__ void __launch_bounds__(PM_THREADS) page_map_kernel(const PageMapParam
 #pragma unroll
         for (int i = 0; i < 3; ++i) sum[i] += v[u][i];
     }
-    if (bad) s_bad = 1;
-    long long inc[3];
+    int inc[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-        long long x = sum[i];
+        int x = sum[i];
 #pragma unroll
         for (int sh = 1; sh < 32; sh <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, x, sh);
+            const int y = __shfl_up_sync(0xffffffffu, x, sh);
             if (lane >= sh) x += y;
         }
         inc[i] = x;
         if (lane == 31) s_part[i][warp] = x;
     }
-    __syncthreads();
-    if (warp < 3) {
-        long long x = s_part[warp][lane];
+    bad = __syncthreads_or(bad);
+    int total[3], at[3];
 #pragma unroll
-        for (int sh = 1; sh < 32; sh <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, x, sh);
+    for (int i = 0; i < 3; ++i) {
+        int x = lane < NT / 32 ? s_part[i][lane] : 0;
+#pragma unroll
+        for (int sh = 1; sh < NT / 32; sh <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, sh);
             if (lane >= sh) x += y;
         }
-        s_part[warp][lane] = x;
+        total[i] = __shfl_sync(0xffffffffu, x, NT / 32 - 1);
+        const int before = __shfl_sync(0xffffffffu, x, max(warp - 1, 0));
+        at[i] = inc[i] - sum[i] + (warp > 0 ? before : 0);
     }
-    __syncthreads();
-    const long long T = s_part[0][31], N = s_part[1][31], R = s_part[2][31];
-    long long at[3];
-#pragma unroll
-    for (int i = 0; i < 3; ++i) at[i] = inc[i] - sum[i] + (warp > 0 ? s_part[i][warp - 1] : 0);
+    const int T = total[0], N = total[1], R = total[2];
 #pragma unroll
     for (int u = 0; u < PM_PER; ++u) {
         const int b = tid * PM_PER + u;
-        // (sums that pass 32 bits fail the checks below and are not used)
-        if (b <= p.batch) { s_tok[b] = (int)at[0]; s_grow[b] = (int)at[1]; s_rel[b] = (int)at[2]; }
+        if (b <= p.batch) { s_tok[b] = at[0]; s_grow[b] = at[1]; s_rel[b] = at[2]; }
 #pragma unroll
         for (int i = 0; i < 3; ++i) at[i] += v[u][i];
     }
-    if (tid == PM_THREADS - 1 && p.batch == PM_MAX_BATCH) { s_tok[p.batch] = (int)T; s_grow[p.batch] = (int)N; s_rel[p.batch] = (int)R; }
-    const long long F = *p.num_free;
-    const bool fits = F >= 0 && F <= p.num_pages && T <= p.max_tokens && F + R <= p.num_pages && N <= F + R;
+    if (tid == NT - 1 && p.batch == NT * PM_PER) { s_tok[p.batch] = T; s_grow[p.batch] = N; s_rel[p.batch] = R; }
+    const long long top = (long long)F + R;                 // the stack's height after the push
     __syncthreads();
     // the j-th page given back, in the order (sequence, logical page)
     auto released = [&](int j) -> int {
         const int b = owner_of(s_rel, p.batch, j);
         return p.page_table[(long long)b * p.max_pages + (p.new_lens[b] + TILE - 1) / TILE + (j - s_rel[b])];
     };
-    if (fits && !s_bad)
-        for (int j = tid; j < (int)R; j += PM_THREADS)
-            if ((unsigned)released(j) >= (unsigned)p.num_pages) s_bad = 1;
-    __syncthreads();
-    const bool ok = fits && !s_bad;
-    cluster.sync();                                         // everything that is overwritten below has been read
+    bool ok = !bad && F >= 0 && F <= p.num_pages && T <= p.max_tokens && top <= p.num_pages && N <= top;
+    if (ok && R > 0) {
+        for (int j = tid; j < R; j += NT) bad |= (unsigned)released(j) >= (unsigned)p.num_pages;
+        ok = !__syncthreads_or(bad);
+    }
 
-    const int gtid = (int)cluster.block_rank() * PM_THREADS + tid, gsize = (int)cluster.num_blocks() * PM_THREADS;
-    if (!ok) {
-        for (int t = gtid; t < p.max_tokens; t += gsize) { p.slots[t] = -1; if (p.positions) p.positions[t] = -1; }
-        if (p.token_offsets) for (int b = gtid; b <= p.batch; b += gsize) p.token_offsets[b] = 0;
-        if (gtid == 0) { *p.num_free_out = (int)F; atomicOr(p.status, STATUS_NO_PAGES); }
-        return;
-    }
-    const int top = (int)(F + R);
-    auto taken = [&](int i) -> int {                        // the i-th page taken
-        const int e = top - 1 - i;
-        return e < F ? p.free_pages[e] : released(e - (int)F);
-    };
-    for (int i = gtid; i < (int)N; i += gsize) {
-        const int b = owner_of(s_grow, p.batch, i);
-        const int page = taken(i);
-        if ((unsigned)page >= (unsigned)p.num_pages) atomicOr(p.status, STATUS_BAD_PAGE);
-        p.page_table[(long long)b * p.max_pages + (p.old_lens[b] + TILE - 1) / TILE + (i - s_grow[b])] = page;
-    }
-    for (int t = gtid; t < p.max_tokens; t += gsize) {
-        long long slot = -1;
-        int pos = -1;
-        if (t < (int)T) {
-            const int b = owner_of(s_tok, p.batch, t);
-            const int o = p.old_lens[b], held = (o + TILE - 1) / TILE;
-            pos = o + (t - s_tok[b]);
-            const int blk = pos / TILE;
-            const int page = blk < held ? p.page_table[(long long)b * p.max_pages + blk] : taken(s_grow[b] + blk - held);
-            if ((unsigned)page < (unsigned)p.num_pages) slot = (long long)page * TILE + (pos & (TILE - 1));
-            else atomicOr(p.status, STATUS_BAD_PAGE);
+    const int gtid = (int)blockIdx.x * NT + tid, gsize = (int)gridDim.x * NT;
+    if (ok) {
+        auto taken = [&](int i) -> int {                    // the i-th page taken
+            const int e = (int)top - 1 - i;
+            return e < F ? p.free_pages[e] : released(e - F);
+        };
+        for (int i = gtid; i < N; i += gsize) {
+            const int b = owner_of(s_grow, p.batch, i);
+            const int page = taken(i);
+            if ((unsigned)page >= (unsigned)p.num_pages) atomicOr(p.status, STATUS_BAD_PAGE);
+            p.page_table[(long long)b * p.max_pages + (p.old_lens[b] + TILE - 1) / TILE + (i - s_grow[b])] = page;
         }
-        p.slots[t] = slot;
-        if (p.positions) p.positions[t] = pos;
+        for (int t = gtid; t < p.max_tokens; t += gsize) {
+            long long slot = -1;
+            int pos = -1;
+            if (t < T) {
+                const int b = owner_of(s_tok, p.batch, t);
+                const int o = p.old_lens[b], held = (o + TILE - 1) / TILE;
+                pos = o + (t - s_tok[b]);
+                const int blk = pos / TILE;
+                const int page = blk < held ? p.page_table[(long long)b * p.max_pages + blk] : taken(s_grow[b] + blk - held);
+                if ((unsigned)page < (unsigned)p.num_pages) slot = (long long)page * TILE + (pos & (TILE - 1));
+                else atomicOr(p.status, STATUS_BAD_PAGE);
+            }
+            p.slots[t] = slot;
+            if (p.positions) p.positions[t] = pos;
+        }
+        // pages given back and not taken again stay on the stack: elements F .. F + R - N - 1, which nobody reads
+        for (int j = gtid; j < R - N; j += gsize) p.free_pages[F + j] = released(j);
+    } else {
+        for (int t = gtid; t < p.max_tokens; t += gsize) { p.slots[t] = -1; if (p.positions) p.positions[t] = -1; }
+        if (gtid == 0) atomicOr(p.status, STATUS_NO_PAGES);
     }
-    // pages given back and not taken again stay on the stack: elements F .. F + R - N - 1, which nobody reads
-    for (int j = gtid; j < (int)(R - N); j += gsize) p.free_pages[F + j] = released(j);
-    if (p.token_offsets) for (int b = gtid; b <= p.batch; b += gsize) p.token_offsets[b] = s_tok[b];
-    if (gtid == 0) *p.num_free_out = (int)(F + R - N);
+    if (p.token_offsets) for (int b = gtid; b <= p.batch; b += gsize) p.token_offsets[b] = ok ? s_tok[b] : 0;
+    if (tid == 0) {
+        bool last = gridDim.x == 1;
+        if (!last) {
+            int old;
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;\n" : "=r"(old) : "l"(p.arrivals) : "memory");
+            last = old == (int)gridDim.x - 1;
+            if (last) *p.arrivals = 0;
+        }
+        if (last) *p.num_free_out = ok ? (int)(top - N) : F;
+    }
 }
 
 // ---- rows of many tokens into the cache ------------------------------------------------------------------
@@ -193,8 +195,21 @@ struct KvWriteParams {
     int* status;
 };
 
+// Quotient in fp32, correctly rounded, where it matters for an E4M3 code: with r the correctly rounded reciprocal of s,
+// q0 = x r and the exact remainder x - q0 s, q0 + r (x - q0 s) rounds to x / s (P. Markstein, "Computation of elementary functions
+// on the IBM RISC System/6000 processor", 1990) as long as nothing leaves the range: s is between 2^-60 and 2^60, a
+// quotient of 1024 or more (infinities and NaN among them) keeps q0, which saturates all the same, and where a remainder
+// underflows the quotient is below 2^-40 and its code zero. 4 instructions instead of a division's dozen.
+__device__ __forceinline__ float quotient(float x, float s, float r) {
+    const float q0 = x * r;
+    const float q1 = fmaf(fmaf(-q0, s, x), r, q0);
+    return fabsf(q0) < 1024.f ? q1 : q0;
+}
+
 // code = the E4M3 value nearest to x / scale (the quotient in fp32, correctly rounded), saturated at +-448.
-__device__ __forceinline__ uint2 quantise8(uint4 w, float scale) {
+template <bool PLAIN>
+__device__ __forceinline__ uint2 quantise8(uint4 w, float scale, float inv) {
+    auto div = [&](float x) { return PLAIN ? __fdiv_rn(x, scale) : quotient(x, scale, inv); };
     const uint32_t in[4] = {w.x, w.y, w.z, w.w};
     uint32_t out[2];
 #pragma unroll
@@ -203,7 +218,7 @@ __device__ __forceinline__ uint2 quantise8(uint4 w, float scale) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const uint32_t x = in[2 * i + j];
-            const float lo = __fdiv_rn(__uint_as_float(x << 16), scale), hi = __fdiv_rn(__uint_as_float(x & 0xffff0000u), scale);
+            const float lo = div(__uint_as_float(x << 16)), hi = div(__uint_as_float(x & 0xffff0000u));
             half[j] = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
         }
         out[i] = half[0] | (half[1] << 16);
@@ -253,7 +268,9 @@ __global__ void __launch_bounds__(KW_WARPS * 32) kv_write_kernel(const KvWritePa
         else off += (s / p.max_ctx) * p.stride_b + (s % p.max_ctx) * p.stride_pos;
         if constexpr (KV8) {
             const float* sc = value ? p.v_scale : p.k_scale;
-            *reinterpret_cast<uint2*>(dst + off + piece * 8) = quantise8(row[i], sc ? __ldg(sc + head[i]) : 1.f);
+            const float scale = sc ? __ldg(sc + head[i]) : 1.f;
+            const bool usual = scale >= 0x1p-60f && scale <= 0x1p60f;
+            *reinterpret_cast<uint2*>(dst + off + piece * 8) = usual ? quantise8<false>(row[i], scale, __frcp_rn(scale)) : quantise8<true>(row[i], scale, 0.f);
         } else {
             *reinterpret_cast<uint4*>(dst + 2 * off + piece * 16) = row[i];
         }

@@ -55,12 +55,6 @@ struct tidal_ctx {
     void* state = nullptr;
     int state_rows = 0;                         // capacity in (sequence, head) rows
     int* status = nullptr;                      // device word, sticky
-    // Scratch of the block selection. It grows by doubling, and what it outgrows is kept until the context goes:
-    // graphs that the caller captured may still name it.
-    void* blk_ws = nullptr;
-    size_t blk_ws_bytes = 0;
-    void* blk_old[64] = {};
-    int blk_old_count = 0;
     int out_bf16 = 0;                           // outputs are written as bf16 instead of fp32
     int attend_newest = 0;                      // sparse layers also attend the newest token (not in the paper)
     int cursor_set = 0;                         // which of the sets of pool cursors the last attention launch used
@@ -71,6 +65,7 @@ struct tidal_ctx {
     cudaEvent_t ev_fork = nullptr, ev_join = nullptr;
     int split_select = 1;
     int layer_overlap = 1;                      // layers of a step may stream their inputs while the layer before them finishes
+    int select_clusters[2][17] = {};            // clusters of 1 .. 16 CTAs that are resident together: block selection, 256 and 512 threads
     int64_t launches = 0;
     // Whole steps are recorded once as CUDA graphs (programmatic dependent launches included) and
     // replayed while every host-visible argument stays the same: one launch per step instead of one
@@ -768,29 +763,6 @@ void remember_last(tidal_ctx* ctx) {
 }
 
 // ---- block-sparse operators --------------------------------------------------------------------------
-// Scratch of a block selection: score rows, the largest bound of every chunk, and per index head the keys and blocks
-// of a candidate list that does not fit shared memory.
-struct BlockWs {
-    size_t scores, amax, wide, wide_blk, total;
-    long long stride;
-    int max_blocks, chunks;
-};
-
-BlockWs block_ws_layout(const tidal_kv_t* kv, int rows, int Hi) {
-    BlockWs w;
-    w.max_blocks = (kv->max_ctx_len + TILE - 1) / TILE;
-    w.stride = (long long)align_up((size_t)w.max_blocks, TB_PER);
-    w.chunks = (w.max_blocks + BS_BLOCKS - 1) / BS_BLOCKS;
-    const size_t B = (size_t)kv->batch;
-    size_t at = 0;
-    w.scores = at;   at += align_up(B * rows * w.stride * sizeof(float), 256);
-    w.amax = at;     at += align_up(B * kv->num_kv_heads * w.chunks * sizeof(float), 256);
-    w.wide = at;     at += align_up(B * Hi * w.max_blocks * sizeof(unsigned long long), 256);
-    w.wide_blk = at; at += align_up(B * Hi * w.max_blocks * sizeof(int), 256);
-    w.total = at;
-    return w;
-}
-
 // The context's device for the length of a call; the caller's own is current again afterwards.
 struct DeviceScope {
     int before = -1;
@@ -803,33 +775,38 @@ struct DeviceScope {
     ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
 };
 
-tidal_status_t ensure_block_ws(tidal_ctx* ctx, size_t bytes, const cudaStream_t* st) {
-    if (ctx->blk_ws_bytes >= bytes) return TIDAL_OK;
-    if (st) {                                   // nothing may be allocated into a capture
-        cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-        if (cudaStreamIsCapturing(*st, &cs) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
-        if (cs != cudaStreamCaptureStatusNone) return TIDAL_ERR_NOMEM;
-    }
-    if (ctx->blk_ws && ctx->blk_old_count == (int)(sizeof ctx->blk_old / sizeof ctx->blk_old[0])) return TIDAL_ERR_NOMEM;
-    const size_t want = std::max(bytes, 2 * ctx->blk_ws_bytes);
-    void* p = nullptr;
-    if (cudaMalloc(&p, want) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
-    if (ctx->blk_ws) ctx->blk_old[ctx->blk_old_count++] = ctx->blk_ws;
-    ctx->blk_ws = p;
-    ctx->blk_ws_bytes = want;
-    return TIDAL_OK;
-}
-
 constexpr int BA_MAX_CLUSTER = 16;
+constexpr size_t SB_SMEM_MAX = sb_smem(SB_MAX_BLOCKS, 1);
+
+// How many clusters of 1 .. 16 CTAs of a kernel the GPU holds at once (the SMs of a processing cluster differ from chip to chip).
+template <typename K>
+void count_clusters(K kernel, int threads, size_t smem, int (&out)[17]) {
+    for (int s = 1; s <= 16; ++s) {
+        cudaLaunchConfig_t cfg;
+        std::memset(&cfg, 0, sizeof cfg);
+        cfg.gridDim = dim3(s, 1, 1);
+        cfg.blockDim = dim3(threads, 1, 1);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = s; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&out[s], kernel, &cfg) != cudaSuccess) { cudaGetLastError(); out[s] = 0; }
+    }
+}
 
 bool prepare_block_kernels() {
     auto wide = [](const void* k) {
         return cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
     };
-    return wide((const void*)block_attn_kernel<false>) && wide((const void*)block_attn_kernel<true>) &&
+    return wide((const void*)block_select_kernel<256>) && wide((const void*)block_select_kernel<512>) &&
+           cudaFuncSetAttribute(block_select_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SB_SMEM_MAX) == cudaSuccess &&
+           cudaFuncSetAttribute(block_select_kernel<512>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SB_SMEM_MAX) == cudaSuccess &&
+           wide((const void*)block_attn_kernel<false>) && wide((const void*)block_attn_kernel<true>) &&
            cudaFuncSetAttribute(block_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ba_smem<false>()) == cudaSuccess &&
            cudaFuncSetAttribute(block_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ba_smem<true>()) == cudaSuccess &&
-           cudaFuncSetAttribute(page_map_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (PM_MAX_BATCH + 1) * (int)sizeof(int)) == cudaSuccess;
+           cudaFuncSetAttribute(page_map_kernel<PM_THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (PM_MAX_BATCH + 1) * (int)sizeof(int)) == cudaSuccess;
 }
 
 void fill_block_cache(BlockCache& c, const tidal_ctx* ctx, const tidal_kv_t* kv, int bound_blocks) {
@@ -920,6 +897,8 @@ tidal_status_t tidal_create(tidal_ctx_t** out, int device, size_t workspace_byte
     const bool compact_ok = cudaFuncSetAttribute(topk_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)compact_smem) == cudaSuccess;
     if (!prepare_block_kernels()) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     if (d0 <= 0 || d1 <= 0 || d2 < d1 || s0 <= 0 || s1 < s0 || e0 < d0 || e1 < d1 || e2 < s0 || !topk_ok || !compact_ok || !split_ok) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
+    count_clusters(block_select_kernel<256>, 256, 64 * 1024, ctx->select_clusters[0]);
+    count_clusters(block_select_kernel<512>, 512, 64 * 1024, ctx->select_clusters[1]);
     ctx->dense_slots = std::min(d0, d1);
     ctx->sparse_slots = s0;
     if (cudaMalloc((void**)&ctx->status, 256) != cudaSuccess || cudaMemset(ctx->status, 0, 256) != cudaSuccess) {
@@ -942,8 +921,6 @@ tidal_status_t tidal_destroy(tidal_ctx_t* ctx) {
     if (ctx->ev_fork) cudaEventDestroy(ctx->ev_fork);
     if (ctx->ev_join) cudaEventDestroy(ctx->ev_join);
     if (ctx->ws) cudaFree(ctx->ws);
-    if (ctx->blk_ws) cudaFree(ctx->blk_ws);
-    for (int i = 0; i < ctx->blk_old_count; ++i) cudaFree(ctx->blk_old[i]);
     if (ctx->state) cudaFree(ctx->state);
     if (ctx->status) cudaFree(ctx->status);
     delete ctx;
@@ -962,8 +939,6 @@ tidal_status_t tidal_reserve(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t k, 
     if (cudaSetDevice(ctx->device) != cudaSuccess) return TIDAL_ERR_CUDA;
     const tidal_status_t rs = ensure_side_stream(ctx);       // a later step's selection layers may use it
     if (rs != TIDAL_OK) return rs;
-    const tidal_status_t rb = ensure_block_ws(ctx, block_ws_layout(kv, kv->num_q_heads, kv->num_q_heads).total, nullptr);
-    if (rb != TIDAL_OK) return rb;
     return ensure_all(ctx, kv, ws_bytes_for(kv, k, num_layers_host));
 }
 
@@ -1350,8 +1325,13 @@ tidal_status_t tidal_page_map(tidal_ctx_t* ctx, int32_t batch, const int32_t* ol
     p.old_lens = old_lens; p.new_lens = new_lens; p.page_table = page_table; p.free_pages = free_pages;
     p.num_free = num_free; p.num_free_out = num_free_out;
     p.slots = (long long*)slots; p.positions = positions; p.token_offsets = token_offsets; p.status = ctx->status;
-    const int cluster = max_tokens > 8 * PM_THREADS ? 8 : 1;
-    return launch_block(ctx, page_map_kernel, p, cluster, PM_THREADS, 3 * ((size_t)batch + 1) * sizeof(int), cluster, (cudaStream_t)stream);
+    p.arrivals = ctx->status + 32;                           // (a line of its own behind the status word, zeroed with it at creation)
+    const size_t smem = 3 * ((size_t)batch + 1) * sizeof(int);
+    // a CTA for every 2048 tokens; one of 256 threads is enough for a decode step's
+    const int grid = std::min(ctx->sm_count, (max_tokens + 2047) / 2048);
+    if (grid <= 1 && batch <= PM_THREADS_SMALL * PM_PER && max_tokens <= 4 * PM_THREADS_SMALL)
+        return launch_block(ctx, page_map_kernel<PM_THREADS_SMALL>, p, 1, PM_THREADS_SMALL, smem, 0, (cudaStream_t)stream);
+    return launch_block(ctx, page_map_kernel<PM_THREADS>, p, std::max(grid, 1), PM_THREADS, smem, 0, (cudaStream_t)stream);
 }
 
 tidal_status_t tidal_kv_write(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t num_tokens, const void* k_new, const void* v_new,
@@ -1409,34 +1389,32 @@ tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     const int Hi = hi_of(kv, granularity);
     if (Hi <= 0 || m > MAX_CTX / TILE) return TIDAL_ERR_INVALID;
     const bool per_qhead = granularity == TIDAL_SEL_PER_QHEAD;
-    const int rows = per_qhead ? kv->num_q_heads : kv->num_kv_heads;
-    const BlockWs w = block_ws_layout(kv, rows, Hi);
-    const long long grid = (long long)kv->batch * kv->num_kv_heads * w.chunks;
-    if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
     DeviceScope dev(ctx->device);
     if (!dev.ok) return TIDAL_ERR_CUDA;
-    cudaStream_t st = (cudaStream_t)stream;
-    if ((rc = ensure_block_ws(ctx, w.total, &st)) != TIDAL_OK) return rc;
-    char* ws = (char*)ctx->blk_ws;
-    ScoreParams s;
-    fill_block_cache(s.c, ctx, kv, bound_blocks);
-    s.q = (const __nv_bfloat16*)q;
-    s.bounds = (const __nv_bfloat16*)bounds;
+    SelectBlocksParams p;
+    fill_block_cache(p.c, ctx, kv, bound_blocks);
+    p.q = (const __nv_bfloat16*)q;
+    p.bounds = (const __nv_bfloat16*)bounds;
     // one KV head's factor changes no order: it matters only where several KV heads are added up
-    s.k_scale = kv->kv_dtype == TIDAL_KV_FP8_E4M3 && granularity == TIDAL_SEL_SHARED ? kv->k_scale : nullptr;
-    s.group_sum = !per_qhead;
-    s.scores = (float*)(ws + w.scores); s.stride = w.stride;
-    s.amax = (float*)(ws + w.amax); s.chunks = w.chunks;
-    if ((rc = launch_block(ctx, block_score_kernel, s, (int)grid, BS_WARPS * 32, 0, 0, st)) != TIDAL_OK) return rc;
-    TopBlocksParams t;
-    t.c = s.c; t.q = s.q; t.bounds = s.bounds; t.k_scale = s.k_scale;
-    t.scores = s.scores; t.stride = s.stride; t.amax = s.amax; t.chunks = s.chunks;
-    t.rows = rows; t.Hi = Hi; t.m = m; t.keep_first = keep_first; t.keep_last = keep_last;
-    t.idx = idx; t.idx_count = idx_count;
-    t.wide = (unsigned long long*)(ws + w.wide); t.wide_blk = (int*)(ws + w.wide_blk);
-    // 16 blocks per thread: up to 4096 blocks fit 256 threads, whose barriers and scans are shorter
-    if (w.max_blocks <= 256 * TB_PER) return launch_block(ctx, block_topk_kernel<256>, t, kv->batch * Hi, 256, 0, 0, st);
-    return launch_block(ctx, block_topk_kernel<1024>, t, kv->batch * Hi, 1024, 0, 0, st);
+    p.k_scale = kv->kv_dtype == TIDAL_KV_FP8_E4M3 && granularity == TIDAL_SEL_SHARED ? kv->k_scale : nullptr;
+    p.mode = granularity; p.m = m; p.keep_first = keep_first; p.keep_last = keep_last;
+    p.npad = (int)align_up((size_t)p.c.max_blocks, 32);
+    p.idx = idx; p.idx_count = idx_count;
+    const int items = granularity == TIDAL_SEL_SHARED ? kv->batch : kv->batch * kv->num_kv_heads;
+    const int rows = per_qhead ? p.c.G : 1;
+    // Few items over long contexts: 512 threads with an SM each. Otherwise 256, two CTAs per SM (see the kernel).
+    const int wide = p.c.max_blocks > 8192 || (items <= 16 && p.c.max_blocks > 2048);
+    const int threads = wide ? 512 : 256;
+    // The largest cluster that the item has work for (16 blocks per warp, a row to rank per CTA) with all items resident
+    // together; and large enough that the rows that a CTA owns fit its shared memory.
+    const int tiles = (p.c.max_blocks + 15) / 16, useful = std::max(rows, (tiles + threads / 32 - 1) / (threads / 32));
+    auto per_cta = [&](int s) { return (rows + s - 1) / s; };
+    int cluster = std::min(SB_MAX_CLUSTER, useful);
+    while (cluster > 1 && ctx->select_clusters[wide][cluster] < items) --cluster;
+    while (cluster < rows && sb_smem(p.npad, per_cta(cluster)) > SB_SMEM_MAX) ++cluster;
+    const size_t smem = sb_smem(p.npad, per_cta(cluster));
+    if (wide) return launch_block(ctx, block_select_kernel<512>, p, items * cluster, 512, smem, cluster, (cudaStream_t)stream);
+    return launch_block(ctx, block_select_kernel<256>, p, items * cluster, 256, smem, cluster, (cudaStream_t)stream);
 }
 
 tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const void* q, const int32_t* idx, const int32_t* idx_count,

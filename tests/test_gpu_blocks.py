@@ -716,12 +716,10 @@ def test_a_serving_loop(td, fp8, gran):
 
 @pytest.mark.parametrize("fp8", [False, True])
 def test_a_captured_step_replayed_over_changing_lengths(fp8):
-    """The whole step as one graph from a fresh context's first call on; eager calls of another shape, for which the context's
-    scratch grows, come in between."""
+    """The whole step as one graph from a fresh context's first call on; eager calls of another shape come in between."""
     t = binding.Tidal(0)
     try:
         s = Serving(t, 4, 8, 2, fp8, total=40, width=20, cap=400)
-        t.reserve(s.lay, 16)
         side = torch.cuda.Stream()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.stream(side):
@@ -743,27 +741,28 @@ def test_a_captured_step_replayed_over_changing_lengths(fp8):
         t.close()
 
 
-def test_scratch_is_not_allocated_into_a_capture():
+def test_the_first_call_of_a_context_can_be_captured():
+    """No call here allocates: nothing has to be reserved before a capture."""
     t = binding.Tidal(0)
     try:
-        lay = make([400], 8, 2, "hnd", seed=1)
-        q, bounds = query(lay, 1), t.block_bounds(lay)
+        lay = make([40000], 8, 2, "hnd", seed=1)
+        q = query(lay, 1)
+        bounds = torch.zeros(binding.block_bounds_shape(lay), dtype=torch.bfloat16, device=DEV)
         idx, cnt = torch.zeros(1, 8, 4, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
-        x = torch.zeros(8, device=DEV)
+        out = torch.zeros(1, 8, D, device=DEV)
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         side = torch.cuda.Stream()
         with torch.cuda.stream(side):
             with torch.cuda.graph(graph, stream=side):
-                x += 1
-                with pytest.raises(binding.TidalError) as e:
-                    t.block_select(lay, bounds, q, 4, idx=idx, idx_count=cnt)
-                assert e.value.status == binding.ERR_NOMEM
+                t.block_bounds(lay, bounds)
+                t.block_select(lay, bounds, q, 4, idx=idx, idx_count=cnt)
+                t.block_attn(lay, q, idx, cnt, out=out)
         graph.replay()
         torch.cuda.synchronize()
-        assert (x == 1).all()
-        t.block_select(lay, bounds, q, 4, idx=idx, idx_count=cnt)
         assert torch.equal(idx.cpu(), ref_select(lay, q, 4, 0, 0, 0)[0])
+        ref, tol = ref_attn(lay, q, idx.cpu())
+        close(out, ref, tol, "captured")
         del graph
     finally:
         t.close()

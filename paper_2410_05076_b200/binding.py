@@ -1,4 +1,5 @@
-"""Thin ctypes binding of libtidal.so (same names as include/tidal.h).
+"""Thin binding of libtidal.so (same names as include/tidal.h): ctypes, and for the calls whose kernels take only a few
+microseconds the C++ of csrc/fast_call.cpp.
 
 Argument marshalling only: every step of the attention path runs in the CUDA
 kernels behind the C-ABI. PyTorch supplies device memory and the current
@@ -56,11 +57,12 @@ class TidalError(RuntimeError):
 
 
 _lib = None
+_fast = None             # csrc/fast_call.cpp: the block-sparse and page calls, whose kernels take a few microseconds
 
 
 def load() -> C.CDLL:
     """Load libtidal.so, building it with nvcc first if it is missing or stale."""
-    global _lib
+    global _lib, _fast
     if _lib is not None:
         return _lib
     path = _build.LIB
@@ -123,7 +125,10 @@ def load() -> C.CDLL:
     L.tidal_launch_count.restype = I64
     L.tidal_strerror.argtypes = [I32]
     L.tidal_strerror.restype = C.c_char_p
-    _lib = L
+    from . import _fast_call as fast
+    fast.init(*[C.cast(f, P).value for f in (L.tidal_page_map, L.tidal_kv_write, L.tidal_block_bounds, L.tidal_block_select,
+                                             L.tidal_block_attn)], C.sizeof(tidal_kv_t))
+    _lib, _fast = L, fast
     return L
 
 
@@ -168,21 +173,6 @@ def _check(status: int, what: str) -> None:
         raise TidalError(status, what)
 
 
-def _need(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, device: int, shape=None, contiguous: bool = True) -> int:
-    """Address of a tensor that a call reads or writes, after the checks that the C side cannot make (0 for None)."""
-    if t is None:
-        return 0
-    if t.dtype is not dtype:
-        raise ValueError(f"{name}: {dtype} is wanted, got {t.dtype}")
-    if t.get_device() != device:
-        raise ValueError(f"{name}: a tensor on cuda:{device} is wanted, got one on {t.device}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(shape)} is wanted, got {tuple(t.shape)}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous tensor is wanted")
-    return t.data_ptr()
-
-
 def block_bounds_shape(layer) -> tuple:
     """Shape of the bf16 tensor of a cache's key bounds: one entry per physical page of a paged cache, one per 16
     positions of each sequence of a contiguous one (for its max_ctx_len; a larger third dimension is fine)."""
@@ -217,6 +207,10 @@ class Tidal:
         _check(self.lib.tidal_create(C.byref(self.ctx), device, workspace_bytes), "tidal_create")
         self.device = device
         self.out_dtype = torch.float32
+
+    @property
+    def _handle(self) -> int:
+        return self.ctx.value or 0
 
     def close(self) -> None:
         if getattr(self, "ctx", None) and self.ctx.value:
@@ -365,8 +359,7 @@ class Tidal:
 
     # ---- paged caches filled on the device, block-sparse attention ------------------------------------------------
 
-    def _stream(self) -> int:
-        return torch.cuda.current_stream(self.device).cuda_stream
+    # (arguments are checked and the current stream of the context's device is looked up in csrc/fast_call.cpp)
 
     def page_map(self, old_lens: torch.Tensor, new_lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor,
                  num_free: torch.Tensor, slots: torch.Tensor, num_free_out: Optional[torch.Tensor] = None,
@@ -377,46 +370,18 @@ class Tidal:
         last. num_free_out receives the new count (default: num_free itself); positions (int32 [max_tokens])
         and token_offsets (int32 [B + 1]) are optional outputs. Returns slots. A request that does not fit changes
         nothing and shows in device_status() as ERR_PAGES."""
-        i32, dev = torch.int32, self.device
-        out = num_free if num_free_out is None else num_free_out
-        B, cap = old_lens.numel(), slots.numel()
-        if page_table.dim() != 2 or page_table.shape[0] != B:
-            raise ValueError(f"page_table: [{B}, pages] is wanted, got {tuple(page_table.shape)}")
-        if num_free.numel() != 1 or out.numel() != 1:
-            raise ValueError("num_free, num_free_out: one element is wanted")
-        _check(self.lib.tidal_page_map(
-            self.ctx, B, _need(old_lens, "old_lens", i32, dev), _need(new_lens, "new_lens", i32, dev, (B,)),
-            _need(page_table, "page_table", i32, dev), page_table.shape[1], free_pages.numel(),
-            _need(free_pages, "free_pages", i32, dev), _need(num_free, "num_free", i32, dev),
-            _need(out, "num_free_out", i32, dev), cap, _need(slots, "slots", torch.int64, dev),
-            _need(positions, "positions", i32, dev, (cap,)), _need(token_offsets, "token_offsets", i32, dev, (B + 1,)),
-            self._stream()), "tidal_page_map")
+        rc = _fast.page_map(self._handle, self.device, old_lens, new_lens, page_table, free_pages, num_free, slots, num_free_out,
+                            positions, token_offsets)
+        if rc:
+            raise TidalError(rc, "tidal_page_map")
         return slots
 
     def kv_write(self, layer, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor) -> None:
         """Write the rows of T tokens (bf16 [T, Hkv, d]; only the two inner dimensions have to be contiguous) at their slots
         (int64 [T]; -1: skipped) of the layer's cache; an FP8 cache quantises them with its scales."""
-        s = kv_struct(layer)
-        T = slots.numel()
-        for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-            if t.shape != (T, s.num_kv_heads, s.head_dim):
-                raise ValueError(f"{name}: shape {(T, s.num_kv_heads, s.head_dim)} is wanted, got {tuple(t.shape)}")
-            if T and (t.stride(2) != 1 or (t.stride(1) != s.head_dim and s.num_kv_heads > 1)):
-                raise ValueError(f"{name}: the rows of a token have to be contiguous")
-        bf = torch.bfloat16
-        _check(self.lib.tidal_kv_write(
-            self.ctx, C.byref(s), T, _need(k_new, "k_new", bf, self.device, None, False),
-            _need(v_new, "v_new", bf, self.device, None, False), k_new.stride(0), v_new.stride(0),
-            _need(slots, "slots", torch.int64, self.device), self._stream()), "tidal_kv_write")
-
-    @staticmethod
-    def _bound_blocks(s: tidal_kv_t, bounds: torch.Tensor) -> int:
-        paged = s.kv_layout == KV_PAGED
-        blocks = bounds.shape[0 if paged else 2] if bounds.dim() == (4 if paged else 5) else -1
-        want = (blocks, s.num_kv_heads, 2, s.head_dim) if paged else (s.batch, s.num_kv_heads, blocks, 2, s.head_dim)
-        if bounds.shape != want:
-            raise ValueError(f"bounds: shape {want} is wanted, got {tuple(bounds.shape)}")
-        return blocks
+        rc = _fast.kv_write(self._handle, self.device, kv_struct(layer), k_new, v_new, slots)
+        if rc:
+            raise TidalError(rc, "tidal_kv_write")
 
     def block_bounds(self, layer, bounds: Optional[torch.Tensor] = None, start_lens: Optional[torch.Tensor] = None,
                      max_new: int = 0) -> torch.Tensor:
@@ -426,10 +391,9 @@ class Tidal:
         s = kv_struct(layer)
         if bounds is None:
             bounds = torch.zeros(block_bounds_shape(s), dtype=torch.bfloat16, device=f"cuda:{self.device}")
-        _check(self.lib.tidal_block_bounds(
-            self.ctx, C.byref(s), _need(start_lens, "start_lens", torch.int32, self.device, (s.batch,)), max_new,
-            _need(bounds, "bounds", torch.bfloat16, self.device), self._bound_blocks(s, bounds), self._stream()),
-            "tidal_block_bounds")
+        rc = _fast.block_bounds(self._handle, self.device, s, bounds, start_lens, max_new)
+        if rc:
+            raise TidalError(rc, "tidal_block_bounds")
         return bounds
 
     def block_select(self, layer, bounds: torch.Tensor, q: torch.Tensor, m: int, granularity: int = SEL_PER_QHEAD,
@@ -437,32 +401,26 @@ class Tidal:
                      idx_count: Optional[torch.Tensor] = None):
         """The m blocks per index head with the largest upper bound of their logits, the first keep_first and the last
         keep_last blocks among them. Returns (idx int32 [B, Hi, m] ascending and -1 padded, idx_count int32 [B])."""
-        s, dev = kv_struct(layer), self.device
-        hi = {SEL_PER_QHEAD: s.num_q_heads, SEL_PER_KVHEAD: s.num_kv_heads, SEL_SHARED: 1}.get(granularity, 1)
+        s = kv_struct(layer)
         if idx is None:
+            hi = {SEL_PER_QHEAD: s.num_q_heads, SEL_PER_KVHEAD: s.num_kv_heads, SEL_SHARED: 1}.get(granularity, 1)
             idx = torch.empty(s.batch, hi, max(m, 1), dtype=torch.int32, device=q.device)
         if idx_count is None:
             idx_count = torch.empty(s.batch, dtype=torch.int32, device=q.device)
-        _check(self.lib.tidal_block_select(
-            self.ctx, C.byref(s), _need(q, "q", torch.bfloat16, dev, (s.batch, s.num_q_heads, s.head_dim)),
-            _need(bounds, "bounds", torch.bfloat16, dev), self._bound_blocks(s, bounds), m, granularity, keep_first,
-            keep_last, _need(idx, "idx", torch.int32, dev, (s.batch, hi, max(m, 1))),
-            _need(idx_count, "idx_count", torch.int32, dev, (s.batch,)), self._stream()), "tidal_block_select")
+        rc = _fast.block_select(self._handle, self.device, s, bounds, q, m, granularity, keep_first, keep_last, idx, idx_count)
+        if rc:
+            raise TidalError(rc, "tidal_block_select")
         return idx, idx_count
 
     def block_attn(self, layer, q: torch.Tensor, idx: torch.Tensor, idx_count: Optional[torch.Tensor] = None,
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention over the blocks listed in idx (int32 [B, Hi, m], block_select's or any other)."""
-        s, dev = kv_struct(layer), self.device
-        shape = (s.batch, s.num_q_heads, s.head_dim)
+        s = kv_struct(layer)
         if out is None:
-            out = torch.empty(shape, dtype=self.out_dtype, device=q.device)
-        if idx.dim() != 3 or idx.shape[0] != s.batch:
-            raise ValueError(f"idx: [{s.batch}, Hi, m] is wanted, got {tuple(idx.shape)}")
-        _check(self.lib.tidal_block_attn(
-            self.ctx, C.byref(s), _need(q, "q", torch.bfloat16, dev, shape), _need(idx, "idx", torch.int32, dev),
-            _need(idx_count, "idx_count", torch.int32, dev, (s.batch,)), idx.shape[2], idx.shape[1],
-            _need(out, "out", self.out_dtype, dev, shape), self._stream()), "tidal_block_attn")
+            out = torch.empty(s.batch, s.num_q_heads, s.head_dim, dtype=self.out_dtype, device=q.device)
+        rc = _fast.block_attn(self._handle, self.device, s, q, idx, idx_count, out, self.out_dtype is torch.bfloat16)
+        if rc:
+            raise TidalError(rc, "tidal_block_attn")
         return out
 
     def device_status(self) -> int:

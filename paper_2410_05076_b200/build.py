@@ -1,9 +1,11 @@
-"""Build libtidal.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Build libtidal.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _fast_call.so (tensors in, C calls out; see
+csrc/fast_call.cpp) with g++ against the installed torch."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -12,20 +14,42 @@ SOURCES = ["tidal_api.cu"]
 DEPS = ["tidal_api.cu", "attn_kernels.cuh", "block_kernels.cuh", "page_kernels.cuh", "split_select_kernels.cuh", "topk_kernels.cuh", os.path.join("..", "..", "include", "tidal.h")]
 
 
+FAST = os.path.join(HERE, "_fast_call.so")
+FAST_DEPS = ["fast_call.cpp", os.path.join("..", "..", "include", "tidal.h")]
+
+
 def nvcc_path() -> str:
     cand = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "bin", "nvcc")
     return cand if os.path.exists(cand) else "nvcc"
 
 
-def is_stale() -> bool:
-    if not os.path.exists(LIB):
+def _older(target: str, deps) -> bool:
+    if not os.path.exists(target):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(os.path.join(CSRC, d)) > t for d in DEPS)
+    t = os.path.getmtime(target)
+    return any(os.path.getmtime(os.path.join(CSRC, d)) > t for d in deps)
+
+
+def is_stale() -> bool:
+    return _older(LIB, DEPS) or _older(FAST, FAST_DEPS)
+
+
+def _build_fast() -> None:
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
+    tmp = FAST + f".tmp{os.getpid()}"
+    subprocess.check_call(
+        ["g++", "-O2", "-std=c++20", "-shared", "-fPIC", "-fvisibility=hidden", f"-I{os.path.join(root, 'include')}",
+         f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}", "-o", tmp, os.path.join(CSRC, "fast_call.cpp"),
+         f"-L{os.path.join(root, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
+    os.replace(tmp, FAST)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not is_stale():
+    if force or _older(FAST, FAST_DEPS):
+        _build_fast()
+    if not force and not _older(LIB, DEPS):
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",

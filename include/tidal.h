@@ -343,7 +343,9 @@ tidal_status_t tidal_block_bounds(tidal_ctx_t *ctx, const tidal_kv_t *kv, const 
  * with bounds that are not finite have an unspecified rank.
  *   idx       int32 [batch, Hi, m]: block numbers in ascending order, padded with -1.
  *   idx_count int32 [batch] or NULL: receives m'.
- * m <= 16384. Uses no scratch memory. */
+ * m <= 16384. With max_ctx_len <= 16384 no scratch memory is used; beyond that it is the context's and may grow inside the
+ * call unless `stream` is being captured (TIDAL_ERR_NOMEM then; tidal_reserve provides it). Graphs captured earlier stay
+ * valid when it grows. */
 tidal_status_t tidal_block_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const void *q, const void *bounds, int32_t bound_blocks,
                                   int32_t m, int32_t granularity, int32_t keep_first, int32_t keep_last, int32_t *idx,
                                   int32_t *idx_count, void *stream);

@@ -15,7 +15,9 @@
 #include <new>
 
 #include "attn_kernels.cuh"
+#include "block_attn_kernels.cuh"
 #include "block_kernels.cuh"
+#include "block_select_kernels.cuh"
 #include "page_kernels.cuh"
 #include "split_select_kernels.cuh"
 #include "topk_kernels.cuh"
@@ -55,6 +57,12 @@ struct tidal_ctx {
     void* state = nullptr;
     int state_rows = 0;                         // capacity in (sequence, head) rows
     int* status = nullptr;                      // device word, sticky
+    // Scores of the block selection over long contexts. It grows by doubling, and what it outgrows is kept until the context
+    // goes: graphs that the caller captured may still name it.
+    void* blk_ws = nullptr;
+    size_t blk_ws_bytes = 0;
+    void* blk_old[64] = {};
+    int blk_old_count = 0;
     int out_bf16 = 0;                           // outputs are written as bf16 instead of fp32
     int attend_newest = 0;                      // sparse layers also attend the newest token (not in the paper)
     int cursor_set = 0;                         // which of the sets of pool cursors the last attention launch used
@@ -65,7 +73,8 @@ struct tidal_ctx {
     cudaEvent_t ev_fork = nullptr, ev_join = nullptr;
     int split_select = 1;
     int layer_overlap = 1;                      // layers of a step may stream their inputs while the layer before them finishes
-    int select_clusters[2][17] = {};            // clusters of 1 .. 16 CTAs that are resident together: block selection, 256 and 512 threads
+    int select_clusters[17] = {};               // clusters of 1 .. 16 CTAs that are resident together: block selection
+    int attn_clusters[17] = {};                 // the same for eight-warp CTAs of the block attention
     int64_t launches = 0;
     // Whole steps are recorded once as CUDA graphs (programmatic dependent launches included) and
     // replayed while every host-visible argument stays the same: one launch per step instead of one
@@ -763,6 +772,40 @@ void remember_last(tidal_ctx* ctx) {
 }
 
 // ---- block-sparse operators --------------------------------------------------------------------------
+// Scratch of a block selection over long contexts: score rows and the largest bound of every chunk.
+struct BlockWs {
+    size_t scores, amax, total;
+    int npad, chunks;
+};
+
+BlockWs block_ws_layout(const tidal_kv_t* kv, int rows) {
+    BlockWs w;
+    const int blocks = (kv->max_ctx_len + TILE - 1) / TILE;
+    w.npad = (int)align_up((size_t)blocks, 32);
+    w.chunks = (blocks + SS_BLOCKS - 1) / SS_BLOCKS;
+    w.scores = 0;
+    w.amax = align_up((size_t)kv->batch * rows * w.npad * sizeof(float), 256);
+    w.total = w.amax + align_up((size_t)kv->batch * kv->num_kv_heads * w.chunks * sizeof(float), 256);
+    return w;
+}
+
+tidal_status_t ensure_block_ws(tidal_ctx* ctx, size_t bytes, const cudaStream_t* st) {
+    if (ctx->blk_ws_bytes >= bytes) return TIDAL_OK;
+    if (st) {                                   // nothing may be allocated into a capture
+        cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(*st, &cs) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
+        if (cs != cudaStreamCaptureStatusNone) return TIDAL_ERR_NOMEM;
+    }
+    if (ctx->blk_ws && ctx->blk_old_count == (int)(sizeof ctx->blk_old / sizeof ctx->blk_old[0])) return TIDAL_ERR_NOMEM;
+    const size_t want = std::max(bytes, 2 * ctx->blk_ws_bytes);
+    void* p = nullptr;
+    if (cudaMalloc(&p, want) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
+    if (ctx->blk_ws) ctx->blk_old[ctx->blk_old_count++] = ctx->blk_ws;
+    ctx->blk_ws = p;
+    ctx->blk_ws_bytes = want;
+    return TIDAL_OK;
+}
+
 // The context's device for the length of a call; the caller's own is current again afterwards.
 struct DeviceScope {
     int before = -1;
@@ -775,8 +818,7 @@ struct DeviceScope {
     ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
 };
 
-constexpr int BA_MAX_CLUSTER = 16;
-constexpr size_t SB_SMEM_MAX = sb_smem(SB_MAX_BLOCKS, 1);
+constexpr int BA_SMEM_MAX = (int)ba_smem_most(8);
 
 // How many clusters of 1 .. 16 CTAs of a kernel the GPU holds at once (the SMs of a processing cluster differ from chip to chip).
 template <typename K>
@@ -800,12 +842,18 @@ bool prepare_block_kernels() {
     auto wide = [](const void* k) {
         return cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
     };
-    return wide((const void*)block_select_kernel<256>) && wide((const void*)block_select_kernel<512>) &&
-           cudaFuncSetAttribute(block_select_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SB_SMEM_MAX) == cudaSuccess &&
-           cudaFuncSetAttribute(block_select_kernel<512>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SB_SMEM_MAX) == cudaSuccess &&
-           wide((const void*)block_attn_kernel<false>) && wide((const void*)block_attn_kernel<true>) &&
-           cudaFuncSetAttribute(block_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ba_smem<false>()) == cudaSuccess &&
-           cudaFuncSetAttribute(block_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ba_smem<true>()) == cudaSuccess &&
+    auto room = [](auto kernel, size_t bytes) {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    };
+    return wide((const void*)block_select_kernel) && room(block_select_kernel, sc_smem(SC_MAX_BLOCKS, MAX_GROUP)) &&
+           room(block_rank_kernel<256, 4>, 4096 * 8) && room(block_rank_kernel<512, 4>, 8192 * 8) &&
+           room(block_rank_kernel<1024, 1>, 4096 * 8) && room(block_rank_kernel<1024, 2>, 8192 * 8) && room(block_rank_kernel<1024, 4>, 16384 * 8) &&
+           wide((const void*)block_attn_kernel<false, 4>) && wide((const void*)block_attn_kernel<true, 4>) &&
+           wide((const void*)block_attn_kernel<false, 8>) && wide((const void*)block_attn_kernel<true, 8>) &&
+           cudaFuncSetAttribute(block_attn_kernel<false, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
+           cudaFuncSetAttribute(block_attn_kernel<true, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
+           cudaFuncSetAttribute(block_attn_kernel<false, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
+           cudaFuncSetAttribute(block_attn_kernel<true, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
            cudaFuncSetAttribute(page_map_kernel<PM_THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (PM_MAX_BATCH + 1) * (int)sizeof(int)) == cudaSuccess;
 }
 
@@ -897,8 +945,8 @@ tidal_status_t tidal_create(tidal_ctx_t** out, int device, size_t workspace_byte
     const bool compact_ok = cudaFuncSetAttribute(topk_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)compact_smem) == cudaSuccess;
     if (!prepare_block_kernels()) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     if (d0 <= 0 || d1 <= 0 || d2 < d1 || s0 <= 0 || s1 < s0 || e0 < d0 || e1 < d1 || e2 < s0 || !topk_ok || !compact_ok || !split_ok) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
-    count_clusters(block_select_kernel<256>, 256, 64 * 1024, ctx->select_clusters[0]);
-    count_clusters(block_select_kernel<512>, 512, 64 * 1024, ctx->select_clusters[1]);
+    count_clusters(block_select_kernel, SC_THREADS, sc_smem(SC_MAX_BLOCKS, 1), ctx->select_clusters);
+    count_clusters(block_attn_kernel<false, 8>, 256, ba_smem<false>(MAX_GROUP, BA_MAX_CLUSTER, 8), ctx->attn_clusters);
     ctx->dense_slots = std::min(d0, d1);
     ctx->sparse_slots = s0;
     if (cudaMalloc((void**)&ctx->status, 256) != cudaSuccess || cudaMemset(ctx->status, 0, 256) != cudaSuccess) {
@@ -921,6 +969,8 @@ tidal_status_t tidal_destroy(tidal_ctx_t* ctx) {
     if (ctx->ev_fork) cudaEventDestroy(ctx->ev_fork);
     if (ctx->ev_join) cudaEventDestroy(ctx->ev_join);
     if (ctx->ws) cudaFree(ctx->ws);
+    if (ctx->blk_ws) cudaFree(ctx->blk_ws);
+    for (int i = 0; i < ctx->blk_old_count; ++i) cudaFree(ctx->blk_old[i]);
     if (ctx->state) cudaFree(ctx->state);
     if (ctx->status) cudaFree(ctx->status);
     delete ctx;
@@ -939,6 +989,8 @@ tidal_status_t tidal_reserve(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t k, 
     if (cudaSetDevice(ctx->device) != cudaSuccess) return TIDAL_ERR_CUDA;
     const tidal_status_t rs = ensure_side_stream(ctx);       // a later step's selection layers may use it
     if (rs != TIDAL_OK) return rs;
+    const tidal_status_t rb = ensure_block_ws(ctx, block_ws_layout(kv, kv->num_q_heads).total, nullptr);
+    if (rb != TIDAL_OK) return rb;
     return ensure_all(ctx, kv, ws_bytes_for(kv, k, num_layers_host));
 }
 
@@ -1398,23 +1450,34 @@ tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     // one KV head's factor changes no order: it matters only where several KV heads are added up
     p.k_scale = kv->kv_dtype == TIDAL_KV_FP8_E4M3 && granularity == TIDAL_SEL_SHARED ? kv->k_scale : nullptr;
     p.mode = granularity; p.m = m; p.keep_first = keep_first; p.keep_last = keep_last;
-    p.npad = (int)align_up((size_t)p.c.max_blocks, 32);
     p.idx = idx; p.idx_count = idx_count;
+    p.npad = (int)align_up((size_t)p.c.max_blocks, 32);
+    p.scores = nullptr; p.amax = nullptr; p.chunks = 0;
     const int items = granularity == TIDAL_SEL_SHARED ? kv->batch : kv->batch * kv->num_kv_heads;
     const int rows = per_qhead ? p.c.G : 1;
-    // Few items over long contexts: 512 threads with an SM each. Otherwise 256, two CTAs per SM (see the kernel).
-    const int wide = p.c.max_blocks > 8192 || (items <= 16 && p.c.max_blocks > 2048);
-    const int threads = wide ? 512 : 256;
-    // The largest cluster that the item has work for (16 blocks per warp, a row to rank per CTA) with all items resident
-    // together; and large enough that the rows that a CTA owns fit its shared memory.
-    const int tiles = (p.c.max_blocks + 15) / 16, useful = std::max(rows, (tiles + threads / 32 - 1) / (threads / 32));
-    auto per_cta = [&](int s) { return (rows + s - 1) / s; };
-    int cluster = std::min(SB_MAX_CLUSTER, useful);
-    while (cluster > 1 && ctx->select_clusters[wide][cluster] < items) --cluster;
-    while (cluster < rows && sb_smem(p.npad, per_cta(cluster)) > SB_SMEM_MAX) ++cluster;
-    const size_t smem = sb_smem(p.npad, per_cta(cluster));
-    if (wide) return launch_block(ctx, block_select_kernel<512>, p, items * cluster, 512, smem, cluster, (cudaStream_t)stream);
-    return launch_block(ctx, block_select_kernel<256>, p, items * cluster, 256, smem, cluster, (cudaStream_t)stream);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (p.c.max_blocks <= SC_MAX_BLOCKS) {
+        // The largest cluster that the item has work for (16 blocks per warp, a row to rank per CTA) with all items resident together.
+        const int useful = std::max(rows, (p.c.max_blocks + 16 * SC_WARPS - 1) / (16 * SC_WARPS));
+        int cluster = std::min(SB_MAX_CLUSTER, useful);
+        while (cluster > 1 && ctx->select_clusters[cluster] < items) --cluster;
+        return launch_block(ctx, block_select_kernel, p, items * cluster, SC_THREADS, sc_smem(p.npad, (rows + cluster - 1) / cluster), cluster, st);
+    }
+    const BlockWs w = block_ws_layout(kv, per_qhead ? kv->num_q_heads : kv->num_kv_heads);
+    const long long grid = (long long)kv->batch * kv->num_kv_heads * w.chunks;
+    if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    if ((rc = ensure_block_ws(ctx, w.total, &st)) != TIDAL_OK) return rc;
+    p.scores = (float*)((char*)ctx->blk_ws + w.scores); p.amax = (float*)((char*)ctx->blk_ws + w.amax);
+    p.chunks = w.chunks;
+    if ((rc = launch_block(ctx, block_score_kernel, p, (int)grid, SS_WARPS * 32, 0, 0, st)) != TIDAL_OK) return rc;
+    const int rank_rows = kv->batch * Hi;
+    const size_t keys = (size_t)p.npad * 8;
+    const bool few = rank_rows <= ctx->sm_count;
+    if (p.c.max_blocks > 8192) return launch_block(ctx, block_rank_kernel<1024, 4>, p, rank_rows, 1024, keys, 0, st);
+    if (p.c.max_blocks > 4096) return few ? launch_block(ctx, block_rank_kernel<1024, 2>, p, rank_rows, 1024, keys, 0, st)
+                                          : launch_block(ctx, block_rank_kernel<512, 4>, p, rank_rows, 512, keys, 0, st);
+    return few ? launch_block(ctx, block_rank_kernel<1024, 1>, p, rank_rows, 1024, keys, 0, st)
+               : launch_block(ctx, block_rank_kernel<256, 4>, p, rank_rows, 256, keys, 0, st);
 }
 
 tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const void* q, const int32_t* idx, const int32_t* idx_count,
@@ -1437,11 +1500,22 @@ tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const vo
     p.k_scale = fp8 ? kv->k_scale : nullptr;
     p.v_scale = fp8 ? kv->v_scale : nullptr;
     const int items = kv->batch * (Hi == kv->num_q_heads ? kv->num_q_heads : kv->num_kv_heads);
-    // clusters as large as two CTAs per SM allow, while every warp has two blocks or more
-    int cluster = 1;
-    while (cluster < BA_MAX_CLUSTER && (long long)items * cluster * 2 <= 2LL * ctx->sm_count && cluster * BA_WARPS * 2 <= m) cluster *= 2;
-    if (fp8) return launch_block(ctx, block_attn_kernel<true>, p, items * cluster, BA_WARPS * 32, ba_smem<true>(), cluster, (cudaStream_t)stream);
-    return launch_block(ctx, block_attn_kernel<false>, p, items * cluster, BA_WARPS * 32, ba_smem<false>(), cluster, (cudaStream_t)stream);
+    const int ncols = Hi == kv->num_q_heads ? 1 : p.c.G;
+    cudaStream_t st = (cudaStream_t)stream;
+    // The largest cluster that leaves every warp a block, with all items resident together.
+    int cluster = std::max(1, std::min(BA_MAX_CLUSTER, m / 8));
+    while (cluster > 1 && ctx->attn_clusters[cluster] < items) --cluster;
+    auto launch = [&](auto kernel8, auto kernel4, auto smem_of, auto over_ring) -> tidal_status_t {
+        const int warps = ctx->attn_clusters[cluster] >= items ? 8 : 4;
+        if (warps == 4) {
+            cluster = 1;
+            while (cluster < 8 && (long long)items * cluster * 2 <= 2LL * ctx->sm_count && cluster * 4 * 2 <= m) cluster *= 2;
+        }
+        p.over_ring = over_ring(ncols, cluster, warps);
+        return launch_block(ctx, warps == 8 ? kernel8 : kernel4, p, items * cluster, warps * 32, smem_of(ncols, cluster, warps), cluster, st);
+    };
+    if (fp8) return launch(block_attn_kernel<true, 8>, block_attn_kernel<true, 4>, ba_smem<true>, ba_over_ring<true>);
+    return launch(block_attn_kernel<false, 8>, block_attn_kernel<false, 4>, ba_smem<false>, ba_over_ring<false>);
 }
 
 int64_t tidal_launch_count(const tidal_ctx_t* ctx) { return ctx ? ctx->launches : 0; }

@@ -233,6 +233,9 @@ SELECT = [
     ([1500], 8, 1, 90, 0, 3),
     ([3000, 64], 8, 8, 5, 7, 7),                          # more kept blocks than the budget
     ([20000], 4, 1, 100, 0, 1),
+    ([90000, 17, 0, 33333], 8, 2, 70, 2, 1),
+    ([16400, 16385, 70001], 12, 3, 1025, 0, 0),
+    ([170000], 2, 2, 33, 1, 1),
 ]
 
 
@@ -254,7 +257,7 @@ def test_select_gives_the_set_of_the_scores_in_64_bits(td, layout, fp8, gran, le
 
 
 @pytest.mark.parametrize("kind", ["equal", "zero", "few_values", "one_outlier", "near_ties", "nan"])
-@pytest.mark.parametrize("ctx", [3000, 80000])
+@pytest.mark.parametrize("ctx", [3000, 50000, 80000, 200000])
 def test_select_with_ties_and_ranges_that_collapse(td, kind, ctx):
     """Rows whose border falls among many equal or almost equal scores: the histogram's bin holds most of the row."""
     lay = make([ctx], 4, 2, "hnd", seed=9)
@@ -741,15 +744,18 @@ def test_a_captured_step_replayed_over_changing_lengths(fp8):
         t.close()
 
 
-def test_the_first_call_of_a_context_can_be_captured():
-    """No call here allocates: nothing has to be reserved before a capture."""
+@pytest.mark.parametrize("ctx", [900, 40000])
+def test_the_first_call_of_a_context_can_be_captured(ctx):
+    """Short contexts need nothing reserved before a capture, long ones do."""
     t = binding.Tidal(0)
     try:
-        lay = make([40000], 8, 2, "hnd", seed=1)
+        lay = make([ctx], 8, 2, "hnd", seed=1)
         q = query(lay, 1)
         bounds = torch.zeros(binding.block_bounds_shape(lay), dtype=torch.bfloat16, device=DEV)
         idx, cnt = torch.zeros(1, 8, 4, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
         out = torch.zeros(1, 8, D, device=DEV)
+        if ctx > 16384:
+            t.reserve(lay, 16)
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         side = torch.cuda.Stream()
@@ -763,6 +769,60 @@ def test_the_first_call_of_a_context_can_be_captured():
         assert torch.equal(idx.cpu(), ref_select(lay, q, 4, 0, 0, 0)[0])
         ref, tol = ref_attn(lay, q, idx.cpu())
         close(out, ref, tol, "captured")
+        del graph
+    finally:
+        t.close()
+
+
+def test_scratch_is_not_allocated_into_a_capture():
+    t = binding.Tidal(0)
+    try:
+        lay = make([40000], 8, 2, "hnd", seed=1)
+        q, bounds = query(lay, 1), t.block_bounds(lay)
+        idx, cnt = torch.zeros(1, 8, 4, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        x = torch.zeros(8, device=DEV)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graph, stream=side):
+                x += 1
+                with pytest.raises(binding.TidalError) as e:
+                    t.block_select(lay, bounds, q, 4, idx=idx, idx_count=cnt)
+                assert e.value.status == binding.ERR_NOMEM
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (x == 1).all()
+        t.block_select(lay, bounds, q, 4, idx=idx, idx_count=cnt)
+        assert torch.equal(idx.cpu(), ref_select(lay, q, 4, 0, 0, 0)[0])
+        del graph
+    finally:
+        t.close()
+
+
+def test_a_captured_selection_outlives_the_growth_of_its_scratch():
+    t = binding.Tidal(0)
+    try:
+        lay = make([30000], 8, 2, "paged", seed=2)
+        q, bounds = query(lay, 2), t.block_bounds(lay)
+        idx, cnt = torch.zeros(1, 2, 50, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        t.block_select(lay, bounds, q, 50, 1, idx=idx, idx_count=cnt)
+        graph = torch.cuda.CUDAGraph()
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graph, stream=side):
+                t.block_select(lay, bounds, q, 50, 1, idx=idx, idx_count=cnt)
+        big = make([60000, 50000, 70000], 8, 2, "paged", seed=3)
+        qb = query(big, 3)
+        big_idx, _ = t.block_select(big, t.block_bounds(big), qb, 30)
+        assert torch.equal(big_idx.cpu(), ref_select(big, qb, 30, 0, 0, 0)[0])
+        for i in range(3):
+            q.copy_(query(lay, 10 + i))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(idx.cpu(), ref_select(lay, q, 50, 1, 0, 0)[0])
         del graph
     finally:
         t.close()

@@ -36,7 +36,7 @@ struct SelectBlocksParams {
     int* idx_count;
     // two launches:
     float* scores;                                          // [batch, query heads or KV heads, npad]
-    float* amax;                                            // [batch, Hkv, chunks] largest |bound| of a chunk of blocks
+    float* err;                                             // [the same rows, chunks] e over a chunk of blocks
     int chunks;
 };
 
@@ -74,40 +74,59 @@ __device__ __forceinline__ int cta_scan(int v, int* s_part) {
     return x - v + __reduce_add_sync(0xffffffffu, w);
 }
 
-// One block's score in 64 bits for query heads h0 .. h1 - 1, by a warp: four channels per lane and head. The queries are
-// read from shared memory (rows of SB_QROW from head h0 on) where a group's are there, else from global memory.
-__device__ __noinline__ double wide_score(const SelectBlocksParams& p, const __nv_bfloat16* group_q, int b, int h0, int h1, int blk, int lane) {
+// One block's score in 64 bits, by a warp: every lane four channels of each head. near_bounds: the bounds of the lane's channels
+// (zero without a page); near_score: `heads` query heads of one KV head, their rows in shared memory; wide_score: query heads h0 ..
+// h1 - 1 of any KV heads.
+__device__ __forceinline__ void near_bounds(const SelectBlocksParams& p, int b, int g, int blk, int lane, uint2& lo, uint2& hi) {
     const BlockCache& c = p.c;
     int page = 0;
     if (c.paged) {
         page = __ldg(c.page_table + (long long)b * c.max_pages + blk);
-        if ((unsigned)page >= (unsigned)c.num_pages) return 0.0;
+        if ((unsigned)page >= (unsigned)c.num_pages) { lo = hi = make_uint2(0u, 0u); return; }
     }
+    const uint2* bp = reinterpret_cast<const uint2*>(p.bounds + bounds_row(c, b, blk, page, g) * BOUND_ELEMS) + lane;
+    lo = __ldg(bp);
+    hi = __ldg(bp + 32);
+}
+__device__ __forceinline__ void wide_add(double (&sum)[4], uint2 q, uint2 lo, uint2 hi) {      // four chains: the latency is what counts
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t qw = i & 2 ? q.y : q.x, lw = i & 2 ? lo.y : lo.x, hw = i & 2 ? hi.y : hi.x;
+        const uint32_t bw = (i & 1 ? qw : qw << 16) >> 31 ? lw : hw;              // a negative q takes the least key
+        const float qf = __uint_as_float(i & 1 ? qw & 0xffff0000u : qw << 16);
+        const float bf = __uint_as_float(i & 1 ? bw & 0xffff0000u : bw << 16);
+        sum[i] = fma((double)qf, (double)bf, sum[i]);
+    }
+}
+__device__ __forceinline__ double warp_sum(double x) {
+#pragma unroll
+    for (int sh = 16; sh >= 1; sh >>= 1) x += __shfl_xor_sync(0xffffffffu, x, sh);
+    return x;
+}
+__device__ __forceinline__ double near_score(const __nv_bfloat16* group_q, int heads, uint2 lo, uint2 hi, int lane) {
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 2
+    for (int h = 0; h < heads; ++h) wide_add(sum, reinterpret_cast<const uint2*>(group_q + h * SB_QROW)[lane], lo, hi);
+    return warp_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+}
+__device__ __noinline__ double wide_score(const SelectBlocksParams& p, const __nv_bfloat16* group_q, int b, int h0, int h1, int blk, int lane) {
+    const BlockCache& c = p.c;
     double acc = 0.0;
     int h = h0;
 #pragma unroll 1
     for (int g = h0 / c.G; h < h1; ++g) {
-        const uint2* bp = reinterpret_cast<const uint2*>(p.bounds + bounds_row(c, b, blk, page, g) * BOUND_ELEMS) + lane;
-        const uint2 lo = __ldg(bp), hi = __ldg(bp + 32);
-        double part = 0.0;
+        uint2 lo, hi;
+        near_bounds(p, b, g, blk, lane, lo, hi);
+        double sum[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 1
         for (; h < h1 && h < (g + 1) * c.G; ++h) {
             const __nv_bfloat16* qrow = group_q ? group_q + (h - h0) * SB_QROW : p.q + ((long long)b * c.Hq + h) * HEAD_DIM;
-            const uint2 q = reinterpret_cast<const uint2*>(qrow)[lane];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t qw = i & 2 ? q.y : q.x, lw = i & 2 ? lo.y : lo.x, hw = i & 2 ? hi.y : hi.x;
-                const uint32_t bw = (i & 1 ? qw : qw << 16) >> 31 ? lw : hw;      // a negative q takes the least key
-                const float qf = __uint_as_float(i & 1 ? qw & 0xffff0000u : qw << 16);
-                const float bf = __uint_as_float(i & 1 ? bw & 0xffff0000u : bw << 16);
-                part = fma((double)qf, (double)bf, part);
-            }
+            wide_add(sum, reinterpret_cast<const uint2*>(qrow)[lane], lo, hi);
         }
+        const double part = (sum[0] + sum[1]) + (sum[2] + sum[3]);
         acc += p.k_scale ? part * (double)__ldg(p.k_scale + g) : part;
     }
-#pragma unroll
-    for (int sh = 16; sh >= 1; sh >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, sh);
-    return acc;
+    return warp_sum(acc);
 }
 
 // What one head adds to e per unit of the largest |bound|: 2^-15 max|q| + (24 + Hkv) 2^-24 sum|q|, by a warp that holds four
@@ -123,31 +142,55 @@ __device__ __forceinline__ float query_part(uint2 q, int Hkv) {
     return big * (1.f / 32768.f) + sum * (float)(24 + Hkv) * (1.f / 16777216.f);
 }
 
+// A matrix instruction that starts from zero; its results as two pairs of fp32.
+__device__ __forceinline__ void mma_from_zero(unsigned long long (&d)[2], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    float r[4];
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(d[0]) : "f"(r[0]), "f"(r[1]));
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(d[1]) : "f"(r[2]), "f"(r[3]));
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {      // two fp32 additions
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // The scores of a tile of 16 blocks against a group of query heads: s[0], s[1] for row gid and heads 2 tig, 2 tig + 1; s[2], s[3]
-// for row gid + 8. neg / pos: the lane's pieces tig + 4 j of q-, q+ of head gid (zero beyond the group). x0, x1: the lane's
-// pieces of rows gid and gid + 8. Raises amax to the largest magnitude seen, infinity where that is not finite.
+// for row gid + 8. query(half, j): the lane's piece tig + 4 j of q- (half 0) or q+ (1) of head gid, zero beyond the group. x0, x1:
+// the lane's pieces of rows gid and gid + 8. low, high: running maxima of the bits of the least and of the greatest keys,
+// from which largest_bound() tells the largest magnitude: as unsigned numbers the bits of the least keys are largest for the
+// most negative one (or, if there is none, for the largest), as signed numbers those of the greatest for the largest.
 template <typename Q>
-__device__ __forceinline__ void score_tile(const uint4 (&x0)[8], const uint4 (&x1)[8], Q&& query, float (&s)[4], float& amax) {
-    s[0] = s[1] = s[2] = s[3] = 0.f;
-    uint32_t top = 0u, least = 0u;
+__device__ __forceinline__ void score_tile(const uint4 (&x0)[8], const uint4 (&x1)[8], Q&& query, float (&s)[4], uint32_t& low, uint32_t& high) {
+    unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint4 q4 = query(j >> 2, j & 3);
-        float d[4] = {0.f, 0.f, 0.f, 0.f}, e[4] = {0.f, 0.f, 0.f, 0.f};
-        mma_bf16_16816(d, x0[j].x, x1[j].x, x0[j].y, x1[j].y, q4.x, q4.y);
-        mma_bf16_16816(e, x0[j].z, x1[j].z, x0[j].w, x1[j].w, q4.z, q4.w);
+        unsigned long long d[2], e[2];
+        mma_from_zero(d, x0[j].x, x1[j].x, x0[j].y, x1[j].y, q4.x, q4.y);
+        mma_from_zero(e, x0[j].z, x1[j].z, x0[j].w, x1[j].w, q4.z, q4.w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] += d[i] + e[i];
-        // the greatest of hi and of -lo bounds both in magnitude
-        const uint32_t all[8] = {x0[j].x, x0[j].y, x0[j].z, x0[j].w, x1[j].x, x1[j].y, x1[j].z, x1[j].w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { if (j < 4) least = bmin2(least, all[i]); else top = bmax2(top, all[i]); }
+        for (int i = 0; i < 2; ++i) sum[i] = add2(sum[i], add2(d[i], e[i]));
+        if (j < 4) {
+            low = __vimax3_u16x2(low, x0[j].x, x0[j].y); low = __vimax3_u16x2(low, x0[j].z, x0[j].w);
+            low = __vimax3_u16x2(low, x1[j].x, x1[j].y); low = __vimax3_u16x2(low, x1[j].z, x1[j].w);
+        } else {
+            high = __vimax3_s16x2(high, x0[j].x, x0[j].y); high = __vimax3_s16x2(high, x0[j].z, x0[j].w);
+            high = __vimax3_s16x2(high, x1[j].x, x1[j].y); high = __vimax3_s16x2(high, x1[j].z, x1[j].w);
+        }
     }
-    const float t = fmaxf(fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u)),
-                          -fminf(__uint_as_float(least << 16), __uint_as_float(least & 0xffff0000u)));
-    const uint32_t a = (top & 0x7f807f80u) ^ 0x7f807f80u, b = (least & 0x7f807f80u) ^ 0x7f807f80u;
-    const bool finite = (a & 0xffffu) && (a >> 16) && (b & 0xffffu) && (b >> 16);
-    amax = fmaxf(amax, finite ? t : INFINITY);
+    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(s[0]), "=f"(s[1]) : "l"(sum[0]));
+    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(s[2]), "=f"(s[3]) : "l"(sum[1]));
+}
+// Start: low = 0, high = 0x80008000. Infinity where a bound is not finite: there is no error bound then.
+__device__ __forceinline__ float largest_bound(uint32_t low, uint32_t high) {
+    const uint32_t a = max(low & 0x7fffu, (low >> 16) & 0x7fffu);
+    // (a negative greatest key is smaller in magnitude than its least one)
+    const uint32_t b = max((high & 0x8000u) ? 0u : high & 0x7fffu, (high >> 31) ? 0u : high >> 16);
+    const uint32_t m = max(a, b);
+    return m >= 0x7f80u ? INFINITY : __uint_as_float(m << 16);
 }
 
 // ---- ranking one row ---------------------------------------------------------------------------------------------
@@ -287,6 +330,10 @@ __device__ __forceinline__ void rank_row(const SelectBlocksParams& p, RankShared
 #pragma unroll 1
             for (int w = tid; w < words; w += NT) sh.take[w] |= sh.cand[w];
         } else if (!all && ncand <= SB_CAND) {
+            // (A warp per candidate asks for its bounds already: if 64 bits are needed, they are there when the ranks are.)
+            const bool early = group_q != nullptr && ncand <= NW;
+            uint2 near_lo = make_uint2(0u, 0u), near_hi = near_lo;
+            if (early && warp < ncand) near_bounds(p, b, h0 / p.c.G, sh.blk[warp], lane, near_lo, near_hi);
             // ranks by x; the want-th and the next
             int place = 0;
             if (tid < ncand) {
@@ -303,12 +350,21 @@ __device__ __forceinline__ void rank_row(const SelectBlocksParams& p, RankShared
                 if (tid < ncand && place < want) take(sh.blk[tid]);
             } else {
                 // 64 bits for those within 2e of the border; the others are certain
+                if (early) {
+                    if (warp < ncand) {
+                        const float d = sh.x[warp] - edge;
+                        unsigned long long k = d > 0.f ? ~0ull : 0ull;
+                        if (fabsf(d) <= two_e) k = wide_key(near_score(group_q, h1 - h0, near_lo, near_hi, lane));
+                        if (lane == 0) sh.key[warp] = k;
+                    }
+                } else {
 #pragma unroll 1
-                for (int i = warp; i < ncand; i += NW) {
-                    const float d = sh.x[i] - edge;
-                    unsigned long long k = d > 0.f ? ~0ull : 0ull;
-                    if (fabsf(d) <= two_e) k = wide_key(wide_score(p, group_q, b, h0, h1, sh.blk[i], lane));
-                    if (lane == 0) sh.key[i] = k;
+                    for (int i = warp; i < ncand; i += NW) {
+                        const float d = sh.x[i] - edge;
+                        unsigned long long k = d > 0.f ? ~0ull : 0ull;
+                        if (fabsf(d) <= two_e) k = wide_key(wide_score(p, group_q, b, h0, h1, sh.blk[i], lane));
+                        if (lane == 0) sh.key[i] = k;
+                    }
                 }
                 __syncthreads();
                 if (tid < ncand) {
@@ -418,7 +474,7 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
             *reinterpret_cast<uint32_t*>(&s_q[2][h][2 * w]) = x;
         }
         const float factor = p.k_scale ? __ldg(p.k_scale + g) : 1.f;
-        float gmax = 0.f;
+        uint32_t low = 0u, high = 0x80008000u;
         bool staged = false;
 #pragma unroll 1
         for (int first = (rank * NW + warp) * 16; first < n; first += size * NW * 16) {
@@ -441,7 +497,7 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
             }
             if (!staged) { asm volatile("bar.sync 1, %0;\n" ::"n"(NT) : "memory"); staged = true; }      // s_q is there
             float s[4];
-            score_tile(x0, x1, [&](int half, int j) { return *reinterpret_cast<const uint4*>(&s_q[half][gid][8 * (tig + 4 * j)]); }, s, gmax);
+            score_tile(x0, x1, [&](int half, int j) { return *reinterpret_cast<const uint4*>(&s_q[half][gid][8 * (tig + 4 * j)]); }, s, low, high);
             if (first_write) { cluster_wait(); first_write = false; }
             if (per_qhead) {
 #pragma unroll
@@ -469,7 +525,7 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
             }
         }
         if (!staged) asm volatile("bar.sync 1, %0;\n" ::"n"(NT) : "memory");
-        amax = fmaxf(amax, gmax * fabsf(factor));
+        amax = fmaxf(amax, largest_bound(low, high) * fabsf(factor));
         if ((shared_set || g == g1 - 1) && rank < owners && warp < c.G) {
             const float part = query_part(reinterpret_cast<const uint2*>(s_q[2][warp])[lane], c.Hkv);
             if (lane == 0) s_qpart[warp] = g > g0 ? s_qpart[warp] + part : part;
@@ -501,99 +557,166 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
 }
 
 // ---- long contexts: scores by the whole GPU, then a CTA per row ----------------------------------------------------
-constexpr int SS_WARPS = 4;
-constexpr int SS_BLOCKS = SS_WARPS * 16;                    // blocks per CTA of the score kernel: a chunk
+// The scores are a stream of 8 KB tiles (16 blocks of one KV head). Every warp has SS_TILES of them in a row and a private
+// cp.async ring in shared memory; a slot is free as soon as its tile is in registers, so that two tiles are under way while
+// one is worked on. (With loads straight into registers a warp had nothing under way while it worked.)
+constexpr int SS_WARPS = 4, SS_TILES = 4, SS_STAGES = 2;
+constexpr int SS_BLOCKS = SS_WARPS * SS_TILES * 16;         // blocks per CTA: a chunk
+constexpr int SS_ROW = BOUND_ELEMS * 2;                     // bytes of a block's bounds
+constexpr int SS_SLOT = 16 * SS_ROW;
+constexpr size_t SS_SMEM = (size_t)SS_WARPS * SS_STAGES * SS_SLOT;
 
-__global__ void __launch_bounds__(SS_WARPS * 32) block_score_kernel(const __grid_constant__ SelectBlocksParams p) {
+__global__ void __launch_bounds__(SS_WARPS * 32, 3) block_score_kernel(const __grid_constant__ SelectBlocksParams p) {
     const BlockCache& c = p.c;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-    const int pair = blockIdx.x / p.chunks, chunk = blockIdx.x - pair * p.chunks;
-    const int b = pair / c.Hkv, g = pair - b * c.Hkv;
-    const int r0 = chunk * SS_BLOCKS + warp * 16 + gid, r1 = r0 + 8;
+    extern __shared__ __align__(128) uint8_t ss_ring[];
     __shared__ float s_amax[SS_WARPS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    // KV heads innermost: the CTAs that run together then read neighbouring 512 bytes of the same physical pages.
+    const int part = blockIdx.x / c.Hkv, g = blockIdx.x - part * c.Hkv;
+    const int b = part / p.chunks, chunk = part - b * p.chunks;
+    const int blk0 = (chunk * SS_WARPS + warp) * SS_TILES * 16;          // this warp's first block
     pdl_wait();
     pdl_trigger();
-    // Nothing waits for the length: bounds (and table entries) up to max_blocks may be read whatever they hold, and the
-    // rows beyond the length become zeros before they count.
     const int len = c.ctx_lens[b];
-    int page0 = 0, page1 = 0;
-    if (c.paged) {
-        const int* row = c.page_table + (long long)b * c.max_pages;
-        page0 = r0 < c.max_blocks ? __ldg(row + r0) : -1;
-        page1 = r1 < c.max_blocks ? __ldg(row + r1) : -1;
-    }
-    auto source = [&](int blk, int page) -> const uint4* {
-        if (blk >= c.max_blocks || (c.paged && (unsigned)page >= (unsigned)c.num_pages)) return nullptr;
-        return reinterpret_cast<const uint4*>(p.bounds + bounds_row(c, b, blk, page, g) * BOUND_ELEMS) + tig;
-    };
-    const uint4 *src0 = source(r0, page0), *src1 = source(r1, page1);
-    uint4 x0[8], x1[8];
+    // Rows of the bounds, in units of `pitch`, of this warp's blocks: lane l keeps blocks l, l + 32, ... Table entries are read along
+    // with the length, as far as the table goes, whatever it holds there.
+    constexpr int PER = SS_TILES / 2;
+    int at[PER];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        x0[j] = src0 ? __ldg(src0 + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
-        x1[j] = src1 ? __ldg(src1 + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < PER; ++i) {
+        at[i] = blk0 + lane + 32 * i;
+        if (c.paged) at[i] = at[i] < c.max_blocks ? __ldg(c.page_table + (long long)b * c.max_pages + at[i]) : -1;
     }
     uint4 q4[4];
     const uint4* qp = reinterpret_cast<const uint4*>(p.q + ((long long)b * c.Hq + g * c.G + min(gid, c.G - 1)) * HEAD_DIM) + tig;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) q4[j] = __ldg(qp + 4 * j);
-    const int n = (max(min(len, c.max_ctx), 0) + TILE - 1) / TILE;
-    if (chunk * SS_BLOCKS >= n) return;
-    if ((r0 < n && !src0) || (r1 < n && !src1)) atomicOr(c.status, STATUS_BAD_PAGE);
     const bool on = gid < c.G;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (r0 >= n) x0[j] = make_uint4(0u, 0u, 0u, 0u);
-        if (r1 >= n) x1[j] = make_uint4(0u, 0u, 0u, 0u);
-    }
-    float s[4], amax = 0.f;
-    score_tile(x0, x1, [&](int half, int j) {
-        uint4 r;
-        r.x = on ? (half ? bmax2(q4[j].x, 0u) : bmin2(q4[j].x, 0u)) : 0u;
-        r.y = on ? (half ? bmax2(q4[j].y, 0u) : bmin2(q4[j].y, 0u)) : 0u;
-        r.z = on ? (half ? bmax2(q4[j].z, 0u) : bmin2(q4[j].z, 0u)) : 0u;
-        r.w = on ? (half ? bmax2(q4[j].w, 0u) : bmin2(q4[j].w, 0u)) : 0u;
-        return r;
-    }, s, amax);
-    if (p.mode == 0) {
-        float* row = p.scores + ((long long)b * c.Hq + g * c.G) * p.npad;
+    for (int j = 0; j < 4; ++j) q4[j] = on ? __ldg(qp + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
+    const int n = (max(min(len, c.max_ctx), 0) + TILE - 1) / TILE;
+    if (chunk * SS_BLOCKS >= n) return;
+    if (c.paged) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int col = 2 * tig + i;
-            if (col < c.G) {
-                if (r0 < n) row[(long long)col * p.npad + r0] = s[i];
-                if (r1 < n) row[(long long)col * p.npad + r1] = s[2 + i];
+        for (int i = 0; i < PER; ++i)
+            if (blk0 + lane + 32 * i < n && (unsigned)at[i] >= (unsigned)c.num_pages) {
+                atomicOr(c.status, STATUS_BAD_PAGE);
+                at[i] = 0;                                  // (any page: a block without one has no score to speak of)
             }
-        }
-    } else {
-        float x = s[0] + s[1], y = s[2] + s[3];
-        x += __shfl_xor_sync(0xffffffffu, x, 1); y += __shfl_xor_sync(0xffffffffu, y, 1);
-        x += __shfl_xor_sync(0xffffffffu, x, 2); y += __shfl_xor_sync(0xffffffffu, y, 2);
-        const float f = p.k_scale ? __ldg(p.k_scale + g) : 1.f;
-        float* row = p.scores + ((long long)b * c.Hkv + g) * p.npad;
-        if (tig == 0 && r0 < n) row[r0] = x * f;
-        if (tig == 0 && r1 < n) row[r1] = y * f;
     }
+    const uint8_t* base = reinterpret_cast<const uint8_t*>(p.bounds) + (c.paged ? (long long)g : ((long long)b * c.Hkv + g) * c.bound_blocks) * SS_ROW + lane * 16;
+    const long long pitch = c.paged ? (long long)c.Hkv * SS_ROW : SS_ROW;
+    const uint32_t ring = smem_u32(ss_ring) + warp * SS_STAGES * SS_SLOT;
+    const int valid = min(SS_TILES * 16, n - blk0), tiles = valid > 0 ? (valid + 15) / 16 : 0;
+    // One instruction copies a block's 512 bytes; piece c of row r goes to c ^ ((r & 1) << 2), so that the fragment reads
+    // below (two rows, four pieces per eight lanes) meet no bank twice. The last block stands in for those behind it.
+    auto issue = [&](int t, uint32_t slot) {
+        int mine = at[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) if ((t >> 1) == i) mine = at[i];
+        const int first = (t & 1) * 16, last = min(15, valid - 1 - t * 16);
+        const uint32_t even = slot + lane * 16, odd = slot + (lane ^ 4) * 16;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = __shfl_sync(0xffffffffu, mine, first + min(r, last));
+            cp_async16_full((r & 1 ? odd : even) + r * SS_ROW, base + row * pitch);
+        }
+    };
+    uint4 qs[2][4];                                         // q-, q+
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        qs[0][j] = make_uint4(bmin2(q4[j].x, 0u), bmin2(q4[j].y, 0u), bmin2(q4[j].z, 0u), bmin2(q4[j].w, 0u));
+        qs[1][j] = make_uint4(bmax2(q4[j].x, 0u), bmax2(q4[j].y, 0u), bmax2(q4[j].z, 0u), bmax2(q4[j].w, 0u));
+    }
+    uint32_t low = 0u, high = 0x80008000u;
+    const float f = p.k_scale ? __ldg(p.k_scale + g) : 1.f;
+    float* const row = p.scores + (p.mode == 0 ? (long long)b * c.Hq + g * c.G : (long long)b * c.Hkv + g) * p.npad;
+#pragma unroll
+    for (int t = 0; t < SS_STAGES; ++t) {
+        if (t < tiles) issue(t, ring + t * SS_SLOT);
+        cp_async_commit();
+    }
+    uint32_t slot = ring;
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t) {
+        cp_async_wait<SS_STAGES - 1>();
+        __syncwarp();
+        uint4 x0[8], x1[8];
+        const uint32_t frag = slot + gid * SS_ROW, swz = (gid & 1) << 2;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint32_t a[4], d[4];
+            lds128(frag + (((tig + 4 * j) ^ swz) << 4), a);
+            lds128(frag + 8 * SS_ROW + (((tig + 4 * j) ^ swz) << 4), d);
+            x0[j] = make_uint4(a[0], a[1], a[2], a[3]);
+            x1[j] = make_uint4(d[0], d[1], d[2], d[3]);
+        }
+        __syncwarp();                                       // every lane has its pieces: the slot is free
+        if (t + SS_STAGES < tiles) issue(t + SS_STAGES, slot);
+        cp_async_commit();
+        slot = slot == ring + (SS_STAGES - 1) * SS_SLOT ? ring : slot + SS_SLOT;
+        float s[4];
+        score_tile(x0, x1, [&](int half, int j) { return qs[half][j]; }, s, low, high);
+        const int r0 = blk0 + t * 16 + gid, r1 = r0 + 8;
+        if (p.mode == 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int col = 2 * tig + i;
+                if (col < c.G) {
+                    if (r0 < n) row[(long long)col * p.npad + r0] = s[i];
+                    if (r1 < n) row[(long long)col * p.npad + r1] = s[2 + i];
+                }
+            }
+        } else {
+            float x = s[0] + s[1], y = s[2] + s[3];
+            x += __shfl_xor_sync(0xffffffffu, x, 1); y += __shfl_xor_sync(0xffffffffu, y, 1);
+            x += __shfl_xor_sync(0xffffffffu, x, 2); y += __shfl_xor_sync(0xffffffffu, y, 2);
+            if (tig == 0 && r0 < n) row[r0] = x * f;
+            if (tig == 0 && r1 < n) row[r1] = y * f;
+        }
+    }
+    float amax = largest_bound(low, high);
+    // ---- the chunk's share of e, per row ---------------------------------------------------------------------------------
     amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
     if (lane == 0) s_amax[warp] = amax;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        float m = s_amax[0];
+    if (warp == 0) {
 #pragma unroll
-        for (int w = 1; w < SS_WARPS; ++w) m = fmaxf(m, s_amax[w]);
-        p.amax[(long long)pair * p.chunks + chunk] = m;
+        for (int w = 0; w < SS_WARPS; ++w) amax = fmaxf(amax, s_amax[w]);
+        // 2^-15 max|q| + (24 + Hkv) 2^-24 sum|q| of head gid, whose row the four lanes of a gid hold between them
+        float big = 0.f, sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t w[4] = {q4[j].x, q4[j].y, q4[j].z, q4[j].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float lo = fabsf(__uint_as_float(w[i] << 16)), hi = fabsf(__uint_as_float(w[i] & 0xffff0000u));
+                big = fmaxf(big, fmaxf(lo, hi));
+                sum += lo + hi;
+            }
+        }
+#pragma unroll
+        for (int sh = 1; sh <= 2; sh <<= 1) {
+            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, sh));
+            sum += __shfl_xor_sync(0xffffffffu, sum, sh);
+        }
+        float e = on ? amax * (big * (1.f / 32768.f) + sum * (float)(24 + c.Hkv) * (1.f / 16777216.f)) * fabsf(f) : 0.f;
+        if (p.mode == 0) {
+            if (on && tig == 0) p.err[((long long)b * c.Hq + g * c.G + gid) * p.chunks + chunk] = e;
+        } else {
+#pragma unroll
+            for (int sh = 4; sh <= 16; sh <<= 1) e += __shfl_xor_sync(0xffffffffu, e, sh);
+            if (lane == 0) p.err[((long long)b * c.Hkv + g) * p.chunks + chunk] = e;
+        }
     }
 }
 
 // Dynamic shared memory: 8 bytes per block for keys.
 template <int NT, int V>
 __global__ void __launch_bounds__(NT) block_rank_kernel(const __grid_constant__ SelectBlocksParams p) {
-    constexpr int NW = NT / 32;
     const BlockCache& c = p.c;
     extern __shared__ __align__(16) uint8_t rk_keys[];
     __shared__ __align__(16) RankShared<NT, V> sh;
     __shared__ __align__(16) __nv_bfloat16 s_q[8][SB_QROW];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     const bool shared_set = p.mode == 2, per_qhead = p.mode == 0;
     const int Hi = per_qhead ? c.Hq : (shared_set ? 1 : c.Hkv);
     const int b = blockIdx.x / Hi, hi = blockIdx.x - b * Hi;
@@ -603,7 +726,8 @@ __global__ void __launch_bounds__(NT) block_rank_kernel(const __grid_constant__ 
     // (rows of npad scores: what lies behind the length is read, and ignored when the length is there)
     const int len = c.ctx_lens[b];
     const int sum_rows = shared_set ? c.Hkv : 1;
-    const float* row = p.scores + ((long long)b * (per_qhead ? c.Hq : c.Hkv) + (shared_set ? 0 : hi)) * p.npad;
+    const long long row0 = (long long)b * (per_qhead ? c.Hq : c.Hkv) + (shared_set ? 0 : hi);
+    const float* row = p.scores + row0 * p.npad;
     float v[V][4];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -612,6 +736,12 @@ __global__ void __launch_bounds__(NT) block_rank_kernel(const __grid_constant__ 
         if (at < p.npad) t = __ldcg(reinterpret_cast<const float4*>(row + at));
         v[j][0] = t.x; v[j][1] = t.y; v[j][2] = t.z; v[j][3] = t.w;
     }
+    const int errs = sum_rows * p.chunks;
+    const float err0 = tid < errs ? __ldcg(p.err + row0 * p.chunks + tid) : 0.f;
+    if (!shared_set)                                        // the members' queries, for scores in 64 bits
+        for (int i = tid; i < members * (HEAD_DIM / 4); i += NT)
+            reinterpret_cast<uint2*>(s_q[i / (HEAD_DIM / 4)])[i % (HEAD_DIM / 4)] =
+                __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h0) * HEAD_DIM) + i);
 #pragma unroll 1
     for (int r = 1; r < sum_rows; ++r)
 #pragma unroll
@@ -623,20 +753,11 @@ __global__ void __launch_bounds__(NT) block_rank_kernel(const __grid_constant__ 
             }
         }
     const int n = (max(min(len, c.max_ctx), 0) + TILE - 1) / TILE, used = (n + SS_BLOCKS - 1) / SS_BLOCKS;
-    // e: the sum over the member heads is at most their number times the largest
-    float err = 0.f;
+    // e: the sum over the rows added up is at most their number times the largest
+    float err = tid < errs && tid % p.chunks < used ? err0 : 0.f;
 #pragma unroll 1
-    for (int h = h0 + warp; h < h1; h += NW) {
-        const int g = h / c.G;
-        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h) * HEAD_DIM) + lane);
-        float big = 0.f;
-        const float* am = p.amax + ((long long)b * c.Hkv + g) * p.chunks;
-#pragma unroll 4
-        for (int i = lane; i < used; i += 32) big = fmaxf(big, __ldcg(am + i));
-        big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
-        if (!shared_set) reinterpret_cast<uint2*>(s_q[h - h0])[lane] = q;
-        err = fmaxf(err, (float)members * big * query_part(q, c.Hkv) * (p.k_scale ? fabsf(__ldg(p.k_scale + g)) : 1.f));
-    }
+    for (int i = tid + NT; i < errs; i += NT) if (i % p.chunks < used) err = fmaxf(err, __ldcg(p.err + row0 * p.chunks + i));
+    err *= (float)sum_rows;
     if (hi == 0 && tid == 0 && p.idx_count) p.idx_count[b] = min(p.m, n);
     rank_row<NT, V>(p, sh, v, err, shared_set ? nullptr : &s_q[0][0], reinterpret_cast<unsigned long long*>(rk_keys), b, h0, h1, n,
                     p.idx + ((long long)b * Hi + hi) * p.m);

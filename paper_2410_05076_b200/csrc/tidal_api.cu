@@ -772,9 +772,9 @@ void remember_last(tidal_ctx* ctx) {
 }
 
 // ---- block-sparse operators --------------------------------------------------------------------------
-// Scratch of a block selection over long contexts: score rows and the largest bound of every chunk.
+// Scratch of a block selection over long contexts: score rows and their error bounds per chunk.
 struct BlockWs {
-    size_t scores, amax, total;
+    size_t scores, err, total;
     int npad, chunks;
 };
 
@@ -784,8 +784,8 @@ BlockWs block_ws_layout(const tidal_kv_t* kv, int rows) {
     w.npad = (int)align_up((size_t)blocks, 32);
     w.chunks = (blocks + SS_BLOCKS - 1) / SS_BLOCKS;
     w.scores = 0;
-    w.amax = align_up((size_t)kv->batch * rows * w.npad * sizeof(float), 256);
-    w.total = w.amax + align_up((size_t)kv->batch * kv->num_kv_heads * w.chunks * sizeof(float), 256);
+    w.err = align_up((size_t)kv->batch * rows * w.npad * sizeof(float), 256);
+    w.total = w.err + align_up((size_t)kv->batch * rows * w.chunks * sizeof(float), 256);
     return w;
 }
 
@@ -846,8 +846,8 @@ bool prepare_block_kernels() {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
     };
     return wide((const void*)block_select_kernel) && room(block_select_kernel, sc_smem(SC_MAX_BLOCKS, MAX_GROUP)) &&
-           room(block_rank_kernel<256, 4>, 4096 * 8) && room(block_rank_kernel<512, 4>, 8192 * 8) &&
-           room(block_rank_kernel<1024, 1>, 4096 * 8) && room(block_rank_kernel<1024, 2>, 8192 * 8) && room(block_rank_kernel<1024, 4>, 16384 * 8) &&
+           room(block_score_kernel, SS_SMEM) && room(block_rank_kernel<256, 4>, 4096 * 8) && room(block_rank_kernel<512, 4>, 8192 * 8) &&
+           room(block_rank_kernel<1024, 4>, 16384 * 8) &&
            wide((const void*)block_attn_kernel<false, 4>) && wide((const void*)block_attn_kernel<true, 4>) &&
            wide((const void*)block_attn_kernel<false, 8>) && wide((const void*)block_attn_kernel<true, 8>) &&
            cudaFuncSetAttribute(block_attn_kernel<false, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
@@ -1394,8 +1394,8 @@ tidal_status_t tidal_kv_write(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t nu
     if (num_tokens == 0) return TIDAL_OK;
     if (!k_new || !v_new || !slots || (((uintptr_t)k_new | (uintptr_t)v_new) & 15)) return TIDAL_ERR_INVALID;
     if (k_stride < 0 || v_stride < 0 || ((k_stride | v_stride) & 7)) return TIDAL_ERR_INVALID;
-    const long long units = (long long)num_tokens * kv->num_kv_heads;
-    const long long grid = (units + KW_UNITS * KW_WARPS - 1) / (KW_UNITS * KW_WARPS);
+    const long long runs = ((long long)num_tokens + KW_TOKENS - 1) / KW_TOKENS;
+    const long long grid = (runs * kv->num_kv_heads + KW_WARPS - 1) / KW_WARPS;
     if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
     DeviceScope dev(ctx->device);
     if (!dev.ok) return TIDAL_ERR_CUDA;
@@ -1452,7 +1452,7 @@ tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     p.mode = granularity; p.m = m; p.keep_first = keep_first; p.keep_last = keep_last;
     p.idx = idx; p.idx_count = idx_count;
     p.npad = (int)align_up((size_t)p.c.max_blocks, 32);
-    p.scores = nullptr; p.amax = nullptr; p.chunks = 0;
+    p.scores = nullptr; p.err = nullptr; p.chunks = 0;
     const int items = granularity == TIDAL_SEL_SHARED ? kv->batch : kv->batch * kv->num_kv_heads;
     const int rows = per_qhead ? p.c.G : 1;
     cudaStream_t st = (cudaStream_t)stream;
@@ -1467,17 +1467,16 @@ tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     const long long grid = (long long)kv->batch * kv->num_kv_heads * w.chunks;
     if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
     if ((rc = ensure_block_ws(ctx, w.total, &st)) != TIDAL_OK) return rc;
-    p.scores = (float*)((char*)ctx->blk_ws + w.scores); p.amax = (float*)((char*)ctx->blk_ws + w.amax);
+    p.scores = (float*)((char*)ctx->blk_ws + w.scores); p.err = (float*)((char*)ctx->blk_ws + w.err);
     p.chunks = w.chunks;
-    if ((rc = launch_block(ctx, block_score_kernel, p, (int)grid, SS_WARPS * 32, 0, 0, st)) != TIDAL_OK) return rc;
+    if ((rc = launch_block(ctx, block_score_kernel, p, (int)grid, SS_WARPS * 32, SS_SMEM, 0, st)) != TIDAL_OK) return rc;
+    // Sixteen scores per thread, with as few threads as that takes: their barriers and scans are the shorter chain (131072
+    // positions, 8 rows: 13.1 us with 512 threads, 13.9 with 1024; ragged batch of 8 x 65536, 256 rows: 25.2 us with 256, 28.3 with 1024).
     const int rank_rows = kv->batch * Hi;
     const size_t keys = (size_t)p.npad * 8;
-    const bool few = rank_rows <= ctx->sm_count;
     if (p.c.max_blocks > 8192) return launch_block(ctx, block_rank_kernel<1024, 4>, p, rank_rows, 1024, keys, 0, st);
-    if (p.c.max_blocks > 4096) return few ? launch_block(ctx, block_rank_kernel<1024, 2>, p, rank_rows, 1024, keys, 0, st)
-                                          : launch_block(ctx, block_rank_kernel<512, 4>, p, rank_rows, 512, keys, 0, st);
-    return few ? launch_block(ctx, block_rank_kernel<1024, 1>, p, rank_rows, 1024, keys, 0, st)
-               : launch_block(ctx, block_rank_kernel<256, 4>, p, rank_rows, 256, keys, 0, st);
+    if (p.c.max_blocks > 4096) return launch_block(ctx, block_rank_kernel<512, 4>, p, rank_rows, 512, keys, 0, st);
+    return launch_block(ctx, block_rank_kernel<256, 4>, p, rank_rows, 256, keys, 0, st);
 }
 
 tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const void* q, const int32_t* idx, const int32_t* idx_count,

@@ -202,11 +202,21 @@ struct KvWriteParams {
 // long as nothing leaves the range. So it is used where s is between 2^-60 and 2^60 and the largest of the eight
 // quotients is below 1024 (a remainder that underflows then belongs to a quotient below 2^-40, whose code is
 // zero); a division otherwise. Two elements per instruction: with one, and a guard on each, the kernel was bound by its
-// instructions (104 us with divisions, 87 us with single fused multiply-adds, for 62.5 us worth of bytes).
+// instructions: 65536 tokens of 8 heads 104 us with divisions, 87 us with single fused multiply-adds, 67 us this way (6.0 TB/s).
 __device__ __forceinline__ unsigned long long pair_of(float lo, float hi) {
     unsigned long long d;
     asm("mov.b64 %0, {%1, %2};\n" : "=l"(d) : "f"(lo), "f"(hi));
     return d;
+}
+__device__ __noinline__ uint2 quantise8_unusual(uint4 w, float scale) {
+    const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+    uint32_t half[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float lo = __fdiv_rn(__uint_as_float(in[i] << 16), scale), hi = __fdiv_rn(__uint_as_float(in[i] & 0xffff0000u), scale);
+        half[i] = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+    }
+    return make_uint2(half[0] | (half[1] << 16), half[2] | (half[3] << 16));
 }
 __device__ __forceinline__ uint2 quantise8(uint4 w, float scale, float inv, bool usual) {
     const uint32_t in[4] = {w.x, w.y, w.z, w.w};
@@ -227,13 +237,7 @@ __device__ __forceinline__ uint2 quantise8(uint4 w, float scale, float inv, bool
             half[i] = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
         }
     } else {
-#pragma unroll 1
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t x = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
-            const float lo = __fdiv_rn(__uint_as_float(x << 16), scale), hi = __fdiv_rn(__uint_as_float(x & 0xffff0000u), scale);
-            const uint32_t h = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
-            if (i == 0) half[0] = h; else if (i == 1) half[1] = h; else if (i == 2) half[2] = h; else half[3] = h;
-        }
+        return quantise8_unusual(w, scale);
     }
     return make_uint2(half[0] | (half[1] << 16), half[2] | (half[3] << 16));
 }
@@ -241,12 +245,13 @@ __device__ __forceinline__ uint2 quantise8(uint4 w, float scale, float inv, bool
 constexpr int KW_TOKENS = 4, KW_WARPS = 8;
 
 template <bool KV8>
-__global__ void __launch_bounds__(KW_WARPS * 32) kv_write_kernel(const KvWriteParams p) {
+__global__ void __launch_bounds__(KW_WARPS * 32, 6) kv_write_kernel(const KvWriteParams p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int piece = lane & 15;
     const bool value = lane >= 16;
-    const long long w = (long long)blockIdx.x * KW_WARPS + warp;
-    const int run = (int)(w / p.Hkv), g = (int)(w - (long long)run * p.Hkv);
+    const unsigned w = blockIdx.x * KW_WARPS + warp;         // (the host keeps them below 2^32)
+    const unsigned run = w / (unsigned)p.Hkv;
+    const int g = (int)(w - run * (unsigned)p.Hkv);
     const long long t0 = (long long)run * KW_TOKENS;
     pdl_wait();
     pdl_trigger();
@@ -278,8 +283,10 @@ __global__ void __launch_bounds__(KW_WARPS * 32) kv_write_kernel(const KvWritePa
             if (slot[i] != -1 && lane == 0) atomicOr(p.status, STATUS_BAD_INDEX);      // -1: padding
             continue;
         }
-        const long long off = head + (p.paged ? (long long)(s / TILE) * p.stride_page + (long long)(s % TILE) * p.stride_pos
-                                              : (long long)(s / (unsigned)p.max_ctx) * p.stride_b + (long long)(s % (unsigned)p.max_ctx) * p.stride_pos);
+        // (pages, and sequences times positions, fit 32 bits and 48 bits)
+        long long off = head;
+        if (p.paged) off += (long long)(unsigned)(s / TILE) * p.stride_page + (long long)(unsigned)(s % TILE) * p.stride_pos;
+        else off += (long long)(s / (unsigned)p.max_ctx) * p.stride_b + (long long)(s % (unsigned)p.max_ctx) * p.stride_pos;
         if constexpr (KV8) *reinterpret_cast<uint2*>(dst + off + piece * 8) = quantise8(row[i], scale, inv, usual);
         else *reinterpret_cast<uint4*>(dst + 2 * off + piece * 16) = row[i];
     }

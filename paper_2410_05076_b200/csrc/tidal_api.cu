@@ -1396,7 +1396,7 @@ tidal_status_t tidal_kv_write(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t nu
     if (k_stride < 0 || v_stride < 0 || ((k_stride | v_stride) & 7)) return TIDAL_ERR_INVALID;
     const long long runs = ((long long)num_tokens + KW_TOKENS - 1) / KW_TOKENS;
     const long long grid = (runs * kv->num_kv_heads + KW_WARPS - 1) / KW_WARPS;
-    if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    if (grid * KW_WARPS > 0xffffffffLL) return TIDAL_ERR_UNSUPPORTED;
     DeviceScope dev(ctx->device);
     if (!dev.ok) return TIDAL_ERR_CUDA;
     KvWriteParams p;

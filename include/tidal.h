@@ -355,7 +355,7 @@ tidal_status_t tidal_block_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const 
  * reported as TIDAL_ERR_INDEX; a repeated block counts once per occurrence; any order. Only the first idx_count[b]
  * entries are read when idx_count is given, else m. A head without a valid entry gets zeros. num_index_heads
  * must be Hq, Hkv or 1. Output type as set by tidal_set_output_dtype; softmax weights enter the product with V
- * with 16 bits or more, statistics and sums are fp32. tidal_set_attend_newest has no effect here (keep_last does that).
+ * with 22 bits or more, statistics and sums are fp32. tidal_set_attend_newest has no effect here (keep_last does that).
  * Uses no scratch memory. */
 tidal_status_t tidal_block_attn(tidal_ctx_t *ctx, const tidal_kv_t *kv, const void *q, const int32_t *idx,
                                 const int32_t *idx_count, int32_t m, int32_t num_index_heads, float *out, void *stream);

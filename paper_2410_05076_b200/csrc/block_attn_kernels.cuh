@@ -12,9 +12,9 @@ namespace tidal {
 // output, a slice each; one cluster barrier later they add up what they received. So the kernel needs no scratch
 // memory, no counters and no second launch.
 // The matrix instructions have positions as rows and the group's heads as columns: S^T = K Q^T, O^T += V^T P^T, so K and V are read
-// once per KV head. The softmax weights enter the second product as the sum of two 16-bit numbers (bf16 over a bf16 cache,
-// fp16 over an 8-bit one): 2^-16 relative instead of 2^-8 for one, for eight more matrix instructions per block on a path that
-// waits for memory.
+// once per KV head. The softmax weights enter the second product as a sum of 16-bit numbers, three of bf16 over a bf16 cache (2^-24
+// relative), two of fp16 over an 8-bit one (2^-22): the path waits for memory, and the further matrix instructions cost it
+// 1 to 2 % (131072 positions, 256 blocks per KV head: 8.6 against 8.7 us) where one bf16 would leave 2^-8.
 struct BlockAttnParams {
     BlockCache c;
     const __nv_bfloat16* q;
@@ -29,12 +29,20 @@ struct BlockAttnParams {
     const float* v_scale;
 };
 
+// Weights that are split into fp16 numbers carry a factor 2^14 (which the sums share, so it cancels): the second number of a weight
+// below 2^-13 would otherwise fall below fp16's normal range.
+constexpr float W16_SHIFT = 14.f;
+
 template <int N>
 struct IntConst { static constexpr int value = N; };
 
+// Softmax state of a warp: running maxima (base 2) and sums of this lane's heads 2 tig, 2 tig + 1; o[t][0] their O^T elements in the first
+// fragment row of run t, o[t][1] in the second, as pairs of fp32. A block's products go into fresh accumulators that are then added:
+// the matrix instruction cuts what it adds to an accumulator, always downwards, which over the 32 blocks of a warp
+// left 1.1e-6 relative instead of 0.3e-6.
 struct BlockAcc {
     float m[2], l[2];
-    float o[8][4];
+    f32pair o[8][2];
 };
 
 // Raises the running maxima to cover this block's scaled logits; all lanes that share a tig agree afterwards.
@@ -50,24 +58,35 @@ __device__ __forceinline__ void raise_max(BlockAcc& acc, float mx0, float mx1) {
         const float a1 = (g1 == -INFINITY) ? 1.f : fast_exp2(acc.m[1] - g1);
         acc.l[0] *= a0;
         acc.l[1] *= a1;
+        const f32pair a = pair2(a0, a1);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) { acc.o[t][0] *= a0; acc.o[t][1] *= a1; acc.o[t][2] *= a0; acc.o[t][3] *= a1; }
+        for (int t = 0; t < 8; ++t) { acc.o[t][0] = mul2(acc.o[t][0], a); acc.o[t][1] = mul2(acc.o[t][1], a); }
         acc.m[0] = g0;
         acc.m[1] = g1;
     }
 }
 
 // Softmax weights of one block from its scaled logits t (rows gid, gid + 8; this lane's two heads).
+template <bool W16>
 __device__ __forceinline__ void block_weights(BlockAcc& acc, const float (&s)[4], float scale_log2, int nvalid, int gid, float (&w)[4]) {
     const bool v0 = gid < nvalid, v1 = gid + 8 < nvalid;
     const float t0 = v0 ? s[0] * scale_log2 : -INFINITY, t1 = v0 ? s[1] * scale_log2 : -INFINITY;
     const float t2 = v1 ? s[2] * scale_log2 : -INFINITY, t3 = v1 ? s[3] * scale_log2 : -INFINITY;
     raise_max(acc, fmaxf(t0, t2), fmaxf(t1, t3));
-    const float m0 = (acc.m[0] == -INFINITY) ? 0.f : acc.m[0], m1 = (acc.m[1] == -INFINITY) ? 0.f : acc.m[1];
+    const float shift = W16 ? W16_SHIFT : 0.f;
+    const float m0 = ((acc.m[0] == -INFINITY) ? 0.f : acc.m[0]) - shift, m1 = ((acc.m[1] == -INFINITY) ? 0.f : acc.m[1]) - shift;
     w[0] = fast_exp2(t0 - m0); w[1] = fast_exp2(t1 - m1);
     w[2] = fast_exp2(t2 - m0); w[3] = fast_exp2(t3 - m1);
     acc.l[0] += w[0] + w[2];
     acc.l[1] += w[1] + w[3];
+}
+
+__device__ __forceinline__ void add_block(BlockAcc& acc, const float (&d)[8][4]) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        acc.o[t][0] = add2(acc.o[t][0], pair2(d[t][0], d[t][1]));
+        acc.o[t][1] = add2(acc.o[t][1], pair2(d[t][2], d[t][3]));
+    }
 }
 
 // One block of a bf16 cache: 16 key rows at ks, 16 value rows at vs, 256 bytes each, piece c of row r at c ^ (r & 7).
@@ -87,20 +106,31 @@ __device__ __forceinline__ void consume_block(uint32_t ks, uint32_t vs, const ui
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] += s2[i];
     float w[4];
-    block_weights(acc, s, scale_log2, nvalid, gid, w);
+    block_weights<false>(acc, s, scale_log2, nvalid, gid, w);
+    // the weights as h + l + r, each rounded to bf16
+    auto low = [](uint32_t v) { return __uint_as_float(v << 16); };
+    auto high = [](uint32_t v) { return __uint_as_float(v & 0xffff0000u); };
     const uint32_t h0 = pack_bf16(w[0], w[1]), h1 = pack_bf16(w[2], w[3]);
-    const uint32_t l0 = pack_bf16(w[0] - __uint_as_float(h0 << 16), w[1] - __uint_as_float(h0 & 0xffff0000u));
-    const uint32_t l1 = pack_bf16(w[2] - __uint_as_float(h1 << 16), w[3] - __uint_as_float(h1 & 0xffff0000u));
+    w[0] -= low(h0); w[1] -= high(h0); w[2] -= low(h1); w[3] -= high(h1);
+    const uint32_t l0 = pack_bf16(w[0], w[1]), l1 = pack_bf16(w[2], w[3]);
+    const uint32_t r0 = pack_bf16(w[0] - low(l0), w[1] - high(l0)), r1 = pack_bf16(w[2] - low(l1), w[3] - high(l1));
     const uint32_t ph0 = movmatrix_trans(h0), ph1 = movmatrix_trans(h1), pl0 = movmatrix_trans(l0), pl1 = movmatrix_trans(l1);
+    const uint32_t pr0 = movmatrix_trans(r0), pr1 = movmatrix_trans(r1);
     const int rr = lane & 7, mb = (lane >> 3) & 1;
     const uint32_t vl = vs + (rr + ((lane >> 4) << 3)) * 256 + ((rr ^ mb) << 4);
+    // all of the value fragments first, then the products part by part: three in a row into one accumulator would wait for
+    // each other
+    uint32_t a[8][4];
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        uint32_t a[4];
-        ldmatrix_x4_trans(vl ^ (t << 5), a);
-        mma_bf16_16816(acc.o[t], a[0], a[1], a[2], a[3], ph0, ph1);
-        mma_bf16_16816(acc.o[t], a[0], a[1], a[2], a[3], pl0, pl1);
-    }
+    for (int t = 0; t < 8; ++t) ldmatrix_x4_trans(vl ^ (t << 5), a[t]);
+    float d[8][4];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) { d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f; mma_bf16_16816(d[t], a[t][0], a[t][1], a[t][2], a[t][3], pr0, pr1); }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) mma_bf16_16816(d[t], a[t][0], a[t][1], a[t][2], a[t][3], pl0, pl1);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) mma_bf16_16816(d[t], a[t][0], a[t][1], a[t][2], a[t][3], ph0, ph1);
+    add_block(acc, d);
 }
 
 __device__ __forceinline__ float f16_lo(uint32_t w) {
@@ -135,26 +165,28 @@ __device__ __forceinline__ void consume_block8(uint32_t ks, uint32_t vs, const u
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] += s2[i];
     float w[4];
-    block_weights(acc, s, scale_log2, nvalid, gid, w);
+    block_weights<true>(acc, s, scale_log2, nvalid, gid, w);
     const uint32_t h0 = pack_f16(w[0], w[1]), h1 = pack_f16(w[2], w[3]);
     const uint32_t l0 = pack_f16(w[0] - f16_lo(h0), w[1] - f16_hi(h0)), l1 = pack_f16(w[2] - f16_lo(h1), w[3] - f16_hi(h1));
     const uint32_t ph0 = movmatrix_trans(h0), ph1 = movmatrix_trans(h1), pl0 = movmatrix_trans(l0), pl1 = movmatrix_trans(l1);
     const int rr = lane & 7, mi = lane >> 3;
     const uint32_t vbase = vs + (rr + ((mi >> 1) << 3)) * ROW_BYTES8;
+    uint32_t a[8][4];                                       // as in consume_block: fragments first, then products part by part
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         uint32_t m[4];
         ldmatrix_x4_trans(vbase + ((uint32_t)((2 * u + (mi & 1)) ^ rr) << 4), m);
-        uint32_t x0, y0, x2, y2, x1, y1, x3, y3;
-        e4m3x4_to_f16x2x2(__byte_perm(m[0], 0, 0x3120), x0, y0);
-        e4m3x4_to_f16x2x2(__byte_perm(m[2], 0, 0x3120), x2, y2);
-        mma_f16_16816(acc.o[2 * u], x0, y0, x2, y2, ph0, ph1);
-        mma_f16_16816(acc.o[2 * u], x0, y0, x2, y2, pl0, pl1);
-        e4m3x4_to_f16x2x2(__byte_perm(m[1], 0, 0x3120), x1, y1);
-        e4m3x4_to_f16x2x2(__byte_perm(m[3], 0, 0x3120), x3, y3);
-        mma_f16_16816(acc.o[2 * u + 1], x1, y1, x3, y3, ph0, ph1);
-        mma_f16_16816(acc.o[2 * u + 1], x1, y1, x3, y3, pl0, pl1);
+        e4m3x4_to_f16x2x2(__byte_perm(m[0], 0, 0x3120), a[2 * u][0], a[2 * u][1]);
+        e4m3x4_to_f16x2x2(__byte_perm(m[2], 0, 0x3120), a[2 * u][2], a[2 * u][3]);
+        e4m3x4_to_f16x2x2(__byte_perm(m[1], 0, 0x3120), a[2 * u + 1][0], a[2 * u + 1][1]);
+        e4m3x4_to_f16x2x2(__byte_perm(m[3], 0, 0x3120), a[2 * u + 1][2], a[2 * u + 1][3]);
     }
+    float d[8][4];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) { d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f; mma_f16_16816(d[t], a[t][0], a[t][1], a[t][2], a[t][3], pl0, pl1); }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) mma_f16_16816(d[t], a[t][0], a[t][1], a[t][2], a[t][3], ph0, ph1);
+    add_block(acc, d);
 }
 
 constexpr int BA_STAGES = 3, BA_STAGES8 = 6;                // the same bytes in flight
@@ -300,7 +332,7 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 2 : 1) block_attn_kernel(co
     acc.m[0] = acc.m[1] = -INFINITY;
     acc.l[0] = acc.l[1] = 0.f;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) { acc.o[t][0] = acc.o[t][1] = acc.o[t][2] = acc.o[t][3] = 0.f; }
+    for (int t = 0; t < 8; ++t) acc.o[t][0] = acc.o[t][1] = 0ull;
 
     // One rolled loop, which first fills the ring and then refills it one block behind: unrolled over the slots the code does
     // not fit the instruction cache (a line fetched costs as much as the instructions in it twice over). The valid
@@ -358,8 +390,8 @@ __global__ void __launch_bounds__(NW * 32, NW == 4 ? 2 : 1) block_attn_kernel(co
                     const uint32_t at = cluster_addr(box + 4 * (uint32_t)(me * pitch + (q - dst * runs) * 16), dst);
                     // fragment rows: gid and gid + 8 of the run; over an 8-bit cache 2 gid and 2 gid + 1
                     const int d0 = KV8 ? 2 * gid : gid, d1 = KV8 ? d0 + 1 : d0 + 8;
-                    asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(at + 4 * d0), "f"(acc.o[t][u] * vscale) : "memory");
-                    asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(at + 4 * d1), "f"(acc.o[t][2 + u] * vscale) : "memory");
+                    asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(at + 4 * d0), "f"(half2(acc.o[t][0], u) * vscale) : "memory");
+                    asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(at + 4 * d1), "f"(half2(acc.o[t][1], u) * vscale) : "memory");
                 }
             }
         }

@@ -153,6 +153,34 @@ __global__ void __launch_bounds__(BB_WARPS * 32) block_bounds_kernel(const Bound
     }
 }
 
+// ---- pairs of fp32 in one instruction --------------------------------------------------------------------------
+using f32pair = unsigned long long;
+__device__ __forceinline__ f32pair pair2(float lo, float hi) {
+    f32pair d;
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ float half2(f32pair v, int i) {
+    float lo, hi;
+    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(lo), "=f"(hi) : "l"(v));
+    return i ? hi : lo;
+}
+__device__ __forceinline__ f32pair add2(f32pair a, f32pair b) {
+    f32pair d;
+    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32pair mul2(f32pair a, f32pair b) {
+    f32pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32pair fma2(f32pair a, f32pair b, f32pair c) {
+    f32pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+
 // ---- thread-block clusters -----------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
     uint32_t a;

@@ -143,20 +143,14 @@ __device__ __forceinline__ float query_part(uint2 q, int Hkv) {
 }
 
 // A matrix instruction that starts from zero; its results as two pairs of fp32.
-__device__ __forceinline__ void mma_from_zero(unsigned long long (&d)[2], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_from_zero(f32pair (&d)[2], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     float r[4];
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
                  : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-    asm("mov.b64 %0, {%1, %2};\n" : "=l"(d[0]) : "f"(r[0]), "f"(r[1]));
-    asm("mov.b64 %0, {%1, %2};\n" : "=l"(d[1]) : "f"(r[2]), "f"(r[3]));
+    d[0] = pair2(r[0], r[1]);
+    d[1] = pair2(r[2], r[3]);
 }
-__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {      // two fp32 additions
-    unsigned long long d;
-    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-
 // The scores of a tile of 16 blocks against a group of query heads: s[0], s[1] for row gid and heads 2 tig, 2 tig + 1; s[2], s[3]
 // for row gid + 8. query(half, j): the lane's piece tig + 4 j of q- (half 0) or q+ (1) of head gid, zero beyond the group. x0, x1:
 // the lane's pieces of rows gid and gid + 8. low, high: running maxima of the bits of the least and of the greatest keys,
@@ -164,11 +158,11 @@ __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigne
 // most negative one (or, if there is none, for the largest), as signed numbers those of the greatest for the largest.
 template <typename Q>
 __device__ __forceinline__ void score_tile(const uint4 (&x0)[8], const uint4 (&x1)[8], Q&& query, float (&s)[4], uint32_t& low, uint32_t& high) {
-    unsigned long long sum[2] = {0ull, 0ull};
+    f32pair sum[2] = {0ull, 0ull};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint4 q4 = query(j >> 2, j & 3);
-        unsigned long long d[2], e[2];
+        f32pair d[2], e[2];
         mma_from_zero(d, x0[j].x, x1[j].x, x0[j].y, x1[j].y, q4.x, q4.y);
         mma_from_zero(e, x0[j].z, x1[j].z, x0[j].w, x1[j].w, q4.z, q4.w);
 #pragma unroll
@@ -181,8 +175,8 @@ __device__ __forceinline__ void score_tile(const uint4 (&x0)[8], const uint4 (&x
             high = __vimax3_s16x2(high, x1[j].x, x1[j].y); high = __vimax3_s16x2(high, x1[j].z, x1[j].w);
         }
     }
-    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(s[0]), "=f"(s[1]) : "l"(sum[0]));
-    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(s[2]), "=f"(s[3]) : "l"(sum[1]));
+    s[0] = half2(sum[0], 0); s[1] = half2(sum[0], 1);
+    s[2] = half2(sum[1], 0); s[3] = half2(sum[1], 1);
 }
 // Start: low = 0, high = 0x80008000. Infinity where a bound is not finite: there is no error bound then.
 __device__ __forceinline__ float largest_bound(uint32_t low, uint32_t high) {

@@ -4,7 +4,7 @@
 
 #include <cuda_fp8.h>
 
-#include "attn_kernels.cuh"
+#include "block_kernels.cuh"
 
 namespace tidal {
 
@@ -203,11 +203,6 @@ struct KvWriteParams {
 // quotients is below 1024 (a remainder that underflows then belongs to a quotient below 2^-40, whose code is
 // zero); a division otherwise. Two elements per instruction: with one, and a guard on each, the kernel was bound by its
 // instructions: 65536 tokens of 8 heads 104 us with divisions, 87 us with single fused multiply-adds, 67 us this way (6.0 TB/s).
-__device__ __forceinline__ unsigned long long pair_of(float lo, float hi) {
-    unsigned long long d;
-    asm("mov.b64 %0, {%1, %2};\n" : "=l"(d) : "f"(lo), "f"(hi));
-    return d;
-}
 __device__ __noinline__ uint2 quantise8_unusual(uint4 w, float scale) {
     const uint32_t in[4] = {w.x, w.y, w.z, w.w};
     uint32_t half[4];
@@ -224,17 +219,12 @@ __device__ __forceinline__ uint2 quantise8(uint4 w, float scale, float inv, bool
     const uint32_t m2 = __vimax3_u16x2(__vimax3_u16x2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu, w.z & 0x7fff7fffu), w.w & 0x7fff7fffu, 0u);
     const float most = __uint_as_float(max(m2 << 16, m2 & 0xffff0000u));          // (magnitudes order like their bits)
     if (usual && most * inv < 1024.f) {
-        const unsigned long long r2 = pair_of(inv, inv), s2 = pair_of(-scale, -scale);
+        const f32pair r2 = pair2(inv, inv), s2 = pair2(-scale, -scale);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const unsigned long long x = pair_of(__uint_as_float(in[i] << 16), __uint_as_float(in[i] & 0xffff0000u));
-            unsigned long long q, e;
-            asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(q) : "l"(x), "l"(r2));
-            asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(e) : "l"(q), "l"(s2), "l"(x));
-            asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(q) : "l"(e), "l"(r2), "l"(q));
-            float lo, hi;
-            asm("mov.b64 {%0, %1}, %2;\n" : "=f"(lo), "=f"(hi) : "l"(q));
-            half[i] = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+            const f32pair x = pair2(__uint_as_float(in[i] << 16), __uint_as_float(in[i] & 0xffff0000u)), q0 = mul2(x, r2);
+            const f32pair q = fma2(fma2(q0, s2, x), r2, q0);
+            half[i] = __nv_cvt_float2_to_fp8x2(make_float2(half2(q, 0), half2(q, 1)), __NV_SATFINITE, __NV_E4M3);
         }
     } else {
         return quantise8_unusual(w, scale);

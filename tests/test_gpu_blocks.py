@@ -133,7 +133,7 @@ def ref_select(lay, q, m, gran, first, last):
 def ref_attn(lay, q, idx, cnt=None):
     """(out, tolerance) in 64 bits. Tolerance: the 16 matrix instructions of a logit add exact products with at most 2^-22 of the
     sum of their magnitudes each, 2^-18 together; the exponent's argument is rounded to fp32 (2^-24 of |t| log2 e, twice) and
-    ex2.approx gives 2^-22; a weight enters the second product with 2^-16 (two bf16, each off by at most 2^-8) and its up to
+    ex2.approx gives 2^-22; a weight enters the second product with 2^-22 (two fp16, each off by at most 2^-11, or three bf16, 2^-8 each) and its up to
     n / 16 instructions add 2^-22 each. An error r of the weights moves a weighted mean of v by at most 2 r max|v|."""
     B, hi = idx.shape[:2]
     hq, G = lay.num_q_heads, lay.num_q_heads // lay.num_kv_heads
@@ -155,7 +155,7 @@ def ref_attn(lay, q, idx, cnt=None):
             kk, vv, qq = k[h // G, pos], v[h // G, pos], q[b, h].double()
             t = (kk @ qq) * scale
             out[b, h] = torch.softmax(t, 0) @ vv
-            r = 2.0 ** -18 * float((kk.abs() @ qq.abs()).max()) * scale + 2.0 ** -22 * float(t.abs().max()) + 2.0 ** -16 + 2.0 ** -22 * (2 + row.numel())
+            r = 2.0 ** -18 * float((kk.abs() @ qq.abs()).max()) * scale + 2.0 ** -22 * float(t.abs().max()) + 2.0 ** -22 + 2.0 ** -22 * (2 + row.numel())
             tol[b, h] = 2 * r * float(vv.abs().max())
     return out, tol
 

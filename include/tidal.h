@@ -324,7 +324,8 @@ tidal_status_t tidal_kv_write(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t nu
 
 /* Key bounds of blocks: for block i of sequence b and KV head g the channelwise least and greatest key over the cached
  * positions of the block (positions at and beyond ctx_lens[b] do not count), as bf16 (exact; for an FP8 cache
- * of the codes' values without the scale), NaN where a key is NaN.
+ * of the codes' values without the scale), NaN where a key is NaN. A page that several sequences share must be full in
+ * all of them.
  *   bounds  device bf16, 16-byte aligned; contiguous caches [batch, num_kv_heads, bound_blocks, 2, head_dim] with
  *           bound_blocks >= ceil(max_ctx_len / 16), paged ones one entry per physical page,
  *           [bound_blocks, num_kv_heads, 2, head_dim] with bound_blocks >= num_pages; least keys first.

@@ -153,8 +153,10 @@ PyObject* kv_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (tokens && (row[i]->stride(2) != 1 || (d.kv->num_kv_heads > 1 && row[i]->stride(1) != d.kv->head_dim)))
                 refuse(std::string(name) + ": the rows of a token have to be contiguous");
         }
-        return f_kv_write(context(a[0]), d.kv, tokens, row[0]->data_ptr(), row[1]->data_ptr(), row[0]->stride(0), row[1]->stride(0),
-                          static_cast<const int64_t*>(slots.data_ptr()), stream_of(dev));
+        // (a single token's stride says nothing: torch may give any)
+        const int64_t one = (int64_t)d.kv->num_kv_heads * d.kv->head_dim;
+        return f_kv_write(context(a[0]), d.kv, tokens, row[0]->data_ptr(), row[1]->data_ptr(), tokens > 1 ? row[0]->stride(0) : one,
+                          tokens > 1 ? row[1]->stride(0) : one, static_cast<const int64_t*>(slots.data_ptr()), stream_of(dev));
     });
 }
 

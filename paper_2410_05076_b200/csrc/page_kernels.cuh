@@ -191,6 +191,7 @@ struct KvWriteParams {
     int num_tokens, Hkv, paged, max_ctx;
     long long num_slots;
     long long stride_b, stride_pos, stride_head, stride_page;
+    unsigned page_bytes, pos_bytes;       // the two strides in bytes where both fit 32 bits, else page_bytes = 0
     const float* k_scale;
     const float* v_scale;
     int* status;
@@ -199,10 +200,15 @@ struct KvWriteParams {
 // Eight elements' codes: the E4M3 values nearest to x / scale (the quotient in fp32, correctly rounded), saturated at +-448.
 // Not a division each: with r the correctly rounded reciprocal of s, q0 = x r and the exact remainder x - q0 s, q0 + r (x - q0 s)
 // rounds to x / s (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990) as
-// long as nothing leaves the range. So it is used where s is between 2^-60 and 2^60 and the largest of the eight
-// quotients is below 1024 (a remainder that underflows then belongs to a quotient below 2^-40, whose code is
-// zero); a division otherwise. Two elements per instruction: with one, and a guard on each, the kernel was bound by its
-// instructions: 65536 tokens of 8 heads 104 us with divisions, 87 us with single fused multiply-adds, 67 us this way (6.0 TB/s).
+// long as nothing leaves the range. So it is used where s is between 2^-60 and 2^60 and the eight elements are below 2^65 (a
+// remainder that underflows then belongs to a quotient below 2^-40, whose code is zero); a division otherwise. Two
+// elements per instruction, and few instructions besides: under load the power limit holds the SM clock at 1.6 GHz and it is the
+// instructions that bound this kernel.
+__device__ __forceinline__ uint32_t babs_max2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 __device__ __noinline__ uint2 quantise8_unusual(uint4 w, float scale) {
     const uint32_t in[4] = {w.x, w.y, w.z, w.w};
     uint32_t half[4];
@@ -216,9 +222,9 @@ __device__ __noinline__ uint2 quantise8_unusual(uint4 w, float scale) {
 __device__ __forceinline__ uint2 quantise8(uint4 w, float scale, float inv, bool usual) {
     const uint32_t in[4] = {w.x, w.y, w.z, w.w};
     uint32_t half[4];
-    const uint32_t m2 = __vimax3_u16x2(__vimax3_u16x2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu, w.z & 0x7fff7fffu), w.w & 0x7fff7fffu, 0u);
-    const float most = __uint_as_float(max(m2 << 16, m2 & 0xffff0000u));          // (magnitudes order like their bits)
-    if (usual && most * inv < 1024.f) {
+    // the largest magnitude of either half; 2^65 and more, infinities and not-a-numbers have both upper exponent bits set
+    const uint32_t most = babs_max2(babs_max2(w.x, w.y), babs_max2(w.z, w.w));
+    if (usual && !(most & (most << 1) & 0x40004000u)) {
         const f32pair r2 = pair2(inv, inv), s2 = pair2(-scale, -scale);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -265,7 +271,8 @@ __global__ void __launch_bounds__(KW_WARPS * 32, 6) kv_write_kernel(const KvWrit
         if (sc) { scale = __ldg(sc + g); inv = __frcp_rn(scale); }
     }
     const bool usual = scale >= 0x1p-60f && scale <= 0x1p60f;
-    const long long head = (long long)g * p.stride_head;
+    constexpr int ESZ = KV8 ? 1 : 2;
+    uint8_t* const base = dst + (long long)g * p.stride_head * ESZ + piece * (KV8 ? 8 : 16);
 #pragma unroll
     for (int i = 0; i < KW_TOKENS; ++i) {
         const unsigned long long s = (unsigned long long)slot[i];
@@ -273,12 +280,16 @@ __global__ void __launch_bounds__(KW_WARPS * 32, 6) kv_write_kernel(const KvWrit
             if (slot[i] != -1 && lane == 0) atomicOr(p.status, STATUS_BAD_INDEX);      // -1: padding
             continue;
         }
-        // (pages, and sequences times positions, fit 32 bits and 48 bits)
-        long long off = head;
-        if (p.paged) off += (long long)(unsigned)(s / TILE) * p.stride_page + (long long)(unsigned)(s % TILE) * p.stride_pos;
-        else off += (long long)(s / (unsigned)p.max_ctx) * p.stride_b + (long long)(s % (unsigned)p.max_ctx) * p.stride_pos;
-        if constexpr (KV8) *reinterpret_cast<uint2*>(dst + off + piece * 8) = quantise8(row[i], scale, inv, usual);
-        else *reinterpret_cast<uint4*>(dst + 2 * off + piece * 16) = row[i];
+        uint8_t* to;
+        if (p.paged) {                                      // (page numbers fit 32 bits; so do the strides, mostly)
+            const unsigned page = (unsigned)(s / TILE), place = (unsigned)s % TILE;
+            if (p.page_bytes) to = base + (unsigned long long)page * p.page_bytes + (unsigned long long)place * p.pos_bytes;
+            else to = base + ((long long)page * p.stride_page + (long long)place * p.stride_pos) * ESZ;
+        } else {
+            to = base + ((long long)(s / (unsigned)p.max_ctx) * p.stride_b + (long long)(s % (unsigned)p.max_ctx) * p.stride_pos) * ESZ;
+        }
+        if constexpr (KV8) *reinterpret_cast<uint2*>(to) = quantise8(row[i], scale, inv, usual);
+        else *reinterpret_cast<uint4*>(to) = row[i];
     }
 }
 

@@ -1407,6 +1407,10 @@ tidal_status_t tidal_kv_write(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t nu
     p.num_tokens = num_tokens; p.Hkv = kv->num_kv_heads; p.paged = kv->kv_layout == TIDAL_KV_PAGED; p.max_ctx = kv->max_ctx_len;
     p.num_slots = p.paged ? (long long)kv->num_pages * TILE : (long long)kv->batch * kv->max_ctx_len;
     p.stride_b = kv->stride_b; p.stride_pos = kv->stride_pos; p.stride_head = kv->stride_head; p.stride_page = kv->stride_page;
+    const long long esz = kv->kv_dtype == TIDAL_KV_FP8_E4M3 ? 1 : 2;
+    if (p.stride_page * esz <= 0xffffffffLL && p.stride_pos * esz <= 0xffffffffLL) {
+        p.page_bytes = (unsigned)(p.stride_page * esz); p.pos_bytes = (unsigned)(p.stride_pos * esz);
+    }
     p.k_scale = kv->k_scale; p.v_scale = kv->v_scale; p.status = ctx->status;
     return launch_block(ctx, kv->kv_dtype == TIDAL_KV_FP8_E4M3 ? kv_write_kernel<true> : kv_write_kernel<false>, p, (int)grid,
                         KW_WARPS * 32, 0, 0, (cudaStream_t)stream);

@@ -292,6 +292,44 @@ def test_select_with_ties_and_ranges_that_collapse(td, kind, ctx):
                 assert torch.equal(idx.long(), ref), (gran, m)
 
 
+def test_select_with_a_query_that_is_not_finite(td):
+    for ctx in (3000, 60000):
+        lay = make([ctx], 4, 2, "hnd", seed=7)
+        q, n = query(lay, 7), pages(ctx)
+        q[0, 1, 5] = float("nan")
+        q[0, 2, 9] = float("inf")
+        for gran in GRANS:
+            idx, _ = td.block_select(lay, td.block_bounds(lay), q, 9, gran, keep_last=1)
+            got = idx.cpu()
+            assert (got[..., 1:] > got[..., :-1]).all() and (got >= 0).all() and (got < n).all() and (got[..., -1] == n - 1).all()
+        ok, _ = td.block_select(lay, td.block_bounds(lay), q, 9, 0, keep_last=1)
+        fine = query(lay, 7)                              # the heads without one keep their sets
+        ref = ref_select(lay, fine, 9, 0, 0, 1)[0]
+        assert torch.equal(ok.cpu()[0, 0], ref[0, 0]) and torch.equal(ok.cpu()[0, 3], ref[0, 3])
+
+
+def test_pages_shared_by_sequences(td):
+    """A common prefix of full pages: one set of bounds serves both."""
+    lay = make([100, 70], 4, 2, "paged", seed=14)
+    lay.page_table[1, :4] = lay.page_table[0, :4]
+    lay.codes[1] = tuple(torch.cat((a[:, :64], b[:, 64:]), 1) for a, b in zip(lay.codes[0], lay.codes[1]))
+    lay.dense[1] = lay.codes[1]
+    q = query(lay, 14)
+    idx, cnt = td.block_select(lay, td.block_bounds(lay), q, 3, 1)
+    assert torch.equal(idx.cpu(), ref_select(lay, q, 3, 1, 0, 0)[0])
+    ref, tol = ref_attn(lay, q, idx.cpu())
+    close(td.block_attn(lay, q, idx, cnt), ref, tol, "shared pages")
+
+
+def test_a_closed_context_refuses(td):
+    t = binding.Tidal(0)
+    lay = make([40], 2, 1, "hnd", seed=0)
+    t.close()
+    with pytest.raises(binding.TidalError) as e:
+        t.block_bounds(lay)
+    assert e.value.status == binding.ERR_INVALID
+
+
 def test_select_score_is_a_bound_that_keeps_the_best_block(td):
     """With one block per head, it holds a key whose logit no other block's bound passes if it holds the dominant key."""
     lay = make([2000], 4, 2, "hnd", seed=21)
@@ -622,6 +660,14 @@ def test_kv_write_saturates_and_rounds_to_even(td):
     want = [448.0, 448.0, 448.0, -448.0, 448.0, -448.0, math.nan, 16.0, 20.0, -16.0, 0.0, 2.0 ** -8, 2.0 ** -9, 0.0, 0.0, 1.0]
     assert all((a == b) or (a != a and b != b) for a, b in zip(got, want)), got
     assert lay.v[0, 0, 4].float()[0] == 224.0
+
+
+def test_kv_write_of_one_token_takes_any_token_stride(td):
+    lay = make([16], 2, 2, "hnd", seed=0, spoil=False)
+    k = torch.randn(2, D, 1, device=DEV).to(torch.bfloat16).permute(2, 0, 1)      # stride 1 between its one token
+    k = torch.as_strided(k.contiguous(), (1, 2, D), (3, D, 1))
+    td.kv_write(lay, k, k, torch.tensor([5], device=DEV))
+    assert torch.equal(lay.k[0, :, 5], k[0]) and torch.equal(lay.v[0, :, 5], k[0])
 
 
 def test_kv_write_skips_and_reports_slots_outside_the_cache(td):

@@ -8,7 +8,10 @@
  * product and keeps the top k (token selection layers), and sparse attention
  * over only the positions kept by the last selection layer (all other
  * layers), and the cache update (the new token's key and value rows written
- * into the cache). Projections, position encodings and FFN are the caller's.
+ * into the cache). Beside it stand a coarser selection of whole blocks of 16
+ * tokens with its attention, and the filling of paged caches (page tables and
+ * slot maps from request lengths, many tokens' rows). Projections, position
+ * encodings and FFN are the caller's.
  *
  * Conventions shared by every call
  *   - All tensor pointers are DEVICE pointers unless a parameter says "host".

@@ -23,6 +23,9 @@ enum { STATUS_NO_PAGES = 8 };            // page_map: the request cannot be met,
 // what is read: the stack is read below F and written from F on, a table is read below P(old) and for shrinking
 // sequences, and written from P(old) on for growing ones. The one word that may be both is num_free: the last CTA to have read it
 // writes it (an arrival count, nobody waits).
+//
+// Bound by its chain (lengths, scan, barrier, search, table, slot), not by its 12 bytes a token: 64 requests' decode step 3.1 us,
+// 295 K tokens of 8 prompts 5.1 us.
 constexpr int PM_PER = 4;                                   // sequences per thread
 constexpr int PM_THREADS = 1024, PM_THREADS_SMALL = 256;
 constexpr int PM_MAX_BATCH = PM_THREADS * PM_PER;
@@ -180,7 +183,8 @@ __global__ void __launch_bounds__(NT) page_map_kernel(const PageMapParams p) {
 // ---- rows of many tokens into the cache ------------------------------------------------------------------
 // One warp per KV head and run of four tokens: lanes 0-15 move key rows, lanes 16-31 value rows, eight elements each, so that
 // every lane has four loads in flight and one scale for all of them. Bound by memory, every row is read and written once: 65536
-// tokens of 8 heads into a bf16 cache 82 us, 6.55 TB/s.
+// tokens of 8 heads into a bf16 cache 82 us, 6.55 TB/s; into an E4M3 cache, quantised, 62 us at full clock (6.5 TB/s), 72 us under
+// the power limit.
 struct KvWriteParams {
     uint8_t* k;
     uint8_t* v;

@@ -344,7 +344,7 @@ tidal_status_t tidal_block_bounds(tidal_ctx_t *ctx, const tidal_kv_t *kv, const 
  * each KV head's part is multiplied by its k_scale, which must be positive). Chosen are the m' = min(m, ceil(ctx_lens[b] / 16))
  * best, equal scores resolved toward the lower block, after the first keep_first and the last keep_last blocks, which count as better than
  * any score (lower ones first if they are more than m). The set is the one that the scores in 64 bits give. Blocks
- * with bounds that are not finite have an unspecified rank.
+ * with bounds, and index heads with queries, that are not finite have an unspecified order.
  *   idx       int32 [batch, Hi, m]: block numbers in ascending order, padded with -1.
  *   idx_count int32 [batch] or NULL: receives m'.
  * m <= 16384. With max_ctx_len <= 16384 no scratch memory is used; beyond that it is the context's and may grow inside the
@@ -357,7 +357,7 @@ tidal_status_t tidal_block_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const 
 /* Attention over the listed blocks: Eq. 1 restricted to the cached positions of the blocks listed for the query head's
  * index head h * Hi / Hq, renormalised over them. -1 is padding; any other entry outside the sequence's blocks is skipped and
  * reported as TIDAL_ERR_INDEX; a repeated block counts once per occurrence; any order. Only the first idx_count[b]
- * entries are read when idx_count is given, else m. A head without a valid entry gets zeros. num_index_heads
+ * entries count when idx_count is given, else m. A head without a valid entry gets zeros. num_index_heads
  * must be Hq, Hkv or 1. Output type as set by tidal_set_output_dtype; softmax weights enter the product with V
  * with 22 bits or more, statistics and sums are fp32. tidal_set_attend_newest has no effect here (keep_last does that).
  * Uses no scratch memory. */

@@ -846,7 +846,11 @@ bool prepare_block_kernels() {
     auto room = [](auto kernel, size_t bytes) {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
     };
-    return wide((const void*)block_select_kernel) && room(block_select_kernel, sc_smem(SC_MAX_BLOCKS, MAX_GROUP)) &&
+    auto select = [&](auto kernel, int blocks) {
+        return wide((const void*)kernel) && room(kernel, sc_smem(blocks, MAX_GROUP, SB_MAX_CLUSTER * SC_WARPS));
+    };
+    return select(block_select_kernel<2, false>, 64) && select(block_select_kernel<8, false>, 256) && select(block_select_kernel<0, false>, SC_MAX_BLOCKS) &&
+           select(block_select_kernel<0, true>, SC_MAX_BLOCKS) && select(block_select_kernel<16, false>, 512) &&
            room(block_score_kernel, SS_SMEM) && room(block_rank_kernel<256, 4>, 4096 * 8) && room(block_rank_kernel<512, 4>, 8192 * 8) &&
            room(block_rank_kernel<1024, 4>, 16384 * 8) &&
            wide((const void*)block_attn_kernel<false, 4>) && wide((const void*)block_attn_kernel<true, 4>) &&
@@ -946,7 +950,7 @@ tidal_status_t tidal_create(tidal_ctx_t** out, int device, size_t workspace_byte
     const bool compact_ok = cudaFuncSetAttribute(topk_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)compact_smem) == cudaSuccess;
     if (!prepare_block_kernels()) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     if (d0 <= 0 || d1 <= 0 || d2 < d1 || s0 <= 0 || s1 < s0 || e0 < d0 || e1 < d1 || e2 < s0 || !topk_ok || !compact_ok || !split_ok) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
-    count_clusters(block_select_kernel, SC_THREADS, sc_smem(SC_MAX_BLOCKS, 1), ctx->select_clusters);
+    count_clusters(block_select_kernel<0, false>, SC_THREADS, sc_smem(SC_MAX_BLOCKS, 1, 0), ctx->select_clusters);
     count_clusters(block_attn_kernel<false, 8>, 256, ba_smem<false>(MAX_GROUP, BA_MAX_CLUSTER, 8), ctx->attn_clusters);
     ctx->dense_slots = std::min(d0, d1);
     ctx->sparse_slots = s0;
@@ -1459,18 +1463,32 @@ tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     p.idx = idx; p.idx_count = idx_count;
     p.npad = (int)align_up((size_t)p.c.max_blocks, 32);
     p.scores = nullptr; p.err = nullptr; p.chunks = 0;
-    const int items = granularity == TIDAL_SEL_SHARED ? kv->batch : kv->batch * kv->num_kv_heads;
+    const bool shared_set = granularity == TIDAL_SEL_SHARED;
+    const int items = shared_set ? kv->batch : kv->batch * kv->num_kv_heads;
     const int rows = per_qhead ? p.c.G : 1;
     cudaStream_t st = (cudaStream_t)stream;
-    // Up to 16384 positions one launch scores and ranks: 1024 positions 6.0 us against 8.5 of two launches, 16384 positions 7.2
-    // against 9.5, eight ragged sequences of them 11.4 against 14.3 (a set per query head; only 256 items of one CTA each are
-    // slower, 27.0 against 25.3). Beyond, a cluster is too few SMs for an item: 131072 positions 19.5 us against 13.1.
+    // Up to 16384 positions one launch scores and ranks: 1024 positions 4.2 us against 8.4 of two launches, 16384 positions 7.0
+    // against 9.5, eight ragged sequences of them 10.3 against 14.3 (a set per query head; only 256 items of one CTA each are
+    // slower, 26.0 against 25.3). Beyond, a cluster is too few SMs for an item: 131072 positions 19.5 us against 12.8.
     if (p.c.max_blocks <= SC_MAX_BLOCKS) {
-        // The largest cluster that the item has work for (16 blocks per warp, a row to rank per CTA) with all items resident together.
-        const int useful = std::max(rows, (p.c.max_blocks + 16 * SC_WARPS - 1) / (16 * SC_WARPS));
-        int cluster = std::min(SB_MAX_CLUSTER, useful);
+        // A cluster with a tile per warp and a CTA per row, or the largest one with which all items are resident together; a shared set
+        // has a tile per KV head (6 sequences of 573 positions, 32 KV heads: 6.8 us; head after head in one CTA 53). Rows are ranked
+        // by a warp each where there are more of them than CTAs, which would rank them one after the other (43 sequences of 2048
+        // positions, 8 KV heads of 8 query heads: 15.2 us against 48.1; 24 of 6000: 17.7 against 29.4), and always up to 1024
+        // positions, with a single CTA (1024 positions, four heads: 4.4 us against 6.0 of a CTA per row; 1376 items of 85
+        // positions: 6.4 against 20.9). Else the CTA is faster (4096 positions, four heads: 7.1 us against 8.3).
+        const int tiles = (p.c.max_blocks + 15) / 16, tasks = shared_set ? tiles * p.c.Hkv : tiles;
+        const int want = shared_set ? tasks : (tasks + SC_WARPS - 1) / SC_WARPS;
+        int cluster = std::min(SB_MAX_CLUSTER, p.c.max_blocks <= 64 ? want : std::max(want, rows));
         while (cluster > 1 && ctx->select_clusters[cluster] < items) --cluster;
-        return launch_block(ctx, block_select_kernel, p, items * cluster, SC_THREADS, sc_smem(p.npad, (rows + cluster - 1) / cluster), cluster, st);
+        const bool by_warp = !shared_set && (p.c.max_blocks <= 64 || (p.c.max_blocks <= 512 && cluster < rows));
+        const int warps = by_warp ? std::max(std::min((tasks + cluster - 1) / cluster, SC_WARPS), (rows + cluster - 1) / cluster) : SC_WARPS;
+        const size_t smem = sc_smem(p.npad, (rows + cluster - 1) / cluster, shared_set ? cluster * warps : 0);
+        auto launch = [&](auto kernel) { return launch_block(ctx, kernel, p, items * cluster, warps * 32, smem, cluster, st); };
+        if (shared_set) return launch(block_select_kernel<0, true>);
+        if (!by_warp) return launch(block_select_kernel<0, false>);
+        if (p.c.max_blocks <= 64) return launch(block_select_kernel<2, false>);
+        return p.c.max_blocks <= 256 ? launch(block_select_kernel<8, false>) : launch(block_select_kernel<16, false>);
     }
     const BlockWs w = block_ws_layout(kv, per_qhead ? kv->num_q_heads : kv->num_kv_heads);
     const long long grid = (long long)kv->batch * kv->num_kv_heads * w.chunks;

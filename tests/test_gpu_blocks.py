@@ -292,6 +292,73 @@ def test_select_with_ties_and_ranges_that_collapse(td, kind, ctx):
                 assert torch.equal(idx.long(), ref), (gran, m)
 
 
+@pytest.mark.parametrize("gran", GRANS)
+@pytest.mark.parametrize("batch,hq,hkv,lo,hi,m", [
+    (45, 32, 32, 0, 85, 3), (40, 16, 2, 900, 3000, 20), (24, 32, 4, 2000, 6000, 40), (40, 8, 1, 16, 1024, 9),
+    (3, 64, 8, 17, 573, 4), (2, 32, 32, 1000, 3000, 33), (1, 40, 5, 16000, 16000, 300), (2, 30, 30, 1025, 4111, 60)])
+def test_select_of_many_items_and_many_heads(td, gran, batch, hq, hkv, lo, hi, m):
+    """A warp per row, a cluster per item, the KV heads of a shared set spread over warps."""
+    lens = [hi - (hi - lo) * i // max(batch - 1, 1) for i in range(batch)]
+    lay = make(lens, hq, hkv, "paged" if batch % 2 else "hnd", False, seed=batch)
+    q = query(lay, m)
+    gi = util.Guarded((batch, index_heads(lay, gran), m), torch.int32, DEV, fill=77)
+    idx, cnt = td.block_select(lay, td.block_bounds(lay), q, m, gran, keep_first=1, keep_last=1, idx=gi.t)
+    ref, ref_cnt = ref_select(lay, q, m, gran, 1, 1)
+    assert torch.equal(cnt.cpu(), ref_cnt)
+    assert torch.equal(idx.cpu(), ref)
+    gi.check("idx")
+    assert td.device_status() == binding.OK
+
+
+@pytest.mark.parametrize("kind", ["equal", "zero", "few_values", "near_ties", "nan"])
+@pytest.mark.parametrize("batch,hq,hkv,ctx", [(1, 8, 2, 1000), (3, 4, 1, 130), (24, 16, 2, 3000), (24, 16, 2, 6000), (1, 24, 12, 1000)])
+def test_select_with_ties_in_rows_ranked_by_a_warp(td, kind, batch, hq, hkv, ctx):
+    lay = make([ctx] * batch, hq, hkv, "hnd", seed=9)
+    n, G = pages(ctx), hq // hkv
+    q, g = query(lay, 5), gen(12)
+    rand = lambda *shape: torch.randn(*shape, 2, D, generator=g, device=DEV).sort(-2).values.to(torch.bfloat16)  # noqa: E731
+    if kind == "zero":
+        bounds = torch.zeros(batch, hkv, n, 2, D, dtype=torch.bfloat16, device=DEV)
+    elif kind == "few_values":
+        bounds = rand(batch, hkv, 3)[:, :, torch.randint(0, 3, (n,), generator=g, device=DEV)].contiguous()
+    elif kind == "nan":
+        bounds = rand(batch, hkv, n)
+        bounds[:, :, 5, 0, 3] = float("nan")
+    else:
+        bounds = rand(batch, hkv, 1).expand(batch, hkv, n, 2, D).contiguous()
+        if kind == "near_ties":                           # equal but for one small channel
+            bounds[..., 1, 17] = (1.0 + torch.randint(0, 60, (batch, hkv, n), generator=g, device=DEV) / 128.0).to(torch.bfloat16) * 2.0 ** -20
+            bounds[..., 0, 17] = 0.0
+    s = torch.maximum(q.double().view(batch, hkv, G, 1, D) * bounds[:, :, None, :, 0].double(),
+                      q.double().view(batch, hkv, G, 1, D) * bounds[:, :, None, :, 1].double()).sum(-1)      # [B, Hkv, G, n]
+    for gran, score in ((0, s.reshape(batch, hq, n)), (1, s.sum(2)), (2, s.sum((1, 2))[:, None])):
+        for m in (1, n // 2, n - 1):
+            idx, _ = td.block_select(lay, bounds, q, m, gran)
+            if kind == "nan":                             # an unspecified set, but a well-formed one
+                got = idx.cpu()
+                assert (got[..., 1:] > got[..., :-1]).all() and (got >= 0).all() and (got < n).all()
+            else:
+                ref = torch.sort(score, dim=-1, descending=True, stable=True).indices[..., :m].sort(-1).values
+                assert torch.equal(idx.long(), ref), (gran, m)
+
+
+@pytest.mark.parametrize("ctx", [900, 3000, 40000])
+def test_select_with_the_smallest_and_largest_numbers(td, ctx):
+    """Subnormal and huge bounds: what is decided in 64 bits is decided there exactly."""
+    lay = make([ctx], 4, 2, "hnd", seed=3)
+    n, g = pages(ctx), gen(13)
+    for scale in (2.0 ** -126, 2.0 ** -133, 2.0 ** 60):
+        q = (torch.randint(-3, 4, (1, 4, D), generator=g, device=DEV).double() * (1.0 if scale < 1 else 2.0 ** 20)).to(torch.bfloat16)
+        bounds = (torch.randint(-8, 9, (1, 2, n, 2, D), generator=g, device=DEV).sort(-2).values.double() * scale).to(torch.bfloat16)
+        assert torch.equal(bounds.double() / scale, (bounds.double() / scale).round())      # (nothing was rounded away)
+        s = torch.maximum(q.double().view(1, 2, 2, 1, D) * bounds[:, :, None, :, 0].double(),
+                          q.double().view(1, 2, 2, 1, D) * bounds[:, :, None, :, 1].double()).sum(-1)
+        for gran, score in ((0, s.reshape(1, 4, n)), (1, s.sum(2)), (2, s.sum((1, 2))[:, None])):
+            idx, _ = td.block_select(lay, bounds, q, 11, gran)
+            ref = torch.sort(score, dim=-1, descending=True, stable=True).indices[..., :11].sort(-1).values
+            assert torch.equal(idx.long(), ref), (scale, gran)
+
+
 def test_select_with_a_query_that_is_not_finite(td):
     for ctx in (3000, 60000):
         lay = make([ctx], 4, 2, "hnd", seed=7)

@@ -190,8 +190,7 @@ __device__ __forceinline__ void consume_block8(uint32_t ks, uint32_t vs, const u
 }
 
 constexpr int BA_STAGES = 3, BA_STAGES8 = 6;                // the same bytes in flight
-// Two shapes: eight warps with an SM to themselves for few items, whose blocks are then all in flight at once; four warps twice on
-// an SM otherwise.
+// Shapes: eight warps with an SM to themselves, or smaller CTAs that share one, eight warps in all (rule in tidal_api.cu).
 constexpr int BA_MAX_CLUSTER = 16;
 
 template <bool KV8>
@@ -205,7 +204,7 @@ __host__ __device__ constexpr size_t ba_inbox(int ncols, int cluster, int warps)
     return (size_t)cluster * warps * ((size_t)(ba_slice(ncols, cluster) + 8) * sizeof(float) + ncols * sizeof(float2)) + 8;
 }
 constexpr size_t BA_SLACK = 256;                            // ring slots start on 256-byte boundaries
-constexpr size_t ba_smem_most(int warps) { return (warps == 4 ? 113 : 227) * 1024; }     // two CTAs of four warps share an SM
+constexpr size_t ba_smem_most(int warps) { return (size_t)(warps == 8 ? 227 : warps == 4 ? 113 : warps == 2 ? 56 : 28) * 1024; }
 template <bool KV8>
 constexpr bool ba_over_ring(int ncols, int cluster, int warps) {
     return cluster == 1 || ba_ring<KV8>(warps) + ba_inbox(ncols, cluster, warps) + BA_SLACK > ba_smem_most(warps);
@@ -216,7 +215,7 @@ constexpr size_t ba_smem(int ncols, int cluster, int warps) {
 }
 
 template <bool KV8, int NW>
-__global__ void __launch_bounds__(NW * 32, NW == 4 ? 2 : 1) block_attn_kernel(const BlockAttnParams p) {
+__global__ void __launch_bounds__(NW * 32, 8 / NW) block_attn_kernel(const BlockAttnParams p) {
     constexpr int STAGES = KV8 ? BA_STAGES8 : BA_STAGES, SLOT = KV8 ? STAGE_BYTES8 : STAGE_BYTES;
     const BlockCache& c = p.c;
     extern __shared__ __align__(128) uint8_t smem_raw[];

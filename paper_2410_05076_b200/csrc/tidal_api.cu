@@ -75,7 +75,7 @@ struct tidal_ctx {
     int split_select = 1;
     int layer_overlap = 1;                      // layers of a step may stream their inputs while the layer before them finishes
     int select_clusters[17] = {};               // clusters of 1 .. 16 CTAs that are resident together: block selection
-    int attn_clusters[17] = {};                 // the same for eight-warp CTAs of the block attention
+    int attn_clusters[17] = {};                 // the same for four-warp CTAs of the block attention
     int64_t launches = 0;
     // Whole steps are recorded once as CUDA graphs (programmatic dependent launches included) and
     // replayed while every host-visible argument stays the same: one launch per step instead of one
@@ -849,16 +849,13 @@ bool prepare_block_kernels() {
     auto select = [&](auto kernel, int blocks) {
         return wide((const void*)kernel) && room(kernel, sc_smem(blocks, MAX_GROUP, SB_MAX_CLUSTER * SC_WARPS));
     };
+    auto attn = [&](auto kernel) { return wide((const void*)kernel) && room(kernel, BA_SMEM_MAX); };
     return select(block_select_kernel<2, false>, 64) && select(block_select_kernel<8, false>, 256) && select(block_select_kernel<0, false>, SC_MAX_BLOCKS) &&
            select(block_select_kernel<0, true>, SC_MAX_BLOCKS) && select(block_select_kernel<16, false>, 512) &&
            room(block_score_kernel, SS_SMEM) && room(block_rank_kernel<256, 4>, 4096 * 8) && room(block_rank_kernel<512, 4>, 8192 * 8) &&
            room(block_rank_kernel<1024, 4>, 16384 * 8) &&
-           wide((const void*)block_attn_kernel<false, 4>) && wide((const void*)block_attn_kernel<true, 4>) &&
-           wide((const void*)block_attn_kernel<false, 8>) && wide((const void*)block_attn_kernel<true, 8>) &&
-           cudaFuncSetAttribute(block_attn_kernel<false, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
-           cudaFuncSetAttribute(block_attn_kernel<true, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
-           cudaFuncSetAttribute(block_attn_kernel<false, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
-           cudaFuncSetAttribute(block_attn_kernel<true, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, BA_SMEM_MAX) == cudaSuccess &&
+           attn(block_attn_kernel<false, 8>) && attn(block_attn_kernel<true, 8>) && attn(block_attn_kernel<false, 4>) && attn(block_attn_kernel<true, 4>) &&
+           attn(block_attn_kernel<false, 2>) && attn(block_attn_kernel<true, 2>) && attn(block_attn_kernel<false, 1>) && attn(block_attn_kernel<true, 1>) &&
            cudaFuncSetAttribute(page_map_kernel<PM_THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (PM_MAX_BATCH + 1) * (int)sizeof(int)) == cudaSuccess;
 }
 
@@ -951,7 +948,7 @@ tidal_status_t tidal_create(tidal_ctx_t** out, int device, size_t workspace_byte
     if (!prepare_block_kernels()) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     if (d0 <= 0 || d1 <= 0 || d2 < d1 || s0 <= 0 || s1 < s0 || e0 < d0 || e1 < d1 || e2 < s0 || !topk_ok || !compact_ok || !split_ok) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     count_clusters(block_select_kernel<0, false>, SC_THREADS, sc_smem(SC_MAX_BLOCKS, 1, 0), ctx->select_clusters);
-    count_clusters(block_attn_kernel<false, 8>, 256, ba_smem<false>(MAX_GROUP, BA_MAX_CLUSTER, 8), ctx->attn_clusters);
+    count_clusters(block_attn_kernel<false, 4>, 128, ba_smem<false>(MAX_GROUP, BA_MAX_CLUSTER, 4), ctx->attn_clusters);
     ctx->dense_slots = std::min(d0, d1);
     ctx->sparse_slots = s0;
     if (cudaMalloc((void**)&ctx->status, 256) != cudaSuccess || cudaMemset(ctx->status, 0, 256) != cudaSuccess) {
@@ -1528,23 +1525,35 @@ tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const vo
     const int items = kv->batch * (Hi == kv->num_q_heads ? kv->num_q_heads : kv->num_kv_heads);
     const int ncols = Hi == kv->num_q_heads ? 1 : p.c.G;
     cudaStream_t st = (cudaStream_t)stream;
-    // Eight warps per CTA, an SM each, for few items with long lists, in clusters of four or eight that are resident together and leave
-    // every warp a block (131072 positions, 8 items of 256 blocks: 8.6 us against 8.9 with four warps; 32 items of 128: 9.4
-    // against 9.7). Else four warps, two CTAs per SM, in clusters that fill the GPU once (8 items of 16 blocks: 4.0 us against 4.4;
-    // 64 items of 128: 15.1 against 17.1).
-    auto launch = [&](auto kernel8, auto kernel4, auto smem_of, auto over_ring) -> tidal_status_t {
-        int cluster = 8;
-        while (cluster > 1 && (ctx->attn_clusters[cluster] < items || cluster * 8 > m)) cluster /= 2;
-        const int warps = cluster >= 4 ? 8 : 4;
-        if (warps == 4) {
-            cluster = 1;
-            while (cluster < 16 && (long long)items * cluster * 2 <= ctx->sm_count && cluster * 8 <= m) cluster *= 2;
+    // An item's warps: as many as its list has blocks, or as the GPU has room for, eight per SM. Four to a CTA, in clusters of up to 16 with
+    // an SM per CTA (8 items of 256 blocks: 8.9 us in clusters of 16, 9.9 of 8). Eight to a CTA where the items leave no room for
+    // more CTAs (32 items of 256 blocks over an 8-bit cache: 10.3 us against 13.6 with four) and the list is long enough to pay for
+    // the larger merge, which grows with the heads (64 items of 16 blocks of 8 heads: 9.7 us, 6.5 with four). Single warps in
+    // clusters of four, which spread more evenly, for long lists of more items than SMs (256 items of 128 blocks, 8 bits: 25.1 us
+    // against 26.1). Two or one to a CTA where there are more items than CTAs of four that the GPU holds (384 items of 10
+    // blocks: 7.0 us against 9.7; 704 of 2: 5.1 against 10.5).
+    auto launch = [&](auto kernel8, auto kernel4, auto kernel2, auto kernel1, auto smem_of, auto over_ring) -> tidal_status_t {
+        const int sms = ctx->sm_count, list = std::min(m, p.c.max_blocks);
+        int cluster = 1, warps = 4;
+        if (items > 4 * sms) {
+            warps = 1;
+        } else if (items > 2 * sms) {
+            warps = 2;
+        } else if (items > sms) {
+            if (list >= 64 && ctx->attn_clusters[4] > 0) warps = 1, cluster = 4;
+        } else {
+            while (cluster < BA_MAX_CLUSTER && items * cluster * 2 <= sms && cluster * 5 < list && ctx->attn_clusters[cluster * 2] >= items) cluster *= 2;
+            if (cluster <= 4 && cluster * 4 < list && items * cluster * 2 > sms && (cluster == 1 || list >= cluster * (8 + 4 * ncols))) warps = 8;
         }
         p.over_ring = over_ring(ncols, cluster, warps);
-        return launch_block(ctx, warps == 8 ? kernel8 : kernel4, p, items * cluster, warps * 32, smem_of(ncols, cluster, warps), cluster, st);
+        return launch_block(ctx, warps == 8 ? kernel8 : warps == 4 ? kernel4 : warps == 2 ? kernel2 : kernel1, p, items * cluster, warps * 32,
+                            smem_of(ncols, cluster, warps), cluster, st);
     };
-    if (fp8) return launch(block_attn_kernel<true, 8>, block_attn_kernel<true, 4>, ba_smem<true>, ba_over_ring<true>);
-    return launch(block_attn_kernel<false, 8>, block_attn_kernel<false, 4>, ba_smem<false>, ba_over_ring<false>);
+    if (fp8)
+        return launch(block_attn_kernel<true, 8>, block_attn_kernel<true, 4>, block_attn_kernel<true, 2>, block_attn_kernel<true, 1>, ba_smem<true>,
+                      ba_over_ring<true>);
+    return launch(block_attn_kernel<false, 8>, block_attn_kernel<false, 4>, block_attn_kernel<false, 2>, block_attn_kernel<false, 1>, ba_smem<false>,
+                  ba_over_ring<false>);
 }
 
 int64_t tidal_launch_count(const tidal_ctx_t* ctx) { return ctx ? ctx->launches : 0; }

@@ -453,6 +453,24 @@ def test_attention_over_listed_blocks(td, layout, fp8, lens, hq, hkv, m):
     assert td.device_status() == binding.OK
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("batch,hq,hkv,hi,m,ctx", [
+    (10, 32, 32, 32, 3, 150), (20, 33, 33, 33, 5, 90), (60, 32, 8, 8, 2, 70), (80, 64, 8, 8, 3, 60), (19, 64, 8, 1, 9, 200),
+    (3, 64, 8, 64, 70, 1500), (25, 56, 8, 8, 66, 1200), (12, 32, 4, 4, 70, 1300), (4, 64, 16, 1, 40, 900), (2, 16, 16, 16, 400, 7000)])
+def test_attention_of_many_items(td, fp8, batch, hq, hkv, hi, m, ctx):
+    """One, two, four and eight warps to a CTA, alone and in clusters."""
+    lens = [ctx - (ctx - 1) * i // (batch + 1) for i in range(batch)]
+    lens[batch // 2] = 0
+    lay = make(lens, hq, hkv, "paged", fp8, seed=batch)
+    q, idx = query(lay, m), some_blocks(lens, hi, m, m)
+    guard = util.Guarded((batch, hq, D), torch.float32, DEV, fill=9e9)
+    td.block_attn(lay, q, idx.to(DEV), out=guard.t)
+    ref, tol = ref_attn(lay, q, idx)
+    close(guard.t, ref, tol, "many items")
+    guard.check("out")
+    assert td.device_status() == binding.OK
+
+
 def test_attention_bf16_outputs(td):
     lay = make([900, 55], 8, 2, "paged", seed=1)
     q, idx = query(lay, 1), some_blocks([900, 55], 2, 20, 4)

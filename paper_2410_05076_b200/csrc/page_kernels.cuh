@@ -25,9 +25,9 @@ enum { STATUS_NO_PAGES = 8 };            // page_map: the request cannot be met,
 // writes it (an arrival count, nobody waits).
 //
 // Bound by its chain (lengths, scan, barrier, search, table, slot), not by its 12 bytes a token: 64 requests' decode step 3.1 us,
-// 295 K tokens of 8 prompts 5.1 us.
+// 295 K tokens of 8 prompts 4.9 us.
 constexpr int PM_PER = 4;                                   // sequences per thread
-constexpr int PM_THREADS = 1024, PM_THREADS_SMALL = 256;
+constexpr int PM_THREADS = 1024, PM_THREADS_SMALL = 256;        // by the number of sequences (rule in tidal_api.cu)
 constexpr int PM_MAX_BATCH = PM_THREADS * PM_PER;
 
 struct PageMapParams {
@@ -146,13 +146,13 @@ __global__ void __launch_bounds__(NT) page_map_kernel(const PageMapParams p) {
             if ((unsigned)page >= (unsigned)p.num_pages) atomicOr(p.status, STATUS_BAD_PAGE);
             p.page_table[(long long)b * p.max_pages + (p.old_lens[b] + TILE - 1) / TILE + (i - s_grow[b])] = page;
         }
-        for (int t = gtid; t < p.max_tokens; t += gsize) {
+        for (unsigned t = gtid; t < (unsigned)p.max_tokens; t += gsize) {          // (max_tokens + gsize may pass 2^31)
             long long slot = -1;
             int pos = -1;
-            if (t < T) {
-                const int b = owner_of(s_tok, p.batch, t);
+            if (t < (unsigned)T) {
+                const int b = owner_of(s_tok, p.batch, (int)t);
                 const int o = p.old_lens[b], held = (o + TILE - 1) / TILE;
-                pos = o + (t - s_tok[b]);
+                pos = o + ((int)t - s_tok[b]);
                 const int blk = pos / TILE;
                 const int page = blk < held ? p.page_table[(long long)b * p.max_pages + blk] : taken(s_grow[b] + blk - held);
                 if ((unsigned)page < (unsigned)p.num_pages) slot = (long long)page * TILE + (pos & (TILE - 1));
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(NT) page_map_kernel(const PageMapParams p) {
         // pages given back and not taken again stay on the stack: elements F .. F + R - N - 1, which nobody reads
         for (int j = gtid; j < R - N; j += gsize) p.free_pages[F + j] = released(j);
     } else {
-        for (int t = gtid; t < p.max_tokens; t += gsize) { p.slots[t] = -1; if (p.positions) p.positions[t] = -1; }
+        for (unsigned t = gtid; t < (unsigned)p.max_tokens; t += gsize) { p.slots[t] = -1; if (p.positions) p.positions[t] = -1; }
         if (gtid == 0) atomicOr(p.status, STATUS_NO_PAGES);
     }
     if (p.token_offsets) for (int b = gtid; b <= p.batch; b += gsize) p.token_offsets[b] = ok ? s_tok[b] : 0;

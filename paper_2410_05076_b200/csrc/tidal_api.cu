@@ -1381,12 +1381,15 @@ tidal_status_t tidal_page_map(tidal_ctx_t* ctx, int32_t batch, const int32_t* ol
     p.slots = (long long*)slots; p.positions = positions; p.token_offsets = token_offsets; p.status = ctx->status;
     p.arrivals = ctx->status + 32;                           // (a line of its own behind the status word, zeroed with it at creation)
     const size_t smem = 3 * ((size_t)batch + 1) * sizeof(int);
-    // A CTA for every 2048 tokens (295 K tokens of 8 prompts: 5.1 us, 26.5 with one cluster). A decode step's few tokens and lengths
-    // take one of 256 threads, whose barriers and scans are the shorter chain: 64 requests 3.1 us, 3.8 with 1024 threads.
-    const int grid = std::min(ctx->sm_count, (max_tokens + 2047) / 2048);
-    if (grid <= 1 && batch <= PM_THREADS_SMALL * PM_PER && max_tokens <= 4 * PM_THREADS_SMALL)
-        return launch_block(ctx, page_map_kernel<PM_THREADS_SMALL>, p, 1, PM_THREADS_SMALL, smem, 0, (cudaStream_t)stream);
-    return launch_block(ctx, page_map_kernel<PM_THREADS>, p, std::max(grid, 1), PM_THREADS, smem, 0, (cudaStream_t)stream);
+    // CTAs of 256 threads, whose barriers and scans are the shorter chain, for as many sequences as their scan holds, one for every
+    // 512 tokens (64 requests' decode step: 3.1 us, 3.8 with 1024 threads; 295 K tokens of 8 prompts: 4.9 us, 5.1 with 1024 threads
+    // for every 2048).
+    if (batch <= PM_THREADS_SMALL * PM_PER) {
+        const int grid = std::max(1, std::min(4 * ctx->sm_count, (int)(((long long)max_tokens + 511) / 512)));
+        return launch_block(ctx, page_map_kernel<PM_THREADS_SMALL>, p, grid, PM_THREADS_SMALL, smem, 0, (cudaStream_t)stream);
+    }
+    const int grid = std::max(1, std::min(ctx->sm_count, (int)(((long long)max_tokens + 2047) / 2048)));
+    return launch_block(ctx, page_map_kernel<PM_THREADS>, p, grid, PM_THREADS, smem, 0, (cudaStream_t)stream);
 }
 
 tidal_status_t tidal_kv_write(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t num_tokens, const void* k_new, const void* v_new,

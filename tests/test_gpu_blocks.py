@@ -652,6 +652,23 @@ def test_page_map_large_batches(td, batch):
     assert td.device_status() == binding.OK
 
 
+@pytest.mark.parametrize("fits", [True, False])
+def test_page_map_with_the_largest_number_of_tokens(td, fits):
+    """max_tokens next to 2^31: what is behind the last token is filled, and no counter wraps."""
+    cap = 2 ** 31 - 1
+    slots = torch.full((cap,), 7, dtype=torch.int64, device=DEV)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    old, new = ints([3, 0]), ints([40, 17 if fits else 10 ** 6])
+    table, free = torch.zeros(2, 4, dtype=torch.int32, device=DEV), torch.arange(9, dtype=torch.int32, device=DEV)
+    td.page_map(old, new, table, free, ints([8]), slots)
+    assert td.device_status() == (binding.OK if fits else binding.ERR_PAGES)
+    used = 54 if fits else 0
+    assert (slots[:used] >= 0).all()
+    assert all(int((part != -1).sum()) == 0 for part in slots[used:].split(2 ** 28))
+    del slots
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("why", ["pages", "tokens", "length", "negative", "count", "page", "overfull"])
 @pytest.mark.parametrize("cap", [400, 20000])
 def test_page_map_that_does_not_fit_changes_nothing(td, why, cap):

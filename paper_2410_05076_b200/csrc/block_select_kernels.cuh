@@ -888,28 +888,29 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
 }
 
 // ---- long contexts: scores by the whole GPU, then a CTA per row ----------------------------------------------------
-// The scores are a stream of 8 KB tiles (16 blocks of one KV head). Every warp has SS_TILES of them in a row and a private
-// cp.async ring in shared memory; a slot is free as soon as its tile is in registers, so that two tiles are under way while
-// one is worked on. (With loads straight into registers a warp had nothing under way while it worked.)
-constexpr int SS_WARPS = 4, SS_TILES = 4, SS_STAGES = 2;
-constexpr int SS_BLOCKS = SS_WARPS * SS_TILES * 16;         // blocks per CTA: a chunk
+// The scores are a stream of 8 KB tiles (16 blocks of one KV head). A warp, which is a CTA (so that what is left at the end is small),
+// has SS_TILES of them in a row and a cp.async ring in shared memory; a slot is free as soon as its tile is in registers, so
+// that two tiles are under way while one is worked on. (With loads straight into registers a warp had nothing under way while it
+// worked. Four warps to a CTA and two slots: 12.8 and 23.3 us for the whole selection of 131072 positions and of a ragged batch of
+// 8 x 65536; a warp and three slots: 12.4 and 22.8; four slots, with fewer CTAs per SM: 13.7 and 23.7.)
+constexpr int SS_TILES = 4, SS_STAGES = 3;
+constexpr int SS_BLOCKS = SS_TILES * 16;                    // blocks per warp: a chunk
 constexpr int SS_ROW = BOUND_ELEMS * 2;                     // bytes of a block's bounds
 constexpr int SS_SLOT = 16 * SS_ROW;
-constexpr size_t SS_SMEM = (size_t)SS_WARPS * SS_STAGES * SS_SLOT;
+constexpr size_t SS_SMEM = (size_t)SS_STAGES * SS_SLOT;
 
-__global__ void __launch_bounds__(SS_WARPS * 32, 3) block_score_kernel(const __grid_constant__ SelectBlocksParams p) {
+__global__ void __launch_bounds__(32, 9) block_score_kernel(const __grid_constant__ SelectBlocksParams p) {
     const BlockCache& c = p.c;
     extern __shared__ __align__(128) uint8_t ss_ring[];
-    __shared__ float s_amax[SS_WARPS];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    const int lane = threadIdx.x, gid = lane >> 2, tig = lane & 3;
     // KV heads innermost: the CTAs that run together then read neighbouring 512 bytes of the same physical pages.
     const int part = blockIdx.x / c.Hkv, g = blockIdx.x - part * c.Hkv;
     const int b = part / p.chunks, chunk = part - b * p.chunks;
-    const int blk0 = (chunk * SS_WARPS + warp) * SS_TILES * 16;          // this warp's first block
+    const int blk0 = chunk * SS_BLOCKS;                     // the first block
     pdl_wait();
     pdl_trigger();
     const int len = c.ctx_lens[b];
-    // Rows of the bounds, in units of `pitch`, of this warp's blocks: lane l keeps blocks l, l + 32, ... Table entries are read along
+    // Rows of the bounds, in units of `pitch`, of the chunk's blocks: lane l keeps blocks l, l + 32, ... Table entries are read along
     // with the length, as far as the table goes, whatever it holds there.
     constexpr int PER = SS_TILES / 2;
     int at[PER];
@@ -924,7 +925,7 @@ __global__ void __launch_bounds__(SS_WARPS * 32, 3) block_score_kernel(const __g
 #pragma unroll
     for (int j = 0; j < 4; ++j) q4[j] = on ? __ldg(qp + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
     const int n = (max(min(len, c.max_ctx), 0) + TILE - 1) / TILE;
-    if (chunk * SS_BLOCKS >= n) return;
+    if (blk0 >= n) return;
     if (c.paged) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
@@ -935,8 +936,8 @@ __global__ void __launch_bounds__(SS_WARPS * 32, 3) block_score_kernel(const __g
     }
     const uint8_t* base = reinterpret_cast<const uint8_t*>(p.bounds) + (c.paged ? (long long)g : ((long long)b * c.Hkv + g) * c.bound_blocks) * SS_ROW + lane * 16;
     const long long pitch = c.paged ? (long long)c.Hkv * SS_ROW : SS_ROW;
-    const uint32_t ring = smem_u32(ss_ring) + warp * SS_STAGES * SS_SLOT;
-    const int valid = min(SS_TILES * 16, n - blk0), tiles = valid > 0 ? (valid + 15) / 16 : 0;
+    const uint32_t ring = smem_u32(ss_ring);
+    const int valid = min(SS_BLOCKS, n - blk0), tiles = (valid + 15) / 16;
     // One instruction copies a block's 512 bytes; piece c of row r goes to c ^ ((r & 1) << 2), so that the fragment reads
     // below (two rows, four pieces per eight lanes) meet no bank twice. The last block stands in for those behind it.
     auto issue = [&](int t, uint32_t slot) {
@@ -1004,39 +1005,32 @@ __global__ void __launch_bounds__(SS_WARPS * 32, 3) block_score_kernel(const __g
             if (tig == 0 && r1 < n) row[r1] = y * f;
         }
     }
-    float amax = largest_bound(low, high);
     // ---- the chunk's share of e, per row ---------------------------------------------------------------------------------
-    amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
-    if (lane == 0) s_amax[warp] = amax;
-    __syncthreads();
-    if (warp == 0) {
+    const float amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(largest_bound(low, high))));
+    // 2^-15 max|q| + (24 + Hkv) 2^-24 sum|q| of head gid, whose row the four lanes of a gid hold between them
+    float big = 0.f, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < SS_WARPS; ++w) amax = fmaxf(amax, s_amax[w]);
-        // 2^-15 max|q| + (24 + Hkv) 2^-24 sum|q| of head gid, whose row the four lanes of a gid hold between them
-        float big = 0.f, sum = 0.f;
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t w[4] = {q4[j].x, q4[j].y, q4[j].z, q4[j].w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t w[4] = {q4[j].x, q4[j].y, q4[j].z, q4[j].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float lo = fabsf(__uint_as_float(w[i] << 16)), hi = fabsf(__uint_as_float(w[i] & 0xffff0000u));
-                big = fmaxf(big, fmaxf(lo, hi));
-                sum += lo + hi;
-            }
+        for (int i = 0; i < 4; ++i) {
+            const float lo = fabsf(__uint_as_float(w[i] << 16)), hi = fabsf(__uint_as_float(w[i] & 0xffff0000u));
+            big = fmaxf(big, fmaxf(lo, hi));
+            sum += lo + hi;
         }
+    }
 #pragma unroll
-        for (int sh = 1; sh <= 2; sh <<= 1) {
-            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, sh));
-            sum += __shfl_xor_sync(0xffffffffu, sum, sh);
-        }
-        float e = on ? amax * (big * (1.f / 32768.f) + sum * (float)(24 + c.Hkv) * (1.f / 16777216.f)) * fabsf(f) : 0.f;
-        if (p.mode == 0) {
-            if (on && tig == 0) p.err[((long long)b * c.Hq + g * c.G + gid) * p.chunks + chunk] = e;
-        } else {
+    for (int sh = 1; sh <= 2; sh <<= 1) {
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, sh));
+        sum += __shfl_xor_sync(0xffffffffu, sum, sh);
+    }
+    float e = on ? amax * (big * (1.f / 32768.f) + sum * (float)(24 + c.Hkv) * (1.f / 16777216.f)) * fabsf(f) : 0.f;
+    if (p.mode == 0) {
+        if (on && tig == 0) p.err[((long long)b * c.Hq + g * c.G + gid) * p.chunks + chunk] = e;
+    } else {
 #pragma unroll
-            for (int sh = 4; sh <= 16; sh <<= 1) e += __shfl_xor_sync(0xffffffffu, e, sh);
-            if (lane == 0) p.err[((long long)b * c.Hkv + g) * p.chunks + chunk] = e;
-        }
+        for (int sh = 4; sh <= 16; sh <<= 1) e += __shfl_xor_sync(0xffffffffu, e, sh);
+        if (lane == 0) p.err[((long long)b * c.Hkv + g) * p.chunks + chunk] = e;
     }
 }
 
@@ -1088,7 +1082,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) block_rank_kernel(const __grid_c
     const int n = (max(min(len, c.max_ctx), 0) + TILE - 1) / TILE, used = (n + SS_BLOCKS - 1) / SS_BLOCKS;
     // e: the sum over the rows added up is at most their number times the largest
     float err = tid < errs && tid % p.chunks < used ? err0 : 0.f;
-#pragma unroll 1
+#pragma unroll 4
     for (int i = tid + NT; i < errs; i += NT) if (i % p.chunks < used) err = fmaxf(err, __ldcg(p.err + row0 * p.chunks + i));
     err *= (float)sum_rows;
     if (hi == 0 && tid == 0 && p.idx_count) p.idx_count[b] = min(p.m, n);

@@ -1496,7 +1496,7 @@ tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     if ((rc = ensure_block_ws(ctx, w.total, &st)) != TIDAL_OK) return rc;
     p.scores = (float*)((char*)ctx->blk_ws + w.scores); p.err = (float*)((char*)ctx->blk_ws + w.err);
     p.chunks = w.chunks;
-    if ((rc = launch_block(ctx, block_score_kernel, p, (int)grid, SS_WARPS * 32, SS_SMEM, 0, st)) != TIDAL_OK) return rc;
+    if ((rc = launch_block(ctx, block_score_kernel, p, (int)grid, 32, SS_SMEM, 0, st)) != TIDAL_OK) return rc;
     // Sixteen scores per thread, with as few threads as that takes: their barriers and scans are the shorter chain (131072
     // positions, 8 rows: 13.1 us with 512 threads, 13.9 with 1024; ragged batch of 8 x 65536, 256 rows: 25.2 us with 256, 28.3 with 1024).
     const int rank_rows = kv->batch * Hi;

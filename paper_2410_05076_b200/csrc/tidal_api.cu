@@ -1531,10 +1531,12 @@ tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const vo
     // An item's warps: as many as its list has blocks, or as the GPU has room for, eight per SM. Four to a CTA, in clusters of up to 16 with
     // an SM per CTA (8 items of 256 blocks: 8.9 us in clusters of 16, 9.9 of 8). Eight to a CTA where the items leave no room for
     // more CTAs (32 items of 256 blocks over an 8-bit cache: 10.3 us against 13.6 with four) and the list is long enough to pay for
-    // the larger merge, which grows with the heads (64 items of 16 blocks of 8 heads: 9.7 us, 6.5 with four). Single warps in
-    // clusters of four, which spread more evenly, for long lists of more items than SMs (256 items of 128 blocks, 8 bits: 25.1 us
-    // against 26.1). Two or one to a CTA where there are more items than CTAs of four that the GPU holds (384 items of 10
-    // blocks: 7.0 us against 9.7; 704 of 2: 5.1 against 10.5).
+    // the larger merge, which grows with the heads (64 items of 16 blocks of 8 heads: 9.7 us, 6.5 with four). Single warps, in
+    // clusters of four to six that fill seven of an SM's eight places (not all clusters would find eight), for more items than SMs with
+    // lists that pay for the merge: warps spread more evenly than CTAs of four (160 items of 128 blocks, 8 bits: 19.3 us
+    // against 25.4; 256 items: 25.2 against 26.1; 160 items of 24 blocks, 4 heads: 9.4 against 9.0; 256 of 64, 8 heads: 21.8 against
+    // 18.5). Two or one to a CTA where there are more items than CTAs of four that the GPU holds (384 items of 10 blocks:
+    // 7.0 us against 9.7; 704 of 2: 5.1 against 10.5).
     auto launch = [&](auto kernel8, auto kernel4, auto kernel2, auto kernel1, auto smem_of, auto over_ring) -> tidal_status_t {
         const int sms = ctx->sm_count, list = std::min(m, p.c.max_blocks);
         int cluster = 1, warps = 4;
@@ -1543,7 +1545,8 @@ tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const vo
         } else if (items > 2 * sms) {
             warps = 2;
         } else if (items > sms) {
-            if (list >= 64 && ctx->attn_clusters[4] > 0) warps = 1, cluster = 4;
+            const int share = std::min(7 * sms / items, 6);
+            if (share >= 4 && ncols <= 4 && list >= 16 * ncols && ctx->attn_clusters[share] > 0) warps = 1, cluster = share;
         } else {
             while (cluster < BA_MAX_CLUSTER && items * cluster * 2 <= sms && cluster * 5 < list && ctx->attn_clusters[cluster * 2] >= items) cluster *= 2;
             if (cluster <= 4 && cluster * 4 < list && items * cluster * 2 > sms && (cluster == 1 || list >= cluster * (8 + 4 * ncols))) warps = 8;

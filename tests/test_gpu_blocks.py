@@ -456,7 +456,8 @@ def test_attention_over_listed_blocks(td, layout, fp8, lens, hq, hkv, m):
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("batch,hq,hkv,hi,m,ctx", [
     (10, 32, 32, 32, 3, 150), (20, 33, 33, 33, 5, 90), (60, 32, 8, 8, 2, 70), (80, 64, 8, 8, 3, 60), (19, 64, 8, 1, 9, 200),
-    (3, 64, 8, 64, 70, 1500), (25, 56, 8, 8, 66, 1200), (12, 32, 4, 4, 70, 1300), (4, 64, 16, 1, 40, 900), (2, 16, 16, 16, 400, 7000)])
+    (3, 64, 8, 64, 70, 1500), (25, 56, 8, 8, 66, 1200), (12, 32, 4, 4, 70, 1300), (4, 64, 16, 1, 40, 900), (2, 16, 16, 16, 400, 7000), (5, 32, 32, 32, 30, 600),
+    (12, 64, 16, 16, 70, 1300), (23, 8, 8, 8, 20, 500)])
 def test_attention_of_many_items(td, fp8, batch, hq, hkv, hi, m, ctx):
     """One, two, four and eight warps to a CTA, alone and in clusters."""
     lens = [ctx - (ctx - 1) * i // (batch + 1) for i in range(batch)]

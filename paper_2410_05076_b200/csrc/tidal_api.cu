@@ -1469,7 +1469,7 @@ tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     cudaStream_t st = (cudaStream_t)stream;
     // Up to 16384 positions one launch scores and ranks: 1024 positions 4.2 us against 8.4 of two launches, 16384 positions 7.0
     // against 9.5, eight ragged sequences of them 10.3 against 14.3 (a set per query head; only 256 items of one CTA each are
-    // slower, 26.0 against 25.3). Beyond, a cluster is too few SMs for an item: 131072 positions 19.5 us against 12.8.
+    // slower, 26.0 against 25.3). Beyond, a cluster is too few SMs for an item: 131072 positions 19.5 us against 12.4.
     if (p.c.max_blocks <= SC_MAX_BLOCKS) {
         // A cluster with a tile per warp and a CTA per row, or the largest one with which all items are resident together; a shared set
         // has a tile per KV head (6 sequences of 573 positions, 32 KV heads: 6.8 us; head after head in one CTA 53). Rows are ranked
@@ -1498,7 +1498,8 @@ tidal_status_t tidal_block_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     p.chunks = w.chunks;
     if ((rc = launch_block(ctx, block_score_kernel, p, (int)grid, 32, SS_SMEM, 0, st)) != TIDAL_OK) return rc;
     // Sixteen scores per thread, with as few threads as that takes: their barriers and scans are the shorter chain (131072
-    // positions, 8 rows: 13.1 us with 512 threads, 13.9 with 1024; ragged batch of 8 x 65536, 256 rows: 25.2 us with 256, 28.3 with 1024).
+    // positions, 8 rows: 512 threads take 0.8 us less than 1024; ragged batch of 8 x 65536, 256 rows: 256 threads 3.1 us less than
+    // 1024, and 3.3 us less than 128 with 32 scores each).
     const int rank_rows = kv->batch * Hi;
     const size_t keys = (size_t)p.npad * 8;
     if (p.c.max_blocks > 8192) return launch_block(ctx, block_rank_kernel<1024, 4>, p, rank_rows, 1024, keys, 0, st);

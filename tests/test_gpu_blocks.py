@@ -231,7 +231,7 @@ SELECT = [
     ([4096], 8, 2, 16, 0, 0),
     ([999, 2047, 33], 15, 3, 31, 3, 0),
     ([1500], 8, 1, 90, 0, 3),
-    ([3000, 64], 8, 8, 5, 7, 7),                          # more kept blocks than the budget
+    ([3000, 64], 8, 8, 5, 7, 7),                          # more kept blocks than m
     ([20000], 4, 1, 100, 0, 1),
     ([90000, 17, 0, 33333], 8, 2, 70, 2, 1),
     ([16400, 16385, 70001], 12, 3, 1025, 0, 0),

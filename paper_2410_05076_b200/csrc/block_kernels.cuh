@@ -181,6 +181,11 @@ __device__ __forceinline__ f32pair fma2(f32pair a, f32pair b, f32pair c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
+__device__ __forceinline__ f32pair fma2_rm(f32pair a, f32pair b, f32pair c) {       // rounded downwards: x - x is -0
+    f32pair d;
+    asm("fma.rm.f32x2 %0, %1, %2, %3;\n" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
 
 // ---- thread-block clusters -----------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {

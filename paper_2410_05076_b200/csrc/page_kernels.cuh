@@ -205,7 +205,8 @@ struct KvWriteParams {
 // Not a division each: with r the correctly rounded reciprocal of s, q0 = x r and the exact remainder x - q0 s, q0 + r (x - q0 s)
 // rounds to x / s (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990) as
 // long as nothing leaves the range. So it is used where s is between 2^-60 and 2^60 and the eight elements are below 2^65 (a
-// remainder that underflows then belongs to a quotient below 2^-40, whose code is zero); a division otherwise. Two
+// remainder that underflows then belongs to a quotient below 2^-40, whose code is zero); a division otherwise. The remainder
+// is rounded downwards, which changes nothing but the sign of a zero: -0, unlike +0, leaves the sign of q0 as it is. Two
 // elements per instruction, and few instructions besides: under load the power limit holds the SM clock at 1.6 GHz and it is the
 // instructions that bound this kernel.
 __device__ __forceinline__ uint32_t babs_max2(uint32_t a, uint32_t b) {
@@ -233,7 +234,7 @@ __device__ __forceinline__ uint2 quantise8(uint4 w, float scale, float inv, bool
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const f32pair x = pair2(__uint_as_float(in[i] << 16), __uint_as_float(in[i] & 0xffff0000u)), q0 = mul2(x, r2);
-            const f32pair q = fma2(fma2(q0, s2, x), r2, q0);
+            const f32pair q = fma2(fma2_rm(q0, s2, x), r2, q0);
             half[i] = __nv_cvt_float2_to_fp8x2(make_float2(half2(q, 0), half2(q, 1)), __NV_SATFINITE, __NV_E4M3);
         }
     } else {

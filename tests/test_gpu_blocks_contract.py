@@ -1,0 +1,66 @@
+"""What the header and the design notes promise of the block-sparse and page calls beyond their results on usual input: signs
+of zeros, memory that is held, the status word, far pages, the precision of the softmax weights."""
+import pytest
+import torch
+
+from paper_2410_05076_b200 import binding, synth
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+D, BLK = 128, 16
+
+
+@pytest.fixture()
+def td():
+    t = binding.Tidal(0)
+    yield t
+    t.close()
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def hnd(k, v, hq, fp8=False, scales=None, sm_scale=0.0):
+    """One sequence, [Hkv, n, 128] keys and values side by side."""
+    hkv, n = k.shape[:2]
+    buf = torch.stack((k, v), 2).to(torch.float8_e4m3fn if fp8 else torch.bfloat16)[None].contiguous()
+    more = dict(k_scale=scales[0], v_scale=scales[1]) if scales else {}
+    return synth.LayerKV(k=buf[..., 0, :], v=buf[..., 1, :], batch=1, num_q_heads=hq, num_kv_heads=hkv, head_dim=D, ctx_lens=i32([n]),
+                         max_ctx_len=n, stride_b=hkv * n * 2 * D, stride_pos=2 * D, stride_head=n * 2 * D, sm_scale=sm_scale,
+                         kv_dtype=int(fp8), keep=[buf], **more)
+
+
+# ---- writing tokens ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("scale", [1.0, 0.037, 2.0 ** 70])
+def test_quantised_zeros_keep_their_sign(td, scale):
+    """IEEE: -0 / s = -0 for a positive s, whose nearest code is 0x80; and quotients that round to zero keep theirs."""
+    sc = torch.full((1,), scale, device=DEV)
+    zero = torch.zeros(1, BLK, D, device=DEV)
+    lay = hnd(zero, zero, 1, True, (sc, sc))
+    x = torch.zeros(1, 1, D)
+    x[0, 0, ::2] = -0.0
+    x[0, 0, 4:12] = torch.tensor([-1e-30, 1e-30, -1e-38, 1e-38, -9.2e-41, 9.2e-41, -1.0, 1.0])
+    x = x.to(torch.bfloat16).to(DEV)
+    td.kv_write(lay, x, x, torch.tensor([3], device=DEV))
+    want = (x.float().cpu() / sc.cpu()).to(torch.float8_e4m3fn).view(torch.uint8)[0, 0]
+    assert int(want[0]) == 0x80 and int(want[1]) == 0
+    for got in (lay.k, lay.v):
+        assert torch.equal(got[0, 0, 3].contiguous().view(torch.uint8).cpu(), want)
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.037, 3.3e-5, 1234.5, 2.0 ** -60, 2.0 ** 60, 2.0 ** -61, 1.3 * 2.0 ** 60, 2.0 ** -126])
+def test_every_bf16_number_gets_the_code_of_its_quotient(td, scale):
+    """All 65536 of them, zeros of both signs, subnormal numbers, infinities and not-a-numbers included."""
+    x = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(512, 1, D)
+    sc = torch.full((1,), scale, device=DEV)
+    zero = torch.zeros(1, 512, D, device=DEV)
+    lay = hnd(zero, zero, 1, True, (sc, sc))
+    td.kv_write(lay, x.to(DEV), x.to(DEV), torch.arange(512, device=DEV))
+    quotient = x[:, 0].float() / sc.cpu()
+    want = quotient.clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+    nan = quotient.isnan()
+    for got in (lay.k, lay.v):
+        got = got[0, 0].contiguous().view(torch.uint8).cpu()
+        assert ((got[nan] & 0x7F) == 0x7F).all() and torch.equal(got[~nan], want[~nan])

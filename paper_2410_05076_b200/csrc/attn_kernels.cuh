@@ -161,6 +161,11 @@ __device__ __forceinline__ void store_out(const AttnParams& p, long long i, floa
 }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
+// Reads of global memory are ordinary loads, ordered behind pdl_wait(). The non-coherent path (ld.global.nc) is for data that
+// does not change while a kernel lives, and here a kernel's life begins while the one before it may still write page
+// tables, slots, index lists, bounds or cache rows.
+template <typename T>
+__device__ __forceinline__ T read_global(const T* p) { return *p; }
 
 __device__ __forceinline__ void lds128(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];\n"
@@ -697,7 +702,7 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
         int newest_pos = -1;
         if (MODE == MODE_SPARSE && NEWEST) {
             const int cnt = total - 1;
-            const int last = cnt > 0 ? __ldg(idx_row + cnt - 1) : -1;
+            const int last = cnt > 0 ? read_global(idx_row + cnt - 1) : -1;
             if (N > 0 && last != N - 1) newest_pos = N - 1;
         }
 
@@ -767,7 +772,7 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
             if (MODE != MODE_SPARSE || tile < 0) return -1;
             const int e = tile * TILE + c16;
             if (NEWEST && e == total - 1) return newest_pos;
-            return (e < total) ? __ldg(idx_row + e) : -1;
+            return (e < total) ? read_global(idx_row + e) : -1;
         };
         long long offA = 0;
         bool validA = false;
@@ -777,7 +782,7 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
             offA = 0;
             if (validA) {
                 if (p.paged) {
-                    const int page = __ldg(p.page_table + (long long)b * p.max_pages + (pos >> 4));
+                    const int page = read_global(p.page_table + (long long)b * p.max_pages + (pos >> 4));
                     if ((unsigned)page < (unsigned)p.num_pages) {
                         offA = (long long)page * p.stride_page + (long long)(pos & 15) * p.stride_pos + head_off;
                     } else {
@@ -812,7 +817,7 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
                 long long off;
                 bool ok = true;
                 if (p.paged) {
-                    const int page = __ldg(p.page_table + (long long)b * p.max_pages + tile);
+                    const int page = read_global(p.page_table + (long long)b * p.max_pages + tile);
                     ok = (unsigned)page < (unsigned)p.num_pages;
                     if (!ok && lane == 0) atomicOr(p.status, STATUS_BAD_PAGE);
                     off = (ok ? (long long)page * p.stride_page : 0) + item_off + lane_src;
@@ -920,7 +925,7 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
 #pragma unroll
                 for (int sl = 0; sl < 2; ++sl) {
                     const int c = tig + 4 * sl;         // this lane's 16-code piece of a key row = 32 bytes of the query row
-                    const uint4 t0 = __ldg(qp + 2 * c), t1 = __ldg(qp + 2 * c + 1);
+                    const uint4 t0 = read_global(qp + 2 * c), t1 = read_global(qp + 2 * c + 1);
                     const uint32_t w[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
                     for (int i = 0; i < 8; ++i) qf8[sl][i] = on ? bf16x2_to_f16x2(w[i]) : 0u;
@@ -928,15 +933,15 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint4 t = __ldg(qp + 4 * j + tig);
+                    const uint4 t = read_global(qp + 4 * j + tig);
                     qf[j][0] = on ? t.x : 0u; qf[j][1] = on ? t.y : 0u; qf[j][2] = on ? t.z : 0u; qf[j][3] = on ? t.w : 0u;
                 }
             }
         }
         // 8-bit caches: the key scale of this KV head goes into the logit scale, the value scale is applied
         // to the accumulators once, at the end
-        const float kscale = (KV8 && p.k_scale) ? __ldg(p.k_scale + g) : 1.f;
-        const float vscale = (KV8 && p.v_scale) ? __ldg(p.v_scale + g) : 1.f;
+        const float kscale = (KV8 && p.k_scale) ? read_global(p.k_scale + g) : 1.f;
+        const float vscale = (KV8 && p.v_scale) ? read_global(p.v_scale + g) : 1.f;
         const float seg_scale = p.scale * kscale, seg_scale_log2 = p.scale_log2 * kscale;
 
 
@@ -1321,7 +1326,7 @@ __device__ __forceinline__ void kv_append_rows(const AppendParams& p) {
     if (piece * 16 >= HEAD_DIM * p.elem_bytes) return;
     const char* from = reinterpret_cast<const char*>(lane < 16 ? p.k_new : p.v_new) + src * p.elem_bytes + piece * 16;
     char* to = reinterpret_cast<char*>(lane < 16 ? p.k : p.v) + off * p.elem_bytes + piece * 16;
-    *reinterpret_cast<uint4*>(to) = __ldg(reinterpret_cast<const uint4*>(from));
+    *reinterpret_cast<uint4*>(to) = read_global(reinterpret_cast<const uint4*>(from));
 }
 
 __global__ void __launch_bounds__(128) kv_append_kernel(const AppendParams p) { kv_append_rows(p); }

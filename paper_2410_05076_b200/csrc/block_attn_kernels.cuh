@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(NW * 32, 8 / NW) block_attn_kernel(const Block
     // Blocks of this warp: list entries me + i * stride; lane l keeps what entry l of a run of 32 needs. (A run's entries are
     // read one run ahead, the first along with the lengths: the list has m of them whatever the count says.)
     const long long e0 = (long long)me + (long long)lane * stride;
-    int next_blk = e0 < p.m ? __ldg(row + e0) : -1;
+    int next_blk = e0 < p.m ? read_global(row + e0) : -1;
     const int n = cached_len(c, b);
     const int cnt = p.idx_count ? min(p.idx_count[b], p.m) : p.m;
     const int count = cnt > me ? (cnt - me + stride - 1) / stride : 0;
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(NW * 32, 8 / NW) block_attn_kernel(const Block
             const long long e = e0 + (long long)i * stride;
             const int blk = e < cnt ? next_blk : -1;
             const long long ahead = e + 32ll * stride;
-            next_blk = ahead < p.m ? __ldg(row + ahead) : -1;
+            next_blk = ahead < p.m ? read_global(row + ahead) : -1;
             my_rows = 0;
             my_off = 0;
             if (blk < -1 || (blk >= 0 && (long long)blk * TILE >= n)) atomicOr(c.status, STATUS_BAD_INDEX);
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(NW * 32, 8 / NW) block_attn_kernel(const Block
                 my_rows = min(TILE, n - blk * TILE);
                 my_off = (long long)g * c.stride_head;
                 if (c.paged) {
-                    const int page = __ldg(c.page_table + (long long)b * c.max_pages + blk);
+                    const int page = read_global(c.page_table + (long long)b * c.max_pages + blk);
                     if ((unsigned)page < (unsigned)c.num_pages) my_off += (long long)page * c.stride_page;
                     else { my_rows = 0; my_off = 0; atomicOr(c.status, STATUS_BAD_PAGE); }
                 } else {
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(NW * 32, 8 / NW) block_attn_kernel(const Block
 #pragma unroll
             for (int sl = 0; sl < 2; ++sl) {
                 const int pc = tig + 4 * sl;
-                const uint4 t0 = __ldg(qp + 2 * pc), t1 = __ldg(qp + 2 * pc + 1);
+                const uint4 t0 = read_global(qp + 2 * pc), t1 = read_global(qp + 2 * pc + 1);
                 const uint32_t w[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
                 for (int i = 0; i < 8; ++i) qf8[sl][i] = on ? bf16x2_to_f16x2(w[i]) : 0u;
@@ -319,14 +319,14 @@ __global__ void __launch_bounds__(NW * 32, 8 / NW) block_attn_kernel(const Block
             const uint32_t* qw = reinterpret_cast<const uint32_t*>(qrow);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint32_t w0 = __ldg(qw + 8 * j + tig), w1 = __ldg(qw + 8 * j + 4 + tig);
+                const uint32_t w0 = read_global(qw + 8 * j + tig), w1 = read_global(qw + 8 * j + 4 + tig);
                 qf[j][0] = on ? w0 : 0u;
                 qf[j][1] = on ? w1 : 0u;
             }
         }
     }
-    const float scale_log2 = p.scale_log2 * ((KV8 && p.k_scale) ? __ldg(p.k_scale + g) : 1.f);
-    const float vscale = (KV8 && p.v_scale) ? __ldg(p.v_scale + g) : 1.f;
+    const float scale_log2 = p.scale_log2 * ((KV8 && p.k_scale) ? read_global(p.k_scale + g) : 1.f);
+    const float vscale = (KV8 && p.v_scale) ? read_global(p.v_scale + g) : 1.f;
     BlockAcc acc;
     acc.m[0] = acc.m[1] = -INFINITY;
     acc.l[0] = acc.l[1] = 0.f;

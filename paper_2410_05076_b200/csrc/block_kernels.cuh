@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(BB_WARPS * 32) block_bounds_kernel(const Bound
     int page = 0;
     long long off = (long long)g * c.stride_head;
     if (c.paged) {
-        page = __ldg(c.page_table + (long long)b * c.max_pages + blk);
+        page = read_global(c.page_table + (long long)b * c.max_pages + blk);
         if ((unsigned)page >= (unsigned)c.num_pages) { if (lane == 0) atomicOr(c.status, STATUS_BAD_PAGE); return; }
         off += (long long)page * c.stride_page;
     } else {
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(BB_WARPS * 32) block_bounds_kernel(const Bound
         const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(c.k) + off + r0 * c.stride_pos + piece * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (r0 + 2 * i < rows) x[i] = __ldg(reinterpret_cast<const uint4*>(src + 2 * i * c.stride_pos));
+            if (r0 + 2 * i < rows) x[i] = read_global(reinterpret_cast<const uint4*>(src + 2 * i * c.stride_pos));
         uint32_t lo[4] = {BPINF, BPINF, BPINF, BPINF}, hi[4] = {BNINF, BNINF, BNINF, BNINF};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(BB_WARPS * 32) block_bounds_kernel(const Bound
         const uint8_t* src = c.k + off + r0 * c.stride_pos + piece * 16;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (r0 + 4 * i < rows) x[i] = __ldg(reinterpret_cast<const uint4*>(src + 4 * i * c.stride_pos));
+            if (r0 + 4 * i < rows) x[i] = read_global(reinterpret_cast<const uint4*>(src + 4 * i * c.stride_pos));
         uint32_t lo[8], hi[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) { lo[j] = BPINF; hi[j] = BNINF; }

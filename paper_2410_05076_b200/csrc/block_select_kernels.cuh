@@ -82,12 +82,12 @@ __device__ __forceinline__ void near_bounds(const SelectBlocksParams& p, int b, 
     const BlockCache& c = p.c;
     int page = 0;
     if (c.paged) {
-        page = __ldg(c.page_table + (long long)b * c.max_pages + blk);
+        page = read_global(c.page_table + (long long)b * c.max_pages + blk);
         if ((unsigned)page >= (unsigned)c.num_pages) { lo = hi = make_uint2(0u, 0u); return; }
     }
     const uint2* bp = reinterpret_cast<const uint2*>(p.bounds + bounds_row(c, b, blk, page, g) * BOUND_ELEMS) + lane;
-    lo = __ldg(bp);
-    hi = __ldg(bp + 32);
+    lo = read_global(bp);
+    hi = read_global(bp + 32);
 }
 // A bf16 number, as the upper half of an fp32's bits, in 64 bits: its fields put into place are its value times 2^-896, subnormal ones
 // included (infinities and not-a-numbers become 2^128 and more). Two integer instructions and a product; the
@@ -129,7 +129,7 @@ __device__ __noinline__ double wide_score(const SelectBlocksParams& p, const __n
             wide_add(sum, reinterpret_cast<const uint2*>(qrow)[lane], lo, hi);
         }
         const double part = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        acc += p.k_scale ? part * (double)__ldg(p.k_scale + g) : part;
+        acc += p.k_scale ? part * (double)read_global(p.k_scale + g) : part;
     }
     return warp_sum(acc);
 }
@@ -233,9 +233,9 @@ __device__ __noinline__ void shared_keys(const SelectBlocksParams& p, const floa
                     double sum[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 1
                     for (int h = 0; h < c.G; ++h)
-                        wide_add(sum, __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + ga * c.G + h) * HEAD_DIM) + lane), lo[a], hi[a]);
+                        wide_add(sum, read_global(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + ga * c.G + h) * HEAD_DIM) + lane), lo[a], hi[a]);
                     const double part = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    acc += p.k_scale ? part * (double)__ldg(p.k_scale + ga) : part;
+                    acc += p.k_scale ? part * (double)read_global(p.k_scale + ga) : part;
                 }
             }
             acc = warp_sum(acc);
@@ -497,7 +497,7 @@ __device__ __noinline__ double2 near_pair(const SelectBlocksParams& p, int b, in
     double x[4] = {0.0, 0.0, 0.0, 0.0}, y[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 1
     for (int h = h0; h < h1; ++h) {
-        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h) * HEAD_DIM) + lane);
+        const uint2 q = read_global(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h) * HEAD_DIM) + lane);
         wide_add(x, q, lo[0], hi[0]);
         wide_add(y, q, lo[1], hi[1]);
     }
@@ -707,24 +707,26 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
     bool first = true;
 
     auto load = [&](int tile, int g, uint4 (&x0)[8], uint4 (&x1)[8]) {
-        auto source = [&](int blk) -> const uint4* {        // null: zeros
-            int page = 0;
-            if (c.paged && blk < c.max_blocks) page = __ldg(c.page_table + (long long)b * c.max_pages + blk);      // (does not wait for the length)
+        auto entry = [&](int blk) -> int {                  // (does not wait for the length)
+            return c.paged && blk < c.max_blocks ? read_global(c.page_table + (long long)b * c.max_pages + blk) : 0;
+        };
+        const int page0 = entry(tile * 16 + gid), page1 = entry(tile * 16 + gid + 8);
+        auto source = [&](int blk, int page) -> const uint4* {         // null: zeros
             if (blk >= n) return nullptr;
             if (c.paged && (unsigned)page >= (unsigned)c.num_pages) { atomicOr(c.status, STATUS_BAD_PAGE); return nullptr; }
             return reinterpret_cast<const uint4*>(p.bounds + bounds_row(c, b, blk, page, g) * BOUND_ELEMS) + tig;
         };
-        const uint4 *src0 = source(tile * 16 + gid), *src1 = source(tile * 16 + gid + 8);
+        const uint4 *src0 = source(tile * 16 + gid, page0), *src1 = source(tile * 16 + gid + 8, page1);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            x0[j] = src0 ? __ldg(src0 + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
-            x1[j] = src1 ? __ldg(src1 + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
+            x0[j] = src0 ? read_global(src0 + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
+            x1[j] = src1 ? read_global(src1 + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
         }
     };
     auto load_query = [&](int g, uint4 (&q4)[4]) {
         const uint4* qp = reinterpret_cast<const uint4*>(p.q + ((long long)b * c.Hq + g * c.G + min(gid, c.G - 1)) * HEAD_DIM) + tig;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q4[j] = gid < c.G ? __ldg(qp + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
+        for (int j = 0; j < 4; ++j) q4[j] = gid < c.G ? read_global(qp + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
     };
     auto part_of = [](const uint4 (&q4)[4]) {
         return [&](int half, int j) -> uint4 {              // q-, q+
@@ -741,10 +743,10 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
     // what the row's heads add to e, by the warp that ranks the row, or a share of them by every warp
     auto query_share = [&]() {
         if (per_qhead) {
-            if (mine) qsum = query_part(__ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h0) * HEAD_DIM) + lane), c.Hkv);
+            if (mine) qsum = query_part(read_global(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h0) * HEAD_DIM) + lane), c.Hkv);
         } else {
 #pragma unroll 1
-            for (int h = h0 + wid; h < h1; h += W) qsum += query_part(__ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h) * HEAD_DIM) + lane), c.Hkv);
+            for (int h = h0 + wid; h < h1; h += W) qsum += query_part(read_global(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h) * HEAD_DIM) + lane), c.Hkv);
         }
     };
     int slices = 1;
@@ -797,7 +799,7 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
                 uint4 x0[8], x1[8], q4[4];
                 load(tile, g, x0, x1);
                 load_query(g, q4);
-                const float factor = p.k_scale ? __ldg(p.k_scale + g) : 1.f;
+                const float factor = p.k_scale ? read_global(p.k_scale + g) : 1.f;
                 if (first) { query_share(); first = false; if (size > 1) cluster_wait(); }
                 uint32_t low = 0u, high = 0x80008000u;
                 float s[4], x, y;
@@ -822,7 +824,7 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
     if constexpr (V == 0 && !SHARED) {                      // the group's queries, for scores in 64 bits
         for (int i = tid; i < c.G * (HEAD_DIM / 4); i += SC_THREADS)
             reinterpret_cast<uint2*>(sh.q[i / (HEAD_DIM / 4)])[i % (HEAD_DIM / 4)] =
-                __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + g0 * c.G) * HEAD_DIM) + i);
+                read_global(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + g0 * c.G) * HEAD_DIM) + i);
     }
     if (size > 1) cluster_arrive();                         // every score of the item is where it belongs ...
     if (g0 == 0 && rank == 0 && tid == 0 && p.idx_count) p.idx_count[b] = min(p.m, n);
@@ -917,13 +919,13 @@ __global__ void __launch_bounds__(32, 9) block_score_kernel(const __grid_constan
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         at[i] = blk0 + lane + 32 * i;
-        if (c.paged) at[i] = at[i] < c.max_blocks ? __ldg(c.page_table + (long long)b * c.max_pages + at[i]) : -1;
+        if (c.paged) at[i] = at[i] < c.max_blocks ? read_global(c.page_table + (long long)b * c.max_pages + at[i]) : -1;
     }
     uint4 q4[4];
     const uint4* qp = reinterpret_cast<const uint4*>(p.q + ((long long)b * c.Hq + g * c.G + min(gid, c.G - 1)) * HEAD_DIM) + tig;
     const bool on = gid < c.G;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) q4[j] = on ? __ldg(qp + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
+    for (int j = 0; j < 4; ++j) q4[j] = on ? read_global(qp + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
     const int n = (max(min(len, c.max_ctx), 0) + TILE - 1) / TILE;
     if (blk0 >= n) return;
     if (c.paged) {
@@ -959,7 +961,7 @@ __global__ void __launch_bounds__(32, 9) block_score_kernel(const __grid_constan
         qs[1][j] = make_uint4(bmax2(q4[j].x, 0u), bmax2(q4[j].y, 0u), bmax2(q4[j].z, 0u), bmax2(q4[j].w, 0u));
     }
     uint32_t low = 0u, high = 0x80008000u;
-    const float f = p.k_scale ? __ldg(p.k_scale + g) : 1.f;
+    const float f = p.k_scale ? read_global(p.k_scale + g) : 1.f;
     float* const row = p.scores + (p.mode == 0 ? (long long)b * c.Hq + g * c.G : (long long)b * c.Hkv + g) * p.npad;
 #pragma unroll
     for (int t = 0; t < SS_STAGES; ++t) {
@@ -1068,7 +1070,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) block_rank_kernel(const __grid_c
     if (!shared_set)                                        // the members' queries, for scores in 64 bits
         for (int i = tid; i < members * (HEAD_DIM / 4); i += NT)
             reinterpret_cast<uint2*>(s_q[i / (HEAD_DIM / 4)])[i % (HEAD_DIM / 4)] =
-                __ldg(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h0) * HEAD_DIM) + i);
+                read_global(reinterpret_cast<const uint2*>(p.q + ((long long)b * c.Hq + h0) * HEAD_DIM) + i);
 #pragma unroll 2
     for (int r = 1; r < sum_rows; ++r)
 #pragma unroll

@@ -266,14 +266,14 @@ __global__ void __launch_bounds__(KW_WARPS * 32, 6) kv_write_kernel(const KvWrit
     for (int i = 0; i < KW_TOKENS; ++i) {
         slot[i] = -1;
         if (t0 + i < p.num_tokens) {
-            slot[i] = __ldg(p.slots + t0 + i);
-            row[i] = __ldg(src + i * (stride >> 3));
+            slot[i] = read_global(p.slots + t0 + i);
+            row[i] = read_global(src + i * (stride >> 3));
         }
     }
     float scale = 1.f, inv = 1.f;
     if constexpr (KV8) {
         const float* sc = value ? p.v_scale : p.k_scale;
-        if (sc) { scale = __ldg(sc + g); inv = __frcp_rn(scale); }
+        if (sc) { scale = read_global(sc + g); inv = __frcp_rn(scale); }
     }
     const bool usual = scale >= 0x1p-60f && scale <= 0x1p60f;
     constexpr int ESZ = KV8 ? 1 : 2;

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(NW * 32, 1) score_pass_kernel(const AttnParams
     auto issue = [&](uint32_t ks, int& tile) {
         const __nv_bfloat16* src;
         if (p.paged) {
-            const int page = __ldg(p.page_table + tile);
+            const int page = read_global(p.page_table + tile);
             const bool ok = (unsigned)page < (unsigned)p.num_pages;
             if (!ok) {
                 if (lane == 0) atomicOr(p.status, STATUS_BAD_PAGE);
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(NW * 32, 1) score_pass_kernel(const AttnParams
         const bool on = gid < ncols;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t w0 = __ldg(qw + 8 * j + tig), w1 = __ldg(qw + 8 * j + 4 + tig);
+            const uint32_t w0 = read_global(qw + 8 * j + tig), w1 = read_global(qw + 8 * j + 4 + tig);
             qf[j][0] = on ? w0 : 0u;
             qf[j][1] = on ? w1 : 0u;
         }
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(NW * 32, 2) value_pass_kernel(const AttnParams
     auto issue = [&](uint32_t vs, int& tile) {
         const __nv_bfloat16* src;
         if (p.paged) {
-            const int page = __ldg(p.page_table + tile);
+            const int page = read_global(p.page_table + tile);
             const bool ok = (unsigned)page < (unsigned)p.num_pages;
             if (!ok) {
                 if (lane == 0) atomicOr(p.status, STATUS_BAD_PAGE);
@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(NW * 32, 1) score_pass_flat_kernel(const AttnP
             const bool on = gid < ncols;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint32_t w0 = __ldg(qw + 8 * j + tig), w1 = __ldg(qw + 8 * j + 4 + tig);
+                const uint32_t w0 = read_global(qw + 8 * j + tig), w1 = read_global(qw + 8 * j + 4 + tig);
                 qf[j][0] = on ? w0 : 0u;
                 qf[j][1] = on ? w1 : 0u;
             }
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(NW * 32, 1) score_pass_flat_kernel(const AttnP
         auto issue = [&](uint32_t ks, int& tile) {
             const __nv_bfloat16* src;
             if (p.paged) {
-                const int page = __ldg(pages + tile);
+                const int page = read_global(pages + tile);
                 const bool ok = (unsigned)page < (unsigned)p.num_pages;
                 if (!ok) {
                     if (lane == 0) atomicOr(p.status, STATUS_BAD_PAGE);
@@ -804,7 +804,7 @@ __global__ void __launch_bounds__(NW * 32, 2) value_pass_flat_kernel(const AttnP
         auto issue = [&](uint32_t vs, int& tile) {
             const __nv_bfloat16* src;
             if (p.paged) {
-                const int page = __ldg(pages + tile);
+                const int page = read_global(pages + tile);
                 const bool ok = (unsigned)page < (unsigned)p.num_pages;
                 if (!ok) {
                     if (lane == 0) atomicOr(p.status, STATUS_BAD_PAGE);
@@ -1005,7 +1005,7 @@ __global__ void __launch_bounds__(NW * 32, 1) score_pass8_kernel(const AttnParam
         const uint8_t* src;
         bool ok = true;
         if (p.paged) {
-            const int page = __ldg(p.page_table + tile);
+            const int page = read_global(p.page_table + tile);
             ok = (unsigned)page < (unsigned)p.num_pages;
             if (!ok && lane == 0) atomicOr(p.status, STATUS_BAD_PAGE);
             src = kbase + (ok ? (long long)page * p.stride_page : 0);
@@ -1058,13 +1058,13 @@ __global__ void __launch_bounds__(NW * 32, 1) score_pass8_kernel(const AttnParam
 #pragma unroll
         for (int sl = 0; sl < 2; ++sl) {
             const int c = tig + 4 * sl;
-            const uint4 t0 = __ldg(qp + 2 * c), t1 = __ldg(qp + 2 * c + 1);
+            const uint4 t0 = read_global(qp + 2 * c), t1 = read_global(qp + 2 * c + 1);
             const uint32_t w[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) qf8[sl][i] = on ? bf16x2_to_f16x2(w[i]) : 0u;
         }
     }
-    const float scale = p.scale * (p.k_scale ? __ldg(p.k_scale + g) : 1.f);
+    const float scale = p.scale * (p.k_scale ? read_global(p.k_scale + g) : 1.f);
     float m0 = -INFINITY, m1 = -INFINITY;
     const uint32_t klane = gid * ROW_BYTES8;
     const uint32_t kswz = (gid & 1) << 2;
@@ -1233,7 +1233,7 @@ __global__ void __launch_bounds__(NW * 32, 2) value_pass8_kernel(const AttnParam
         const uint8_t* src;
         bool ok = true;
         if (p.paged) {
-            const int page = __ldg(p.page_table + tile);
+            const int page = read_global(p.page_table + tile);
             ok = (unsigned)page < (unsigned)p.num_pages;
             if (!ok && lane == 0) atomicOr(p.status, STATUS_BAD_PAGE);
             src = vbase + (ok ? (long long)page * p.stride_page : 0);
@@ -1348,7 +1348,7 @@ __global__ void __launch_bounds__(NW * 32, 2) value_pass8_kernel(const AttnParam
         l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
     }
     __syncthreads();                                   // all rings drained; reuse the shared memory
-    const float vscale = p.v_scale ? __ldg(p.v_scale + g) : 1.f;
+    const float vscale = p.v_scale ? read_global(p.v_scale + g) : 1.f;
     float* mo = reinterpret_cast<float*>(smem);       // [NW][8][128]
     float* ml = mo + NW * 8 * HEAD_DIM;               // [NW][8]
 #pragma unroll

@@ -364,8 +364,9 @@ tidal_status_t tidal_block_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const 
 tidal_status_t tidal_block_attn(tidal_ctx_t *ctx, const tidal_kv_t *kv, const void *q, const int32_t *idx,
                                 const int32_t *idx_count, int32_t m, int32_t num_index_heads, float *out, void *stream);
 
-/* Waits for `stream`, then returns and clears the sticky device status word: TIDAL_OK,
- * TIDAL_ERR_INDEX, TIDAL_ERR_PAGES, TIDAL_ERR_INTERNAL, or TIDAL_ERR_CUDA if the stream reports an error. */
+/* Waits for `stream`, then reports and clears one kind of what the device has noted since: TIDAL_ERR_INTERNAL before
+ * TIDAL_ERR_PAGES before TIDAL_ERR_INDEX. What else was noted stays for the next call, so that TIDAL_OK says that nothing
+ * is left. TIDAL_ERR_CUDA if the stream reports an error. */
 tidal_status_t tidal_device_status(tidal_ctx_t *ctx, void *stream);
 
 /* Kernels launched through this context since it was created. */

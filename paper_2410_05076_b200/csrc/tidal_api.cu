@@ -1356,10 +1356,13 @@ tidal_status_t tidal_device_status(tidal_ctx_t* ctx, void* stream) {
     if (cudaStreamSynchronize(st) != cudaSuccess) return TIDAL_ERR_CUDA;
     int word = 0;
     if (cudaMemcpy(&word, ctx->status, sizeof word, cudaMemcpyDeviceToHost) != cudaSuccess) return TIDAL_ERR_CUDA;
-    if (word != 0 && cudaMemset(ctx->status, 0, sizeof(int)) != cudaSuccess) return TIDAL_ERR_CUDA;
-    if (word & STATUS_SPLIT_OVERFLOW) return TIDAL_ERR_INTERNAL;
-    if (word & STATUS_NO_PAGES) return TIDAL_ERR_PAGES;
-    return word ? TIDAL_ERR_INDEX : TIDAL_OK;
+    if (word == 0) return TIDAL_OK;
+    // one kind of trouble per call; the others wait for the next
+    const int told = word & STATUS_SPLIT_OVERFLOW ? STATUS_SPLIT_OVERFLOW : word & STATUS_NO_PAGES ? STATUS_NO_PAGES : word;
+    const int rest = word & ~told;
+    if (cudaMemcpyAsync(ctx->status, &rest, sizeof rest, cudaMemcpyHostToDevice, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess) return TIDAL_ERR_CUDA;
+    return told == STATUS_SPLIT_OVERFLOW ? TIDAL_ERR_INTERNAL : told == STATUS_NO_PAGES ? TIDAL_ERR_PAGES : TIDAL_ERR_INDEX;
 }
 
 

@@ -64,3 +64,15 @@ def test_every_bf16_number_gets_the_code_of_its_quotient(td, scale):
     for got in (lay.k, lay.v):
         got = got[0, 0].contiguous().view(torch.uint8).cpu()
         assert ((got[nan] & 0x7F) == 0x7F).all() and torch.equal(got[~nan], want[~nan])
+
+
+# ---- the status word -----------------------------------------------------------------------------------------------
+
+def test_two_kinds_of_trouble_are_both_reported(td):
+    zero = torch.zeros(1, BLK, D, device=DEV)
+    lay = hnd(zero, zero, 1)
+    rows = torch.ones(1, 1, D, dtype=torch.bfloat16, device=DEV)
+    td.kv_write(lay, rows, rows, torch.tensor([BLK], device=DEV))                    # behind the cache
+    td.page_map(i32([0]), i32([17]), i32([[0, 0]]), i32([0]), i32([1]), torch.zeros(17, dtype=torch.int64, device=DEV))      # two pages, one free
+    assert sorted([td.device_status(), td.device_status()]) == sorted([binding.ERR_PAGES, binding.ERR_INDEX])
+    assert td.device_status() == binding.OK

@@ -116,7 +116,9 @@ tidal_status_t tidal_destroy(tidal_ctx_t *ctx);
  * that scale with batch * num_q_heads. num_layers_host is the layer count of later
  * tidal_decode_step_host calls (0 if that call is not used). After it, calls with shapes no larger
  * allocate nothing and do not synchronise, so they can be captured into a CUDA graph from the first
- * one on. May allocate and synchronise itself; call it outside any capture. */
+ * one on. May allocate and synchronise itself; call it outside any capture. For max_ctx_len > 16384 it
+ * also allocates the scratch of tidal_block_select (a fiftieth of the rest); if only that does not fit,
+ * it succeeds without, and tidal_block_select returns TIDAL_ERR_NOMEM when it finds no memory either. */
 tidal_status_t tidal_reserve(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t k, int32_t num_layers_host);
 
 /* Workspace a call with this cache shape and budget k needs (split-context

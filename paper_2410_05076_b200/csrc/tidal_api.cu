@@ -991,9 +991,12 @@ tidal_status_t tidal_reserve(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t k, 
     if (cudaSetDevice(ctx->device) != cudaSuccess) return TIDAL_ERR_CUDA;
     const tidal_status_t rs = ensure_side_stream(ctx);       // a later step's selection layers may use it
     if (rs != TIDAL_OK) return rs;
-    const tidal_status_t rb = ensure_block_ws(ctx, block_ws_layout(kv, kv->num_q_heads).total, nullptr);
-    if (rb != TIDAL_OK) return rb;
-    return ensure_all(ctx, kv, ws_bytes_for(kv, k, num_layers_host));
+    const tidal_status_t ra = ensure_all(ctx, kv, ws_bytes_for(kv, k, num_layers_host));
+    // Scratch of block selections over contexts that need some: the last, and no reason to fail, for callers that select no blocks
+    // can do without it and tidal_block_select says itself when it is missing.
+    if (ra == TIDAL_OK && (kv->max_ctx_len + TILE - 1) / TILE > SC_MAX_BLOCKS)
+        ensure_block_ws(ctx, block_ws_layout(kv, kv->num_q_heads).total, nullptr);
+    return ra;
 }
 
 static void fill_append(AppendParams& a, const tidal_ctx* ctx, const tidal_kv_t* kv, const void* k_new,

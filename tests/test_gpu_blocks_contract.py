@@ -31,6 +31,22 @@ def hnd(k, v, hq, fp8=False, scales=None, sm_scale=0.0):
                          kv_dtype=int(fp8), keep=[buf], **more)
 
 
+def one_page(batch, hq, hkv, ctx):
+    """`batch` sequences of one token each that share a page, in a cache for up to `ctx` positions."""
+    pool = torch.zeros(1, hkv, BLK, 2, D, dtype=torch.bfloat16, device=DEV)
+    lay = synth.LayerKV(k=pool[..., 0, :], v=pool[..., 1, :], batch=batch, num_q_heads=hq, num_kv_heads=hkv, head_dim=D,
+                        ctx_lens=torch.ones(batch, dtype=torch.int32, device=DEV), max_ctx_len=ctx, stride_pos=2 * D,
+                        stride_head=BLK * 2 * D, stride_page=hkv * BLK * 2 * D, keep=[pool], max_pages_per_seq=ctx // BLK,
+                        page_table=torch.zeros(batch, ctx // BLK, dtype=torch.int32, device=DEV))
+    lay.num_pages = 1
+    return lay
+
+
+def free_bytes():
+    torch.cuda.synchronize()
+    return torch.cuda.mem_get_info(0)[0]
+
+
 # ---- writing tokens ------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("scale", [1.0, 0.037, 2.0 ** 70])
@@ -76,3 +92,62 @@ def test_two_kinds_of_trouble_are_both_reported(td):
     td.page_map(i32([0]), i32([17]), i32([[0, 0]]), i32([0]), i32([1]), torch.zeros(17, dtype=torch.int64, device=DEV))      # two pages, one free
     assert sorted([td.device_status(), td.device_status()]) == sorted([binding.ERR_PAGES, binding.ERR_INDEX])
     assert td.device_status() == binding.OK
+
+
+def used_by(fn):
+    """Device memory that a call takes for good (code that it loads apart: it has run before)."""
+    before = free_bytes()
+    fn()
+    return before - free_bytes()
+
+
+# ---- memory --------------------------------------------------------------------------------------------------------
+
+def test_reserve_holds_nothing_for_selections_that_need_no_scratch():
+    """Up to 16384 positions tidal_block_select uses none: a reservation takes what the token selection takes."""
+    lay = one_page(1024, 32, 4, 16384)
+    q = torch.zeros(1024, 32, D, dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros(1024, 32, D, device=DEV)
+    idx, cnt = torch.zeros(1024, 32, 4, dtype=torch.int32, device=DEV), torch.zeros(1024, dtype=torch.int32, device=DEV)
+    torch.cuda.empty_cache()
+    a, b, c = binding.Tidal(0), binding.Tidal(0), binding.Tidal(0)
+    c.select_attn(lay, q, 4, out=out, idx=idx, idx_count=cnt)
+    c.close()
+    try:
+        called = used_by(lambda: a.select_attn(lay, q, 4, out=out, idx=idx, idx_count=cnt))
+        reserved = used_by(lambda: b.reserve(lay, 4))
+        assert reserved <= called + 2 ** 25, (reserved, called)         # (the scratch of 1024 blocks in 32768 rows: 128 MB)
+    finally:
+        a.close(); b.close()
+
+
+def fill(leave):
+    """Takes all of the device's memory but `leave` bytes."""
+    torch.cuda.empty_cache()
+    return torch.empty(free_bytes() - leave, dtype=torch.uint8, device=DEV)
+
+
+def test_a_reservation_for_token_selection_does_not_fail_for_block_scratch():
+    """Memory for all of the token calls, but not for 256 MB of block scores besides."""
+    lay = one_page(64, 64, 8, 262144)
+    a, b = binding.Tidal(0), binding.Tidal(0)
+    try:
+        q = torch.zeros(64, 64, D, dtype=torch.bfloat16, device=DEV)
+        out = torch.zeros(64, 64, D, device=DEV)
+        idx, cnt = torch.zeros(64, 64, 4, dtype=torch.int32, device=DEV), torch.zeros(64, dtype=torch.int32, device=DEV)
+        b.select_attn(lay, q, 4, out=out, idx=idx, idx_count=cnt)
+        b.close()
+        b = binding.Tidal(0)
+        torch.cuda.empty_cache()
+        called = used_by(lambda: a.select_attn(lay, q, 4, out=out, idx=idx, idx_count=cnt))
+        a.close()
+        most = fill(called + (160 << 20))
+        try:
+            b.reserve(lay, 4)
+        finally:
+            del most
+            torch.cuda.empty_cache()
+        b.select_attn(lay, q, 4, out=out, idx=idx, idx_count=cnt)
+        assert b.device_status() == binding.OK
+    finally:
+        a.close(); b.close()

@@ -798,9 +798,13 @@ tidal_status_t ensure_block_ws(tidal_ctx* ctx, size_t bytes, const cudaStream_t*
         if (cs != cudaStreamCaptureStatusNone) return TIDAL_ERR_NOMEM;
     }
     if (ctx->blk_ws && ctx->blk_old_count == (int)(sizeof ctx->blk_old / sizeof ctx->blk_old[0])) return TIDAL_ERR_NOMEM;
-    const size_t want = std::max(bytes, 2 * ctx->blk_ws_bytes);
+    size_t want = std::max(bytes, 2 * ctx->blk_ws_bytes);
     void* p = nullptr;
-    if (cudaMalloc(&p, want) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
+    if (cudaMalloc(&p, want) != cudaSuccess) {
+        cudaGetLastError();
+        want = bytes;                           // twice as much is for the sake of later calls: this one can do without
+        if (cudaMalloc(&p, want) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
+    }
     if (ctx->blk_ws) ctx->blk_old[ctx->blk_old_count++] = ctx->blk_ws;
     ctx->blk_ws = p;
     ctx->blk_ws_bytes = want;

@@ -121,10 +121,38 @@ def test_reserve_holds_nothing_for_selections_that_need_no_scratch():
         a.close(); b.close()
 
 
+def long_select(t, batch, hq):
+    lay = one_page(batch, hq, hq // 8, 262144)
+    q = torch.zeros(batch, hq, D, dtype=torch.bfloat16, device=DEV)
+    bounds = torch.zeros(binding.block_bounds_shape(lay), dtype=torch.bfloat16, device=DEV)
+    idx, cnt = torch.zeros(batch, hq, 1, dtype=torch.int32, device=DEV), torch.zeros(batch, dtype=torch.int32, device=DEV)
+    return lambda: t.block_select(lay, bounds, q, 1, idx=idx, idx_count=cnt)
+
+
 def fill(leave):
     """Takes all of the device's memory but `leave` bytes."""
     torch.cuda.empty_cache()
     return torch.empty(free_bytes() - leave, dtype=torch.uint8, device=DEV)
+
+
+def test_scratch_grows_to_what_is_needed_where_twice_does_not_fit(td):
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    small, large = long_select(td, 128, 64), long_select(td, 160, 64)   # 512 MB and 640 MB
+    small()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            small()                                                     # (a graph names the first buffer: it stays)
+    most = fill(900 << 20)
+    try:
+        large()
+        assert td.device_status() == binding.OK
+    finally:
+        del most
+        torch.cuda.empty_cache()
+    graph.replay()
+    assert td.device_status() == binding.OK
+    del graph
 
 
 def test_a_reservation_for_token_selection_does_not_fail_for_block_scratch():

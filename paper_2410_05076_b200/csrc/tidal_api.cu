@@ -58,10 +58,11 @@ struct tidal_ctx {
     void* state = nullptr;
     int state_rows = 0;                         // capacity in (sequence, head) rows
     int* status = nullptr;                      // device word, sticky
-    // Scores of the block selection over long contexts. It grows by doubling, and what it outgrows is kept until the context
-    // goes: graphs that the caller captured may still name it.
+    // Scores of the block selection over long contexts. It grows by doubling; what it outgrows is kept until the context
+    // goes if a call was captured with it, since the caller's graph then still names it, and given back otherwise.
     void* blk_ws = nullptr;
     size_t blk_ws_bytes = 0;
+    bool blk_named = false;                     // a captured call uses blk_ws
     void* blk_old[64] = {};
     int blk_old_count = 0;
     int out_bf16 = 0;                           // outputs are written as bf16 instead of fp32
@@ -791,13 +792,17 @@ BlockWs block_ws_layout(const tidal_kv_t* kv, int rows) {
 }
 
 tidal_status_t ensure_block_ws(tidal_ctx* ctx, size_t bytes, const cudaStream_t* st) {
-    if (ctx->blk_ws_bytes >= bytes) return TIDAL_OK;
     if (st) {                                   // nothing may be allocated into a capture
         cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-        if (cudaStreamIsCapturing(*st, &cs) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
-        if (cs != cudaStreamCaptureStatusNone) return TIDAL_ERR_NOMEM;
+        const bool known = cudaStreamIsCapturing(*st, &cs) == cudaSuccess;
+        if (!known) cudaGetLastError();
+        if (!known || cs != cudaStreamCaptureStatusNone) {
+            if (ctx->blk_ws_bytes < bytes) return TIDAL_ERR_NOMEM;
+            ctx->blk_named = true;
+        }
     }
-    if (ctx->blk_ws && ctx->blk_old_count == (int)(sizeof ctx->blk_old / sizeof ctx->blk_old[0])) return TIDAL_ERR_NOMEM;
+    if (ctx->blk_ws_bytes >= bytes) return TIDAL_OK;
+    if (ctx->blk_named && ctx->blk_old_count == (int)(sizeof ctx->blk_old / sizeof ctx->blk_old[0])) return TIDAL_ERR_NOMEM;
     size_t want = std::max(bytes, 2 * ctx->blk_ws_bytes);
     void* p = nullptr;
     if (cudaMalloc(&p, want) != cudaSuccess) {
@@ -805,9 +810,15 @@ tidal_status_t ensure_block_ws(tidal_ctx* ctx, size_t bytes, const cudaStream_t*
         want = bytes;                           // twice as much is for the sake of later calls: this one can do without
         if (cudaMalloc(&p, want) != cudaSuccess) { cudaGetLastError(); return TIDAL_ERR_NOMEM; }
     }
-    if (ctx->blk_ws) ctx->blk_old[ctx->blk_old_count++] = ctx->blk_ws;
+    if (ctx->blk_named) {
+        ctx->blk_old[ctx->blk_old_count++] = ctx->blk_ws;
+    } else if (ctx->blk_ws) {
+        cudaDeviceSynchronize();
+        cudaFree(ctx->blk_ws);
+    }
     ctx->blk_ws = p;
     ctx->blk_ws_bytes = want;
+    ctx->blk_named = false;
     return TIDAL_OK;
 }
 

@@ -129,6 +129,17 @@ def long_select(t, batch, hq):
     return lambda: t.block_select(lay, bounds, q, 1, idx=idx, idx_count=cnt)
 
 
+def test_outgrown_scratch_that_no_graph_names_is_given_back(td):
+    small, large = long_select(td, 64, 64), long_select(td, 192, 64)    # 16384 blocks: 256 MB and 768 MB of scores
+    small()
+    before = free_bytes()
+    large()
+    grown = before - free_bytes()
+    assert grown <= 2 ** 29 + 2 ** 25, grown                            # 512 MB more
+    small(); large()
+    assert td.device_status() == binding.OK
+
+
 def fill(leave):
     """Takes all of the device's memory but `leave` bytes."""
     torch.cuda.empty_cache()

@@ -3,12 +3,14 @@ microseconds the C++ of csrc/fast_call.cpp.
 
 Argument marshalling only: every step of the attention path runs in the CUDA
 kernels behind the C-ABI. PyTorch supplies device memory and the current
-stream. If the shared library is missing and cannot be built the import of
-this module's `load()` raises; there is no fallback of any kind.
+stream. If the shared library is missing and cannot be built, this module's
+`load()` raises, and so does the first block-sparse or page call without the
+C++ part; there is no fallback of any kind.
 """
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 from typing import Optional, Sequence
 
@@ -62,7 +64,7 @@ _fast = None             # csrc/fast_call.cpp: the block-sparse and page calls, 
 
 def load() -> C.CDLL:
     """Load libtidal.so, building it with nvcc first if it is missing or stale."""
-    global _lib, _fast
+    global _lib
     if _lib is not None:
         return _lib
     path = _build.LIB
@@ -125,11 +127,30 @@ def load() -> C.CDLL:
     L.tidal_launch_count.restype = I64
     L.tidal_strerror.argtypes = [I32]
     L.tidal_strerror.restype = C.c_char_p
-    from . import _fast_call as fast
-    fast.init(*[C.cast(f, P).value for f in (L.tidal_page_map, L.tidal_kv_write, L.tidal_block_bounds, L.tidal_block_select,
-                                             L.tidal_block_attn)], C.sizeof(tidal_kv_t))
-    _lib, _fast = L, fast
+    _lib = L
     return L
+
+
+def _fast_calls():
+    """The module of csrc/fast_call.cpp, built with g++ first if it is missing or stale, at the first call that goes through
+    it: the other calls need neither it nor what it is built with."""
+    global _fast
+    if _fast is not None:
+        return _fast
+    path = _build.fast_path()
+    try:
+        if _build.fast_is_stale():
+            _build.build_fast()
+        spec = importlib.util.spec_from_file_location(__package__ + "._fast_call", path)
+        fast = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(fast)
+    except Exception as exc:  # no silent fallback here either
+        raise ImportError(f"{os.path.basename(path)} (csrc/fast_call.cpp) could not be built or loaded: {exc}") from exc
+    L = load()
+    fast.init(*[C.cast(f, C.c_void_p).value for f in (L.tidal_page_map, L.tidal_kv_write, L.tidal_block_bounds, L.tidal_block_select,
+                                                      L.tidal_block_attn)], C.sizeof(tidal_kv_t))
+    _fast = fast
+    return fast
 
 
 def strerror(status: int) -> str:
@@ -370,7 +391,7 @@ class Tidal:
         last. num_free_out receives the new count (default: num_free itself); positions (int32 [max_tokens])
         and token_offsets (int32 [B + 1]) are optional outputs. Returns slots. A request that does not fit changes
         nothing and shows in device_status() as ERR_PAGES."""
-        rc = _fast.page_map(self._handle, self.device, old_lens, new_lens, page_table, free_pages, num_free, slots, num_free_out,
+        rc = (_fast or _fast_calls()).page_map(self._handle, self.device, old_lens, new_lens, page_table, free_pages, num_free, slots, num_free_out,
                             positions, token_offsets)
         if rc:
             raise TidalError(rc, "tidal_page_map")
@@ -379,7 +400,7 @@ class Tidal:
     def kv_write(self, layer, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor) -> None:
         """Write the rows of T tokens (bf16 [T, Hkv, d]; only the two inner dimensions have to be contiguous) at their slots
         (int64 [T]; -1: skipped) of the layer's cache; an FP8 cache quantises them with its scales."""
-        rc = _fast.kv_write(self._handle, self.device, kv_struct(layer), k_new, v_new, slots)
+        rc = (_fast or _fast_calls()).kv_write(self._handle, self.device, kv_struct(layer), k_new, v_new, slots)
         if rc:
             raise TidalError(rc, "tidal_kv_write")
 
@@ -391,7 +412,7 @@ class Tidal:
         s = kv_struct(layer)
         if bounds is None:
             bounds = torch.zeros(block_bounds_shape(s), dtype=torch.bfloat16, device=f"cuda:{self.device}")
-        rc = _fast.block_bounds(self._handle, self.device, s, bounds, start_lens, max_new)
+        rc = (_fast or _fast_calls()).block_bounds(self._handle, self.device, s, bounds, start_lens, max_new)
         if rc:
             raise TidalError(rc, "tidal_block_bounds")
         return bounds
@@ -407,7 +428,7 @@ class Tidal:
             idx = torch.empty(s.batch, hi, max(m, 1), dtype=torch.int32, device=q.device)
         if idx_count is None:
             idx_count = torch.empty(s.batch, dtype=torch.int32, device=q.device)
-        rc = _fast.block_select(self._handle, self.device, s, bounds, q, m, granularity, keep_first, keep_last, idx, idx_count)
+        rc = (_fast or _fast_calls()).block_select(self._handle, self.device, s, bounds, q, m, granularity, keep_first, keep_last, idx, idx_count)
         if rc:
             raise TidalError(rc, "tidal_block_select")
         return idx, idx_count
@@ -418,7 +439,7 @@ class Tidal:
         s = kv_struct(layer)
         if out is None:
             out = torch.empty(s.batch, s.num_q_heads, s.head_dim, dtype=self.out_dtype, device=q.device)
-        rc = _fast.block_attn(self._handle, self.device, s, q, idx, idx_count, out, self.out_dtype is torch.bfloat16)
+        rc = (_fast or _fast_calls()).block_attn(self._handle, self.device, s, q, idx, idx_count, out, self.out_dtype is torch.bfloat16)
         if rc:
             raise TidalError(rc, "tidal_block_attn")
         return out

@@ -1,5 +1,6 @@
-"""Build libtidal.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _fast_call.so (tensors in, C calls out; see
-csrc/fast_call.cpp) with g++ against the installed torch."""
+"""Build libtidal.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _fast_call (tensors in, C calls out; see
+csrc/fast_call.cpp) with g++ against the installed torch. The library needs neither torch's nor Python's headers and
+is built and loaded without the other."""
 from __future__ import annotations
 
 import os
@@ -14,8 +15,13 @@ SOURCES = ["tidal_api.cu"]
 DEPS = ["tidal_api.cu", "attn_kernels.cuh", "block_kernels.cuh", "block_select_kernels.cuh", "block_attn_kernels.cuh", "page_kernels.cuh", "split_select_kernels.cuh", "topk_kernels.cuh", os.path.join("..", "..", "include", "tidal.h")]
 
 
-FAST = os.path.join(HERE, "_fast_call.so")
 FAST_DEPS = ["fast_call.cpp", os.path.join("..", "..", "include", "tidal.h")]
+
+
+def fast_path() -> str:
+    """The file's name says for which Python and which torch it was built: another one's is not taken for it."""
+    import torch
+    return os.path.join(HERE, f"_fast_call-torch{torch.__version__}{sysconfig.get_config_var('EXT_SUFFIX')}")
 
 
 def nvcc_path() -> str:
@@ -31,25 +37,30 @@ def _older(target: str, deps) -> bool:
 
 
 def is_stale() -> bool:
-    return _older(LIB, DEPS) or _older(FAST, FAST_DEPS)
+    return _older(LIB, DEPS)
 
 
-def _build_fast() -> None:
+def fast_is_stale() -> bool:
+    return _older(fast_path(), FAST_DEPS)
+
+
+def build_fast() -> str:
     import torch
     root = os.path.dirname(torch.__file__)
     cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
-    tmp = FAST + f".tmp{os.getpid()}"
+    path = fast_path()
+    tmp = path + f".tmp{os.getpid()}"
     subprocess.check_call(
         ["g++", "-O2", "-std=c++20", "-shared", "-fPIC", "-fvisibility=hidden", f"-I{os.path.join(root, 'include')}",
          f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}", "-o", tmp, os.path.join(CSRC, "fast_call.cpp"),
          f"-L{os.path.join(root, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
-    os.replace(tmp, FAST)
+    os.replace(tmp, path)
+    return path
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if force or _older(FAST, FAST_DEPS):
-        _build_fast()
-    if not force and not _older(LIB, DEPS):
+    """libtidal.so, where it is missing or older than its sources."""
+    if not force and not is_stale():
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -65,3 +76,4 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_fast() if "--force" in sys.argv or fast_is_stale() else fast_path())

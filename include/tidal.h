@@ -359,7 +359,7 @@ tidal_status_t tidal_block_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const 
 /* Attention over the listed blocks: Eq. 1 restricted to the cached positions of the blocks listed for the query head's
  * index head h * Hi / Hq, renormalised over them. -1 is padding; any other entry outside the sequence's blocks is skipped and
  * reported as TIDAL_ERR_INDEX; a repeated block counts once per occurrence; any order. Only the first idx_count[b]
- * entries count when idx_count is given, else m. A head without a valid entry gets zeros. num_index_heads
+ * entries count when idx_count is given, else m (at most 2^30). A head without a valid entry gets zeros. num_index_heads
  * must be Hq, Hkv or 1. Output type as set by tidal_set_output_dtype; softmax weights enter the product with V
  * with 22 bits or more, statistics and sums are fp32. tidal_set_attend_newest has no effect here (keep_last does that).
  * Uses no scratch memory. */

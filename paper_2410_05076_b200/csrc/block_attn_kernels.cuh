@@ -192,6 +192,7 @@ __device__ __forceinline__ void consume_block8(uint32_t ks, uint32_t vs, const u
 constexpr int BA_STAGES = 3, BA_STAGES8 = 6;                // the same bytes in flight
 // Shapes: eight warps with an SM to themselves, or smaller CTAs that share one, eight warps in all (rule in tidal_api.cu).
 constexpr int BA_MAX_CLUSTER = 16;
+constexpr int BA_MAX_LIST = 1 << 30;                        // entries of a list: 32 bits hold an entry number and a round of all warps besides
 
 template <bool KV8>
 constexpr size_t ba_ring(int warps) { return (size_t)warps * (KV8 ? BA_STAGES8 * STAGE_BYTES8 : BA_STAGES * STAGE_BYTES); }

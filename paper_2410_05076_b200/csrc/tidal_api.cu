@@ -1535,6 +1535,7 @@ tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const vo
     if (rc != TIDAL_OK) return rc;
     const int Hi = num_index_heads;
     if (Hi != kv->num_q_heads && Hi != kv->num_kv_heads && Hi != 1) return TIDAL_ERR_INVALID;
+    if (m > BA_MAX_LIST) return TIDAL_ERR_UNSUPPORTED;
     DeviceScope dev(ctx->device);
     if (!dev.ok) return TIDAL_ERR_CUDA;
     BlockAttnParams p;

@@ -185,8 +185,8 @@ def kv_struct(layer) -> tidal_kv_t:
     return s
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+def _stream(device: Optional[int] = None) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _check(status: int, what: str) -> None:
@@ -445,7 +445,9 @@ class Tidal:
         return out
 
     def device_status(self) -> int:
-        return self.lib.tidal_device_status(self.ctx, _stream())
+        """Waits for the current stream of the context's device, then returns and clears one kind of what its work has noted
+        (OK: nothing is left)."""
+        return self.lib.tidal_device_status(self.ctx, _stream(self.device))
 
     def launch_count(self) -> int:
         return self.lib.tidal_launch_count(self.ctx)

@@ -193,11 +193,6 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(addr), "r"(rank));
     return a;
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(cluster_addr(addr, rank)) : "memory");
-    return v;
-}
 __device__ __forceinline__ void st_cluster(uint32_t addr, int rank, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(cluster_addr(addr, rank)), "f"(v) : "memory");
 }

@@ -684,6 +684,7 @@ __host__ __device__ constexpr size_t sc_smem(int npad, int rows_per_cta, int sum
 
 template <int V, bool SHARED>
 __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __grid_constant__ SelectBlocksParams p) {
+    static_assert(V == 0 || !SHARED, "a set that all heads share is ranked by a CTA");
     const BlockCache& c = p.c;
     extern __shared__ __align__(16) uint8_t sc_rows[];
     __shared__ __align__(16) RankByCta<V> sh;
@@ -844,13 +845,7 @@ __global__ void __launch_bounds__(SC_THREADS, 2) block_select_kernel(const __gri
         float* const row = reinterpret_cast<float*>(sc_rows + (size_t)warp * p.npad * 8);
         float v[V], sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            v[j] = j * 32 + lane < padded ? row[j * 32 + lane] : 0.f;
-            if constexpr (SHARED) {
-#pragma unroll 4
-                for (int i = 1; i < slices; ++i) if (j * 32 + lane < padded) v[j] += row[i * padded + j * 32 + lane];
-            }
-        }
+        for (int j = 0; j < V; ++j) v[j] = j * 32 + lane < padded ? row[j * 32 + lane] : 0.f;
         for (int i = lane; i < W; i += 32) { err = fmaxf(err, s_part[i].x); sum += s_part[i].y; }
         err = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(err)));
         if (!per_qhead) {

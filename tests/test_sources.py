@@ -22,3 +22,11 @@ def test_nothing_is_read_through_the_non_coherent_path():
     for name, text in code().items():
         for word in (r"\b__ldg\b", r"ld\.global\.nc", r"ld\.global\S*\.nc\b", r"__restrict__"):
             assert not re.search(word, text), (name, word)
+
+
+def test_every_device_function_is_called():
+    text = " ".join(code().values())
+    names = re.findall(r"__device__[^;{}()]*?(\w+)\s*\([^;{]*\)\s*\{", text)
+    assert len(names) > 50
+    unused = sorted({n for n in names if len(re.findall(r"\b%s\b" % n, text)) < 2})
+    assert not unused, unused

@@ -314,8 +314,8 @@ tidal_status_t tidal_page_map(tidal_ctx_t *ctx, int32_t batch, const int32_t *ol
  * [num_kv_heads, head_dim] contiguous at t * k_stride / t * v_stride elements (multiples of 8; the bases 16-byte aligned),
  * so they may be slices of a fused projection's output. slots: device int64 [num_tokens]; paged caches: page * 16 + place
  * (tidal_page_map), contiguous ones: sequence * max_ctx_len + position. -1 is skipped; any other slot outside
- * the cache is skipped and reported as TIDAL_ERR_INDEX. If a slot is named twice, which of its rows stays is
- * not specified. An FP8 cache receives E4M3 codes: x / k_scale[g] (fp32 quotient; v_scale for values) rounded to
+ * the cache is skipped and reported as TIDAL_ERR_INDEX. If a slot is named twice, what it then holds is
+ * not specified: pieces of both tokens' rows are possible. An FP8 cache receives E4M3 codes: x / k_scale[g] (fp32 quotient; v_scale for values) rounded to
  * the nearest code, ties to even, saturated at +-448, NaN kept. The cache is WRITTEN although the descriptor declares it
  * const; ctx_lens and page_table are not read. */
 tidal_status_t tidal_kv_write(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t num_tokens, const void *k_new, const void *v_new,

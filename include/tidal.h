@@ -335,7 +335,8 @@ tidal_status_t tidal_kv_write(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t nu
  *           bound_blocks >= ceil(max_ctx_len / 16), paged ones one entry per physical page,
  *           [bound_blocks, num_kv_heads, 2, head_dim] with bound_blocks >= num_pages; least keys first.
  *   start_lens  device int32 [batch] or NULL: only blocks from start_lens[b] / 16 on are computed (the tokens before
- *           start_lens[b] were there at the last call); NULL: all of them. Other blocks keep their bounds.
+ *           start_lens[b] were there at the last call), for a sequence that has become shorter from ctx_lens[b] / 16 on; NULL: all
+ *           of them. Other blocks keep their bounds.
  *   max_new host upper bound of ctx_lens[b] - start_lens[b], which sizes the launch (tokens beyond it may be left out);
  *           0: not known. */
 tidal_status_t tidal_block_bounds(tidal_ctx_t *ctx, const tidal_kv_t *kv, const int32_t *start_lens, int32_t max_new,

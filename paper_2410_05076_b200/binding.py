@@ -407,8 +407,8 @@ class Tidal:
     def block_bounds(self, layer, bounds: Optional[torch.Tensor] = None, start_lens: Optional[torch.Tensor] = None,
                      max_new: int = 0) -> torch.Tensor:
         """Channelwise least and greatest key of every block of 16 positions (bf16, see block_bounds_shape): of all
-        blocks, or of those that hold positions from start_lens (int32 [B]) on. max_new: host bound of the tokens
-        that came since start_lens (0: not known)."""
+        blocks, or of those that hold positions from start_lens (int32 [B]) on (of the last one, where a sequence has become
+        shorter). max_new: host bound of the tokens that came since start_lens (0: not known)."""
         s = kv_struct(layer)
         if bounds is None:
             bounds = torch.zeros(block_bounds_shape(s), dtype=torch.bfloat16, device=f"cuda:{self.device}")

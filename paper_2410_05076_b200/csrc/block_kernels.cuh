@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(BB_WARPS * 32) block_bounds_kernel(const Bound
     if (pair >= (long long)c.batch * c.Hkv) return;
     const int b = (int)(pair / c.Hkv), g = (int)(pair - (long long)b * c.Hkv);
     const int n = cached_len(c, b);
-    const int start = p.start_lens ? max(p.start_lens[b], 0) : 0;
+    const int start = p.start_lens ? max(min(p.start_lens[b], n), 0) : 0;      // (shorter now: its last block has lost keys)
     const long long blk_l = (long long)(start / TILE) + (w - pair * p.blocks);
     if (blk_l * TILE >= n) return;
     const int blk = (int)blk_l, rows = min(TILE, n - blk * TILE);

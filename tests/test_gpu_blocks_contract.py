@@ -17,6 +17,10 @@ def td():
     t.close()
 
 
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
 def i32(v):
     return torch.tensor(v, dtype=torch.int32, device=DEV)
 
@@ -80,6 +84,35 @@ def test_every_bf16_number_gets_the_code_of_its_quotient(td, scale):
     for got in (lay.k, lay.v):
         got = got[0, 0].contiguous().view(torch.uint8).cpu()
         assert ((got[nan] & 0x7F) == 0x7F).all() and torch.equal(got[~nan], want[~nan])
+
+
+# ---- key bounds ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("max_new", [0, 1])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_bounds_follow_sequences_that_become_shorter(td, fp8, max_new):
+    """Tokens taken back (100 -> 97) no longer count in the last block's bounds, although it starts before the old length."""
+    old, new = [100, 100, 64, 40, 33, 16, 5, 5], [97, 20, 48, 41, 32, 0, 5, 1]
+    hkv, width = 3, 7
+    keys = torch.randn(len(old) * width, hkv, BLK, 2, D, generator=gen(1), device=DEV).to(torch.float8_e4m3fn if fp8 else torch.bfloat16)
+    lens = i32(old)
+    lay = synth.LayerKV(k=keys[..., 0, :], v=keys[..., 1, :], batch=len(old), num_q_heads=hkv, num_kv_heads=hkv, head_dim=D, ctx_lens=lens,
+                        max_ctx_len=112, stride_pos=2 * D, stride_head=BLK * 2 * D, stride_page=hkv * BLK * 2 * D, kv_dtype=int(fp8),
+                        page_table=torch.randperm(len(old) * width, generator=gen(2), device=DEV).to(torch.int32).view(len(old), width),
+                        max_pages_per_seq=width, keep=[keys])
+    bounds = td.block_bounds(lay)
+    start = lens.clone()
+    lens.copy_(i32(new))
+    td.block_bounds(lay, bounds, start_lens=start, max_new=max_new)
+    fresh = td.block_bounds(lay)
+    for b, n in enumerate(new):
+        page = lay.page_table[b, : -(-n // BLK)].long()
+        assert torch.equal(bounds[page], fresh[page]), (b, n)
+        rows = keys[page][..., 0, :].float().transpose(1, 2).flatten(0, 1)[:n]                      # [n, Hkv, 128]
+        if n:
+            last = rows[(n - 1) // BLK * BLK:]
+            assert torch.equal(bounds[page[-1]].float(), torch.stack((last.amin(0), last.amax(0)), 1))
+    assert td.device_status() == binding.OK
 
 
 # ---- the status word -----------------------------------------------------------------------------------------------

@@ -14,7 +14,7 @@ namespace tidal {
 // The matrix instructions have positions as rows and the group's heads as columns: S^T = K Q^T, O^T += V^T P^T, so K and V are read
 // once per KV head. The softmax weights enter the second product as a sum of 16-bit numbers, three of bf16 over a bf16 cache (2^-24
 // relative), two of fp16 over an 8-bit one (2^-22): the path waits for memory, and the further matrix instructions cost it
-// 1 to 2 % (131072 positions, 256 blocks per KV head: 8.6 against 8.7 us) where one bf16 would leave 2^-8.
+// 1 to 2 % (131072 positions, 256 blocks per KV head: 8.8 us) where one bf16 would leave 2^-8.
 struct BlockAttnParams {
     BlockCache c;
     const __nv_bfloat16* q;

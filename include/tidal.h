@@ -10,8 +10,11 @@
  * layers), and the cache update (the new token's key and value rows written
  * into the cache). Beside it stand a coarser selection of whole blocks of 16
  * tokens with its attention, and the filling of paged caches (page tables and
- * slot maps from request lengths, many tokens' rows). Projections, position
- * encodings and FFN are the caller's.
+ * slot maps from request lengths, many tokens' rows), and what a prompt needs
+ * on its way there: norms and rotary positions of queries and keys, attention
+ * of chunks of new tokens, the attention weight every cached position receives
+ * and the eviction of those that receive least. Projections and FFN are the
+ * caller's; the decode step takes queries and keys that are position-encoded.
  *
  * Conventions shared by every call
  *   - All tensor pointers are DEVICE pointers unless a parameter says "host".
@@ -54,7 +57,7 @@ enum {
     TIDAL_ERR_UNSUPPORTED = -2,   /* valid request outside what is built (head_dim != 128, ...) */
     TIDAL_ERR_NOMEM = -3,         /* workspace allocation failed */
     TIDAL_ERR_CUDA = -4,          /* a CUDA runtime call failed */
-    TIDAL_ERR_TIMEOUT = -5,       /* reserved: a bounded device-side wait expired (no kernel waits on another) */
+    TIDAL_ERR_TIMEOUT = -5,       /* a bounded wait of a kernel on its own copies or products expired: a bug, results invalid */
     TIDAL_ERR_INDEX = -6,         /* device saw a token index or page id out of range */
     TIDAL_ERR_TOO_LARGE = -7,     /* tidal_sparse_attn_noalloc only: problem exceeds its fixed scratch */
     TIDAL_ERR_PAGES = -9,         /* tidal_page_map: the request does not fit its arrays or the pool (nothing was changed) */
@@ -367,8 +370,116 @@ tidal_status_t tidal_block_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const 
 tidal_status_t tidal_block_attn(tidal_ctx_t *ctx, const tidal_kv_t *kv, const void *q, const int32_t *idx,
                                 const int32_t *idx_count, int32_t m, int32_t num_index_heads, float *out, void *stream);
 
+/* ---- Queries and keys of new tokens: norms and rotary positions ------------------------------------------------- */
+
+/* How positions rotate the channels of a head, filled by tidal_rope_init and passed to the calls below by its address (read on the
+ * host, inside the call). */
+enum { TIDAL_ROPE_HALF = 0, TIDAL_ROPE_INTERLEAVED = 1 };   /* channel i turns with channel i + rotary_dim / 2, or 2 i with 2 i + 1 */
+typedef struct {
+    int32_t rotary_dim;      /* channels 0 .. rotary_dim - 1 turn, the others stay: 16, 32, .. 128 */
+    int32_t layout;          /* TIDAL_ROPE_HALF or TIDAL_ROPE_INTERLEAVED */
+    float scale;             /* factor on cosines and sines */
+    int32_t reserved;
+    uint64_t step[64];       /* turns per position of every pair of channels, in 2^-64 of a turn */
+} tidal_rope_t;
+
+/* Frequencies, on the host: inv_freq[i], i < rotary_dim / 2, in radians per position, and the factor on cosines and sines (1 but for
+ * RAMP). With f_i = base^(-2 i / rotary_dim):
+ *   PLAIN   f_i.   LINEAR  f_i / factor.   BASE  f_i of the base  base * factor^(rotary_dim / (rotary_dim - 2))
+ *   BANDS   f_i / factor where a pair turns fewer than `low` times over trained_len positions, f_i where it turns more than
+ *           `high` times, linear in the number of turns between: (1 - s) f_i / factor + s f_i, s = (turns - low) / (high - low)
+ *   RAMP    r f_i / factor + (1 - r) f_i, r rising linearly from 0 to 1 over the channel numbers from floor(c(high)) to ceil(c(low)), with
+ *           c(n) = rotary_dim ln(trained_len / (2 pi n)) / (2 ln base) the one that turns n times; factor on cosines and
+ *           sines 0.1 ln(factor) + 1
+ * factor >= 1; 0 < low < high and trained_len > 0 where they are used. */
+enum { TIDAL_ROPE_PLAIN = 0, TIDAL_ROPE_LINEAR = 1, TIDAL_ROPE_BASE = 2, TIDAL_ROPE_BANDS = 3, TIDAL_ROPE_RAMP = 4 };
+tidal_status_t tidal_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double low, double high,
+                                      double trained_len, double *inv_freq, double *cos_scale);
+
+/* Fills `rope` from frequencies (host double [rotary_dim / 2], tidal_rope_frequencies' or any others, finite). */
+tidal_status_t tidal_rope_init(tidal_rope_t *rope, int32_t rotary_dim, int32_t layout, const double *inv_freq, double cos_scale);
+
+/* Queries and keys of num_tokens tokens normed (optional) and rotated to their positions.
+ *   q, k       device bf16, token t's rows [num_q_heads, 128] / [num_kv_heads, 128] contiguous at t * q_stride / t * k_stride elements
+ *              (multiples of 8; bases 16-byte aligned); one of the two may be NULL with 0 heads.
+ *   positions  device int32 [num_tokens]; a negative one (tidal_page_map's padding) leaves the token's rows unwritten.
+ *   q_weight, k_weight  device bf16 [128], 16-byte aligned, or NULL: with a weight w a row x becomes
+ *              x w / sqrt(mean(x^2) + eps) first, the mean over the head's 128 channels; with NULL it is not normed.
+ *   q_out, k_out  like q and k with their own strides; may be q and k themselves (same stride), no other overlap.
+ * Pair (a, b) at position p becomes (a c - b s, b c + a s), c, s = scale * cos, sin(p f). Angles are exact to 2^-32 of a turn at any
+ * position; arithmetic is fp32, rounded once. */
+tidal_status_t tidal_rope(tidal_ctx_t *ctx, const tidal_rope_t *rope, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads,
+                          const void *q, int64_t q_stride, const void *k, int64_t k_stride, const int32_t *positions,
+                          const void *q_weight, const void *k_weight, float eps, void *q_out, int64_t q_out_stride, void *k_out,
+                          int64_t k_out_stride, void *stream);
+
+/* The same with the keys, and the tokens' values, written into a layer's cache through a slot map (as tidal_kv_write: -1 is skipped, any other slot
+ * outside the cache skipped and reported as TIDAL_ERR_INDEX, a slot named twice unspecified; a token with a negative position is
+ * skipped altogether). Heads are the descriptor's. An FP8 cache receives the codes nearest to key / k_scale[g], the key in fp32 and
+ * rounded only there; values as tidal_kv_write quantises them. q may be NULL (then q_out too). The cache is WRITTEN although
+ * the descriptor declares it const; ctx_lens and page_table are not read. */
+tidal_status_t tidal_rope_write(tidal_ctx_t *ctx, const tidal_rope_t *rope, const tidal_kv_t *kv, int32_t num_tokens, const void *q,
+                                int64_t q_stride, const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                                const int32_t *positions, const int64_t *slots, const void *q_weight, const void *k_weight, float eps,
+                                void *q_out, int64_t q_out_stride, void *stream);
+
+/* ---- Chunks of new tokens --------------------------------------------------------------------------------------- */
+
+/* Attention of the last tokens of every sequence: sequence b's queries are rows q_offsets[b] .. q_offsets[b + 1] - 1 of q, its n newest
+ * tokens in order, whose keys and values the cache holds already (ctx_lens counts them): row i is the token at position
+ * p = ctx_lens[b] - n + i. It sees position j where j < ctx_lens[b], j <= p if causal != 0, and j > p - window if window > 0.
+ *   q          device bf16, token t's rows [num_q_heads, 128] contiguous at t * q_stride elements (a multiple of 8; base 16-byte aligned)
+ *   q_offsets  device int32 [batch + 1], ascending from 0 to at most num_tokens (tidal_page_map's token_offsets); others are cut to that and
+ *              reported as TIDAL_ERR_INDEX. Sequences may bring no token, one, or all they have.
+ *   max_new    host upper bound of the new tokens of a sequence (tokens beyond it may be left out); 0: not known
+ *   out        [num_tokens, num_q_heads, 128] contiguous, type as set by tidal_set_output_dtype; lse: float [num_tokens, num_q_heads] or NULL,
+ *              ln of the sum of exp(scaled logit) over what the row sees. Rows behind q_offsets[batch] are left as they were.
+ * A row that sees nothing gets zeros and -infinity. What lies behind a sequence in its last page or row block may be anything. Pages whose
+ * id is outside the pool are skipped and reported. k_scale must be positive. Softmax weights enter the product with V as
+ * bf16 (FP8 caches: fp16, and the query as fp16 too); maxima, sums and outputs are fp32. No scratch memory. */
+tidal_status_t tidal_chunk_attn(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t num_tokens, const void *q, int64_t q_stride,
+                                const int32_t *q_offsets, int32_t max_new, int32_t causal, int32_t window, float *out, float *lse,
+                                void *stream);
+
+/* The attention weight that every cached position receives from those queries:
+ *   weights[b, h, j] = decay * weights[b, h, j] + sum over the queries that see j and the query heads of h of exp(logit - lse)
+ * with lse as tidal_chunk_attn wrote it for the same arguments. num_weight_heads: num_kv_heads (a sum per KV head), or 1 (over all heads).
+ *   weights  device float [batch, num_weight_heads, stride], stride >= max_ctx_len; entries j < ctx_lens[b] are written, the chunk's own
+ *            positions as if their weight before had been 0 (so nothing need be cleared when a sequence has become shorter and
+ *            grows again), and with decay 0 all of them.
+ *   last     > 0: only the last so many queries of each chunk count
+ * The sum's order does not change from call to call. No scratch memory. */
+tidal_status_t tidal_chunk_weights(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t num_tokens, const void *q, int64_t q_stride,
+                                   const int32_t *q_offsets, int32_t max_new, int32_t causal, int32_t window, int32_t last,
+                                   const float *lse, float decay, float *weights, int64_t stride, int32_t num_weight_heads, void *stream);
+
+/* ---- Eviction ----------------------------------------------------------------------------------------------------- */
+
+/* The positions that stay: per sequence and weight head the m' = min(m, ctx_lens[b]) with the largest weights, equal ones (0 and -0 are equal)
+ * resolved toward the lower position, not-a-numbers last, after the first keep_first and the last keep_last positions, which count as better than
+ * any weight (lower ones first if they are more than m).
+ *   kept      int32 [batch, num_weight_heads, m]: positions in ascending order, padded with -1
+ *   new_lens  int32 [batch]: m'; not kv->ctx_lens
+ * weights as above. Only the descriptor's lengths and shape are read. No scratch memory. */
+tidal_status_t tidal_evict_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const float *weights, int64_t stride, int32_t num_weight_heads,
+                                  int32_t m, int32_t keep_first, int32_t keep_last, int32_t *kept, int32_t *new_lens, void *stream);
+
+/* Key and value rows of listed positions moved to the front, in the lists' order: row j of sequence b and KV head g becomes row
+ * kept[b, h, j], j < counts[b] (at most m), h = g or 0. num_list_heads: num_kv_heads, or 1 for one list for all heads. Lists of
+ * tidal_evict_select, or tidal_select_attn's idx of granularity PER_KVHEAD or SHARED.
+ *   into      NULL: within the cache; lists are ascending then, and no page belongs to two sequences. Otherwise the descriptor of the cache
+ *             that receives the rows (same heads and element type; its ctx_lens is not read), of which no row is one that the lists name.
+ *   weights   NULL, or float [batch, num_list_heads, stride] moved along to weights_out [.., stride_out], stride >= kv->max_ctx_len and
+ *             stride_out >= min(m, the receiving max_ctx_len); within the cache weights_out may be weights, otherwise not.
+ * -1 is skipped, another position outside [0, ctx_lens[b]) skipped and reported as TIDAL_ERR_INDEX, a page id outside the pool likewise.
+ * ctx_lens holds the lengths before; the caller then takes new_lens (tidal_page_map gives the pages back), and key
+ * bounds are computed anew. The cache is WRITTEN although the descriptor declares it const. */
+tidal_status_t tidal_kv_gather(tidal_ctx_t *ctx, const tidal_kv_t *kv, const tidal_kv_t *into, const int32_t *kept, const int32_t *counts,
+                               int32_t m, int32_t num_list_heads, const float *weights, int64_t stride, float *weights_out,
+                               int64_t stride_out, void *stream);
+
 /* Waits for `stream`, then reports and clears one kind of what the device has noted since: TIDAL_ERR_INTERNAL before
- * TIDAL_ERR_PAGES before TIDAL_ERR_INDEX. What else was noted stays for the next call, so that TIDAL_OK says that nothing
+ * TIDAL_ERR_TIMEOUT before TIDAL_ERR_PAGES before TIDAL_ERR_INDEX. What else was noted stays for the next call, so that TIDAL_OK says that nothing
  * is left. TIDAL_ERR_CUDA if the stream reports an error. */
 tidal_status_t tidal_device_status(tidal_ctx_t *ctx, void *stream);
 

@@ -25,6 +25,8 @@ KV_CONTIG, KV_PAGED = 0, 1
 KV_BF16, KV_FP8_E4M3 = 0, 1
 SEL_PER_QHEAD, SEL_PER_KVHEAD, SEL_SHARED = 0, 1, 2
 LAYER_FULL, LAYER_SELECT, LAYER_SPARSE = 0, 1, 2
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
 
 EXPORTS = [
     "tidal_create", "tidal_destroy", "tidal_workspace_bytes", "tidal_full_attn", "tidal_select_attn",
@@ -33,6 +35,8 @@ EXPORTS = [
     "tidal_decode_step_append", "tidal_set_graphs", "tidal_set_output_dtype", "tidal_set_attend_newest",
     "tidal_set_layer_overlap", "tidal_reserve", "tidal_set_select_margin",
     "tidal_page_map", "tidal_kv_write", "tidal_block_bounds", "tidal_block_select", "tidal_block_attn",
+    "tidal_rope_frequencies", "tidal_rope_init", "tidal_rope", "tidal_rope_write", "tidal_chunk_attn", "tidal_chunk_weights",
+    "tidal_evict_select", "tidal_kv_gather",
 ]
 
 BLOCK = 16               # positions per block of the block-sparse calls, and per page
@@ -50,6 +54,10 @@ class tidal_kv_t(C.Structure):
         ("ctx_lens", C.c_void_p), ("max_ctx_len", C.c_int32), ("sm_scale", C.c_float),
         ("kv_dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
     ]
+
+
+class tidal_rope_t(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scale", C.c_float), ("reserved", C.c_int32), ("step", C.c_uint64 * 64)]
 
 
 class TidalError(RuntimeError):
@@ -121,6 +129,24 @@ def load() -> C.CDLL:
     L.tidal_block_select.restype = I32
     L.tidal_block_attn.argtypes = [P, KVP, P, P, P, I32, I32, P, P]
     L.tidal_block_attn.restype = I32
+    PD, D64 = C.POINTER(C.c_double), C.c_double
+    RP = C.POINTER(tidal_rope_t)
+    L.tidal_rope_frequencies.argtypes = [I32, D64, I32, D64, D64, D64, D64, PD, PD]
+    L.tidal_rope_frequencies.restype = I32
+    L.tidal_rope_init.argtypes = [RP, I32, I32, PD, D64]
+    L.tidal_rope_init.restype = I32
+    L.tidal_rope.argtypes = [P, RP, I32, I32, I32, P, I64, P, I64, P, P, P, C.c_float, P, I64, P, I64, P]
+    L.tidal_rope.restype = I32
+    L.tidal_rope_write.argtypes = [P, RP, KVP, I32, P, I64, P, I64, P, I64, P, P, P, P, C.c_float, P, I64, P]
+    L.tidal_rope_write.restype = I32
+    L.tidal_chunk_attn.argtypes = [P, KVP, I32, P, I64, P, I32, I32, I32, P, P, P]
+    L.tidal_chunk_attn.restype = I32
+    L.tidal_chunk_weights.argtypes = [P, KVP, I32, P, I64, P, I32, I32, I32, I32, P, C.c_float, P, I64, I32, P]
+    L.tidal_chunk_weights.restype = I32
+    L.tidal_evict_select.argtypes = [P, KVP, P, I64, I32, I32, I32, I32, P, P, P]
+    L.tidal_evict_select.restype = I32
+    L.tidal_kv_gather.argtypes = [P, KVP, KVP, P, P, I32, I32, P, I64, P, I64, P]
+    L.tidal_kv_gather.restype = I32
     L.tidal_device_status.argtypes = [P, P]
     L.tidal_device_status.restype = I32
     L.tidal_launch_count.argtypes = [P]
@@ -147,8 +173,10 @@ def _fast_calls():
     except Exception as exc:  # no silent fallback here either
         raise ImportError(f"{os.path.basename(path)} (csrc/fast_call.cpp) could not be built or loaded: {exc}") from exc
     L = load()
-    fast.init(*[C.cast(f, C.c_void_p).value for f in (L.tidal_page_map, L.tidal_kv_write, L.tidal_block_bounds, L.tidal_block_select,
-                                                      L.tidal_block_attn)], C.sizeof(tidal_kv_t))
+    fast.init(C.sizeof(tidal_kv_t), C.sizeof(tidal_rope_t),
+              *[C.cast(f, C.c_void_p).value for f in (L.tidal_page_map, L.tidal_kv_write, L.tidal_block_bounds, L.tidal_block_select, L.tidal_block_attn,
+                                                      L.tidal_rope, L.tidal_rope_write, L.tidal_chunk_attn, L.tidal_chunk_weights,
+                                                      L.tidal_evict_select, L.tidal_kv_gather)])
     _fast = fast
     return fast
 
@@ -201,6 +229,26 @@ def block_bounds_shape(layer) -> tuple:
     if s.kv_layout == KV_PAGED:
         return (s.num_pages, s.num_kv_heads, 2, s.head_dim)
     return (s.batch, s.num_kv_heads, -(-s.max_ctx_len // BLOCK), 2, s.head_dim)
+
+
+def rope_plan(rotary_dim: int = 128, base: float = 10000.0, layout: int = ROPE_HALF, scaling: int = ROPE_PLAIN, factor: float = 1.0,
+              low: float = 1.0, high: float = 4.0, trained_len: float = 8192.0, inv_freq: Optional[Sequence[float]] = None,
+              cos_scale: float = 1.0) -> tidal_rope_t:
+    """How positions rotate the first rotary_dim channels of a head: frequencies base^(-2 i / rotary_dim), scaled as tidal.h says for
+    ROPE_LINEAR, ROPE_BASE, ROPE_BANDS and ROPE_RAMP, or inv_freq (radians per position of each pair) with the factor cos_scale on cosines and
+    sines. Made once and passed to rope and rope_write."""
+    L, plan, half = load(), tidal_rope_t(), max(rotary_dim // 2, 1)
+    freq = (C.c_double * half)()
+    if inv_freq is not None:
+        if len(inv_freq) != half:
+            raise ValueError(f"inv_freq: {half} frequencies are wanted, got {len(inv_freq)}")
+        freq[:] = [float(x) for x in inv_freq]
+    else:
+        s = C.c_double()
+        _check(L.tidal_rope_frequencies(rotary_dim, base, scaling, factor, low, high, trained_len, freq, C.byref(s)), "tidal_rope_frequencies")
+        cos_scale = s.value
+    _check(L.tidal_rope_init(C.byref(plan), rotary_dim, layout, freq, cos_scale), "tidal_rope_init")
+    return plan
 
 
 def sparse_attn_noalloc(layer, q: torch.Tensor, idx: torch.Tensor, idx_count: Optional[torch.Tensor] = None,
@@ -443,6 +491,84 @@ class Tidal:
         if rc:
             raise TidalError(rc, "tidal_block_attn")
         return out
+
+    # ---- a prompt's way into the cache: norms and rotary positions, chunk attention, eviction -------------------------
+
+    def rope(self, plan: tidal_rope_t, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
+             q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+             q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+        """Queries and keys of T tokens (bf16 [T, H, 128]; only the two inner dimensions have to be contiguous) normed per head where a
+        weight (bf16 [128]) is given and rotated to their positions (int32 [T]; negative: left unwritten). q_out and k_out may be q
+        and k. Returns (q_out, k_out)."""
+        if q_out is None and q is not None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k_out is None and k is not None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        rc = (_fast or _fast_calls()).rope(self._handle, self.device, plan, q, k, positions, q_weight, k_weight, eps, q_out, k_out)
+        if rc:
+            raise TidalError(rc, "tidal_rope")
+        return q_out, k_out
+
+    def rope_write(self, layer, plan: tidal_rope_t, q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor,
+                   positions: torch.Tensor, slots: torch.Tensor, q_weight: Optional[torch.Tensor] = None,
+                   k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None):
+        """rope with the keys, and the values, written at their slots (int64 [T]; -1: skipped) of the layer's cache; an FP8 cache
+        quantises them with its scales. Returns q_out (None without q)."""
+        if q_out is None and q is not None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        rc = (_fast or _fast_calls()).rope_write(self._handle, self.device, kv_struct(layer), plan, q, k_new, v_new, positions, slots, q_weight,
+                                                 k_weight, eps, q_out)
+        if rc:
+            raise TidalError(rc, "tidal_rope_write")
+        return q_out
+
+    def chunk_attn(self, layer, q: torch.Tensor, q_offsets: torch.Tensor, max_new: int = 0, causal: bool = True, window: int = 0,
+                   out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of every sequence's newest tokens (q: bf16 [T, Hq, 128], sequence b's rows q_offsets[b] .. q_offsets[b + 1] - 1; the cache
+        holds their keys and values already) over all cached positions up to their own, or the last `window` of them. max_new: host bound of
+        the tokens of a sequence (0: not known). lse: optional fp32 [T, Hq] output."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.out_dtype, device=q.device)
+        rc = (_fast or _fast_calls()).chunk_attn(self._handle, self.device, kv_struct(layer), q, q_offsets, max_new, 1 if causal else 0, window, out,
+                                                 self.out_dtype is torch.bfloat16, lse)
+        if rc:
+            raise TidalError(rc, "tidal_chunk_attn")
+        return out
+
+    def chunk_weights(self, layer, q: torch.Tensor, q_offsets: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor, decay: float = 1.0,
+                      max_new: int = 0, causal: bool = True, window: int = 0, last: int = 0) -> torch.Tensor:
+        """weights (fp32 [B, Hkv or 1, >= max_ctx_len]) = decay * weights + the attention weight that every cached position receives from
+        those queries (from the last `last` of each chunk, if > 0); lse is chunk_attn's. A chunk's own positions count as 0 before."""
+        rc = (_fast or _fast_calls()).chunk_weights(self._handle, self.device, kv_struct(layer), q, q_offsets, lse, weights, decay, max_new,
+                                                    1 if causal else 0, window, last)
+        if rc:
+            raise TidalError(rc, "tidal_chunk_weights")
+        return weights
+
+    def evict_select(self, layer, weights: torch.Tensor, m: int, keep_first: int = 0, keep_last: int = 0, kept: Optional[torch.Tensor] = None,
+                     new_lens: Optional[torch.Tensor] = None):
+        """The m positions per sequence and weight head with the largest weights, the first keep_first and the last keep_last among them.
+        Returns (kept int32 [B, heads, m] ascending and -1 padded, new_lens int32 [B])."""
+        s = kv_struct(layer)
+        if kept is None:
+            kept = torch.empty(s.batch, weights.shape[1], max(m, 1), dtype=torch.int32, device=weights.device)
+        if new_lens is None:
+            new_lens = torch.empty(s.batch, dtype=torch.int32, device=weights.device)
+        rc = (_fast or _fast_calls()).evict_select(self._handle, self.device, s, weights, m, keep_first, keep_last, kept, new_lens)
+        if rc:
+            raise TidalError(rc, "tidal_evict_select")
+        return kept, new_lens
+
+    def kv_gather(self, layer, kept: torch.Tensor, counts: torch.Tensor, into=None, weights: Optional[torch.Tensor] = None,
+                  weights_out: Optional[torch.Tensor] = None) -> None:
+        """The rows of the listed positions (kept: int32 [B, Hkv or 1, m], counts[b] of them) moved to the front of the layer's cache, or
+        copied to the cache `into`; weights along, to weights_out (within the cache: in place by default)."""
+        if weights is not None and weights_out is None and into is None:
+            weights_out = weights
+        rc = (_fast or _fast_calls()).kv_gather(self._handle, self.device, kv_struct(layer), None if into is None else kv_struct(into), kept, counts,
+                                                weights, weights_out)
+        if rc:
+            raise TidalError(rc, "tidal_kv_gather")
 
     def device_status(self) -> int:
         """Waits for the current stream of the context's device, then returns and clears one kind of what its work has noted

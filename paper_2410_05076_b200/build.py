@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtidal.so")
 SOURCES = ["tidal_api.cu"]
-DEPS = ["tidal_api.cu", "attn_kernels.cuh", "block_kernels.cuh", "block_select_kernels.cuh", "block_attn_kernels.cuh", "page_kernels.cuh", "split_select_kernels.cuh", "topk_kernels.cuh", os.path.join("..", "..", "include", "tidal.h")]
+DEPS = ["tidal_api.cu", "attn_kernels.cuh", "block_kernels.cuh", "block_select_kernels.cuh", "block_attn_kernels.cuh", "chunk_kernels.cuh", "evict_kernels.cuh", "page_kernels.cuh", "rope_kernels.cuh", "split_select_kernels.cuh", "topk_kernels.cuh", "weight_kernels.cuh", os.path.join("..", "..", "include", "tidal.h")]
 
 
 FAST_DEPS = ["fast_call.cpp", os.path.join("..", "..", "include", "tidal.h")]

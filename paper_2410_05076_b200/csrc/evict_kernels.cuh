@@ -1,0 +1,293 @@
+// Eviction from a cache by accumulated weight: which positions stay (evict_select_kernel), and their rows and weights moved
+// together (gather_copy_kernel into another cache, gather_inplace_kernel within one).
+#pragma once
+
+#include "block_kernels.cuh"
+
+namespace tidal {
+
+// ---- the m positions with the largest weights ------------------------------------------------------------------
+// A cluster per (sequence, weight head): every CTA keeps the order-preserving keys of its slice of the row in shared memory (one
+// read of memory in all), and three rounds of 2048, 2048 and 1024 bins over the cluster's histograms find the m-th largest key and how many of
+// the positions that share it still belong to the set. In a round every CTA counts its slice, adds up its share of the
+// bins over all CTAs and hands the sums to all, so that each finds the bin for itself. Then each CTA counts what it
+// keeps and writes it behind what the CTAs before it keep, in ascending order; of equal weights the lower positions.
+// Bound by that chain of barriers, not by its 4 bytes a position.
+struct EvictParams {
+    const float* weights;                                   // [batch][heads][stride]
+    long long stride;
+    const int* ctx_lens;
+    int max_ctx, heads, m, keep_first, keep_last;
+    int slice_max;                                          // keys that a CTA has room for
+    int* kept;                                              // [batch][heads][m]
+    int* new_lens;                                          // [batch]
+};
+
+constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32, EV_BINS = 2048, EV_MAX_CLUSTER = 16;
+constexpr size_t EV_SMEM_MAX = 160 * 1024;
+
+// Order-preserving: larger weight, larger key; -0 as 0; not-a-number below everything. Kept positions are above everything.
+__device__ __forceinline__ uint32_t evict_key(float w) {
+    if (!(w == w)) return 0u;
+    const uint32_t b = __float_as_uint(w + 0.f);
+    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ int ld_cluster(uint32_t addr, int rank) {
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];\n" : "=r"(v) : "r"(cluster_addr(addr, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_cluster_int(uint32_t addr, int rank, int v) {
+    asm volatile("st.shared::cluster.s32 [%0], %1;\n" ::"r"(cluster_addr(addr, rank)), "r"(v) : "memory");
+}
+
+__global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictParams p) {
+    extern __shared__ uint32_t ev_keys[];
+    __shared__ int s_hist[EV_BINS], s_all[EV_BINS], s_part[EV_WARPS], s_found[2], s_mine[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int C, rank;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(C));
+    asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+    const int row = blockIdx.x / C, b = row / p.heads;
+    pdl_wait();
+    pdl_trigger();
+    const int n = max(min(read_global(p.ctx_lens + b), p.max_ctx), 0);
+    const int want = min(p.m, n);
+    int* const kept = p.kept + (long long)row * p.m;
+    if (rank == 0 && tid == 0 && row == b * p.heads) p.new_lens[b] = want;
+    for (int i = want + rank * EV_THREADS + tid; i < p.m; i += C * EV_THREADS) kept[i] = -1;
+    if (want == n) {                                        // everything stays
+        for (int i = rank * EV_THREADS + tid; i < n; i += C * EV_THREADS) kept[i] = i;
+        return;                                             // (the whole cluster)
+    }
+    const int slice = (n + C - 1) / C, lo = min(rank * slice, n), cnt = min(slice, n - lo);
+    const float* const w = p.weights + (long long)row * p.stride + lo;
+    for (int i = tid; i < cnt; i += EV_THREADS) {
+        const int pos = lo + i;
+        const bool keep = pos < p.keep_first || pos >= n - p.keep_last;
+        ev_keys[i] = keep ? 0xffffffffu : evict_key(read_global(w + i));
+    }
+    // the want-th largest key, digit by digit from the top
+    uint32_t prefix = 0, known = 0;
+    int left = want;                                        // of the keys that share the prefix
+    const uint32_t all_addr = smem_u32(s_all), hist_addr = smem_u32(s_hist), mine_addr = smem_u32(s_mine);
+#pragma unroll 1
+    for (int round = 0; round < 3; ++round) {
+        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048;
+        for (int i = tid; i < bins; i += EV_THREADS) s_hist[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < cnt; i += EV_THREADS) {
+            const uint32_t key = ev_keys[i];
+            if ((key & known) == prefix) atomicAdd(&s_hist[(key >> shift) & (bins - 1)], 1);
+        }
+        if (C > 1) {
+            cluster_arrive(); cluster_wait();
+            const int per = (bins + C - 1) / C;
+            for (int i = rank * per + tid; i < min((rank + 1) * per, bins); i += EV_THREADS) {
+                int sum = 0;
+                for (int r = 0; r < C; ++r) sum += ld_cluster(hist_addr + i * 4, r);
+                for (int r = 0; r < C; ++r) st_cluster_int(all_addr + i * 4, r, sum);
+            }
+            cluster_arrive(); cluster_wait();
+        } else {
+            __syncthreads();
+            for (int i = tid; i < bins; i += EV_THREADS) s_all[i] = s_hist[i];
+            __syncthreads();
+        }
+        // bins from the top: thread t holds bins bins - 1 - 2 t and the one below it (bins - 1 - t in the last round)
+        const int per = bins / EV_THREADS;
+        int v[2], sum = 0;
+        for (int u = 0; u < 2; ++u) { v[u] = u < per ? s_all[bins - 1 - tid * per - u] : 0; sum += v[u]; }
+        int x = sum;
+#pragma unroll
+        for (int sh = 1; sh < 32; sh <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, sh); if (lane >= sh) x += y; }
+        if (lane == 31) s_part[warp] = x;
+        __syncthreads();
+        int y = s_part[lane];
+#pragma unroll
+        for (int sh = 1; sh < 32; sh <<= 1) { const int z = __shfl_up_sync(0xffffffffu, y, sh); if (lane >= sh) y += z; }
+        const int before = __shfl_sync(0xffffffffu, y, max(warp - 1, 0));
+        int above = x - sum + (warp ? before : 0);
+        for (int u = 0; u < per; ++u) {
+            if (above < left && above + v[u] >= left) { s_found[0] = bins - 1 - tid * per - u; s_found[1] = left - above; }
+            above += v[u];
+        }
+        __syncthreads();
+        prefix |= (uint32_t)s_found[0] << shift;
+        known |= (uint32_t)(bins - 1) << shift;
+        left = s_found[1];
+    }
+    // every warp a run of the slice: how much it keeps for certain, and how much shares the last key
+    const int run = ((cnt + EV_WARPS - 1) / EV_WARPS + 31) / 32 * 32;
+    const int from = min(warp * run, cnt), to = min(from + run, cnt);
+    int more = 0, same = 0;
+    for (int i = from; i < to; i += 32) {
+        const uint32_t key = i + lane < to ? ev_keys[i + lane] : 0u;
+        more += __popc(__ballot_sync(0xffffffffu, i + lane < to && key > prefix));
+        same += __popc(__ballot_sync(0xffffffffu, i + lane < to && key == prefix));
+    }
+    __shared__ int s_more[EV_WARPS], s_same[EV_WARPS];
+    if (lane == 0) { s_more[warp] = more; s_same[warp] = same; }
+    __syncthreads();
+    int a = s_more[lane], e = s_same[lane];
+#pragma unroll
+    for (int sh = 1; sh < 32; sh <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, a, sh), z = __shfl_up_sync(0xffffffffu, e, sh);
+        if (lane >= sh) { a += y; e += z; }
+    }
+    if (tid == 31) { s_mine[0] = a; s_mine[1] = e; }
+    int more_at = __shfl_sync(0xffffffffu, a, max(warp - 1, 0)), same_at = __shfl_sync(0xffffffffu, e, max(warp - 1, 0));
+    if (warp == 0) more_at = same_at = 0;
+    if (C > 1) {
+        cluster_arrive(); cluster_wait();
+        for (int r = 0; r < rank; ++r) { more_at += ld_cluster(mine_addr, r); same_at += ld_cluster(mine_addr + 4, r); }
+        cluster_arrive();                                   // (waited for at the end: nobody leaves while it is read)
+    }
+    for (int i = from; i < to; i += 32) {
+        const uint32_t key = i + lane < to ? ev_keys[i + lane] : 0u;
+        const unsigned gt = __ballot_sync(0xffffffffu, i + lane < to && key > prefix), eq = __ballot_sync(0xffffffffu, i + lane < to && key == prefix);
+        const unsigned below = (1u << lane) - 1u;
+        const int e_at = same_at + __popc(eq & below);
+        const bool mine = ((gt >> lane) & 1) || (((eq >> lane) & 1) && e_at < left);
+        if (mine) kept[more_at + __popc(gt & below) + min(e_at, left)] = lo + i + lane;
+        more_at += __popc(gt);
+        same_at += __popc(eq);
+    }
+    if (C > 1) cluster_wait();
+}
+
+// ---- rows of listed positions moved to the front -----------------------------------------------------------------
+struct GatherParams {
+    BlockCache from;
+    uint8_t* k;                                             // where the rows go: another cache, or this one
+    uint8_t* v;
+    long long stride_b, stride_pos, stride_head, stride_page;
+    const int* page_table;
+    int max_pages, num_pages, paged, max_ctx;
+    const int* kept;                                        // [batch][heads][m]
+    const int* counts;                                      // [batch]
+    int heads, m, row_bytes;
+    const float* weights;
+    float* weights_out;
+    long long w_stride, wo_stride;
+};
+
+constexpr int GA_WARPS = 8, GA_UNROLL = 4;
+
+// Byte offset of position pos (element offset times the element's size), -1 where a page id is outside the pool.
+__device__ __forceinline__ long long cache_row(const int* table, int max_pages, int num_pages, int paged, long long stride_b, long long stride_pos,
+                                               long long stride_page, int b, int pos, int* status) {
+    if (!paged) return b * stride_b + pos * stride_pos;
+    const int page = read_global(table + (long long)b * max_pages + pos / TILE);
+    if ((unsigned)page >= (unsigned)num_pages) { atomicOr(status, STATUS_BAD_PAGE); return -1; }
+    return page * stride_page + (pos % TILE) * stride_pos;
+}
+
+// How many rows of sequence b are moved, and the source of the j-th (-1: none).
+__device__ __forceinline__ int gather_count(const GatherParams& p, int b) { return max(min(read_global(p.counts + b), p.m), 0); }
+__device__ __forceinline__ int gather_source(const GatherParams& p, int b, int g, int j, int n) {
+    const int pos = read_global(p.kept + ((long long)b * p.heads + (p.heads > 1 ? g : 0)) * p.m + j);
+    if ((unsigned)pos >= (unsigned)n) { if (pos != -1) atomicOr(p.from.status, STATUS_BAD_INDEX); return -1; }
+    return pos;
+}
+
+// Into another cache: a warp takes four or eight rows, all their loads in flight together. 16 bytes per lane: a position's key and value
+// row fill a warp (16 bits) or half of one (8 bits). Bound by memory.
+template <bool KV8>
+__global__ void __launch_bounds__(GA_WARPS * 32) gather_copy_kernel(const GatherParams p) {
+    constexpr int ROWS = KV8 ? 2 : 1, PER = GA_UNROLL * ROWS, LANES = 32 / ROWS;
+    constexpr int ESZ = KV8 ? 1 : 2;
+    const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES, piece = l % (LANES / 2);
+    const bool value = l >= LANES / 2;
+    const BlockCache& c = p.from;
+    const long long unit = (long long)blockIdx.x * GA_WARPS + (threadIdx.x >> 5);
+    const int groups = (p.m + PER - 1) / PER;
+    const long long pair = unit / groups;
+    pdl_wait();
+    pdl_trigger();
+    if (pair >= (long long)c.batch * c.Hkv) return;
+    const int b = (int)(pair / c.Hkv), g = (int)(pair - (long long)b * c.Hkv);
+    const int j0 = (int)(unit - pair * groups) * PER;
+    const int cnt = min(gather_count(p, b), p.max_ctx), n = cached_len(c, b);
+    if (j0 >= cnt) return;
+    uint4 w[GA_UNROLL];
+    uint8_t* to[GA_UNROLL];
+#pragma unroll
+    for (int u = 0; u < GA_UNROLL; ++u) {
+        const int j = j0 + u * ROWS + sub;
+        to[u] = nullptr;
+        if (j >= cnt) continue;
+        const int pos = gather_source(p, b, g, j, n);
+        if (pos < 0) continue;
+        if (p.weights && piece == 0 && !value && (p.heads > 1 || g == 0)) {
+            const long long row = (long long)b * p.heads + (p.heads > 1 ? g : 0);
+            p.weights_out[row * p.wo_stride + j] = read_global(p.weights + row * p.w_stride + pos);
+        }
+        const long long src = cache_row(c.page_table, c.max_pages, c.num_pages, c.paged, c.stride_b, c.stride_pos, c.stride_page, b, pos, c.status);
+        const long long dst = cache_row(p.page_table, p.max_pages, p.num_pages, p.paged, p.stride_b, p.stride_pos, p.stride_page, b, j, c.status);
+        if (src < 0 || dst < 0) continue;
+        w[u] = read_global(reinterpret_cast<const uint4*>((value ? c.v : c.k) + (src + g * c.stride_head) * ESZ + piece * 16));
+        to[u] = (value ? p.v : p.k) + (dst + g * p.stride_head) * ESZ + piece * 16;
+    }
+#pragma unroll
+    for (int u = 0; u < GA_UNROLL; ++u)
+        if (to[u]) *reinterpret_cast<uint4*>(to[u]) = w[u];
+}
+
+// Within a cache: the j-th listed position is never below j (the list is ascending), so a row may be written once all rows up to it
+// have been read. A CTA takes a column of 32 bytes of all rows of a sequence and KV head, so that this order is its own affair: it reads
+// GI_ROWS rows, waits for its threads, writes them. The last CTAs move the weights in the same way.
+constexpr int GI_THREADS = 512, GI_COLUMN = 32, GI_UNROLL = 4;
+constexpr int GI_ROWS = GI_THREADS / (GI_COLUMN / 16) * GI_UNROLL;
+
+__global__ void __launch_bounds__(GI_THREADS) gather_inplace_kernel(const GatherParams p) {
+    const int esz = p.row_bytes / HEAD_DIM;
+    const BlockCache& c = p.from;
+    const int columns = 2 * p.row_bytes / GI_COLUMN, tid = threadIdx.x;
+    const long long moves = (long long)c.batch * c.Hkv * columns;
+    pdl_wait();
+    pdl_trigger();
+    if (blockIdx.x >= moves) {                              // weights
+        const int row = (int)(blockIdx.x - moves), b = row / p.heads, g = row - b * p.heads;
+        const int n = cached_len(c, b), cnt = min(gather_count(p, b), n);
+        float* const w = p.weights_out + (long long)row * p.wo_stride;
+        const float* const from = p.weights + (long long)row * p.w_stride;
+        for (int j0 = 0; j0 < cnt; j0 += GI_THREADS) {
+            const int j = j0 + tid, pos = j < cnt ? gather_source(p, b, g, j, n) : -1;
+            float x = 0.f;
+            if (pos >= 0) x = read_global(from + pos);
+            __syncthreads();
+            if (pos >= 0) w[j] = x;
+        }
+        return;
+    }
+    const int col = (int)(blockIdx.x % columns);
+    const long long pair = blockIdx.x / columns;
+    const int b = (int)(pair / c.Hkv), g = (int)(pair - (long long)b * c.Hkv);
+    const int n = cached_len(c, b), cnt = min(gather_count(p, b), n);       // (an ascending list has no more)
+    const int byte = col * GI_COLUMN + (tid % (GI_COLUMN / 16)) * 16;
+    const bool value = byte >= p.row_bytes;
+    uint8_t* const base = (value ? p.v : p.k) + (long long)g * c.stride_head * esz + (value ? byte - p.row_bytes : byte);
+    for (int j0 = 0; j0 < cnt; j0 += GI_ROWS) {
+        uint4 w[GI_UNROLL];
+        long long to[GI_UNROLL];
+#pragma unroll
+        for (int u = 0; u < GI_UNROLL; ++u) {
+            const int j = j0 + u * (GI_ROWS / GI_UNROLL) + tid / (GI_COLUMN / 16);
+            to[u] = -1;
+            const int pos = j < cnt ? gather_source(p, b, g, j, n) : -1;
+            if (pos < 0 || pos == j) continue;              // (a row that stays where it is)
+            const long long src = cache_row(c.page_table, c.max_pages, c.num_pages, c.paged, c.stride_b, c.stride_pos, c.stride_page, b, pos, c.status);
+            const long long dst = cache_row(c.page_table, c.max_pages, c.num_pages, c.paged, c.stride_b, c.stride_pos, c.stride_page, b, j, c.status);
+            if (src < 0 || dst < 0) continue;
+            w[u] = read_global(reinterpret_cast<const uint4*>(base + src * esz));
+            to[u] = dst * esz;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < GI_UNROLL; ++u)
+            if (to[u] >= 0) *reinterpret_cast<uint4*>(base + to[u]) = w[u];
+    }
+}
+
+}  // namespace tidal

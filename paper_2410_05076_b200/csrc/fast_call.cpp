@@ -19,6 +19,12 @@ decltype(&tidal_kv_write) f_kv_write;
 decltype(&tidal_block_bounds) f_block_bounds;
 decltype(&tidal_block_select) f_block_select;
 decltype(&tidal_block_attn) f_block_attn;
+decltype(&tidal_rope) f_rope;
+decltype(&tidal_rope_write) f_rope_write;
+decltype(&tidal_chunk_attn) f_chunk_attn;
+decltype(&tidal_chunk_weights) f_chunk_weights;
+decltype(&tidal_evict_select) f_evict_select;
+decltype(&tidal_kv_gather) f_kv_gather;
 
 struct Refused {};                           // a Python exception is set
 
@@ -95,6 +101,45 @@ struct Descriptor {
     ~Descriptor() { PyBuffer_Release(&view); }
     Descriptor(const Descriptor&) = delete;
 };
+
+// The bytes of a ctypes tidal_rope_t.
+struct Plan {
+    Py_buffer view{};
+    const tidal_rope_t* rope = nullptr;
+    explicit Plan(PyObject* o) {
+        if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Refused{};
+        if (view.len != (Py_ssize_t)sizeof(tidal_rope_t)) { PyBuffer_Release(&view); refuse("plan: not a rope_plan"); }
+        rope = static_cast<const tidal_rope_t*>(view.buf);
+    }
+    ~Plan() { PyBuffer_Release(&view); }
+    Plan(const Plan&) = delete;
+};
+
+// Rows [tokens, heads, head_dim] of bf16, those of a token contiguous; nothing for None.
+struct Rows {
+    void* data = nullptr;
+    int64_t tokens = 0, heads = 0, stride = 0;
+    Rows(PyObject* o, const char* name, int device) {
+        const at::Tensor* t = tensor(o, name, at::kBFloat16, device);
+        if (!t) return;
+        if (t->dim() != 3 || t->size(2) != 128 || t->size(0) > INT32_MAX || t->size(1) > INT32_MAX)
+            refuse(std::string(name) + ": [tokens, heads, 128] is wanted, got " + shape_text(t->sizes().data(), t->dim()));
+        data = t->data_ptr();
+        tokens = t->size(0);
+        heads = t->size(1);
+        if (tokens && heads && (t->stride(2) != 1 || (heads > 1 && t->stride(1) != 128))) refuse(std::string(name) + ": the rows of a token have to be contiguous");
+        stride = tokens > 1 ? t->stride(0) : heads * 128;   // (a single token's stride says nothing: torch may give any)
+    }
+    void like(const Rows& other, const char* name) const {
+        if (!data != !other.data || tokens != other.tokens || heads != other.heads) refuse(std::string(name) + ": the shape of its input is wanted");
+    }
+};
+
+double as_double(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Refused{};
+    return v;
+}
 
 tidal_ctx_t* context(PyObject* o) { return static_cast<tidal_ctx_t*>(PyLong_AsVoidPtr(o)); }
 void* stream_of(int device) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
@@ -216,21 +261,143 @@ PyObject* block_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// init(address of tidal_page_map, kv_write, block_bounds, block_select, block_attn, sizeof the descriptor)
+// rope(ctx, device, plan, q, k, positions, q_weight, k_weight, eps, q_out, k_out)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&]() -> long {
+        const int dev = as_int(a[1], "device");
+        const Plan plan(a[2]);
+        const Rows q(a[3], "q", dev), k(a[4], "k", dev), qo(a[9], "q_out", dev), ko(a[10], "k_out", dev);
+        if (!q.data && !k.data && !q.tokens && !k.tokens && a[3] == Py_None && a[4] == Py_None) refuse("q, k: a tensor is wanted");
+        qo.like(q, "q_out");
+        ko.like(k, "k_out");
+        const int64_t tokens = a[3] != Py_None ? q.tokens : k.tokens;
+        if (a[3] != Py_None && a[4] != Py_None && q.tokens != k.tokens) refuse("k: as many tokens as q's are wanted");
+        return f_rope(context(a[0]), plan.rope, (int32_t)tokens, (int32_t)q.heads, (int32_t)k.heads, q.data, q.stride, k.data, k.stride,
+                      static_cast<const int32_t*>(contiguous_data(a[5], "positions", at::kInt, dev, {tokens})),
+                      contiguous_data(a[6], "q_weight", at::kBFloat16, dev, {128}), contiguous_data(a[7], "k_weight", at::kBFloat16, dev, {128}),
+                      (float)as_double(a[8]), qo.data, qo.stride, ko.data, ko.stride, stream_of(dev));
+    });
+}
+
+// rope_write(ctx, device, descriptor, plan, q, k_new, v_new, positions, slots, q_weight, k_weight, eps, q_out)
+PyObject* rope_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&]() -> long {
+        const int dev = as_int(a[1], "device");
+        const Descriptor d(a[2]);
+        const Plan plan(a[3]);
+        const at::Tensor& slots = required(a[8], "slots", at::kLong, dev);
+        contiguous(slots, "slots");
+        const int64_t tokens = count_of(slots, "slots");
+        const Rows q(a[4], "q", dev), k(a[5], "k_new", dev), v(a[6], "v_new", dev), qo(a[12], "q_out", dev);
+        qo.like(q, "q_out");
+        if (a[4] != Py_None && (q.tokens != tokens || q.heads != d.kv->num_q_heads)) refuse("q: [tokens, num_q_heads, 128] is wanted");
+        for (const auto& r : {std::make_pair(&k, "k_new"), std::make_pair(&v, "v_new")})
+            if (r.first->tokens != tokens || r.first->heads != d.kv->num_kv_heads) refuse(std::string(r.second) + ": [tokens, num_kv_heads, 128] is wanted");
+        return f_rope_write(context(a[0]), plan.rope, d.kv, (int32_t)tokens, q.data, q.stride, k.data, k.stride, v.data, v.stride,
+                            static_cast<const int32_t*>(contiguous_data(a[7], "positions", at::kInt, dev, {tokens})),
+                            static_cast<const int64_t*>(slots.data_ptr()), contiguous_data(a[9], "q_weight", at::kBFloat16, dev, {128}),
+                            contiguous_data(a[10], "k_weight", at::kBFloat16, dev, {128}), (float)as_double(a[11]), qo.data, qo.stride, stream_of(dev));
+    });
+}
+
+// chunk_attn(ctx, device, descriptor, q, q_offsets, max_new, causal, window, out, out is bf16, lse)
+PyObject* chunk_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&]() -> long {
+        const int dev = as_int(a[1], "device");
+        const Descriptor d(a[2]);
+        const tidal_kv_t* kv = d.kv;
+        const Rows q(a[3], "q", dev);
+        if (a[3] == Py_None || q.heads != kv->num_q_heads) refuse("q: [tokens, num_q_heads, 128] is wanted");
+        void* out = contiguous_data(a[8], "out", a[9] == Py_True ? at::kBFloat16 : at::kFloat, dev, {q.tokens, q.heads, 128});
+        void* lse = contiguous_data(a[10], "lse", at::kFloat, dev, {q.tokens, q.heads});
+        return f_chunk_attn(context(a[0]), kv, (int32_t)q.tokens, q.data, q.stride,
+                            static_cast<const int32_t*>(contiguous_data(a[4], "q_offsets", at::kInt, dev, {(int64_t)kv->batch + 1})), as_int(a[5], "max_new"),
+                            as_int(a[6], "causal"), as_int(a[7], "window"), static_cast<float*>(out), static_cast<float*>(lse), stream_of(dev));
+    });
+}
+
+// [batch, heads, stride] of fp32, contiguous; heads and stride come back.
+float* weight_rows(PyObject* o, const char* name, int device, int64_t batch, int64_t& heads, int64_t& stride) {
+    const at::Tensor* t = tensor(o, name, at::kFloat, device);
+    heads = stride = 0;
+    if (!t) return nullptr;
+    contiguous(*t, name);
+    if (t->dim() != 3 || t->size(0) != batch || t->size(1) > INT32_MAX)
+        refuse(std::string(name) + ": [" + std::to_string(batch) + ", heads, positions] is wanted, got " + shape_text(t->sizes().data(), t->dim()));
+    heads = t->size(1);
+    stride = t->size(2);
+    return static_cast<float*>(t->data_ptr());
+}
+
+// chunk_weights(ctx, device, descriptor, q, q_offsets, lse, weights, decay, max_new, causal, window, last)
+PyObject* chunk_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&]() -> long {
+        const int dev = as_int(a[1], "device");
+        const Descriptor d(a[2]);
+        const tidal_kv_t* kv = d.kv;
+        const Rows q(a[3], "q", dev);
+        if (a[3] == Py_None || q.heads != kv->num_q_heads) refuse("q: [tokens, num_q_heads, 128] is wanted");
+        int64_t heads, stride;
+        float* w = weight_rows(a[6], "weights", dev, kv->batch, heads, stride);
+        return f_chunk_weights(context(a[0]), kv, (int32_t)q.tokens, q.data, q.stride,
+                               static_cast<const int32_t*>(contiguous_data(a[4], "q_offsets", at::kInt, dev, {(int64_t)kv->batch + 1})), as_int(a[8], "max_new"),
+                               as_int(a[9], "causal"), as_int(a[10], "window"), as_int(a[11], "last"),
+                               static_cast<const float*>(contiguous_data(a[5], "lse", at::kFloat, dev, {q.tokens, q.heads})), (float)as_double(a[7]), w, stride,
+                               (int32_t)heads, stream_of(dev));
+    });
+}
+
+// evict_select(ctx, device, descriptor, weights, m, keep_first, keep_last, kept, new_lens)
+PyObject* evict_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 9, [&]() -> long {
+        const int dev = as_int(a[1], "device");
+        const Descriptor d(a[2]);
+        int64_t heads, stride;
+        const float* w = weight_rows(a[3], "weights", dev, d.kv->batch, heads, stride);
+        const int m = as_int(a[4], "m");
+        void* kept = contiguous_data(a[7], "kept", at::kInt, dev, {d.kv->batch, heads, m > 1 ? m : 1});
+        void* lens = contiguous_data(a[8], "new_lens", at::kInt, dev, {d.kv->batch});
+        return f_evict_select(context(a[0]), d.kv, w, stride, (int32_t)heads, m, as_int(a[5], "keep_first"), as_int(a[6], "keep_last"),
+                              static_cast<int32_t*>(kept), static_cast<int32_t*>(lens), stream_of(dev));
+    });
+}
+
+// kv_gather(ctx, device, descriptor, descriptor or None, kept, counts, weights, weights_out)
+PyObject* kv_gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&]() -> long {
+        const int dev = as_int(a[1], "device");
+        const Descriptor d(a[2]);
+        const Descriptor into(a[3] == Py_None ? a[2] : a[3]);
+        const at::Tensor& kept = required(a[4], "kept", at::kInt, dev);
+        contiguous(kept, "kept");
+        if (kept.dim() != 3 || kept.size(0) != d.kv->batch || kept.size(1) > INT32_MAX || kept.size(2) > INT32_MAX)
+            refuse("kept: [" + std::to_string(d.kv->batch) + ", heads, m] is wanted, got " + shape_text(kept.sizes().data(), kept.dim()));
+        int64_t heads, stride, heads_out, stride_out;
+        const float* w = weight_rows(a[6], "weights", dev, d.kv->batch, heads, stride);
+        float* wo = weight_rows(a[7], "weights_out", dev, d.kv->batch, heads_out, stride_out);
+        if ((w && heads != kept.size(1)) || (wo && heads_out != kept.size(1))) refuse("weights, weights_out: as many heads as kept's are wanted");
+        return f_kv_gather(context(a[0]), d.kv, a[3] == Py_None ? nullptr : into.kv, static_cast<const int32_t*>(kept.data_ptr()),
+                           static_cast<const int32_t*>(contiguous_data(a[5], "counts", at::kInt, dev, {d.kv->batch})), (int32_t)kept.size(2),
+                           (int32_t)kept.size(1), w, stride, wo, stride_out, stream_of(dev));
+    });
+}
+
+// init(sizes of the cache descriptor and the rope plan, addresses of tidal_page_map, kv_write, block_bounds, block_select, block_attn, rope,
+// rope_write, chunk_attn, chunk_weights, evict_select, kv_gather)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 6, [&]() -> long {
-        if (as_long(a[5]) != (long)sizeof(tidal_kv_t)) refuse("the descriptor's size differs from the library's");
-        f_page_map = reinterpret_cast<decltype(f_page_map)>(PyLong_AsVoidPtr(a[0]));
-        f_kv_write = reinterpret_cast<decltype(f_kv_write)>(PyLong_AsVoidPtr(a[1]));
-        f_block_bounds = reinterpret_cast<decltype(f_block_bounds)>(PyLong_AsVoidPtr(a[2]));
-        f_block_select = reinterpret_cast<decltype(f_block_select)>(PyLong_AsVoidPtr(a[3]));
-        f_block_attn = reinterpret_cast<decltype(f_block_attn)>(PyLong_AsVoidPtr(a[4]));
+    return guarded(n, 13, [&]() -> long {
+        if (as_long(a[0]) != (long)sizeof(tidal_kv_t) || as_long(a[1]) != (long)sizeof(tidal_rope_t)) refuse("a descriptor's size differs from the library's");
+        int i = 2;
+        auto take = [&](auto& f) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(PyLong_AsVoidPtr(a[i++])); };
+        take(f_page_map); take(f_kv_write); take(f_block_bounds); take(f_block_select); take(f_block_attn);
+        take(f_rope); take(f_rope_write); take(f_chunk_attn); take(f_chunk_weights); take(f_evict_select); take(f_kv_gather);
         return 0;
     });
 }
 
 #define ENTRY(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(init), ENTRY(page_map), ENTRY(kv_write), ENTRY(block_bounds), ENTRY(block_select), ENTRY(block_attn),
+                         ENTRY(rope), ENTRY(rope_write), ENTRY(chunk_attn), ENTRY(chunk_weights), ENTRY(evict_select), ENTRY(kv_gather),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

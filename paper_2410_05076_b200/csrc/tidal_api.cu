@@ -12,6 +12,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
+#include <type_traits>
 #include <vector>
 #include <new>
 
@@ -19,9 +20,13 @@
 #include "block_attn_kernels.cuh"
 #include "block_kernels.cuh"
 #include "block_select_kernels.cuh"
+#include "chunk_kernels.cuh"
+#include "evict_kernels.cuh"
 #include "page_kernels.cuh"
+#include "rope_kernels.cuh"
 #include "split_select_kernels.cuh"
 #include "topk_kernels.cuh"
+#include "weight_kernels.cuh"
 
 using namespace tidal;
 
@@ -77,6 +82,8 @@ struct tidal_ctx {
     int layer_overlap = 1;                      // layers of a step may stream their inputs while the layer before them finishes
     int select_clusters[17] = {};               // clusters of 1 .. 16 CTAs that are resident together: block selection
     int attn_clusters[17] = {};                 // the same for four-warp CTAs of the block attention
+    int chunk_clusters[2][17] = {};             // and for the chunk attention (16-bit, 8-bit caches)
+    int evict_clusters[17] = {};                // and for the eviction's choice
     int64_t launches = 0;
     // Whole steps are recorded once as CUDA graphs (programmatic dependent launches included) and
     // replayed while every host-visible argument stays the same: one launch per step instead of one
@@ -918,6 +925,114 @@ tidal_status_t launch_block(tidal_ctx* ctx, void (*kernel)(P), const P& p, int g
     return TIDAL_ERR_CUDA;
 }
 
+// ---- chunks of new tokens ------------------------------------------------------------------------------
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder of tensor maps, found once (the library is not linked against the driver).
+EncodeTiled encode_tiled() {
+    static EncodeTiled found = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult how;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &how) != cudaSuccess ||
+            how != cudaDriverEntryPointSuccess) { cudaGetLastError(); f = nullptr; }
+        return (EncodeTiled)f;
+    }();
+    return found;
+}
+
+constexpr int64_t TMA_STRIDE_LIMIT = 1LL << 40;
+
+// A tensor map of `rank` dimensions, element strides from the second on; the innermost box is 128 bytes, swizzled.
+bool tensor_map(CUtensorMap* map, bool bytes, const void* base, int rank, const uint64_t* dims, const int64_t* strides, const uint32_t* box) {
+    EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    cuuint64_t size[5], pitch[4];
+    cuuint32_t block[5], one[5];
+    for (int i = 0; i < rank; ++i) { size[i] = dims[i]; block[i] = box[i]; one[i] = 1; }
+    for (int i = 1; i < rank; ++i) pitch[i - 1] = (cuuint64_t)strides[i - 1] * (bytes ? 1 : 2);
+    return encode(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), size, pitch, block,
+                  one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Maps of a cache's keys (or values): [page or sequence][head][position][channel], boxes of 64 channels (128 codes) by a page's or
+// a tile's positions. A dimension without a stride has one element, whose coordinate is 0 (the multipliers).
+template <typename P>
+bool cache_maps(P& p, const tidal_kv_t* kv, CUtensorMap* k, CUtensorMap* v) {
+    const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3, paged = kv->kv_layout == TIDAL_KV_PAGED;
+    const int64_t outer = paged ? kv->stride_page : kv->stride_b;
+    const int outer_mul = outer > 0, head_mul = kv->stride_head > 0;
+    p.page_mul = p.batch_mul = outer_mul;
+    p.head_mul = head_mul;
+    const uint64_t dims[4] = {HEAD_DIM, (uint64_t)(paged ? TILE : kv->max_ctx_len), head_mul ? (uint64_t)kv->num_kv_heads : 1,
+                              outer_mul ? (uint64_t)(paged ? kv->num_pages : kv->batch) : 1};
+    const int64_t strides[3] = {kv->stride_pos > 0 ? kv->stride_pos : HEAD_DIM, head_mul ? kv->stride_head : HEAD_DIM, outer_mul ? outer : HEAD_DIM};
+    const uint32_t box[4] = {fp8 ? 128u : 64u, (uint32_t)(paged ? TILE : CH_TILE), 1, 1};
+    return tensor_map(k, fp8, kv->k, 4, dims, strides, box) && (!v || tensor_map(v, fp8, kv->v, 4, dims, strides, box));
+}
+
+bool query_map(CUtensorMap* map, const void* q, int num_tokens, int heads, int64_t stride, int group, int tokens) {
+    const uint64_t dims[3] = {HEAD_DIM, (uint64_t)heads, (uint64_t)num_tokens};
+    const int64_t strides[2] = {HEAD_DIM, num_tokens > 1 ? stride : (int64_t)heads * HEAD_DIM};
+    const uint32_t box[3] = {64, (uint32_t)group, (uint32_t)tokens};
+    return tensor_map(map, false, q, 3, dims, strides, box);
+}
+
+tidal_status_t check_chunk(const tidal_kv_t* kv, int32_t num_tokens, const void* q, int64_t q_stride, const int32_t* q_offsets, int32_t max_new,
+                           int32_t window) {
+    const tidal_status_t rc = check_kv(kv);
+    if (rc != TIDAL_OK) return rc;
+    if (num_tokens < 0 || max_new < 0 || window < 0) return TIDAL_ERR_INVALID;
+    if (num_tokens == 0) return TIDAL_OK;
+    if (!q || !q_offsets || ((uintptr_t)q & 15) || (q_stride & 7)) return TIDAL_ERR_INVALID;
+    if (num_tokens > 1 && q_stride < (int64_t)kv->num_q_heads * HEAD_DIM) return TIDAL_ERR_INVALID;
+    if (kv->kv_layout == TIDAL_KV_PAGED && kv->stride_pos < HEAD_DIM) return TIDAL_ERR_INVALID;
+    const int64_t esz = kv->kv_dtype == TIDAL_KV_FP8_E4M3 ? 1 : 2;
+    for (int64_t stride : {kv->stride_b, kv->stride_pos, kv->stride_head, kv->stride_page})
+        if (stride >= TMA_STRIDE_LIMIT / esz) return TIDAL_ERR_UNSUPPORTED;
+    return q_stride < TMA_STRIDE_LIMIT / 2 ? TIDAL_OK : TIDAL_ERR_UNSUPPORTED;
+}
+
+// Launch as launch_block does, with tensor maps as further arguments.
+template <typename... Args>
+tidal_status_t launch_maps(tidal_ctx* ctx, void (*kernel)(Args...), int grid, int threads, size_t smem, int cluster, cudaStream_t st, const Args&... args) {
+    cudaLaunchConfig_t cfg;
+    std::memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(grid, 1, 1);
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    ctx->launches++;
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess) return TIDAL_OK;
+    cudaGetLastError();
+    return TIDAL_ERR_CUDA;
+}
+
+bool prepare_prompt_kernels(tidal_ctx* ctx) {
+    auto wide = [](const void* k) { return cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess; };
+    auto room = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess; };
+    if (!(wide((const void*)chunk_attn_kernel<false>) && wide((const void*)chunk_attn_kernel<true>) && wide((const void*)evict_select_kernel) &&
+          room(chunk_attn_kernel<false>, ch_smem<false>()) && room(chunk_attn_kernel<true>, ch_smem<true>()) &&
+          room(chunk_weights_kernel<false>, cw_smem(false)) && room(chunk_weights_kernel<true>, cw_smem(true)) && room(evict_select_kernel, EV_SMEM_MAX)))
+        return false;
+    // the softmax warpgroups raise their registers within what the launch holds
+    cudaFuncAttributes a;
+    if (cudaFuncGetAttributes(&a, chunk_attn_kernel<false>) != cudaSuccess || a.numRegs * CH_THREADS < 256 * 216 + 128 * 72) return false;
+    if (cudaFuncGetAttributes(&a, chunk_attn_kernel<true>) != cudaSuccess || a.numRegs * CH_THREADS8 < 256 * 200 + 256 * 56) return false;
+    count_clusters(chunk_attn_kernel<false>, CH_THREADS, ch_smem<false>(), ctx->chunk_clusters[0]);
+    count_clusters(chunk_attn_kernel<true>, CH_THREADS8, ch_smem<true>(), ctx->chunk_clusters[1]);
+    count_clusters(evict_select_kernel, EV_THREADS, EV_SMEM_MAX / 2, ctx->evict_clusters);
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -962,6 +1077,7 @@ tidal_status_t tidal_create(tidal_ctx_t** out, int device, size_t workspace_byte
     const bool compact_ok = cudaFuncSetAttribute(topk_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)compact_smem) == cudaSuccess;
     if (!prepare_block_kernels()) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     if (d0 <= 0 || d1 <= 0 || d2 < d1 || s0 <= 0 || s1 < s0 || e0 < d0 || e1 < d1 || e2 < s0 || !topk_ok || !compact_ok || !split_ok) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
+    if (!prepare_prompt_kernels(ctx)) { cudaGetLastError(); delete ctx; return TIDAL_ERR_CUDA; }
     count_clusters(block_select_kernel<0, false>, SC_THREADS, sc_smem(SC_MAX_BLOCKS, 1, 0), ctx->select_clusters);
     count_clusters(block_attn_kernel<false, 4>, 128, ba_smem<false>(MAX_GROUP, BA_MAX_CLUSTER, 4), ctx->attn_clusters);
     ctx->dense_slots = std::min(d0, d1);
@@ -1376,11 +1492,12 @@ tidal_status_t tidal_device_status(tidal_ctx_t* ctx, void* stream) {
     if (cudaMemcpy(&word, ctx->status, sizeof word, cudaMemcpyDeviceToHost) != cudaSuccess) return TIDAL_ERR_CUDA;
     if (word == 0) return TIDAL_OK;
     // one kind of trouble per call; the others wait for the next
-    const int told = word & STATUS_SPLIT_OVERFLOW ? STATUS_SPLIT_OVERFLOW : word & STATUS_NO_PAGES ? STATUS_NO_PAGES : word;
+    const int told = word & STATUS_SPLIT_OVERFLOW ? STATUS_SPLIT_OVERFLOW : word & STATUS_WAITED_OUT ? STATUS_WAITED_OUT :
+                     word & STATUS_NO_PAGES ? STATUS_NO_PAGES : word;
     const int rest = word & ~told;
     if (cudaMemcpyAsync(ctx->status, &rest, sizeof rest, cudaMemcpyHostToDevice, st) != cudaSuccess ||
         cudaStreamSynchronize(st) != cudaSuccess) return TIDAL_ERR_CUDA;
-    return told == STATUS_SPLIT_OVERFLOW ? TIDAL_ERR_INTERNAL : told == STATUS_NO_PAGES ? TIDAL_ERR_PAGES : TIDAL_ERR_INDEX;
+    return told == STATUS_SPLIT_OVERFLOW ? TIDAL_ERR_INTERNAL : told == STATUS_WAITED_OUT ? TIDAL_ERR_TIMEOUT : told == STATUS_NO_PAGES ? TIDAL_ERR_PAGES : TIDAL_ERR_INDEX;
 }
 
 
@@ -1583,6 +1700,264 @@ tidal_status_t tidal_block_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, const vo
                       ba_over_ring<true>);
     return launch(block_attn_kernel<false, 8>, block_attn_kernel<false, 4>, block_attn_kernel<false, 2>, block_attn_kernel<false, 1>, ba_smem<false>,
                   ba_over_ring<false>);
+}
+
+// ---- a prompt's way into the cache: norms and rotary positions, chunk attention, eviction ----------------
+tidal_status_t tidal_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double low, double high,
+                                      double trained_len, double* inv_freq, double* cos_scale) {
+    if (!inv_freq || !cos_scale || rotary_dim <= 0 || !(base > 1.0) || std::isinf(base)) return TIDAL_ERR_INVALID;
+    if (rotary_dim > HEAD_DIM || rotary_dim % 16) return TIDAL_ERR_UNSUPPORTED;
+    if (scaling < TIDAL_ROPE_PLAIN || scaling > TIDAL_ROPE_RAMP) return TIDAL_ERR_INVALID;
+    if (scaling != TIDAL_ROPE_PLAIN && (!(factor >= 1.0) || std::isinf(factor))) return TIDAL_ERR_INVALID;
+    if (scaling >= TIDAL_ROPE_BANDS && (!(low > 0.0) || !(high > low) || std::isinf(high) || !(trained_len > 0.0) || std::isinf(trained_len))) return TIDAL_ERR_INVALID;
+    const double n = rotary_dim, turn = 6.283185307179586476925;
+    if (scaling == TIDAL_ROPE_BASE) base *= std::pow(factor, n / (n - 2.0));
+    const double lo = std::max(std::floor(n * std::log(trained_len / (turn * high)) / (2.0 * std::log(base))), 0.0);
+    const double hi = std::min(std::ceil(n * std::log(trained_len / (turn * low)) / (2.0 * std::log(base))), n - 1.0);
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / n);
+        if (scaling == TIDAL_ROPE_LINEAR) f /= factor;
+        if (scaling == TIDAL_ROPE_BANDS) {
+            const double s = std::min(std::max((trained_len * f / turn - low) / (high - low), 0.0), 1.0);
+            f = (1.0 - s) * f / factor + s * f;
+        }
+        if (scaling == TIDAL_ROPE_RAMP) {
+            const double r = std::min(std::max((i - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+            f = r * f / factor + (1.0 - r) * f;
+        }
+        inv_freq[i] = f;
+    }
+    *cos_scale = scaling == TIDAL_ROPE_RAMP ? 0.1 * std::log(factor) + 1.0 : 1.0;
+    return TIDAL_OK;
+}
+
+tidal_status_t tidal_rope_init(tidal_rope_t* rope, int32_t rotary_dim, int32_t layout, const double* inv_freq, double cos_scale) {
+    if (!rope || !inv_freq || rotary_dim <= 0 || !std::isfinite(cos_scale)) return TIDAL_ERR_INVALID;
+    if (layout != TIDAL_ROPE_HALF && layout != TIDAL_ROPE_INTERLEAVED) return TIDAL_ERR_INVALID;
+    if (rotary_dim > HEAD_DIM || rotary_dim % 16) return TIDAL_ERR_UNSUPPORTED;
+    for (int i = 0; i < rotary_dim / 2; ++i)
+        if (!std::isfinite(inv_freq[i])) return TIDAL_ERR_INVALID;
+    std::memset(rope, 0, sizeof *rope);
+    rope->rotary_dim = rotary_dim; rope->layout = layout; rope->scale = (float)cos_scale;
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        // the fraction of a turn in 64 bits, in long double: a double's 53 would be off by 2^-22 of a turn at position 2^31
+        const long double t = (long double)inv_freq[i] / 6.283185307179586476925286766559L;
+        long double part = t - std::floor(t);
+        part = std::floor(part * 18446744073709551616.0L + 0.5L);
+        rope->step[i] = part >= 18446744073709551616.0L ? 0 : (uint64_t)part;
+    }
+    return TIDAL_OK;
+}
+
+static tidal_status_t check_rope(const tidal_rope_t* rope, int32_t num_tokens, float eps, const void* q_weight, const void* k_weight) {
+    if (!rope || num_tokens < 0 || !(eps >= 0.f) || std::isinf(eps)) return TIDAL_ERR_INVALID;
+    if (rope->rotary_dim <= 0 || rope->rotary_dim > HEAD_DIM || rope->rotary_dim % 16) return TIDAL_ERR_INVALID;
+    if (rope->layout != TIDAL_ROPE_HALF && rope->layout != TIDAL_ROPE_INTERLEAVED) return TIDAL_ERR_INVALID;
+    return (((uintptr_t)q_weight | (uintptr_t)k_weight) & 15) ? TIDAL_ERR_INVALID : TIDAL_OK;
+}
+// Rows of `heads` heads per token: in place, or apart from each other.
+static bool rope_rows_ok(const void* x, int64_t stride, int heads, int32_t num_tokens) {
+    if (!x || ((uintptr_t)x & 15) || (stride & 7)) return false;
+    return num_tokens <= 1 || stride >= (int64_t)heads * HEAD_DIM;
+}
+
+static tidal_status_t run_rope(tidal_ctx_t* ctx, RopeParams& p, int mode, cudaStream_t st) {
+    const int pairs = (p.Hq + 1) / 2 + (mode == ROPE_BACK ? 1 : 2) * ((p.Hkv + 1) / 2);
+    // A warp per token where there are tokens enough to fill the GPU; for fewer, several warps with a share of the rows each.
+    const long long fill = 16LL * ctx->sm_count;
+    p.parts = (int)std::max(1LL, std::min<long long>((pairs + 1) / 2, fill / std::max(p.num_tokens, 1)));
+    const long long grid = ((long long)p.num_tokens * p.parts + RO_WARPS - 1) / RO_WARPS;
+    if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    const bool half = p.rope.layout == TIDAL_ROPE_HALF, norm = p.q_weight || p.k_weight;
+    auto launch = [&](auto h, auto n) {
+        constexpr bool H = decltype(h)::value, N = decltype(n)::value;
+        return launch_block(ctx, mode == ROPE_BACK ? rope_kernel<H, N, ROPE_BACK> : mode == ROPE_CACHE ? rope_kernel<H, N, ROPE_CACHE> : rope_kernel<H, N, ROPE_CACHE8>,
+                            p, (int)grid, RO_WARPS * 32, 0, 0, st);
+    };
+    using T = std::integral_constant<bool, true>;
+    using F = std::integral_constant<bool, false>;
+    return half ? (norm ? launch(T(), T()) : launch(T(), F())) : (norm ? launch(F(), T()) : launch(F(), F()));
+}
+
+tidal_status_t tidal_rope(tidal_ctx_t* ctx, const tidal_rope_t* rope, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads,
+                          const void* q, int64_t q_stride, const void* k, int64_t k_stride, const int32_t* positions,
+                          const void* q_weight, const void* k_weight, float eps, void* q_out, int64_t q_out_stride, void* k_out,
+                          int64_t k_out_stride, void* stream) {
+    if (!ctx || num_q_heads < 0 || num_kv_heads < 0 || num_q_heads + (int64_t)num_kv_heads == 0) return TIDAL_ERR_INVALID;
+    const tidal_status_t rc = check_rope(rope, num_tokens, eps, q_weight, k_weight);
+    if (rc != TIDAL_OK) return rc;
+    if (num_q_heads > 65535 || num_kv_heads > 65535) return TIDAL_ERR_UNSUPPORTED;
+    if (num_tokens == 0) return TIDAL_OK;
+    if (!positions) return TIDAL_ERR_INVALID;
+    if (num_q_heads ? !rope_rows_ok(q, q_stride, num_q_heads, num_tokens) || !rope_rows_ok(q_out, q_out_stride, num_q_heads, num_tokens) : q || q_out) return TIDAL_ERR_INVALID;
+    if (num_kv_heads ? !rope_rows_ok(k, k_stride, num_kv_heads, num_tokens) || !rope_rows_ok(k_out, k_out_stride, num_kv_heads, num_tokens) : k || k_out) return TIDAL_ERR_INVALID;
+    if (num_tokens > 1 && ((q && q == q_out && q_stride != q_out_stride) || (k && k == k_out && k_stride != k_out_stride))) return TIDAL_ERR_INVALID;
+    RopeParams p;
+    std::memset(&p, 0, sizeof p);
+    p.rope = *rope;
+    p.q = (const __nv_bfloat16*)q; p.k = (const __nv_bfloat16*)k; p.q_stride = q_stride; p.k_stride = k_stride;
+    p.q_out = (__nv_bfloat16*)q_out; p.k_out = (__nv_bfloat16*)k_out; p.qo_stride = q_out_stride; p.ko_stride = k_out_stride;
+    p.positions = positions; p.q_weight = (const __nv_bfloat16*)q_weight; p.k_weight = (const __nv_bfloat16*)k_weight; p.eps = eps;
+    p.num_tokens = num_tokens; p.Hq = num_q_heads; p.Hkv = num_kv_heads; p.status = ctx->status;
+    return run_rope(ctx, p, ROPE_BACK, (cudaStream_t)stream);
+}
+
+tidal_status_t tidal_rope_write(tidal_ctx_t* ctx, const tidal_rope_t* rope, const tidal_kv_t* kv, int32_t num_tokens, const void* q,
+                                int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                                const int32_t* positions, const int64_t* slots, const void* q_weight, const void* k_weight, float eps,
+                                void* q_out, int64_t q_out_stride, void* stream) {
+    if (!ctx) return TIDAL_ERR_INVALID;
+    tidal_status_t rc = check_kv(kv);
+    if (rc != TIDAL_OK || (rc = check_rope(rope, num_tokens, eps, q_weight, k_weight)) != TIDAL_OK) return rc;
+    if (num_tokens == 0) return TIDAL_OK;
+    if (!positions || !slots || !q != !q_out) return TIDAL_ERR_INVALID;
+    if (!rope_rows_ok(k_new, k_stride, kv->num_kv_heads, num_tokens) || !rope_rows_ok(v_new, v_stride, kv->num_kv_heads, num_tokens)) return TIDAL_ERR_INVALID;
+    if (q && (!rope_rows_ok(q, q_stride, kv->num_q_heads, num_tokens) || !rope_rows_ok(q_out, q_out_stride, kv->num_q_heads, num_tokens))) return TIDAL_ERR_INVALID;
+    if (num_tokens > 1 && q && q == q_out && q_stride != q_out_stride) return TIDAL_ERR_INVALID;
+    RopeParams p;
+    std::memset(&p, 0, sizeof p);
+    p.rope = *rope;
+    p.q = (const __nv_bfloat16*)q; p.k = (const __nv_bfloat16*)k_new; p.v = (const __nv_bfloat16*)v_new;
+    p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride;
+    p.q_out = (__nv_bfloat16*)q_out; p.qo_stride = q_out_stride;
+    p.positions = positions; p.q_weight = (const __nv_bfloat16*)q_weight; p.k_weight = (const __nv_bfloat16*)k_weight; p.eps = eps;
+    p.num_tokens = num_tokens; p.Hq = q ? kv->num_q_heads : 0; p.Hkv = kv->num_kv_heads;
+    p.ck = (uint8_t*)const_cast<void*>(kv->k); p.cv = (uint8_t*)const_cast<void*>(kv->v);
+    p.slots = (const long long*)slots; p.paged = kv->kv_layout == TIDAL_KV_PAGED; p.max_ctx = kv->max_ctx_len;
+    p.num_slots = p.paged ? (long long)kv->num_pages * TILE : (long long)kv->batch * kv->max_ctx_len;
+    p.stride_b = kv->stride_b; p.stride_pos = kv->stride_pos; p.stride_head = kv->stride_head; p.stride_page = kv->stride_page;
+    p.k_scale = kv->k_scale; p.v_scale = kv->v_scale; p.status = ctx->status;
+    return run_rope(ctx, p, kv->kv_dtype == TIDAL_KV_FP8_E4M3 ? ROPE_CACHE8 : ROPE_CACHE, (cudaStream_t)stream);
+}
+
+tidal_status_t tidal_chunk_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t num_tokens, const void* q, int64_t q_stride,
+                                const int32_t* q_offsets, int32_t max_new, int32_t causal, int32_t window, float* out, float* lse,
+                                void* stream) {
+    if (!ctx) return TIDAL_ERR_INVALID;
+    const tidal_status_t rc = check_chunk(kv, num_tokens, q, q_stride, q_offsets, max_new, window);
+    if (rc != TIDAL_OK) return rc;
+    if (num_tokens == 0) return TIDAL_OK;
+    if (!out || ((uintptr_t)out & 15) || ((uintptr_t)lse & 3)) return TIDAL_ERR_INVALID;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    ChunkParams p;
+    std::memset(&p, 0, sizeof p);
+    fill_block_cache(p.c, ctx, kv, 0);
+    p.q_offsets = q_offsets; p.num_tokens = num_tokens; p.tile_tokens = CH_TILE / p.c.G;
+    p.causal = causal != 0; p.window = window;
+    p.scale_log2 = (kv->sm_scale > 0.f ? kv->sm_scale : 1.0f / std::sqrt((float)kv->head_dim)) * 1.4426950408889634f;
+    const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3;
+    if (fp8) { p.k_scale = kv->k_scale; p.v_scale = kv->v_scale; }
+    p.out = out; p.out_bf16 = ctx->out_bf16; p.lse = lse;
+    CUtensorMap qm, km, vm;
+    if (!cache_maps(p, kv, &km, &vm) || !query_map(&qm, q, num_tokens, kv->num_q_heads, q_stride, p.c.G, p.tile_tokens)) return TIDAL_ERR_CUDA;
+    // CTA tiles of all sequences: a sequence's last one may be partly filled
+    const long long per = 2 * p.tile_tokens;
+    long long tiles = num_tokens / per + std::min(kv->batch, num_tokens);
+    if (max_new > 0) tiles = std::min(tiles, kv->batch * ((max_new + per - 1) / per));
+    const long long units = tiles * kv->num_kv_heads;
+    // Few rows: the cache is cut over the CTAs of a cluster, as long as all of them run at once and have two tiles of positions each.
+    const int seen = window > 0 ? (int)std::min<long long>(kv->max_ctx_len, (long long)window + per) : kv->max_ctx_len;
+    int ranks = 1;
+    while (ranks < 16 && units * ranks * 2 <= ctx->sm_count && seen >= ranks * 2 * 2 * CH_TILE && ctx->chunk_clusters[fp8][ranks * 2] >= units) ranks *= 2;
+    if (units * ranks > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    return fp8 ? launch_maps(ctx, chunk_attn_kernel<true>, (int)(units * ranks), CH_THREADS8, ch_smem<true>(), ranks, (cudaStream_t)stream, p, qm, km, vm)
+               : launch_maps(ctx, chunk_attn_kernel<false>, (int)(units * ranks), CH_THREADS, ch_smem<false>(), ranks, (cudaStream_t)stream, p, qm, km, vm);
+}
+
+tidal_status_t tidal_chunk_weights(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t num_tokens, const void* q, int64_t q_stride,
+                                   const int32_t* q_offsets, int32_t max_new, int32_t causal, int32_t window, int32_t last,
+                                   const float* lse, float decay, float* weights, int64_t stride, int32_t num_weight_heads, void* stream) {
+    if (!ctx) return TIDAL_ERR_INVALID;
+    const tidal_status_t rc = check_chunk(kv, num_tokens, q, q_stride, q_offsets, max_new, window);
+    if (rc != TIDAL_OK) return rc;
+    if (last < 0 || !weights || ((uintptr_t)weights & 3) || stride < kv->max_ctx_len || !std::isfinite(decay)) return TIDAL_ERR_INVALID;
+    if (num_weight_heads != kv->num_kv_heads && num_weight_heads != 1) return TIDAL_ERR_INVALID;
+    if (num_tokens == 0) return TIDAL_OK;
+    if (!lse || ((uintptr_t)lse & 3)) return TIDAL_ERR_INVALID;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    WeightParams p;
+    std::memset(&p, 0, sizeof p);
+    fill_block_cache(p.c, ctx, kv, 0);
+    p.q_offsets = q_offsets; p.num_tokens = num_tokens;
+    int most = max_new > 0 ? std::min(max_new, num_tokens) : num_tokens;
+    if (last > 0) most = std::min(most, last);
+    p.tile_tokens = std::min(CH_TILE / p.c.G, most);
+    p.causal = causal != 0; p.window = window; p.last = last;
+    p.scale_log2 = (kv->sm_scale > 0.f ? kv->sm_scale : 1.0f / std::sqrt((float)kv->head_dim)) * 1.4426950408889634f;
+    const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3;
+    if (fp8) p.k_scale = kv->k_scale;
+    p.lse = lse; p.decay = decay; p.weights = weights; p.stride = stride; p.heads = num_weight_heads;
+    CUtensorMap qm, km;
+    if (!cache_maps(p, kv, &km, nullptr) || !query_map(&qm, q, num_tokens, kv->num_q_heads, q_stride, p.c.G, p.tile_tokens)) return TIDAL_ERR_CUDA;
+    const long long tiles = (long long)kv->batch * num_weight_heads * ((kv->max_ctx_len + CH_TILE - 1) / CH_TILE);
+    const int grid = (int)std::min<long long>(ctx->sm_count, tiles);
+    return fp8 ? launch_maps(ctx, chunk_weights_kernel<true>, grid, CW_THREADS8, cw_smem(true), 1, (cudaStream_t)stream, p, qm, km)
+               : launch_maps(ctx, chunk_weights_kernel<false>, grid, CW_THREADS, cw_smem(false), 1, (cudaStream_t)stream, p, qm, km);
+}
+
+tidal_status_t tidal_evict_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const float* weights, int64_t stride, int32_t num_weight_heads,
+                                  int32_t m, int32_t keep_first, int32_t keep_last, int32_t* kept, int32_t* new_lens, void* stream) {
+    if (!ctx) return TIDAL_ERR_INVALID;
+    const tidal_status_t rc = check_kv(kv);
+    if (rc != TIDAL_OK) return rc;
+    if (!weights || ((uintptr_t)weights & 3) || !kept || !new_lens || new_lens == kv->ctx_lens) return TIDAL_ERR_INVALID;
+    if (m <= 0 || m > MAX_CTX || keep_first < 0 || keep_last < 0 || stride < kv->max_ctx_len) return TIDAL_ERR_INVALID;
+    if (num_weight_heads != kv->num_kv_heads && num_weight_heads != 1) return TIDAL_ERR_INVALID;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    EvictParams p;
+    std::memset(&p, 0, sizeof p);
+    p.weights = weights; p.stride = stride; p.ctx_lens = kv->ctx_lens; p.max_ctx = kv->max_ctx_len; p.heads = num_weight_heads;
+    p.m = m; p.keep_first = keep_first; p.keep_last = keep_last; p.kept = kept; p.new_lens = new_lens;
+    const int rows = kv->batch * num_weight_heads;
+    // a cluster holds a row; more CTAs than that needs as long as all run at once and have a few thousand keys each
+    int cluster = 1;
+    while ((size_t)((kv->max_ctx_len + cluster - 1) / cluster) * 4 > EV_SMEM_MAX) cluster *= 2;
+    while (cluster < EV_MAX_CLUSTER && kv->max_ctx_len > cluster * 4096 && rows * cluster * 2 <= ctx->sm_count && ctx->evict_clusters[cluster * 2] >= rows) cluster *= 2;
+    p.slice_max = (kv->max_ctx_len + cluster - 1) / cluster;
+    if ((long long)rows * cluster > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    return launch_block(ctx, evict_select_kernel, p, rows * cluster, EV_THREADS, (size_t)p.slice_max * 4, cluster, (cudaStream_t)stream);
+}
+
+tidal_status_t tidal_kv_gather(tidal_ctx_t* ctx, const tidal_kv_t* kv, const tidal_kv_t* into, const int32_t* kept, const int32_t* counts,
+                               int32_t m, int32_t num_list_heads, const float* weights, int64_t stride, float* weights_out,
+                               int64_t stride_out, void* stream) {
+    if (!ctx) return TIDAL_ERR_INVALID;
+    tidal_status_t rc = check_kv(kv);
+    if (rc != TIDAL_OK || (into && (rc = check_kv(into)) != TIDAL_OK)) return rc;
+    if (!kept || !counts || m <= 0 || m > MAX_CTX) return TIDAL_ERR_INVALID;
+    if (num_list_heads != kv->num_kv_heads && num_list_heads != 1) return TIDAL_ERR_INVALID;
+    const tidal_kv_t* to = into ? into : kv;
+    if (to->batch != kv->batch || to->num_kv_heads != kv->num_kv_heads || to->kv_dtype != kv->kv_dtype) return TIDAL_ERR_INVALID;
+    if (!weights != !weights_out) return TIDAL_ERR_INVALID;
+    if (weights && ((((uintptr_t)weights | (uintptr_t)weights_out) & 3) || stride < kv->max_ctx_len || stride_out < std::min(m, to->max_ctx_len))) return TIDAL_ERR_INVALID;
+    if (weights && weights == weights_out && (into || stride != stride_out)) return TIDAL_ERR_INVALID;
+    DeviceScope dev(ctx->device);
+    if (!dev.ok) return TIDAL_ERR_CUDA;
+    GatherParams p;
+    std::memset(&p, 0, sizeof p);
+    fill_block_cache(p.from, ctx, kv, 0);
+    p.k = (uint8_t*)const_cast<void*>(to->k); p.v = (uint8_t*)const_cast<void*>(to->v);
+    p.stride_b = to->stride_b; p.stride_pos = to->stride_pos; p.stride_head = to->stride_head; p.stride_page = to->stride_page;
+    p.page_table = to->page_table; p.max_pages = to->max_pages_per_seq; p.num_pages = to->num_pages;
+    p.paged = to->kv_layout == TIDAL_KV_PAGED; p.max_ctx = to->max_ctx_len;
+    p.kept = kept; p.counts = counts; p.heads = num_list_heads; p.m = m;
+    const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3;
+    p.row_bytes = HEAD_DIM * (fp8 ? 1 : 2);
+    p.weights = weights; p.weights_out = weights_out; p.w_stride = stride; p.wo_stride = stride_out;
+    if (into) {
+        const long long per = GA_UNROLL * (fp8 ? 2 : 1);
+        const long long grid = ((long long)kv->batch * kv->num_kv_heads * ((m + per - 1) / per) + GA_WARPS - 1) / GA_WARPS;
+        if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+        return launch_block(ctx, fp8 ? gather_copy_kernel<true> : gather_copy_kernel<false>, p, (int)grid, GA_WARPS * 32, 0, 0, (cudaStream_t)stream);
+    }
+    const long long grid = (long long)kv->batch * kv->num_kv_heads * (2 * p.row_bytes / GI_COLUMN) + (weights ? (long long)kv->batch * num_list_heads : 0);
+    if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
+    return launch_block(ctx, gather_inplace_kernel, p, (int)grid, GI_THREADS, 0, 0, (cudaStream_t)stream);
 }
 
 int64_t tidal_launch_count(const tidal_ctx_t* ctx) { return ctx ? ctx->launches : 0; }

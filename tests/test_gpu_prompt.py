@@ -1,0 +1,635 @@
+"""A prompt's way through the cache: rotary positions and norms, chunk attention, attention weights per cached position, eviction;
+against plain definitions in 64 bits."""
+import copy
+import math
+
+import pytest
+import torch
+
+from paper_2410_05076_b200 import binding
+from tests import util
+from tests.test_gpu_blocks import BLK, D, DEV, gen, make, pages
+
+pytestmark = pytest.mark.gpu
+HALF, INTER = binding.ROPE_HALF, binding.ROPE_INTERLEAVED
+
+
+@pytest.fixture(scope="module")
+def td():
+    t = binding.Tidal(0)
+    yield t
+    assert t.device_status() == binding.OK
+    t.close()
+
+
+@pytest.fixture(scope="module")
+def td16():
+    t = binding.Tidal(0)
+    t.set_output_bf16(True)
+    yield t
+    assert t.device_status() == binding.OK
+    t.close()
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, generator=gen(seed), device=DEV).to(torch.bfloat16)
+
+
+# ---- norms and rotary positions ------------------------------------------------------------------------------------
+
+def ref_rope(x, pos, freq, scale, layout, weight, eps):
+    """In 64 bits; angles from integer positions and exact frequencies."""
+    x = x.double()
+    if weight is not None:
+        x = x / torch.sqrt((x * x).mean(-1, keepdim=True) + eps) * weight.double()
+    n = 2 * len(freq)
+    # p f mod 2 pi in two pieces of p, so that a double's 53 bits do for positions up to 2^31
+    f = torch.tensor(freq, dtype=torch.float64, device=DEV)
+    p = pos.double()[:, None]
+    angle = torch.remainder(torch.floor(p / 65536) * torch.remainder(65536 * f, 2 * math.pi), 2 * math.pi) + torch.remainder(p, 65536) * f
+    c, s = torch.cos(angle)[:, None] * scale, torch.sin(angle)[:, None] * scale
+    out = x.clone()
+    a, b = (x[..., : n // 2], x[..., n // 2: n]) if layout == HALF else (x[..., :n:2], x[..., 1:n:2])
+    ra, rb = a * c - b * s, b * c + a * s
+    if layout == HALF:
+        out[..., : n // 2], out[..., n // 2: n] = ra, rb
+    else:
+        out[..., :n:2], out[..., 1:n:2] = ra, rb
+    return out
+
+
+def rope_bound(ref, far):
+    """fp32: the turn is off by 2^-32 + p 2^-65 and rounded to fp32 (2^-25), cosine and sine by 2^-23 (1 ulp and the factor), a product
+    chain of five roundings and the norm's (sum of 128 squares in 8 + 4 additions, rsqrt within 2^-22): 2^-20 of the largest element of a
+    row in all, doubled for the pair; then a rounding to bf16, 2^-8 of the value. The reference's own angle is good to
+    p 2^-52 (its frequencies are doubles, so are the library's)."""
+    return (2.0 ** -19 + far * 2.0 ** -50) * ref.abs().amax(-1, keepdim=True) + 2.0 ** -8 * ref.abs() + 2.0 ** -120
+
+
+def rope_inputs(T, hq, hkv, far, seed=0):
+    qkv = randn(seed, T, hq + 2 * hkv, D)
+    pos = torch.randint(0, far, (T,), generator=gen(seed + 1), device=DEV).to(torch.int32)
+    if T > 1:
+        pos[0], pos[-1] = 0, far - 1
+    return qkv[:, :hq], qkv[:, hq: hq + hkv], qkv[:, hq + hkv:], pos
+
+
+def frequencies(n, base=10000.0):
+    return [base ** (-2 * i / n) for i in range(n // 2)]
+
+
+@pytest.mark.parametrize("layout", [HALF, INTER])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("T,hq,hkv,rotary,far", [(1, 1, 1, 128, 2 ** 31 - 1), (3, 7, 1, 16, 100), (64, 32, 8, 128, 262144), (17, 15, 5, 96, 2 ** 24 + 5),
+                                                 (1000, 8, 2, 64, 131072), (7000, 4, 4, 112, 7000)])
+def test_rope(td, layout, norm, T, hq, hkv, rotary, far):
+    q, k, _, pos = rope_inputs(T, hq, hkv, far, seed=T)
+    qw, kw = (1 + 0.3 * randn(1, D), 1 - 0.3 * randn(2, D)) if norm else (None, None)
+    plan = binding.rope_plan(rotary, layout=layout)
+    qo, ko = util.Guarded((T, hq, D), torch.bfloat16, DEV), util.Guarded((T, hkv, D), torch.bfloat16, DEV)
+    got = td.rope(plan, q, k, pos, qw, kw, 1e-5, qo.t, ko.t)
+    assert got[0] is qo.t and got[1] is ko.t
+    for x, y, w in ((q, qo, qw), (k, ko, kw)):
+        ref = ref_rope(x, pos, frequencies(rotary), 1.0, layout, w, 1e-5)
+        assert ((y.t.double() - ref).abs() <= rope_bound(ref, far)).all(), float(((y.t.double() - ref).abs() - rope_bound(ref, far)).max())
+        y.check("rope")
+    if not norm:
+        assert torch.equal(qo.t[..., rotary:], q[..., rotary:])          # channels that do not turn are copied
+    # one weight only, one tensor only
+    only = td.rope(plan, q, None, pos, qw, None, 1e-5)
+    assert only[1] is None and torch.equal(only[0], qo.t)
+    assert torch.equal(td.rope(plan, None, k, pos, None, kw, 1e-5)[1], ko.t)
+    # in place, in the projection's output
+    td.rope(plan, q, k, pos, qw, kw, 1e-5, q, k)
+    assert torch.equal(q, qo.t) and torch.equal(k, ko.t)
+    assert td.device_status() == binding.OK
+
+
+@pytest.mark.parametrize("scaling,factor,low,high,trained", [(binding.ROPE_PLAIN, 1, 1, 4, 1), (binding.ROPE_LINEAR, 4, 1, 4, 1), (binding.ROPE_BASE, 8, 1, 4, 1),
+                                                             (binding.ROPE_BANDS, 8, 1, 4, 8192), (binding.ROPE_RAMP, 16, 1, 32, 4096)])
+def test_rope_scalings_on_the_device(td, scaling, factor, low, high, trained):
+    q, k, _, pos = rope_inputs(50, 4, 2, 131072)
+    plan = binding.rope_plan(128, base=500000.0, scaling=scaling, factor=factor, low=low, high=high, trained_len=trained)
+    freq = [int(plan.step[i]) * 2.0 ** -64 * 2 * math.pi for i in range(64)]
+    qo, _ = td.rope(plan, q, k, pos)
+    ref = ref_rope(q, pos, freq, plan.scale, HALF, None, 0)
+    assert ((qo.double() - ref).abs() <= rope_bound(ref, 131072)).all()
+
+
+def test_rope_leaves_padding_and_keeps_odd_values_apart(td):
+    """Negative positions are left unwritten; an infinity meets the other channel of its pair and no other."""
+    q, k, _, pos = rope_inputs(40, 3, 1, 1000)
+    pos[::3] = -1
+    pos[1] = -2 ** 31
+    q[2, 0, 100] = math.inf
+    q[4, 1, 3] = math.nan
+    for layout in (HALF, INTER):
+        plan = binding.rope_plan(64, layout=layout)
+        qo, ko = torch.full((40, 3, D), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((40, 1, D), 7.0, dtype=torch.bfloat16, device=DEV)
+        td.rope(plan, q, k, pos, q_out=qo, k_out=ko)
+        assert (qo[pos < 0] == 7).all() and (ko[pos < 0] == 7).all() and (ko[pos >= 0] != 7).any()
+        assert qo[2, 0, 100] == math.inf and int((~torch.isfinite(qo[2])).sum()) == 1       # a channel that does not turn
+        assert int((~torch.isfinite(qo[4])).sum()) == 2
+
+
+def ref_code(x):
+    """The E4M3 value nearest to x (64 bits) is within half a step: 2^-4 of the value, 2^-10 near zero."""
+    return 2.0 ** -4 * x.abs() + 2.0 ** -10
+
+
+@pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,hq,hkv,rotary,norm", [(1, 4, 1, 128, True), (37, 10, 5, 64, False), (300, 32, 8, 128, True)])
+def test_rope_write(td, layout, fp8, T, hq, hkv, rotary, norm):
+    rows = pages(T + 5) * BLK
+    lay = make([rows], hq, hkv, layout, fp8, seed=5)
+    q, k, v, pos = rope_inputs(T, hq, hkv, 131072, seed=T)
+    qw, kw = (1 + 0.3 * randn(1, D), 1 - 0.3 * randn(2, D)) if norm else (None, None)
+    at = torch.randperm(rows, generator=gen(9), device=DEV)[:T]
+    slots = lay.page_table[0, at // BLK].long() * BLK + at % BLK if layout == "paged" else at
+    slots, pos = slots.clone(), pos.clone()
+    if T > 3:
+        slots[1], pos[2] = -1, -1                         # no row in the cache; no token
+    before = [x.clone().view(torch.uint8) for x in lay.keep]
+    plan = binding.rope_plan(rotary, base=500000.0, layout=HALF)
+    qo = torch.full((T, hq, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    assert td.rope_write(lay, plan, q, k, v, pos, slots, qw, kw, 1e-6, qo) is qo
+    same, _ = td.rope(plan, q, None, pos, qw, None, 1e-6, torch.full_like(qo, 7.0))
+    assert torch.equal(qo, same)
+    written = (slots >= 0) & (pos >= 0)
+    ref = ref_rope(k, pos, frequencies(rotary, 500000.0), 1.0, HALF, kw, 1e-6)
+
+    def row(x, i):
+        a = int(at[i])
+        return x[int(lay.page_table[0, a // BLK]), :, a % BLK] if layout == "paged" else x[0, :, a] if layout == "hnd" else x[0, a]
+
+    for i in range(T):
+        if not written[i]:
+            continue
+        kk, vv = row(lay.k, i).float().double(), row(lay.v, i)
+        if fp8:
+            x = ref[i] / lay.k_scale.double()[:, None]
+            bound = ref_code(x) + 1.1 * (2.0 ** -19 + 2.0 ** -33) * x.abs().amax(-1, keepdim=True)
+            assert ((kk - x.clamp(-448, 448)).abs() <= bound).all()
+            want = (v[i].float() / lay.v_scale[:, None]).clamp(-448, 448).to(torch.float8_e4m3fn)
+            assert torch.equal(vv.view(torch.uint8), want.view(torch.uint8))
+        else:
+            assert ((kk - ref[i]).abs() <= rope_bound(ref[i], 131072)).all()
+            assert torch.equal(vv, v[i])
+    # everything else is as it was
+    gone = [x.clone() for x in before]
+    for x, b in zip(lay.keep, gone):
+        now, old = x.view(torch.uint8).view(b.shape), b
+        changed = (now != old).nonzero()
+        assert changed.shape[0] <= int(written.sum()) * hkv * D * 2 * (1 if fp8 else 2)
+    assert td.device_status() == binding.OK
+    # without queries the cache gets the same
+    after = [x.clone().view(torch.uint8) for x in lay.keep]
+    assert td.rope_write(lay, plan, None, k, v, pos, slots, None, kw, 1e-6) is None
+    assert all(torch.equal(x.view(torch.uint8), a) for x, a in zip(lay.keep, after))
+
+
+def test_rope_write_equals_rope_and_kv_write(td):
+    """16 bits: the same rows as in two calls; slots outside the cache are skipped and reported."""
+    one, two = make([64], 8, 2, seed=1), make([64], 8, 2, seed=1)
+    q, k, v, pos = rope_inputs(30, 8, 2, 5000)
+    slots = one.page_table[0, torch.arange(30, device=DEV) // BLK].long() * BLK + torch.arange(30, device=DEV) % BLK
+    plan = binding.rope_plan(128)
+    td.rope_write(one, plan, q, k, v, pos, slots)
+    _, turned = td.rope(plan, None, k, pos)
+    td.kv_write(two, turned, v, slots)
+    a, b = one.keep[0].view(torch.int16), two.keep[0].view(torch.int16)
+    assert torch.equal(a, b)
+    slots[3], slots[4] = one.num_pages * BLK, -2
+    td.rope_write(one, plan, q, k, v, pos, slots)
+    assert torch.equal(one.keep[0].view(torch.int16), a)
+    assert td.device_status() == binding.ERR_INDEX and td.device_status() == binding.OK
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -70, 2.0 ** 70, 0.01])
+def test_rope_write_saturates(td, scale):
+    lay = make([16], 1, 1, "hnd", True)
+    lay.k_scale.fill_(scale)
+    k = torch.full((1, 1, D), 3.0, dtype=torch.bfloat16, device=DEV)
+    k[0, 0, 1] = math.nan
+    td.rope_write(lay, binding.rope_plan(16), None, k, k, i32([0]), torch.tensor([2], device=DEV))
+    want = min(3.0 / scale, 448.0)
+    got = lay.k[0, 0, 2].float()
+    assert torch.isnan(got[1]) and got[0] == torch.tensor(want).to(torch.float8_e4m3fn).float() and got[100] == got[0]
+
+
+# ---- chunk attention ---------------------------------------------------------------------------------------------------
+
+def chunk_inputs(lay, new, seed=0, extra=0):
+    T = sum(new)
+    q = randn(500 + seed, T + extra, lay.num_q_heads + 2 * lay.num_kv_heads, D)[:, : lay.num_q_heads]
+    return q, i32([sum(new[:i]) for i in range(len(new) + 1)])
+
+
+def ref_chunk(lay, q, new, causal=True, window=0, skip=()):
+    """(out, lse, weights, bounds of the three): softmax over what each row sees, in 64 bits. Bounds: a logit's 8 matrix instructions add exact
+    products with at most 2^-22 of the sum of their magnitudes each (2^-19), the exponent's argument is rounded twice (2^-23 of |t|
+    log2 e), exponentials are within 2^-21, the sum of n weights (in chains of at most n / 2, of tiles) within 2^-17: together e. Weights enter
+    the second product as bf16, off by 2^-8 each (fp16: 2^-11, and the running maximum may stand 2^8 below, so that
+    weights below 2^-14 of it are off by 2^-25; the query in fp16 by 2^-25 per channel). An error r of all weights moves the mean by r max|v|."""
+    B, hq, hkv = lay.batch, lay.num_q_heads, lay.num_kv_heads
+    G, scale, fp8 = hq // hkv, lay.sm_scale or 1 / math.sqrt(D), bool(lay.kv_dtype)
+    T = sum(new)
+    out, lse = torch.zeros(T, hq, D, dtype=torch.float64, device=DEV), torch.full((T, hq), -math.inf, dtype=torch.float64, device=DEV)
+    w = torch.zeros(B, hkv, lay.max_ctx_len, dtype=torch.float64, device=DEV)
+    tol_o, tol_l, tol_w = torch.zeros(T, hq, 1, dtype=torch.float64, device=DEV), torch.zeros_like(lse), torch.zeros_like(w)
+    at = 0
+    for b, n in enumerate(new):
+        k, v = lay.dense[b]
+        N = k.shape[1]
+        if n == 0:
+            continue
+        pos = N - n + torch.arange(n, device=DEV)
+        j = torch.arange(N, device=DEV)
+        seen = torch.ones(n, N, dtype=torch.bool, device=DEV)
+        if causal:
+            seen &= j[None] <= pos[:, None]
+        if window:
+            seen &= j[None] > pos[:, None] - window
+        for pg in skip:
+            seen &= (j // BLK != pg)[None]
+        for h in range(hq):
+            g = h // G
+            qq = q[at: at + n, h].double()
+            t = (qq @ k[g].t()) * scale
+            mag = (qq.abs() @ k[g].abs().t()).amax(-1) * scale
+            e = 2.0 ** -19 * mag + 2.0 ** -22 * t.abs().amax(-1) + 2.0 ** -17
+            if fp8:
+                e = e + 2.0 ** -25 * k[g].abs().sum(-1).max() * scale
+            t = t.masked_fill(~seen, -math.inf)
+            some = seen.any(-1)
+            rows = slice(at, at + n)
+            l = torch.logsumexp(t, -1)
+            lse[rows, h] = torch.where(some, l, -math.inf)
+            p = torch.where(some[:, None], torch.softmax(t, -1), 0.0).nan_to_num(0.0)
+            vv = v[g].nan_to_num(0.0)
+            out[rows, h] = p @ vv
+            big = v[g][:, :].abs().amax() if N else 0.0
+            tol_o[rows, h, 0] = (2 * e + 2.0 ** (-11 if fp8 else -8) + (N * 2.0 ** -25 if fp8 else 0)) * big
+            tol_l[rows, h] = e + 2.0 ** -21 * l.abs().nan_to_num(0, 0, 0)
+            w[b, g, :N] += p.sum(0)
+            tol_w[b, g, :N] += (p * (2 * e + 2.0 ** -20 + 2.0 ** -21 * l.abs().nan_to_num(0, 0, 0))[:, None]).sum(0) + 2.0 ** -100
+        at += n
+    return out, lse, w, tol_o, tol_l, tol_w
+
+
+def check_chunk(td, lay, new, causal=True, window=0, max_new=None, seed=0, bf16=False, skip=()):
+    q, off = chunk_inputs(lay, new, seed, extra=3)
+    T = sum(new)
+    og = util.Guarded((T + 3, lay.num_q_heads, D), torch.bfloat16 if bf16 else torch.float32, DEV, fill=9.0)
+    lg = util.Guarded((T + 3, lay.num_q_heads), torch.float32, DEV, fill=9.0)
+    got = td.chunk_attn(lay, q, off, max_new=max(new) if max_new is None else max_new, causal=causal, window=window, out=og.t, lse=lg.t)
+    assert got is og.t
+    out, lse, w, tol_o, tol_l, tol_w = ref_chunk(lay, q, new, causal, window, skip)
+    og.check("out"); lg.check("lse")
+    assert (og.t[T:] == 9).all() and (lg.t[T:] == 9).all()              # rows behind the last sequence
+    blind = torch.isinf(lse)
+    assert torch.equal(torch.isinf(lg.t[:T]), blind) and (lg.t[:T][blind] < 0).all() and (og.t[:T][blind] == 0).all()
+    err = (og.t[:T].double() - out).abs()
+    tol = tol_o + (2.0 ** -8 * (out.abs() + tol_o) if bf16 else 0)
+    assert torch.isfinite(og.t[:T].float()).all()
+    assert (err <= tol).all(), f"out: {float((err - tol).max()):.3e} over, max {float(err.max()):.3e} of {float(out.abs().max()):.3e}"
+    el = (lg.t[:T].double() - lse).abs()[~blind]
+    assert (el <= tol_l[~blind]).all(), f"lse: max {float(el.max()):.3e}"
+    return q, off, lg.t[:T + 3], w, tol_w
+
+
+CHUNKS = [
+    # lengths, new tokens, query heads, KV heads
+    ([1], [1], 1, 1), ([128], [128], 4, 1), ([129], [1], 8, 1), ([700], [33], 8, 2), ([300, 5, 1, 0, 257], [300, 2, 1, 0, 100], 6, 2),
+    ([1000, 17, 640], [0, 17, 1], 10, 2), ([2000], [400], 7, 1), ([50, 50], [50, 0], 16, 2), ([130, 260, 520], [64, 65, 200], 3, 3),
+    ([4103], [7], 8, 2), ([1500] * 6, [1] * 6, 32, 8),
+]
+
+
+@pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lens,new,hq,hkv", CHUNKS)
+def test_chunk_attention(td, layout, fp8, lens, new, hq, hkv):
+    lay = make(lens, hq, hkv, layout, fp8, seed=len(lens) + hq)
+    check_chunk(td, lay, new, max_new=0)
+    assert td.device_status() == binding.OK
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("causal,window", [(True, 1), (True, 40), (True, 129), (True, 100000), (False, 0), (False, 70)])
+@pytest.mark.parametrize("lens,new,hq,hkv", [([700, 90, 3], [300, 90, 1], 8, 2), ([1900, 40], [1, 1], 4, 1)])
+def test_chunk_attention_masks(td, fp8, causal, window, lens, new, hq, hkv):
+    lay = make(lens, hq, hkv, "paged", fp8, seed=window)
+    check_chunk(td, lay, new, causal, window)
+
+
+def test_chunk_attention_options(td, td16):
+    """bf16 outputs, an explicit scale, a bound on the lengths beyond the longest, tokens beyond max_new left out, no log-sum-exp."""
+    lay = make([300, 77], 12, 4, "paged", seed=4, max_len=1000, sm_scale=0.31)
+    q, off, lse, _, _ = check_chunk(td, lay, [140, 77])
+    check_chunk(td16, lay, [140, 77], bf16=True)
+    one, two = td.chunk_attn(lay, q, off), td.chunk_attn(lay, q, off, lse=torch.empty(220, 12, device=DEV))
+    assert torch.equal(one[:217], two[:217])
+    td.chunk_attn(lay, q, off, max_new=1)                 # (no more than left out)
+    one = q[:1].clone()
+    assert torch.equal(td.chunk_attn(make([5], 12, 4, "hnd"), one, i32([0, 1])), td.chunk_attn(make([5], 12, 4, "hnd"), q[:1], i32([0, 1])))
+
+
+def test_chunk_rows_that_see_nothing(td):
+    """More new tokens than the cache counts: the first of them stand before position 0."""
+    lay = make([10, 0], 4, 2, "hnd", seed=1)
+    q = randn(3, 20, 4, D)
+    lse = torch.zeros(20, 4, device=DEV)
+    out = td.chunk_attn(lay, q, i32([0, 15, 20]), lse=lse)
+    dead = torch.tensor([True] * 5 + [False] * 10 + [True] * 5, device=DEV)
+    assert (out[dead] == 0).all() and (lse[dead] == -math.inf).all() and torch.isfinite(lse[~dead]).all()
+    ref = ref_chunk(lay, q[5:15].contiguous(), [10, 0])
+    assert ((out[5:15].double() - ref[0]).abs() <= ref[3]).all()
+
+
+def test_chunk_offsets_out_of_order_are_cut_and_reported(td):
+    lay = make([40, 40, 40], 2, 1, "paged")
+    q = randn(3, 30, 2, D)
+    for off in ([0, 20, 10, 30], [0, 10, 20, 31], [-5, 10, 20, 30]):
+        td.chunk_attn(lay, q, i32(off))
+        assert td.device_status() == binding.ERR_INDEX
+    assert td.device_status() == binding.OK
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_chunk_bad_pages_are_skipped_and_reported(td, fp8):
+    lay = make([400], 4, 2, "paged", fp8, seed=2)
+    table = lay.page_table.clone()
+    lay.page_table[0, 3], lay.page_table[0, 20] = -1, lay.num_pages
+    q, off, lse, w, tol = check_chunk(td, lay, [30], skip=(3, 20))
+    assert td.device_status() == binding.ERR_INDEX
+    got = td.chunk_weights(lay, q, off, lse, torch.full((1, 2, 400), 5.0, device=DEV), decay=0.0)
+    assert ((got.double() - w).abs() <= tol).all() and (got[..., 48:64] == 0).all()
+    assert td.device_status() == binding.ERR_INDEX
+    lay.page_table.copy_(table)
+    td.chunk_attn(lay, q, off)
+    assert td.device_status() == binding.OK
+
+
+def test_chunk_attention_over_infinite_and_missing_numbers(td):
+    """A logit that is not a number, or a value, spoils the rows that see it."""
+    lay = make([260], 2, 1, "hnd", seed=7)
+    q, off = chunk_inputs(lay, [100])
+    lay.k[0, 0, 200, 3] = math.nan
+    lse = torch.empty(100, 2, device=DEV)
+    out = td.chunk_attn(lay, q, off, lse=lse)
+    assert torch.isnan(out[40:]).all() and torch.isnan(lse[40:]).all() and torch.isfinite(out[:40]).all() and torch.isfinite(lse[:40]).all()
+
+
+def test_chunk_of_one_equals_the_decode_step(td):
+    lay = make([900, 31, 4000], 16, 4, "paged", seed=3)
+    q = randn(8, 3, 16, D)
+    a, b = td.chunk_attn(lay, q, i32([0, 1, 2, 3]), max_new=1), td.full_attn(lay, q)
+    big = max(float(v.abs().max()) for _, v in lay.dense)
+    assert float((a - b).abs().max()) <= 2 * 2.0 ** -8 * big            # weights rounded to bf16 in both
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_chunk_attention_beyond_32_bits(td, fp8):
+    """Pages more than 4 GB apart."""
+    hkv, stride = 2, 1 << 16
+    pages_ = (5 << 30) // (stride * (1 if fp8 else 2)) + 8
+    pool = torch.zeros(pages_ * stride, dtype=torch.uint8 if fp8 else torch.bfloat16, device=DEV)
+    pool = pool.view(torch.float8_e4m3fn) if fp8 else pool
+    small = make([70], 4, hkv, "paged", fp8, seed=1)
+    far = torch.tensor([pages_ - 1 - i for i in range(5)], device=DEV)
+    view = pool.view(pages_, stride)[:, : hkv * BLK * 2 * D]
+    (view.view(torch.uint8) if fp8 else view)[far] = (small.keep[0].view(torch.uint8) if fp8 else small.keep[0])[small.page_table[0, :5].long()].reshape(5, -1)
+    lay = copy.copy(small)
+    lay.k, lay.v = view[:, :D], view[:, D:2 * D]
+    lay.stride_page, lay.num_pages = stride, pages_
+    lay.page_table = far[None].to(torch.int32).contiguous()
+    lay.max_pages_per_seq, lay.max_ctx_len = 5, 70
+    q, off = chunk_inputs(lay, [33])
+    lse, lse2 = torch.empty(33, 4, device=DEV), torch.empty(33, 4, device=DEV)
+    assert torch.equal(td.chunk_attn(lay, q, off, lse=lse), td.chunk_attn(small, q, off, lse=lse2)) and torch.equal(lse, lse2)
+    w, w2 = torch.zeros(1, hkv, 70, device=DEV), torch.zeros(1, hkv, 70, device=DEV)
+    assert torch.equal(td.chunk_weights(lay, q, off, lse, w), td.chunk_weights(small, q, off, lse, w2))
+    td.kv_gather(lay, i32([[[3, 69]]]), i32([2]))
+    td.kv_gather(small, i32([[[3, 69]]]), i32([2]))
+    a = view[far[0]].view(torch.uint8)
+    assert torch.equal(a, small.keep[0][small.page_table[0, 0].long()].reshape(-1).view(torch.uint8))
+
+
+# ---- attention weights ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lens,new,hq,hkv", CHUNKS)
+def test_chunk_weights(td, layout, fp8, lens, new, hq, hkv):
+    lay = make(lens, hq, hkv, layout, fp8, seed=len(lens) + hq)
+    q, off, lse, w, tol = check_chunk(td, lay, new)
+    stride = lay.max_ctx_len + 5
+    old = torch.rand(lay.batch, hkv, stride, generator=gen(3), device=DEV)
+    n = torch.tensor(lens, device=DEV)[:, None, None]
+    first = n - torch.tensor(new, device=DEV)[:, None, None]
+    j = torch.arange(stride, device=DEV)
+    for decay, max_new in ((0.0, 0), (1.0, max(new)), (0.75, 0)):
+        g = util.Guarded(old.shape, torch.float32, DEV)
+        g.t.copy_(old if decay else torch.full_like(old, math.nan))
+        assert td.chunk_weights(lay, q, off, lse, g.t, decay=decay, max_new=max_new) is g.t
+        want = torch.where(j < first, decay * old.double(), 0.0)
+        want[..., : lay.max_ctx_len] += w
+        bound = torch.zeros_like(want)
+        bound[..., : lay.max_ctx_len] = tol
+        there = j < n
+        err = (g.t.double() - want).abs()[there.expand_as(want)]
+        assert (err <= (bound + 2.0 ** -23 * want)[there.expand_as(want)]).all(), float(err.max())
+        rest = g.t[(~there).expand_as(want)]
+        assert torch.isnan(rest).all() if not decay else torch.equal(rest, old[(~there).expand_as(want)])
+        g.check("weights")
+    # all heads together; the same sums every time
+    one = td.chunk_weights(lay, q, off, lse, torch.zeros(lay.batch, 1, stride, device=DEV))
+    bound = (tol.sum(1) + 2.0 ** -20 * w.sum(1))
+    assert ((one[:, 0, : lay.max_ctx_len].double() - w.sum(1)).abs() <= bound).all()
+    assert torch.equal(one, td.chunk_weights(lay, q, off, lse, torch.zeros(lay.batch, 1, stride, device=DEV)))
+    assert td.device_status() == binding.OK
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("causal,window,last", [(True, 0, 16), (True, 50, 0), (False, 0, 0), (False, 33, 100), (True, 200, 7), (True, 0, 1000)])
+def test_chunk_weights_masks(td, fp8, causal, window, last):
+    lens, new = [900, 300, 20, 64], [200, 300, 1, 0]
+    lay = make(lens, 6, 2, "paged", fp8, seed=9)
+    q, off, lse, _, _ = check_chunk(td, lay, new, causal, window)
+    got = td.chunk_weights(lay, q, off, lse, torch.zeros(4, 2, 900, device=DEV), causal=causal, window=window, last=last, max_new=300)
+    lse = lse.double()
+    at = 0
+    for b, n in enumerate(new):
+        k = lay.dense[b][0]
+        N = lens[b]
+        pos, j = N - n + torch.arange(n, device=DEV), torch.arange(N, device=DEV)
+        seen = torch.ones(n, N, dtype=torch.bool, device=DEV)
+        if causal:
+            seen &= j[None] <= pos[:, None]
+        if window:
+            seen &= j[None] > pos[:, None] - window
+        if last:
+            seen &= (torch.arange(n, device=DEV) >= n - last)[:, None]
+        for g in range(2):
+            want = torch.zeros(N, dtype=torch.float64, device=DEV)
+            for h in range(3 * g, 3 * g + 3):
+                t = q[at: at + n, h].double() @ k[g].t() / math.sqrt(D)
+                want += torch.where(seen, torch.exp(t - lse[at: at + n, h, None]), 0.0).sum(0)
+            assert ((got[b, g, :N].double() - want).abs() <= 2.0 ** -12 * want + 1e-30).all()
+        at += n
+
+
+# ---- eviction --------------------------------------------------------------------------------------------------------------
+
+def ref_evict(w, lens, m, first, last):
+    B, H, _ = w.shape
+    kept, cnt = torch.full((B, H, m), -1, dtype=torch.int32), torch.zeros(B, dtype=torch.int32)
+    for b in range(B):
+        n = lens[b]
+        cnt[b] = c = min(m, n)
+        for h in range(H):
+            x = w[b, h, :n].double().cpu()
+            x = torch.where(torch.isnan(x), -math.inf, x)
+            rank = torch.where(torch.isnan(w[b, h, :n].cpu()), 0, 1)     # not-a-numbers below -infinity
+            j = torch.arange(n)
+            rank = torch.where((j < first) | (j >= n - last), 2, rank)
+            x = torch.where(rank == 2, 0.0, x) + 0.0
+            order = torch.sort(x, descending=True, stable=True).indices
+            order = order[torch.sort(rank[order], descending=True, stable=True).indices]
+            kept[b, h, :c] = order[:c].sort().values
+    return kept, cnt
+
+
+def weight_cache(lens, hq, hkv, layout="hnd", **kw):
+    return make(lens, hq, hkv, layout, **kw)
+
+
+@pytest.mark.parametrize("kind", ["random", "ties", "zeros", "odd", "steps", "sorted"])
+@pytest.mark.parametrize("lens,heads,m,first,last", [([1], 1, 1, 0, 0), ([40, 0, 17, 16], 2, 16, 1, 2), ([5000, 300, 4097], 3, 4096, 4, 32), ([20000], 2, 777, 0, 0),
+                                                     ([3000] * 40, 1, 1500, 10, 100), ([70000], 1, 4096, 4, 64), ([100, 60], 1, 30, 20, 20), ([2000], 1, 5, 50, 50)])
+def test_evict_select(td, kind, lens, heads, m, first, last):
+    lay = make(lens, 4 * heads, heads, "paged", spoil=False)
+    stride = max(lens) + 3
+    w = torch.rand(len(lens), heads, stride, generator=gen(m), device=DEV) ** 8
+    if kind == "ties":
+        w = torch.floor(w * 20) / 20
+    elif kind == "zeros":
+        w = torch.where(torch.rand(w.shape, generator=gen(1), device=DEV) < 0.9, torch.zeros_like(w), w)
+        w[..., 1::2] *= -1.0                              # both zeros, and negative weights
+    elif kind == "odd":
+        w[..., ::5], w[..., 1::7], w[..., 2::11] = math.nan, math.inf, -math.inf
+    elif kind == "steps":
+        w = torch.arange(stride, device=DEV).float().expand_as(w) // 100
+    elif kind == "sorted":
+        w = w.sort(-1).values
+    w = w.contiguous()
+    kept, cnt = util.Guarded((len(lens), heads, m), torch.int32, DEV), util.Guarded((len(lens),), torch.int32, DEV)
+    got = td.evict_select(lay, w, m, first, last, kept.t, cnt.t)
+    assert got[0] is kept.t and got[1] is cnt.t
+    want = ref_evict(w, lens, m, first, last)
+    assert torch.equal(cnt.t.cpu(), want[1])
+    assert torch.equal(kept.t.cpu(), want[0]), (kept.t.cpu() != want[0]).nonzero()[:5]
+    kept.check("kept"); cnt.check("new_lens")
+
+
+def test_evict_select_of_the_longest_context(td):
+    lay = make([262144], 1, 1, "paged", spoil=False)
+    w = torch.rand(1, 1, 262144, generator=gen(4), device=DEV)
+    for m in (1, 100000, 262143, 262144):
+        kept, cnt = td.evict_select(lay, w, m)
+        want = torch.sort(w[0, 0], descending=True, stable=True).indices[:m].sort().values
+        assert int(cnt) == m and torch.equal(kept[0, 0].long(), want)
+
+
+def gathered(lay, kept, cnt, heads):
+    """Rows after a gather, per sequence: (keys, values) codes of the first cnt positions."""
+    out = []
+    for b in range(lay.batch):
+        c = int(cnt[b])
+        rows = []
+        for g in range(lay.num_kv_heads):
+            idx = kept[b, g if heads > 1 else 0, :c].long()
+            rows.append((lay.codes[b][0][g, idx], lay.codes[b][1][g, idx]))
+        out.append((torch.stack([r[0] for r in rows]), torch.stack([r[1] for r in rows])))
+    return out
+
+
+def read_rows(lay, b, c):
+    pos = torch.arange(c, device=DEV)
+    if lay.paged:
+        pg = lay.page_table[b, pos // BLK].long()
+        return [x.view(torch.uint8)[pg, :, pos % BLK].transpose(0, 1).contiguous().view(x.dtype).float().double() if lay.kv_dtype else x[pg, :, pos % BLK].transpose(0, 1).double()
+                for x in (lay.k, lay.v)]
+    if lay.stride_head > lay.stride_pos:
+        return [x[b, :, :c].float().double() for x in (lay.k, lay.v)]
+    return [x[b, :c].transpose(0, 1).float().double() for x in (lay.k, lay.v)]
+
+
+@pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("lens,hkv,heads,m", [([1], 1, 1, 1), ([40, 0, 17], 2, 2, 16), ([5000, 2300], 3, 3, 2100), ([700, 700], 4, 1, 333), ([3000], 8, 1, 2999)])
+def test_kv_gather(td, layout, fp8, inplace, lens, hkv, heads, m):
+    lay = make(lens, hkv, hkv, layout, fp8, seed=m)
+    stride = max(max(lens), 1) + 1
+    w = torch.rand(len(lens), heads, stride, generator=gen(2), device=DEV)
+    w0 = w.clone()
+    kept, cnt = td.evict_select(lay, w, m)
+    want = gathered(lay, kept, cnt, heads)
+    into = None if inplace else make([min(n, m) for n in lens], hkv, hkv, {"paged": "hnd", "hnd": "nhd", "nhd": "paged"}[layout], fp8, seed=1, max_len=max(min(max(lens), m), 1))
+    keep = [x.clone() for x in lay.keep]
+    out = None if inplace else torch.full((len(lens), heads, m + 2), 5.0, device=DEV)
+    td.kv_gather(lay, kept, cnt, into=into, weights=w, weights_out=out)
+    for b, n in enumerate(lens):
+        c = int(cnt[b])
+        got = read_rows(lay if inplace else into, b, c)
+        assert torch.equal(got[0], want[b][0]) and torch.equal(got[1], want[b][1]), b
+        for h in range(heads):
+            assert torch.equal((w if inplace else out)[b, h, :c], w0[b, h, kept[b, h, :c].long()])
+            if inplace:
+                assert torch.equal(w[b, h, c:], w0[b, h, c:])
+            else:
+                assert (out[b, h, c:] == 5).all()
+    if not inplace:
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(keep, lay.keep)) and torch.equal(w, w0)
+    # without weights the rows are the same
+    again = make(lens, hkv, hkv, layout, fp8, seed=m)
+    td.kv_gather(again, kept, cnt, into=into)
+    assert not inplace or all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(again.keep, lay.keep))
+    assert td.device_status() == binding.OK
+
+
+def test_kv_gather_reports_positions_and_pages_outside(td):
+    lay, into = make([50], 1, 1, "paged"), make([50], 1, 1, "hnd", seed=5)
+    before = into.keep[0].clone()
+    td.kv_gather(lay, i32([[[3, 50, -1, 7, -9]]]), i32([5]), into=into)
+    assert td.device_status() == binding.ERR_INDEX
+    got = into.k[0, 0, :5]
+    assert torch.equal(got[0], lay.codes[0][0][0, 3].to(torch.bfloat16)) and torch.equal(got[3], lay.codes[0][0][0, 7].to(torch.bfloat16))
+    assert torch.equal(got[[1, 2, 4]], before[0, 0, [1, 2, 4], 0])
+    lay.page_table[0, 2] = -3
+    td.kv_gather(lay, i32([[[1, 40]]]), i32([2]), into=into)
+    assert td.device_status() == binding.ERR_INDEX
+    td.kv_gather(lay, i32([[[1, 40]]]), i32([2]))
+    assert td.device_status() == binding.ERR_INDEX
+    td.kv_gather(lay, i32([[[1, 20]]]), i32([-4]))        # counts below nothing move nothing
+    assert td.device_status() == binding.OK
+
+
+def test_gather_takes_the_token_selection_lists(td):
+    """A cache cut down to the positions that a selection layer keeps per KV head attends as the sparse layer does."""
+    lay = make([3000], 8, 2, "hnd", seed=11)
+    q = randn(4, 1, 8, D)
+    _, idx, cnt = td.select_attn(lay, q, 256, binding.SEL_PER_KVHEAD)
+    want = td.sparse_attn(lay, q, idx, cnt)
+    td.kv_gather(lay, idx, cnt)
+    lay.ctx_lens = cnt
+    got = td.full_attn(lay, q)
+    big = float(lay.dense[0][1].abs().max())
+    assert float((got - want).abs().max()) <= 2 * 2.0 ** -8 * big

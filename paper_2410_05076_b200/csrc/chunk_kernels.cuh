@@ -4,6 +4,8 @@
 
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "page_kernels.cuh"
 
 namespace tidal {
@@ -59,6 +61,15 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
 }
+// One lane of a warp whose lanes are together, the same one every time.
+__device__ __forceinline__ bool elected() {
+    uint32_t e;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(e));
+    return e != 0;
+}
+// A value that all lanes of a warp share, as one that the compiler knows they do: descriptors and addresses of products live in uniform registers,
+// and moving them there one by one costs more than a product takes.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
@@ -84,11 +95,39 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* x) {
                  :: TMEM_REGS32(R, 0), "r"(addr) : "memory");
 #undef R
 }
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* x) {
+#define R(i) "r"(x[i])
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};\n"
+                 :: R(0), R(1), R(2), R(3), R(4), R(5), R(6), R(7), R(8), R(9), R(10), R(11), R(12), R(13), R(14), R(15), "r"(addr) : "memory");
+#undef R
+}
 // (the loads above are done: their registers may be read)
 __device__ __forceinline__ void tmem_loaded32(uint32_t* x) {
 #define R(i) "+r"(x[i])
     asm volatile("" : TMEM_REGS32(R, 0));
 #undef R
+}
+
+// 2^t of two numbers in -126 .. 127, off by at most 2.7e-6 of the value: 2^n for the nearest whole n, added to the exponent, times a polynomial of
+// degree 4 with the least largest relative error over the rest in [-1/2, 1/2] (its mean error is 3e-9, so that long sums are good
+// to more). What is below -126 counts as that. Takes from the exponential unit, which has 16 results a clock and SM for 128 multiply-adds.
+__device__ __forceinline__ f32pair exp2_by_polynomial(f32pair t) {
+    float lo = fmaxf(half2(t, 0), -126.f), hi = fmaxf(half2(t, 1), -126.f);
+    t = pair2(lo, hi);
+    const f32pair whole = add2(t, pair2(12582912.f, 12582912.f));          // 1.5 x 2^23: the low bits are the nearest whole number
+    const f32pair rest = fma2(add2(whole, pair2(-12582912.f, -12582912.f)), pair2(-1.f, -1.f), t);
+    f32pair y = fma2(rest, pair2(0.009569674730300903f, 0.009569674730300903f), pair2(0.05591824650764465f, 0.05591824650764465f));
+    y = fma2(y, rest, pair2(0.2402476668357849f, 0.2402476668357849f));
+    y = fma2(y, rest, pair2(0.6931217312812805f, 0.6931217312812805f));
+    y = fma2(y, rest, pair2(0.9999992251396179f, 0.9999992251396179f));
+    lo = __int_as_float(__float_as_int(half2(y, 0)) + (__float_as_int(half2(whole, 0)) << 23));
+    hi = __int_as_float(__float_as_int(half2(y, 1)) + (__float_as_int(half2(whole, 1)) << 23));
+    return pair2(lo, hi);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {         // not-a-number if one is
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 // ---- attention -------------------------------------------------------------------------------------------------------
@@ -120,13 +159,15 @@ constexpr int CH_TILE = 128;                                // positions per til
 constexpr int CH_HALF = CH_TILE * 128;                      // bytes of 64 channels of a tile's rows, 16 bits each
 constexpr int CH_MAT = 2 * CH_HALF;
 constexpr int CH_TAGS = 16;
+constexpr int CH_POLY = 3;                                  // of sixteen pairs of weights, those whose exponentials are polynomials
 constexpr int CH_THREADS = 384, CH_THREADS8 = 512;
 constexpr int CH_RING = 5, CH_RING8 = 4;                       // operand slots: keys and values of a tile take one each
+constexpr int CH_MOST = 6;                                  // of eight products of weights and values, those that begin before all weights are there
 constexpr int CH_RAW = 2;                                   // 8-bit caches: tiles of codes in flight
 template <bool KV8> constexpr size_t ch_smem() { return 1024 + 2 * CH_MAT + (size_t)(KV8 ? CH_RING8 : CH_RING) * CH_MAT + (KV8 ? CH_RAW * CH_HALF : 0); }
 
 struct ChunkShared {
-    unsigned long long q_full, full[5], empty[5], raw_full[2], raw_empty[2], s_full[2], p_full[2], o_done[2];
+    unsigned long long q_full, full[5], empty[5], raw_full[2], raw_empty[2], s_full[2], p_most[2], p_full[2], o_done[2];
     uint32_t tmem;
     int gave_up, seq, tile;
     unsigned bad_pages[CH_TAGS];                            // per tile, bit i: its i-th page is not one
@@ -235,7 +276,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         for (int i = 0; i < RING; ++i) { bar_init(smem_u32(&sh.full[i]), KV8 ? 4 : 1); bar_init(smem_u32(&sh.empty[i]), 1); }
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_u32(&sh.raw_full[i]), 1); bar_init(smem_u32(&sh.raw_empty[i]), 4);
-            bar_init(smem_u32(&sh.s_full[i]), 1); bar_init(smem_u32(&sh.p_full[i]), 4); bar_init(smem_u32(&sh.o_done[i]), 1);
+            bar_init(smem_u32(&sh.s_full[i]), 1); bar_init(smem_u32(&sh.p_most[i]), 4); bar_init(smem_u32(&sh.p_full[i]), 4);
+            bar_init(smem_u32(&sh.o_done[i]), 1);
         }
         sh.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -326,12 +368,52 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     smem_to_async();
                 }
             }
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < CH_TILE; ++j) top = fmaxf(top, __uint_as_float(x[j]));
             if (i == 0) {
-                m = top;
-            } else if (__any_sync(0xffffffffu, valid && (top - m) * scale > 8.f)) {       // (rows that are none must not change others' rounding)
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < CH_TILE; j += 2) top = max3(top, __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+                m = top == top ? top : -INFINITY;
+            }
+            // Weights by the maximum so far, while this tile's own is looked for: it is raised, and the weights are worked out again, only
+            // where that leaves one above 2^8. Whole tiles take some of the exponentials from the polynomial; where positions are masked all come
+            // from the unit, whose 2^-infinity is 0.
+            f32pair sum0, sum1;
+            float top;
+            auto weights = [&](auto whole) -> bool {
+                const float shift = m == -INFINITY ? 0.f : -m * scale;
+                const f32pair scale2 = pair2(scale, scale), shift2 = pair2(shift, shift);
+                sum0 = sum1 = pair2(0.f, 0.f);
+                top = -INFINITY;
+                float other = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t y[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int at = c * 32 + 2 * j;
+                        if (c < 2) {
+                            top = max3(top, __uint_as_float(x[2 * at]), __uint_as_float(x[2 * at + 1]));
+                            other = max3(other, __uint_as_float(x[2 * at + 2]), __uint_as_float(x[2 * at + 3]));
+                        }
+                        const f32pair t = fma2(pair2(__uint_as_float(x[at]), __uint_as_float(x[at + 1])), scale2, shift2);
+                        const f32pair e = decltype(whole)::value && (j * CH_POLY) % 16 < CH_POLY ? exp2_by_polynomial(t) : pair2(fast_exp2(half2(t, 0)), fast_exp2(half2(t, 1)));
+                        if (j & 1) sum1 = add2(sum1, e); else sum0 = add2(sum0, e);
+                        y[j] = KV8 ? pack_f16(half2(e, 0), half2(e, 1)) : pack_bf16(half2(e, 0), half2(e, 1));
+                    }
+                    tmem_st16(S + c * 16, y);
+                    if (c == CH_MOST / 2 - 1) {                           // the products with three quarters of the positions may begin
+                        top = max3(top, other, other);
+                        if (__any_sync(0xffffffffu, valid && (top - m) * scale > 8.f)) return false;      // (rows that are none must not change others' rounding)
+                        tmem_wait_st();
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_u32(&sh.p_most[s]));
+                    }
+                }
+                return true;
+            };
+            const bool whole = !(ragged || partly || bad);
+            while (!(whole ? weights(std::true_type()) : weights(std::false_type()))) {
                 const float up = fmaxf(m, top), f = m == up ? 1.f : fast_exp2((m - up) * scale);
                 l *= f;
                 m = up;
@@ -346,21 +428,9 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     tmem_st32(O + c * 32, y);
                 }
             }
-            const float shift = m == -INFINITY ? 0.f : -m * scale;
-            float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t y[32];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const float a = fast_exp2(fmaf(__uint_as_float(x[c * 64 + 2 * j]), scale, shift));
-                    const float b = fast_exp2(fmaf(__uint_as_float(x[c * 64 + 2 * j + 1]), scale, shift));
-                    sum0 += a; sum1 += b;
-                    y[j] = KV8 ? pack_f16(a, b) : pack_bf16(a, b);
-                }
-                tmem_st32(S + c * 32, y);
-            }
-            l += sum0 + sum1;
+            sum0 = add2(sum0, sum1);
+            l += half2(sum0, 0) + half2(sum0, 1);
+            if (!(top == top)) l = top;                     // (the row's result is not a number)
             tmem_wait_st();
             tmem_fence_before();
             __syncwarp();
@@ -423,46 +493,119 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(KV8 ? 56 : 72));
     }
     if (warp == 8) {
-        // ---- products ----
-        if (lane == 0 && busy) {
+        // ---- products: the whole warp walks, one lane issues ----
+        if (busy) {
             const uint32_t first = mma_shape(!KV8, CH_TILE, false), second = mma_shape(!KV8, HEAD_DIM, true);
-            const bool both = w.twin == 0;
-            bool ok = bar_wait(smem_u32(&sh.q_full), 0, gave_up);
-            if (KV8) for (int s = 0; s < 2 && ok; ++s) ok = bar_wait(smem_u32(&sh.p_full[s]), 0, gave_up);
-            auto here = [&](int item) { return bar_wait(smem_u32(&sh.full[item % RING]), (item / RING) & 1, gave_up); };
-            auto scores = [&](int s, int i) {
-                const int item = 2 * w.at(s, i);
-                if (!here(item)) return false;
-                tmem_fence_after();
-                const uint32_t a = q_smem + (both ? s : 0) * CH_MAT, k = ring + (item % RING) * CH_MAT;
+            const uint32_t acc = uniform(tmem);
+            const int twin = uniform(w.twin), n0 = uniform(w.stream_tiles[0]), n1 = uniform(w.stream_tiles[1]);
+            // Few instructions between products: every one of them waits its turn beside the softmax warps', and the unit's own queue
+            // is two or three products deep.
+            const uint32_t s_full = smem_u32(sh.s_full), p_most = smem_u32(sh.p_most), p_full = smem_u32(sh.p_full), o_done = smem_u32(sh.o_done), full = smem_u32(sh.full), empty = smem_u32(sh.empty);
+            const uint64_t q = smem_matrix(q_smem, 16);
+            auto scores = [&](int s, uint64_t a, int slot) {
+                const uint64_t k = smem_matrix(ring + slot * CH_MAT, 16);
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
-                    const uint32_t off = (kk >> 2) * CH_HALF + (kk & 3) * 32;
-                    mma_ss(tmem + s * CH_TILE, smem_matrix(a + off, 16), smem_matrix(k + off, 16), first, kk > 0);
+                    const uint32_t off = ((kk >> 2) * CH_HALF + (kk & 3) * 32) >> 4;
+                    mma_ss(acc + s * CH_TILE, a + off, k + off, first, kk > 0);
                 }
-                mma_commit(smem_u32(&sh.s_full[s]));
-                if (!both || s == 1) mma_commit(smem_u32(&sh.empty[item % RING]));
-                return true;
+                mma_commit(s_full + 8 * s);
             };
-            auto values = [&](int s, int i) {
-                const int item = 2 * w.at(s, i) + 1;
-                if (!here(item) || !bar_wait(smem_u32(&sh.p_full[s]), (i + (KV8 ? 1 : 0)) & 1, gave_up)) return false;
-                tmem_fence_after();
-                const uint32_t v = ring + (item % RING) * CH_MAT;
+            // (positions 16 k0 .. 16 k1 - 1 of the tile)
+            auto values = [&](int s, int slot, bool add, int k0, int k1) {
+                const uint64_t v = smem_matrix(ring + slot * CH_MAT, CH_HALF);
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    mma_ts(tmem + 256 + s * CH_TILE, tmem + s * CH_TILE + kk * 8, smem_matrix(v + kk * 2048, CH_HALF), second, i > 0 || kk > 0);
-                if (!both || s == 1) mma_commit(smem_u32(&sh.empty[item % RING]));
-                if (i == w.stream_tiles[s] - 1) mma_commit(smem_u32(&sh.o_done[s]));
-                return true;
+                for (int kk = k0; kk < k1; ++kk)
+                    mma_ts(acc + 256 + s * CH_TILE, acc + s * CH_TILE + kk * 8, v + (kk * 2048 >> 4), second, add || kk > 0);
             };
-            const int steps = max(w.stream_tiles[0], w.stream_tiles[1]);
-            for (int s = 0; s < 2 && ok; ++s) if (w.stream_tiles[s] > 0) ok = scores(s, 0);
-            for (int i = 0; i < steps && ok; ++i)
-                for (int s = 0; s < 2 && ok; ++s) {
-                    if (i < w.stream_tiles[s]) ok = values(s, i);
-                    if (ok && i + 1 < w.stream_tiles[s]) ok = scores(s, i + 1);
+            bool ok = bar_wait(smem_u32(&sh.q_full), 0, gave_up);
+            if (KV8) for (int s = 0; s < 2 && ok; ++s) ok = bar_wait(p_full + 8 * s, 0, gave_up);
+            int slot = 0, parity = 0;                       // of the next ring item to be looked for
+            auto next = [&]() {                             // waits for it; its slot
+                ok = ok && bar_wait(full + 8 * slot, parity, gave_up);
+                const int at = slot;
+                if (++slot == RING) { slot = 0; parity ^= 1; }
+                return at;
+            };
+            int most = 0, turn = KV8;                                 // parity of the weights to come
+            if (!twin) {
+                int k = next();
+                tmem_fence_after();
+                if (ok && elected()) {
+                    if (n0 > 0) scores(0, q, k);
+                    scores(1, q + (CH_MAT >> 4), k);
+                    mma_commit(empty + 8 * k);
                 }
+                __syncwarp();
+                int v = next();
+                if (n1 > 1) k = next();
+                for (int i = 0; i < n1 && ok; ++i, turn ^= 1, most ^= 1) {
+                    if (i < n0) {
+                        ok = bar_wait(p_most, most, gave_up);
+                        tmem_fence_after();
+                        if (ok && elected()) values(0, v, i > 0, 0, CH_MOST);
+                        __syncwarp();
+                        ok = ok && bar_wait(p_full, turn, gave_up);
+                        tmem_fence_after();
+                        if (ok && elected()) {
+                            values(0, v, true, CH_MOST, 8);
+                            if (i + 1 < n0) scores(0, q, k);
+                            else mma_commit(o_done);
+                        }
+                        __syncwarp();
+                    }
+                    ok = ok && bar_wait(p_most + 8, most, gave_up);
+                    tmem_fence_after();
+                    if (ok && elected()) values(1, v, i > 0, 0, CH_MOST);
+                    __syncwarp();
+                    ok = ok && bar_wait(p_full + 8, turn, gave_up);
+                    tmem_fence_after();
+                    if (ok && elected()) {
+                        values(1, v, true, CH_MOST, 8);
+                        mma_commit(empty + 8 * v);
+                        if (i + 1 < n1) {
+                            scores(1, q + (CH_MAT >> 4), k);
+                            mma_commit(empty + 8 * k);
+                        } else {
+                            mma_commit(o_done + 8);
+                        }
+                    }
+                    __syncwarp();
+                    if (i + 1 < n1) {
+                        v = next();
+                        if (i + 2 < n1) k = next();
+                    }
+                }
+            } else {
+                int vs = 1, vp = 0, ks = 0, kp = 0;         // slots and parities of the values of tile t and of the keys of tile t + 2
+                auto on = [&](int& at, int& par) { at += 2; if (at >= RING) { at -= RING; par ^= 1; } };
+                const int tiles = n0 + n1;
+                auto keys = [&](int s) {
+                    ok = ok && bar_wait(full + 8 * ks, kp, gave_up);
+                    tmem_fence_after();
+                    if (ok && elected()) {
+                        scores(s, q, ks);
+                        mma_commit(empty + 8 * ks);
+                    }
+                    __syncwarp();
+                    on(ks, kp);
+                };
+                for (int t = 0; t < min(tiles, 2); ++t) keys(t);
+                for (int t = 0; t < tiles && ok; ++t) {
+                    const int s = t & 1;
+                    ok = bar_wait(full + 8 * vs, vp, gave_up) && bar_wait(p_full + 8 * s, turn, gave_up);
+                    tmem_fence_after();
+                    if (ok && elected()) {
+                        values(s, vs, t > 1, 0, 8);
+                        mma_commit(empty + 8 * vs);
+                        if (t + 2 >= tiles) mma_commit(o_done + 8 * s);
+                    }
+                    __syncwarp();
+                    on(vs, vp);
+                    if (t + 2 < tiles) keys(s);
+                    turn ^= s;
+                }
+            }
         }
     } else if (warp == 9 && busy) {
         // ---- copies in ----

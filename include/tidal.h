@@ -434,9 +434,10 @@ tidal_status_t tidal_rope_write(tidal_ctx_t *ctx, const tidal_rope_t *rope, cons
  *   max_new    host upper bound of the new tokens of a sequence (tokens beyond it may be left out); 0: not known
  *   out        [num_tokens, num_q_heads, 128] contiguous, type as set by tidal_set_output_dtype; lse: float [num_tokens, num_q_heads] or NULL,
  *              ln of the sum of exp(scaled logit) over what the row sees. Rows behind q_offsets[batch] are left as they were.
- * A row that sees nothing gets zeros and -infinity. What lies behind a sequence in its last page or row block may be anything. Pages whose
+ * A row that sees nothing (or nothing but pages that are skipped) gets zeros and -infinity. What lies behind a sequence in its last page or row block may be anything. Pages whose
  * id is outside the pool are skipped and reported. k_scale must be positive. Softmax weights enter the product with V as
- * bf16 (FP8 caches: fp16, and the query as fp16 too); maxima, sums and outputs are fp32. No scratch memory. */
+ * bf16 (FP8 caches: fp16, and the query as fp16 too); maxima, sums and outputs are fp32. Scratch memory is of one size and
+ * allocated with the context. */
 tidal_status_t tidal_chunk_attn(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t num_tokens, const void *q, int64_t q_stride,
                                 const int32_t *q_offsets, int32_t max_new, int32_t causal, int32_t window, float *out, float *lse,
                                 void *stream);

@@ -6,6 +6,8 @@
 //                that the top-k kernel can rank them (Section 3: the inner
 //                products are stored during full attention)
 //   MODE_SPARSE  SparseAttention(q, C[rho]): Eq. 1 over the listed positions only
+//   MODE_TOKENS  MODE_FULL for the first of a sequence's new tokens, if it has any: queries and outputs are
+//                rows of packed tokens, the log-sum-exp comes out too, scratch is of fixed size
 //
 // Work decomposition. A CTA owns one (sequence, KV head [or query head], chunk of
 // the context / of the index list). Its warps take 16-position tiles round
@@ -33,7 +35,7 @@
 
 namespace tidal {
 
-enum { MODE_FULL = 0, MODE_SELECT = 1, MODE_SPARSE = 2 };
+enum { MODE_FULL = 0, MODE_SELECT = 1, MODE_SPARSE = 2, MODE_TOKENS = 3 };
 // Bits of the sticky device status word.
 enum { STATUS_BAD_INDEX = 1, STATUS_BAD_PAGE = 2, STATUS_SPLIT_OVERFLOW = 4 };
 
@@ -107,6 +109,11 @@ struct AttnParams {
                                // only before the first write to memory shared with it (partial results, counters)
     int trigger_early;         // with wait_late: let the next kernel's CTAs take the slots of ours as they retire,
                                // without first waiting for the kernel before us (see the host's launch rule)
+    // MODE_TOKENS
+    const int* q_offsets;      // [B + 1] first row of each sequence's new tokens
+    int num_tokens, causal;
+    long long q_stride;        // elements between tokens of q
+    float* lse;                // [num_tokens, Hq] or null
     int* status;
 };
 
@@ -587,7 +594,22 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
     // ---- this CTA's share of the flattened (sequence, item, tile) space ---------------------------
     const bool per_qhead = (MODE == MODE_SPARSE) && (p.Hi == p.Hq);
     const int IY = per_qhead ? p.Hq : p.Hkv;            // items per sequence
+    constexpr bool TOKENS = MODE == MODE_TOKENS;
+    // MODE_TOKENS: the row of sequence b's first new token (-1: none) and how many positions it sees
+    auto new_token = [&](int b, int& seen) -> int {
+        const int x = p.q_offsets[b], z = p.q_offsets[b + 1];
+        const int begin = max(min(x, p.num_tokens), 0), end = max(min(z, p.num_tokens), begin);
+        if (begin != x || end != z) atomicOr(p.status, STATUS_BAD_INDEX);
+        const int N = max(min(p.ctx_lens[b], p.max_ctx), 0);
+        seen = begin == end ? 0 : p.causal ? max(N - (end - begin) + 1, 0) : N;
+        return begin == end ? -1 : begin;
+    };
     auto seq_total = [&](int b) -> int {
+        if constexpr (TOKENS) {
+            int seen;
+            new_token(b, seen);
+            return seen;
+        }
         const int N = min(p.ctx_lens[b], p.max_ctx);
         if (MODE != MODE_SPARSE) return max(N, 0);
         const int cnt = p.idx_count ? min(p.idx_count[b], p.budget) : p.budget;
@@ -917,9 +939,12 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
         // pieces 4j+tig (j = 0..3) of that head's query row.
         uint32_t qf[4][4];
         uint32_t qf8[2][8];                             // 8-bit caches: the query as fp16, see consume_tile8
+        int token = b;
+        if constexpr (TOKENS) { int seen; token = new_token(b, seen); }
         {
             const uint4* qp = reinterpret_cast<const uint4*>(
-                p.q + ((long long)b * p.Hq + head0 + min(gid, ncols - 1)) * HEAD_DIM);
+                TOKENS ? p.q + max(token, 0) * p.q_stride + (long long)(head0 + min(gid, ncols - 1)) * HEAD_DIM
+                       : p.q + ((long long)b * p.Hq + head0 + min(gid, ncols - 1)) * HEAD_DIM);
             const bool on = gid < ncols;
             if constexpr (KV8) {
 #pragma unroll
@@ -1177,25 +1202,39 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
             split = (int)blockIdx.x - first_cta;
         }
         const long long row0 = (long long)b * p.Hq + head0;
+        const long long out0 = (long long)token * p.Hq + head0;
+        // Partial result of a head and split. MODE_TOKENS: two per CTA, since only its first and its last segment can be parts of an item
+        // (split 0 is a CTA's last one, where not all its tiles go to one item).
+        const int item = b * IY + y, first_cta = pooled ? item : (int)((seq_start + (long long)y * tiles_b) / per_cta);
+        auto part_row = [&](int col, int sp) -> long long {
+            if constexpr (TOKENS) return ((long long)(pooled ? first_cta + sp * p.batch * IY : first_cta + sp) * 2 + (!pooled && sp == 0)) * 8 + col;
+            else return (row0 + col) * p.max_splits + sp;
+        };
+        // A part without a score counts for nothing (MODE_TOKENS: one whose scores are not numbers makes the result none either)
+        auto part_factor = [&](float2 ml, float M) { return ml.x == -INFINITY && !(TOKENS && ml.y != 0.f) ? 0.f : M == -INFINITY ? 1.f : fast_exp2(ml.x - M); };
+        auto result = [&](float O, float L) { return (TOKENS ? L != 0.f : L > 0.f) ? O / L : 0.f; };
+        auto log_sum = [&](float M, float L) { return L != 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY; };
         for (int e = threadIdx.x; e < ncols * HEAD_DIM; e += NW * 32) {
             const int col = e >> 7, c = e & 127;
             float M = -INFINITY;
 #pragma unroll
             for (int w = 0; w < NW; ++w) M = fmaxf(M, mml[w * 8 + col].x);
             float L = 0.f, O = 0.f;
-            if (M != -INFINITY) {
+            if (TOKENS || M != -INFINITY) {
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {
                     const float2 ml = mml[w * 8 + col];
-                    const float f = (ml.x == -INFINITY) ? 0.f : fast_exp2(ml.x - M);
+                    const float f = TOKENS ? part_factor(ml, M) : (ml.x == -INFINITY) ? 0.f : fast_exp2(ml.x - M);
                     L += ml.y * f;
                     O += mo[(w * 8 + col) * HEAD_DIM + c] * f;
                 }
             }
             if (nsplits == 1) {
-                store_out(p, (row0 + col) * HEAD_DIM + c, (L > 0.f) ? O / L : 0.f);
+                if (TOKENS && token < 0) continue;
+                store_out(p, (out0 + col) * HEAD_DIM + c, result(O, L));
+                if (TOKENS && p.lse && c == 0) p.lse[out0 + col] = log_sum(M, L);
             } else if (split < p.max_splits) {
-                const long long pr = (row0 + col) * p.max_splits + split;
+                const long long pr = part_row(col, split);
                 p.part_o[pr * HEAD_DIM + c] = O;
                 if (c == 0) p.part_ml[pr] = make_float2(M, L);
             } else if (e == 0) {
@@ -1206,7 +1245,7 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
         if (nsplits > 1) {
             // ---- the last CTA of this item to arrive combines the splits ---------------------------------
             __syncthreads();
-            int* ctr = p.counters + ((long long)b * IY + y) * p.ctr_stride;
+            int* ctr = p.counters + (TOKENS ? (long long)first_cta : (long long)b * IY + y) * p.ctr_stride;
             if (threadIdx.x == 0) {
                 // release: orders the whole CTA's partial stores (made visible to this thread by the barrier)
                 // before the arrival; acquire: the last arrival sees every earlier part's stores
@@ -1225,10 +1264,10 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
                 constexpr int CB = 16;
                 const int e0 = threadIdx.x;                               // first (col, c) element of this thread
                 const bool has0 = e0 < ncols * HEAD_DIM;
-                const float* po0 = p.part_o + ((row0 + (e0 >> 7)) * p.max_splits) * HEAD_DIM + (e0 & 127);
+                auto part_at = [&](int col, int sp) { return p.part_o + part_row(col, sp) * HEAD_DIM; };
                 float v0[CB];
 #pragma unroll
-                for (int u = 0; u < CB; ++u) v0[u] = (has0 && u < ns) ? __ldcg(po0 + (long long)u * HEAD_DIM) : 0.f;
+                for (int u = 0; u < CB; ++u) v0[u] = (has0 && u < ns) ? __ldcg(part_at(e0 >> 7, u) + (e0 & 127)) : 0.f;
                 // The item's pool cursor is cleared for a later launch now, behind this thread's loads (the
                 // fence then costs nothing extra: it returns when they do). The fence makes the cleared
                 // cursor visible device-wide before this CTA can retire: a later launch may request tiles
@@ -1236,26 +1275,25 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
                 // start before this CTA is gone.
                 if (pooled && threadIdx.x == NW * 32 - 1) { *pool = 0; __threadfence(); }
                 for (int col = warp; col < ncols; col += NW) {
-                    const long long pr = (row0 + col) * p.max_splits;
                     float M = -INFINITY;
-                    for (int s = lane; s < ns; s += 32) M = fmaxf(M, __ldcg(&p.part_ml[pr + s].x));
+                    for (int s = lane; s < ns; s += 32) M = fmaxf(M, __ldcg(&p.part_ml[part_row(col, s)].x));
 #pragma unroll
                     for (int sh = 16; sh >= 1; sh >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, sh));
                     float L = 0.f;
                     for (int s = lane; s < ns; s += 32) {
-                        const float2 ml = __ldcg(&p.part_ml[pr + s]);
-                        const float f = (ml.x == -INFINITY || M == -INFINITY) ? 0.f : fast_exp2(ml.x - M);
+                        const float2 ml = __ldcg(&p.part_ml[part_row(col, s)]);
+                        const float f = TOKENS ? part_factor(ml, M) : (ml.x == -INFINITY || M == -INFINITY) ? 0.f : fast_exp2(ml.x - M);
                         fsc[col * p.max_splits + s] = f;
                         L += ml.y * f;
                     }
 #pragma unroll
                     for (int sh = 16; sh >= 1; sh >>= 1) L += __shfl_xor_sync(0xffffffffu, L, sh);
-                    if (lane == 0) linv[col] = (L > 0.f) ? 1.f / L : 0.f;
+                    if (lane == 0) linv[col] = (TOKENS ? L != 0.f : L > 0.f) ? 1.f / L : 0.f;
+                    if (TOKENS && p.lse && lane == 0 && token >= 0) p.lse[out0 + col] = log_sum(M, L);
                 }
                 __syncthreads();
                 for (int e = threadIdx.x; e < ncols * HEAD_DIM; e += NW * 32) {
                     const int col = e >> 7, c = e & 127;
-                    const float* po = p.part_o + ((row0 + col) * p.max_splits) * HEAD_DIM + c;
                     const float* fs = fsc + col * p.max_splits;
                     float O = 0.f;
                     int s = 0;
@@ -1267,12 +1305,12 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
                     for (; s + 8 <= ns; s += 8) {
                         float v[8];
 #pragma unroll
-                        for (int u = 0; u < 8; ++u) v[u] = __ldcg(po + (long long)(s + u) * HEAD_DIM);
+                        for (int u = 0; u < 8; ++u) v[u] = __ldcg(part_at(col, s + u) + c);
 #pragma unroll
                         for (int u = 0; u < 8; ++u) O += v[u] * fs[s + u];
                     }
-                    for (; s < ns; ++s) O += __ldcg(po + (long long)s * HEAD_DIM) * fs[s];
-                    store_out(p, (row0 + col) * HEAD_DIM + c, O * linv[col]);
+                    for (; s < ns; ++s) O += __ldcg(part_at(col, s) + c) * fs[s];
+                    if (!TOKENS || token >= 0) store_out(p, (out0 + col) * HEAD_DIM + c, O * linv[col]);
                 }
                 if (threadIdx.x == 0) *ctr = 0;       // ready for the next launch
             }

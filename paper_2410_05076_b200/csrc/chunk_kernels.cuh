@@ -440,10 +440,10 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         if (n > 0 && bar_wait(smem_u32(&sh.o_done[s]), 0, gave_up)) tmem_fence_after();
         const float vs = KV8 && p.v_scale ? read_global(p.v_scale + w.g) : 1.f;
         if (!joined) {
-            const bool sees = hi > lo;
-            const float inv = n > 0 && sees ? vs / l : 0.f;
+            const bool some = l != 0.f;                     // (a sum that is not a number is some)
+            const float inv = some ? vs / l : 0.f;
             const long long at = ((long long)(w.q_row + token - w.t0) * p.c.Hq + head);
-            if (valid && p.lse) p.lse[at] = sees ? (m == -INFINITY ? m : (m * scale + log2f(l)) * 0.6931471805599453f) : -INFINITY;
+            if (valid && p.lse) p.lse[at] = some ? (m * scale + log2f(l)) * 0.6931471805599453f : -INFINITY;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t y[32];
@@ -455,7 +455,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 }
                 float z[32];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) z[j] = n > 0 && sees ? __uint_as_float(y[j]) * inv : 0.f;
+                for (int j = 0; j < 32; ++j) z[j] = some ? __uint_as_float(y[j]) * inv : 0.f;
                 if (valid && p.out_bf16) {
                     uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at * HEAD_DIM + c * 32);
 #pragma unroll
@@ -694,8 +694,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         const float vs = KV8 && p.v_scale ? read_global(p.v_scale + w.g) : 1.f;
         for (int r = rank + warp * ranks; r < here; r += warps * ranks) {
             const int s = w.twin ? 0 : r / (tt * G), row = w.twin ? r : r % (tt * G);
-            const int token = w.t0 + r / G, head = w.g * G + r % G, pos = w.first + token;
-            const int hi = p.causal ? min(pos + 1, w.ctx) : w.ctx, lo = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
+            const int token = w.t0 + r / G, head = w.g * G + r % G;
             auto ld = [&](uint32_t a) { float v; asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(a) : "memory"); return v; };
             float mi = -INFINITY, li = 0.f;                 // lane i holds part i's (at most 32)
             if (lane < parts) {
@@ -722,14 +721,14 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[j] = fmaf(fi, v[j], o[j]);
             }
-            const bool sees = hi > lo;
+            const bool some = l != 0.f;
             const long long at = (long long)(w.q_row + token - w.t0) * p.c.Hq + head;
-            const float inv = sees ? vs / l : 0.f;
+            const float inv = some ? vs / l : 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = sees ? o[j] * inv : 0.f;
+            for (int j = 0; j < 4; ++j) o[j] = some ? o[j] * inv : 0.f;
             if (p.out_bf16) *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at * HEAD_DIM + lane * 4) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
             else *reinterpret_cast<float4*>(p.out + at * HEAD_DIM + lane * 4) = make_float4(o[0], o[1], o[2], o[3]);
-            if (lane == 0 && p.lse) p.lse[at] = sees ? (m == -INFINITY ? m : (m + log2f(l)) * 0.6931471805599453f) : -INFINITY;
+            if (lane == 0 && p.lse) p.lse[at] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
         }
         if (ranks > 1) { cluster_arrive(); cluster_wait(); }               // nobody leaves while its results are read
     }

@@ -82,6 +82,7 @@ struct tidal_ctx {
     int layer_overlap = 1;                      // layers of a step may stream their inputs while the layer before them finishes
     int select_clusters[17] = {};               // clusters of 1 .. 16 CTAs that are resident together: block selection
     int attn_clusters[17] = {};                 // the same for four-warp CTAs of the block attention
+    void* tok_ws = nullptr;                     // chunk attention of single tokens: partial results, counters and cursors (zero between launches)
     int chunk_clusters[2][17] = {};             // and for the chunk attention (16-bit, 8-bit caches)
     int evict_clusters[17] = {};                // and for the eviction's choice
     int64_t launches = 0;
@@ -1016,12 +1017,44 @@ tidal_status_t launch_maps(tidal_ctx* ctx, void (*kernel)(Args...), int grid, in
     return TIDAL_ERR_CUDA;
 }
 
+// Scratch of the streaming kernel for single new tokens, two partial results of eight heads per CTA (see MODE_TOKENS): of one size for every shape,
+// so that it is allocated with the context.
+constexpr long long TOK_LEAST = 32768;                       // positions of all sequences and KV heads together
+constexpr size_t TOK_ROWS = (size_t)GRID_MAX * 2 * 8;
+constexpr size_t TOK_ML = TOK_ROWS * HEAD_DIM * sizeof(float), TOK_COUNTERS = TOK_ML + TOK_ROWS * sizeof(float2),
+                 TOK_CURSORS = TOK_COUNTERS + (size_t)GRID_MAX * CTR_STRIDE * sizeof(int), TOK_TOTAL = TOK_CURSORS + (size_t)GRID_MAX * CTR_STRIDE * sizeof(int);
+
+template <int NW, int STAGES, bool KV8>
+tidal_status_t launch_tokens(tidal_ctx* ctx, const AttnParams& a, int grid, cudaStream_t st) {
+    return launch_block(ctx, attn_kernel<MODE_TOKENS, NW, STAGES, false, false, KV8>, a, grid, NW * 32, attn_smem<MODE_TOKENS, NW, STAGES, KV8>(), 0, st);
+}
+
+tidal_status_t run_tokens(tidal_ctx* ctx, const tidal_kv_t* kv, int32_t num_tokens, const void* q, int64_t q_stride, const int32_t* q_offsets,
+                          int causal, float* out, float* lse, cudaStream_t st) {
+    AttnParams a;
+    WsLayout none;
+    std::memset(&none, 0, sizeof none);
+    fill_common(a, ctx, kv, q, out, none);
+    char* ws = (char*)ctx->tok_ws;
+    a.part_o = (float*)ws; a.part_ml = (float2*)(ws + TOK_ML);
+    a.counters = (int*)(ws + TOK_COUNTERS); a.tile_ctr = (int*)(ws + TOK_CURSORS);
+    a.max_splits = GRID_MAX;
+    a.q_offsets = q_offsets; a.num_tokens = num_tokens; a.causal = causal; a.q_stride = q_stride; a.lse = lse;
+    a.pdl = 1; a.wait_first = 1;
+    const int grid = dense_grid(ctx, kv);
+    a.splits_per_item = pooled_splits(kv, kv->batch * kv->num_kv_heads, grid);
+    return kv->kv_dtype == TIDAL_KV_FP8_E4M3 ? launch_tokens<DENSE_NW8, DENSE_STAGES8, true>(ctx, a, grid, st) : launch_tokens<DENSE_NW, DENSE_STAGES, false>(ctx, a, grid, st);
+}
+
 bool prepare_prompt_kernels(tidal_ctx* ctx) {
     auto wide = [](const void* k) { return cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess; };
     auto room = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess; };
     if (!(wide((const void*)chunk_attn_kernel<false>) && wide((const void*)chunk_attn_kernel<true>) && wide((const void*)evict_select_kernel) &&
           room(chunk_attn_kernel<false>, ch_smem<false>()) && room(chunk_attn_kernel<true>, ch_smem<true>()) &&
-          room(chunk_weights_kernel<false>, cw_smem(false)) && room(chunk_weights_kernel<true>, cw_smem(true)) && room(evict_select_kernel, EV_SMEM_MAX)))
+          room(chunk_weights_kernel<false>, cw_smem(false)) && room(chunk_weights_kernel<true>, cw_smem(true)) &&
+          room(attn_kernel<MODE_TOKENS, DENSE_NW, DENSE_STAGES>, attn_smem<MODE_TOKENS, DENSE_NW, DENSE_STAGES>()) &&
+          room(attn_kernel<MODE_TOKENS, DENSE_NW8, DENSE_STAGES8, false, false, true>, attn_smem<MODE_TOKENS, DENSE_NW8, DENSE_STAGES8, true>()) &&
+          room(evict_select_kernel, EV_SMEM_MAX)))
         return false;
     // the softmax warpgroups raise their registers within what the launch holds
     cudaFuncAttributes a;
@@ -1085,9 +1118,12 @@ tidal_status_t tidal_create(tidal_ctx_t** out, int device, size_t workspace_byte
     if (cudaMalloc((void**)&ctx->status, 256) != cudaSuccess || cudaMemset(ctx->status, 0, 256) != cudaSuccess) {
         cudaGetLastError(); delete ctx; return TIDAL_ERR_NOMEM;
     }
+    if (cudaMalloc(&ctx->tok_ws, TOK_TOTAL) != cudaSuccess || cudaMemset(ctx->tok_ws, 0, TOK_TOTAL) != cudaSuccess) {
+        cudaGetLastError(); cudaFree(ctx->tok_ws); cudaFree(ctx->status); delete ctx; return TIDAL_ERR_NOMEM;
+    }
     if (workspace_bytes) {
         const tidal_status_t rc = ensure_ws(ctx, workspace_bytes);
-        if (rc != TIDAL_OK) { cudaFree(ctx->status); delete ctx; return rc; }
+        if (rc != TIDAL_OK) { cudaFree(ctx->tok_ws); cudaFree(ctx->status); delete ctx; return rc; }
     }
     *out = ctx;
     return TIDAL_OK;
@@ -1105,6 +1141,7 @@ tidal_status_t tidal_destroy(tidal_ctx_t* ctx) {
     if (ctx->blk_ws) cudaFree(ctx->blk_ws);
     for (int i = 0; i < ctx->blk_old_count; ++i) cudaFree(ctx->blk_old[i]);
     if (ctx->state) cudaFree(ctx->state);
+    if (ctx->tok_ws) cudaFree(ctx->tok_ws);
     if (ctx->status) cudaFree(ctx->status);
     delete ctx;
     return TIDAL_OK;
@@ -1842,6 +1879,11 @@ tidal_status_t tidal_chunk_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t 
     if (!out || ((uintptr_t)out & 15) || ((uintptr_t)lse & 3)) return TIDAL_ERR_INVALID;
     DeviceScope dev(ctx->device);
     if (!dev.ok) return TIDAL_ERR_CUDA;
+    // One token each: a matrix product of 128 rows would be empty but for one group of heads, and the cache streams at memory speed through
+    // the decode kernels (64 sequences of up to 16384: 341 us, 595 as a chunk; 131072: 83 and 139). A short cache by the cluster's CTAs instead (4103 positions of 2 heads:
+    // 14 us, 18 through the pool of tiles).
+    const long long cached = (long long)kv->batch * kv->num_kv_heads * kv->max_ctx_len;
+    if (max_new == 1 && window == 0 && cached >= TOK_LEAST) return run_tokens(ctx, kv, num_tokens, q, q_stride, q_offsets, causal != 0, out, lse, (cudaStream_t)stream);
     ChunkParams p;
     std::memset(&p, 0, sizeof p);
     fill_block_cache(p.c, ctx, kv, 0);

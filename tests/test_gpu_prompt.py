@@ -386,6 +386,50 @@ def test_chunk_attention_over_infinite_and_missing_numbers(td):
     assert torch.isnan(out[40:]).all() and torch.isnan(lse[40:]).all() and torch.isfinite(out[:40]).all() and torch.isfinite(lse[:40]).all()
 
 
+@pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens,new,hq,hkv", [([40000], [1], 8, 1), ([20000], [1], 32, 8), ([9000, 1, 5000, 300, 6000], [1, 1, 0, 1, 1], 6, 2), ([700] * 70, [1] * 69 + [0], 4, 2),
+                                             ([6000, 30000], [0, 1], 5, 1)])
+def test_single_tokens_of_long_caches(td, layout, fp8, causal, lens, new, hq, hkv):
+    """The form that streams the cache: one token a sequence, or none, with max_new = 1."""
+    lay = make(lens, hq, hkv, layout, fp8, seed=len(lens) + hq)
+    assert lay.max_ctx_len * len(lens) * hkv >= 32768
+    for _ in range(2):                                    # (the counters are as they were)
+        q, off, lse, w, tol = check_chunk(td, lay, new, causal, max_new=1)
+    got = td.chunk_weights(lay, q, off, lse, torch.zeros(len(lens), hkv, lay.max_ctx_len, device=DEV), max_new=1, causal=causal)
+    assert ((got.double() - w).abs() <= tol).all()
+    assert td.device_status() == binding.OK
+
+
+def test_single_tokens_where_there_are_more(td):
+    """max_new = 1 and two tokens: the first of them is worked out, with the positions that it sees."""
+    lay = make([30000, 9000], 4, 2, "paged", seed=5)
+    q = randn(6, 3, 4, D)
+    got = td.chunk_attn(lay, q, i32([0, 2, 3]), max_new=1)
+    want = td.chunk_attn(lay, q, i32([0, 2, 3]))
+    big = max(float(v.abs().max()) for _, v in lay.dense)
+    assert float((got - want)[[0, 2]].abs().max()) <= 2 * 2.0 ** -8 * big
+    lay.ctx_lens.copy_(i32([1, 0]))
+    lse = torch.zeros(3, 4, device=DEV)
+    got = td.chunk_attn(lay, q, i32([0, 2, 3]), max_new=1, lse=lse)
+    assert (got[[0, 2]] == 0).all() and (lse[[0, 2]] == -math.inf).all()
+
+
+def test_single_tokens_next_to_numbers_that_are_none(td):
+    lay = make([40000], 4, 2, "hnd", seed=7)
+    q, off = chunk_inputs(lay, [1])
+    want = td.chunk_attn(lay, q, off, max_new=1)
+    lay.k[0, 1, 20000, 3] = math.nan
+    lse = torch.zeros(1, 4, device=DEV)
+    got = td.chunk_attn(lay, q, off, max_new=1, lse=lse)
+    assert torch.isnan(got[:, 2:]).all() and torch.isnan(lse[:, 2:]).all() and torch.isfinite(lse[:, :2]).all()
+    assert float((got - want)[:, :2].abs().max()) <= 2.0 ** -8 * float(lay.dense[0][1].abs().max())
+    off[0] = 5
+    td.chunk_attn(lay, q, off, max_new=1)
+    assert td.device_status() == binding.ERR_INDEX
+
+
 def test_chunk_of_one_equals_the_decode_step(td):
     lay = make([900, 31, 4000], 16, 4, "paged", seed=3)
     q = randn(8, 3, 16, D)

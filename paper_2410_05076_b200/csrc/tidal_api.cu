@@ -1019,7 +1019,6 @@ tidal_status_t launch_maps(tidal_ctx* ctx, void (*kernel)(Args...), int grid, in
 
 // Scratch of the streaming kernel for single new tokens, two partial results of eight heads per CTA (see MODE_TOKENS): of one size for every shape,
 // so that it is allocated with the context.
-constexpr long long TOK_LEAST = 32768;                       // positions of all sequences and KV heads together
 constexpr size_t TOK_ROWS = (size_t)GRID_MAX * 2 * 8;
 constexpr size_t TOK_ML = TOK_ROWS * HEAD_DIM * sizeof(float), TOK_COUNTERS = TOK_ML + TOK_ROWS * sizeof(float2),
                  TOK_CURSORS = TOK_COUNTERS + (size_t)GRID_MAX * CTR_STRIDE * sizeof(int), TOK_TOTAL = TOK_CURSORS + (size_t)GRID_MAX * CTR_STRIDE * sizeof(int);
@@ -1879,11 +1878,9 @@ tidal_status_t tidal_chunk_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t 
     if (!out || ((uintptr_t)out & 15) || ((uintptr_t)lse & 3)) return TIDAL_ERR_INVALID;
     DeviceScope dev(ctx->device);
     if (!dev.ok) return TIDAL_ERR_CUDA;
-    // One token each: a matrix product of 128 rows would be empty but for one group of heads, and the cache streams at memory speed through
-    // the decode kernels (64 sequences of up to 16384: 341 us, 595 as a chunk; 131072: 83 and 139). A short cache by the cluster's CTAs instead (4103 positions of 2 heads:
-    // 14 us, 18 through the pool of tiles).
-    const long long cached = (long long)kv->batch * kv->num_kv_heads * kv->max_ctx_len;
-    if (max_new == 1 && window == 0 && cached >= TOK_LEAST) return run_tokens(ctx, kv, num_tokens, q, q_stride, q_offsets, causal != 0, out, lse, (cudaStream_t)stream);
+    // One token each: products of 128 rows would be empty but for one group of heads, and the cache streams at memory speed through
+    // the decode kernels (64 sequences of up to 16384: 346 us, 600 as a chunk; one of 33 positions: 7.6 and 8.7).
+    if (max_new == 1 && window == 0) return run_tokens(ctx, kv, num_tokens, q, q_stride, q_offsets, causal != 0, out, lse, (cudaStream_t)stream);
     ChunkParams p;
     std::memset(&p, 0, sizeof p);
     fill_block_cache(p.c, ctx, kv, 0);

@@ -23,7 +23,8 @@ struct EvictParams {
     int* new_lens;                                          // [batch]
 };
 
-constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32, EV_BINS = 2048, EV_MAX_CLUSTER = 16;
+constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32, EV_BINS = 2048, EV_MAX_CLUSTER = 8, EV_BATCH = 8, EV_TLOG = 10;
+constexpr int EV_MERGE = EV_BINS / EV_THREADS;               // counts that a thread merges, bins that it scans
 constexpr size_t EV_SMEM_MAX = 160 * 1024;
 
 // Order-preserving: larger weight, larger key; -0 as 0; not-a-number below everything. Kept positions are above everything.
@@ -48,7 +49,7 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
     int C, rank;
     asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(C));
     asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
-    const int row = blockIdx.x / C, b = row / p.heads;
+    const int clog = 31 - __clz(C), row = blockIdx.x >> clog, b = row / p.heads;          // (cluster sizes are powers of two)
     pdl_wait();
     pdl_trigger();
     const int n = max(min(read_global(p.ctx_lens + b), p.max_ctx), 0);
@@ -60,12 +61,18 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
         for (int i = rank * EV_THREADS + tid; i < n; i += C * EV_THREADS) kept[i] = i;
         return;                                             // (the whole cluster)
     }
-    const int slice = (n + C - 1) / C, lo = min(rank * slice, n), cnt = min(slice, n - lo);
+    const int slice = (n + C - 1) >> clog, lo = min(rank * slice, n), cnt = min(slice, n - lo);
     const float* const w = p.weights + (long long)row * p.stride + lo;
-    for (int i = tid; i < cnt; i += EV_THREADS) {
-        const int pos = lo + i;
-        const bool keep = pos < p.keep_first || pos >= n - p.keep_last;
-        ev_keys[i] = keep ? 0xffffffffu : evict_key(read_global(w + i));
+    for (int i0 = tid; i0 < cnt; i0 += EV_BATCH * EV_THREADS) {
+        float x[EV_BATCH];
+#pragma unroll
+        for (int u = 0; u < EV_BATCH; ++u) x[u] = i0 + u * EV_THREADS < cnt ? read_global(w + i0 + u * EV_THREADS) : 0.f;
+#pragma unroll
+        for (int u = 0; u < EV_BATCH; ++u) {
+            const int i = i0 + u * EV_THREADS, pos = lo + i;
+            const bool keep = pos < p.keep_first || pos >= n - p.keep_last;
+            if (i < cnt) ev_keys[i] = keep ? 0xffffffffu : evict_key(x[u]);
+        }
     }
     // the want-th largest key, digit by digit from the top
     uint32_t prefix = 0, known = 0;
@@ -76,17 +83,26 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
         const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048;
         for (int i = tid; i < bins; i += EV_THREADS) s_hist[i] = 0;
         __syncthreads();
-        for (int i = tid; i < cnt; i += EV_THREADS) {
-            const uint32_t key = ev_keys[i];
-            if ((key & known) == prefix) atomicAdd(&s_hist[(key >> shift) & (bins - 1)], 1);
+        for (int i0 = tid; i0 < cnt; i0 += EV_BATCH * EV_THREADS) {
+            uint32_t key[EV_BATCH];
+#pragma unroll
+            for (int u = 0; u < EV_BATCH; ++u) key[u] = i0 + u * EV_THREADS < cnt ? ev_keys[i0 + u * EV_THREADS] : 0u;
+#pragma unroll
+            for (int u = 0; u < EV_BATCH; ++u)
+                if (i0 + u * EV_THREADS < cnt && (key[u] & known) == prefix) atomicAdd(&s_hist[(key[u] >> shift) & (bins - 1)], 1);
         }
         if (C > 1) {
             cluster_arrive(); cluster_wait();
-            const int per = (bins + C - 1) / C;
-            for (int i = rank * per + tid; i < min((rank + 1) * per, bins); i += EV_THREADS) {
+            // this CTA's share of the bins, several threads to a bin with one or two CTAs' counts each
+            const int tlog = max(clog + EV_TLOG - (round == 2 ? 10 : 11), 0), team = 1 << tlog, sub = tid & (team - 1);
+            for (int own = tid >> tlog; own < bins >> clog; own += EV_THREADS >> tlog) {
+                const uint32_t at = (uint32_t)(rank * (bins >> clog) + own) * 4;
                 int sum = 0;
-                for (int r = 0; r < C; ++r) sum += ld_cluster(hist_addr + i * 4, r);
-                for (int r = 0; r < C; ++r) st_cluster_int(all_addr + i * 4, r, sum);
+#pragma unroll
+                for (int u = 0; u < EV_MERGE; ++u) if (sub + u * team < C) sum += ld_cluster(hist_addr + at, sub + u * team);
+                for (int sh = team >> 1; sh; sh >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, sh);
+#pragma unroll
+                for (int u = 0; u < EV_MERGE; ++u) if (sub + u * team < C) st_cluster_int(all_addr + at, sub + u * team, sum);
             }
             cluster_arrive(); cluster_wait();
         } else {
@@ -95,21 +111,23 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
             __syncthreads();
         }
         // bins from the top: thread t holds bins bins - 1 - 2 t and the one below it (bins - 1 - t in the last round)
-        const int per = bins / EV_THREADS;
-        int v[2], sum = 0;
-        for (int u = 0; u < 2; ++u) { v[u] = u < per ? s_all[bins - 1 - tid * per - u] : 0; sum += v[u]; }
+        const int per = bins >> EV_TLOG;
+        int v[EV_MERGE], sum = 0;
+#pragma unroll
+        for (int u = 0; u < EV_MERGE; ++u) { v[u] = u < per ? s_all[bins - 1 - tid * per - u] : 0; sum += v[u]; }
         int x = sum;
 #pragma unroll
         for (int sh = 1; sh < 32; sh <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, sh); if (lane >= sh) x += y; }
         if (lane == 31) s_part[warp] = x;
         __syncthreads();
-        int y = s_part[lane];
+        int y = lane < EV_WARPS ? s_part[lane] : 0;
 #pragma unroll
         for (int sh = 1; sh < 32; sh <<= 1) { const int z = __shfl_up_sync(0xffffffffu, y, sh); if (lane >= sh) y += z; }
         const int before = __shfl_sync(0xffffffffu, y, max(warp - 1, 0));
         int above = x - sum + (warp ? before : 0);
-        for (int u = 0; u < per; ++u) {
-            if (above < left && above + v[u] >= left) { s_found[0] = bins - 1 - tid * per - u; s_found[1] = left - above; }
+#pragma unroll
+        for (int u = 0; u < EV_MERGE; ++u) {
+            if (u < per && above < left && above + v[u] >= left) { s_found[0] = bins - 1 - tid * per - u; s_found[1] = left - above; }
             above += v[u];
         }
         __syncthreads();
@@ -129,7 +147,7 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
     __shared__ int s_more[EV_WARPS], s_same[EV_WARPS];
     if (lane == 0) { s_more[warp] = more; s_same[warp] = same; }
     __syncthreads();
-    int a = s_more[lane], e = s_same[lane];
+    int a = lane < EV_WARPS ? s_more[lane] : 0, e = lane < EV_WARPS ? s_same[lane] : 0;
 #pragma unroll
     for (int sh = 1; sh < 32; sh <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, a, sh), z = __shfl_up_sync(0xffffffffu, e, sh);
@@ -140,7 +158,12 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
     if (warp == 0) more_at = same_at = 0;
     if (C > 1) {
         cluster_arrive(); cluster_wait();
-        for (int r = 0; r < rank; ++r) { more_at += ld_cluster(mine_addr, r); same_at += ld_cluster(mine_addr + 4, r); }
+        int x = 0, y = 0;                                   // what the CTAs before this one keep
+        if (lane < rank) { x = ld_cluster(mine_addr, lane); y = ld_cluster(mine_addr + 4, lane); }
+#pragma unroll
+        for (int sh = 8; sh; sh >>= 1) { x += __shfl_xor_sync(0xffffffffu, x, sh); y += __shfl_xor_sync(0xffffffffu, y, sh); }
+        more_at += __shfl_sync(0xffffffffu, x, 0);
+        same_at += __shfl_sync(0xffffffffu, y, 0);
         cluster_arrive();                                   // (waited for at the end: nobody leaves while it is read)
     }
     for (int i = from; i < to; i += 32) {
@@ -208,17 +231,24 @@ __global__ void __launch_bounds__(GA_WARPS * 32) gather_copy_kernel(const Gather
     if (pair >= (long long)c.batch * c.Hkv) return;
     const int b = (int)(pair / c.Hkv), g = (int)(pair - (long long)b * c.Hkv);
     const int j0 = (int)(unit - pair * groups) * PER;
+    // (the list's entries are asked for together with the lengths that say which of them count)
+    const int* const list = p.kept + ((long long)b * p.heads + (p.heads > 1 ? g : 0)) * p.m;
+    int listed[GA_UNROLL];
+#pragma unroll
+    for (int u = 0; u < GA_UNROLL; ++u) {
+        const int j = j0 + u * ROWS + sub;
+        listed[u] = j < p.m ? read_global(list + j) : -1;
+    }
     const int cnt = min(gather_count(p, b), p.max_ctx), n = cached_len(c, b);
     if (j0 >= cnt) return;
     uint4 w[GA_UNROLL];
     uint8_t* to[GA_UNROLL];
 #pragma unroll
     for (int u = 0; u < GA_UNROLL; ++u) {
-        const int j = j0 + u * ROWS + sub;
+        const int j = j0 + u * ROWS + sub, pos = listed[u];
         to[u] = nullptr;
         if (j >= cnt) continue;
-        const int pos = gather_source(p, b, g, j, n);
-        if (pos < 0) continue;
+        if ((unsigned)pos >= (unsigned)n) { if (pos != -1) atomicOr(c.status, STATUS_BAD_INDEX); continue; }
         if (p.weights && piece == 0 && !value && (p.heads > 1 || g == 0)) {
             const long long row = (long long)b * p.heads + (p.heads > 1 ? g : 0);
             p.weights_out[row * p.wo_stride + j] = read_global(p.weights + row * p.w_stride + pos);

@@ -24,9 +24,11 @@ struct WeightParams {
     float* weights;
     long long stride;
     int heads;                                              // Hkv, or 1: all heads together
+    int strided;                                            // a CTA takes every gridDim.x-th tile instead of a run of them
 };
 
-constexpr int CW_THREADS = 320, CW_THREADS8 = 448, CW_RING = 3, CW_QRING = 3, CW_QRING8 = 2, CW_BUFS = 4;
+constexpr int CW_POLY = 6;                          // of sixteen pairs of weights, those whose exponentials are polynomials (every other one of the first)
+constexpr int CW_THREADS = 384, CW_THREADS8 = 512, CW_RING = 3, CW_QRING = 3, CW_QRING8 = 2, CW_BUFS = 4;
 constexpr size_t cw_smem(bool kv8) { return 1024 + (size_t)(CW_RING + (kv8 ? CW_QRING8 : CW_QRING)) * CH_MAT + (kv8 ? CH_RAW * CH_HALF : 0); }
 
 struct WeightShared {
@@ -34,16 +36,17 @@ struct WeightShared {
     uint32_t tmem;
     int gave_up;
     unsigned bad_pages[CH_TAGS];
-    alignas(16) float lse2[2][2][CH_TILE];                  // per warpgroup and turn: a row's log-sum-exp in base 2 (read four at a time), and what it sees
+    alignas(16) float lse2[2][2][CH_TILE];                  // per warpgroup and turn: minus a row's log-sum-exp in base 2 (read four at a time), and what it sees
     int2 sees[2][2][CH_TILE];
     float sums[2][CH_TILE];
 };
 
-// A walk over a CTA's tiles of positions: every gridDim.x-th of all sequences' and weight heads'.
+// A walk over a CTA's tiles of positions. Where a tile is one product, a run of all sequences' and weight heads' tiles, so that it meets few
+// sequences; where new tokens are many and the tiles they see are not alike, every gridDim.x-th.
 struct WeightWalk {
-    long long at, end;                                      // the tile's number among all, where its sequence ends
-    int b, ctx, tiles, first, begin, chunk;                 // first: position of the first new token; begin: its row; chunk: new tokens
-    int head, key0, g0, g1, t0, q0, q1;                     // the tile; KV heads; first query, products that see the tile
+    long long left;                                         // tiles to come
+    int step, b, ctx, tiles, first, begin, chunk;           // first: position of the first new token; begin: its row; chunk: new tokens
+    int head, tile, key0, g0, g1, t0, q0, q1;               // the tile; KV heads; first query, products that see the tile
 };
 
 __device__ __forceinline__ void weight_sequence(const WeightParams& p, WeightWalk& w, int b) {
@@ -54,28 +57,65 @@ __device__ __forceinline__ void weight_sequence(const WeightParams& p, WeightWal
     w.chunk = max(min(read_global(p.q_offsets + b + 1), p.num_tokens), w.begin) - w.begin;
     w.first = w.ctx - w.chunk;
 }
-__device__ __forceinline__ void weight_start(const WeightParams& p, WeightWalk& w) {
-    w.at = blockIdx.x;
-    weight_sequence(p, w, 0);
-    w.end = (long long)w.tiles * p.heads;
-}
-// The tile at w.at; false behind the last.
-__device__ __forceinline__ bool weight_tile(const WeightParams& p, WeightWalk& w) {
-    while (w.at >= w.end) {
-        if (w.b + 1 >= p.c.batch) return false;
+// From tile w.tile of head w.head on to one that is there (both may stand behind the sequence's last).
+__device__ __forceinline__ void weight_settle(const WeightParams& p, WeightWalk& w) {
+    while (w.tile >= w.tiles) {
+        w.tile -= w.tiles;
+        if (++w.head < p.heads && w.tiles > 0) continue;
+        w.head = 0;
+        if (w.b + 1 >= p.c.batch) { w.left = 0; return; }
         weight_sequence(p, w, w.b + 1);
-        w.end += (long long)w.tiles * p.heads;
     }
-    const int i = (int)(w.at - (w.end - (long long)w.tiles * p.heads));
-    w.head = i / w.tiles;
-    w.key0 = (i - w.head * w.tiles) * CH_TILE;
+}
+// All lanes of a warp together.
+__device__ __forceinline__ void weight_start(const WeightParams& p, WeightWalk& w, int lane) {
+    long long all = 0;
+    for (int b0 = 0; b0 < p.c.batch; b0 += 32) {
+        int n = b0 + lane < p.c.batch ? (cached_len(p.c, b0 + lane) + CH_TILE - 1) / CH_TILE : 0;
+#pragma unroll
+        for (int sh = 16; sh; sh >>= 1) n += __shfl_xor_sync(0xffffffffu, n, sh);
+        all += n;
+    }
+    all *= p.heads;
+    long long at = blockIdx.x;
+    w.step = (int)gridDim.x;
+    w.left = at < all ? (all - at + w.step - 1) / w.step : 0;
+    if (!p.strided) {
+        at = all * blockIdx.x / gridDim.x;
+        w.left = all * (blockIdx.x + 1) / gridDim.x - at;
+        w.step = 1;
+    }
+    // the sequence it lies in: whole ones are passed 32 at a time
+    int b = 0;
+    for (int b0 = 0; b0 < p.c.batch; b0 += 32) {
+        const int n = b0 + lane < p.c.batch ? (cached_len(p.c, b0 + lane) + CH_TILE - 1) / CH_TILE * p.heads : 0;
+        int x = n;
+#pragma unroll
+        for (int sh = 1; sh < 32; sh <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, sh); if (lane >= sh) x += y; }
+        const unsigned over = __ballot_sync(0xffffffffu, x > at);
+        const int last = over ? __ffs(over) - 1 : 31;
+        b = min(b0 + last, p.c.batch - 1);
+        at -= __shfl_sync(0xffffffffu, over ? x - n : x, last);
+        if (over) break;
+    }
+    weight_sequence(p, w, b);
+    w.head = w.tiles > 0 ? (int)(at / w.tiles) : 0;
+    w.tile = (int)(at - (long long)w.head * w.tiles);
+}
+// The next tile; false behind the last.
+__device__ __forceinline__ bool weight_tile(const WeightParams& p, WeightWalk& w) {
+    if (w.left <= 0) return false;
+    weight_settle(p, w);
+    if (w.left <= 0) return false;
+    --w.left;
+    w.key0 = w.tile * CH_TILE;
     w.g0 = p.heads > 1 ? w.head : 0;
     w.g1 = p.heads > 1 ? w.head + 1 : p.c.Hkv;
     w.t0 = p.last > 0 ? max(w.chunk - p.last, 0) : 0;
     const int from = w.first + w.t0, n = w.chunk - w.t0;     // position of the first query that counts, how many
     w.q0 = 0;
-    w.q1 = (n + p.tile_tokens - 1) / p.tile_tokens;
-    if (p.causal) w.q0 = max(w.key0 - from, 0) / p.tile_tokens;
+    w.q1 = n <= p.tile_tokens ? (n > 0) : (n + p.tile_tokens - 1) / p.tile_tokens;
+    if (p.causal && w.key0 > from) w.q0 = (w.key0 - from) / p.tile_tokens;
     if (p.window > 0) {
         const long long last = (long long)w.key0 + CH_TILE - 1 + p.window - 1 - from;      // the last query whose window reaches the tile
         w.q1 = last < 0 ? 0 : (int)min((long long)w.q1, last / p.tile_tokens + 1);
@@ -116,14 +156,15 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
     const int G = p.c.G, tt = p.tile_tokens;
     bool ok = true;
     WeightWalk w;
-    weight_start(p, w);
+    weight_start(p, w, lane);
 
     if (warp < 8) {
         // ---- sums ----
         const int s = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        int step = 0, tile = 0, turn = 0, item = 0;          // products and key tiles so far, own turns, joined tiles
-        for (; ok && weight_tile(p, w); w.at += gridDim.x) {
+        int step = 0, tile = 0, turn = 0, item = 0;          // products and key tiles so far, own fillings, joined tiles
+        long long filled = -1;                              // the queries whose sums are in shared memory
+        for (; ok && weight_tile(p, w); w.tile += w.step) {
             const int key = w.key0 + row, steps = (w.q1 - w.q0) * (w.g1 - w.g0), first_step = step;
             float acc = 0.f;
             for (int g = w.g0; g < w.g1 && ok; ++g) {
@@ -133,44 +174,49 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                     const int t = w.t0 + q * tt, rows = min(tt, w.chunk - t) * G;      // first token, rows that count
                     const int buf = step % CW_BUFS, cols = (rows + 31) & ~31;
                     const float scale = p.scale_log2 * (KV8 && p.k_scale ? read_global(p.k_scale + g) : 1.f);
-                    float* const lse2 = sh.lse2[s][turn & 1];
-                    int2* const sees = sh.sees[s][turn & 1];
-                    ++turn;
-                    const int pos = w.first + t + row / G;
-                    const bool counts = row < rows;
-                    lse2[row] = counts ? read_global(p.lse + (long long)(w.begin + t + row / G) * p.c.Hq + g * G + row % G) * 1.4426950408889634f : 0.f;
-                    sees[row] = counts ? make_int2(p.window > 0 ? max(pos - p.window + 1, 0) : 0, p.causal ? min(pos + 1, w.ctx) : w.ctx) : make_int2(0, 0);
-                    asm volatile("bar.sync %0, 128;\n" ::"r"(1 + s) : "memory");
+                    const long long these = ((long long)w.b * p.c.Hkv + g) << 32 | q;
+                    if (these != filled) {                  // (a run of tiles has the same queries)
+                        filled = these;
+                        ++turn;
+                        const int pos = w.first + t + row / G;
+                        const bool counts = row < rows;
+                        sh.lse2[s][turn & 1][row] = counts ? read_global(p.lse + (long long)(w.begin + t + row / G) * p.c.Hq + g * G + row % G) * -1.4426950408889634f : 0.f;
+                        sh.sees[s][turn & 1][row] = counts ? make_int2(p.window > 0 ? max(pos - p.window + 1, 0) : 0, p.causal ? min(pos + 1, w.ctx) : w.ctx) : make_int2(0, 0);
+                        asm volatile("bar.sync %0, 128;\n" ::"r"(1 + s) : "memory");
+                    }
+                    const float* const lse2 = sh.lse2[s][turn & 1];
+                    const int2* const sees = sh.sees[s][turn & 1];
                     ok = bar_wait(smem_u32(&sh.d_full[buf]), (step / CW_BUFS) & 1, gave_up);
                     if (!ok) break;
                     tmem_fence_after();
-                    const bool all = rows == cols && (!p.causal || w.key0 + CH_TILE - 1 <= w.first + t) &&
-                                     (p.window <= 0 || w.first + t + (rows - 1) / G - p.window < w.key0);
+                    const bool all = (!p.causal || w.key0 + CH_TILE - 1 <= w.first + t) && (p.window <= 0 || w.first + t + (rows - 1) / G - p.window < w.key0);
+                    const f32pair scale2 = pair2(scale, scale);
                     for (int c = 0; c < cols; c += 32) {
                         uint32_t x[32];
                         __syncwarp();
                         tmem_ld32(tmem + lanes + buf * CH_TILE + c, x);
                         tmem_wait_ld();
                         tmem_loaded32(x);
-                        float sum0 = 0.f, sum1 = 0.f;
-                        if (all) {
+                        if (all && c + 32 <= rows) {
+                            f32pair sum0 = pair2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
                             for (int j = 0; j < 32; j += 4) {
                                 const float4 l = *reinterpret_cast<const float4*>(lse2 + c + j);
-                                sum0 += fast_exp2(fmaf(__uint_as_float(x[j]), scale, -l.x));
-                                sum1 += fast_exp2(fmaf(__uint_as_float(x[j + 1]), scale, -l.y));
-                                sum0 += fast_exp2(fmaf(__uint_as_float(x[j + 2]), scale, -l.z));
-                                sum1 += fast_exp2(fmaf(__uint_as_float(x[j + 3]), scale, -l.w));
+                                const f32pair a = fma2(pair2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), scale2, pair2(l.x, l.y));
+                                const f32pair b = fma2(pair2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), scale2, pair2(l.z, l.w));
+                                sum0 = add2(sum0, pair2(fast_exp2(half2(a, 0)), fast_exp2(half2(a, 1))));
+                                sum1 = add2(sum1, j % 32 < CW_POLY * 4 ? exp2_by_polynomial<5>(b) : pair2(fast_exp2(half2(b, 0)), fast_exp2(half2(b, 1))));
                             }
+                            sum0 = add2(sum0, sum1);
+                            part += half2(sum0, 0) + half2(sum0, 1);
                         } else {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) {
                                 const int2 range = sees[c + j];
-                                const float e = fast_exp2(fmaf(__uint_as_float(x[j]), scale, -lse2[c + j]));
-                                if (key >= range.x && key < range.y) sum0 += e;
+                                const float e = fast_exp2(fmaf(__uint_as_float(x[j]), scale, lse2[c + j]));
+                                if (key >= range.x && key < range.y) part += e;
                             }
                         }
-                        part += sum0 + sum1;
                     }
                     tmem_fence_before();
                     __syncwarp();
@@ -197,49 +243,71 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
             }
         }
     } else if (warp == 8) {
-        // ---- products ----
-        if (lane == 0) {
-            int step = 0, tile = 0;
-            for (; ok && weight_tile(p, w); w.at += gridDim.x)
-                for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g, ++tile) {
-                    const int ks = tile % CW_RING;
-                    ok = bar_wait(smem_u32(&sh.k_full[ks]), (tile / CW_RING) & 1, gave_up);
-                    for (int q = w.q0; q < w.q1 && ok; ++q, ++step) {
-                        const int qs = step % QRING, buf = step % CW_BUFS;
-                        const int rows = min(tt, w.chunk - w.t0 - q * tt) * G, cols = (rows + 31) & ~31;
-                        ok = bar_wait(smem_u32(&sh.q_full[qs]), (step / QRING) & 1, gave_up) &&
-                             (step < CW_BUFS || bar_wait(smem_u32(&sh.d_empty[buf]), (step / CW_BUFS - 1) & 1, gave_up));
-                        if (!ok) break;
-                        tmem_fence_after();
-                        const uint32_t a = k_ring + ks * CH_MAT, b = q_ring + qs * CH_MAT, shape = mma_shape(true, cols, false);
+        // ---- products: the whole warp walks, one lane issues (see chunk_attn_kernel) ----
+        const uint32_t d = uniform(tmem);
+        int step = 0, tile = 0, ks = 0, kp = 0, qs = QRING - 1, qp = 1;
+        long long there = -1;                               // the queries in slot qs
+        for (; ok && weight_tile(p, w); w.tile += w.step)
+            for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g, ++tile) {
+                ok = bar_wait(smem_u32(&sh.k_full[ks]), kp, gave_up);
+                for (int q = w.q0; q < w.q1 && ok; ++q, ++step) {
+                    const int buf = step % CW_BUFS;
+                    const int rows = min(tt, w.chunk - w.t0 - q * tt) * G, cols = (rows + 31) & ~31;
+                    const long long these = ((long long)w.b * p.c.Hkv + g) << 32 | q;
+                    const bool fresh = these != there;
+                    if (fresh) {
+                        if (there >= 0 && elected()) mma_commit(smem_u32(&sh.q_empty[qs]));
+                        __syncwarp();
+                        there = these;
+                        if (++qs == QRING) { qs = 0; qp ^= 1; }
+                    }
+                    ok = (!fresh || bar_wait(smem_u32(&sh.q_full[qs]), qp, gave_up)) &&
+                         (step < CW_BUFS || bar_wait(smem_u32(&sh.d_empty[buf]), (step / CW_BUFS - 1) & 1, gave_up));
+                    if (!ok) break;
+                    tmem_fence_after();
+                    const uint64_t a = smem_matrix(k_ring + ks * CH_MAT, 16), b = smem_matrix(q_ring + qs * CH_MAT, 16);
+                    const uint32_t shape = mma_shape(true, uniform(cols), false);
+                    if (elected()) {
 #pragma unroll
                         for (int kk = 0; kk < 8; ++kk) {
-                            const uint32_t off = (kk >> 2) * CH_HALF + (kk & 3) * 32;
-                            mma_ss(tmem + buf * CH_TILE, smem_matrix(a + off, 16), smem_matrix(b + off, 16), shape, kk > 0);
+                            const uint32_t off = ((kk >> 2) * CH_HALF + (kk & 3) * 32) >> 4;
+                            mma_ss(d + buf * CH_TILE, a + off, b + off, shape, kk > 0);
                         }
                         mma_commit(smem_u32(&sh.d_full[buf]));
-                        mma_commit(smem_u32(&sh.q_empty[qs]));
                         if (q == w.q1 - 1) mma_commit(smem_u32(&sh.k_empty[ks]));
                     }
+                    __syncwarp();
                 }
-        }
-    } else if (warp == 9) {
-        // ---- copies in ----
-        int step = 0, tile = 0;
-        for (; ok && weight_tile(p, w); w.at += gridDim.x)
-            for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g, ++tile) {
-                int page = 0;
-                unsigned bad = 0;
-                if (p.c.paged) {
-                    page = p.c.num_pages;                   // (out of range: filled with zeros)
-                    const int blk = w.key0 / TILE + (lane & 7);
-                    if (blk * TILE < w.ctx) {
-                        page = read_global(p.c.page_table + (long long)w.b * p.c.max_pages + blk);
-                        if ((unsigned)page >= (unsigned)p.c.num_pages) { page = p.c.num_pages; bad = 1; }
-                    }
-                    bad = __ballot_sync(0xffffffffu, bad) & 0xffu;
-                    if (bad && lane == 0) atomicOr(p.c.status, STATUS_BAD_PAGE);
+                if (++ks == CW_RING) { ks = 0; kp ^= 1; }
+            }
+    } else if (warp == 9 || warp == 10) {
+        // ---- keys in: two warps, a tile each in turn; the pages of a warp's next tile are looked up before it waits for this one's place ----
+        int tile = 0;                                       // of all (tile, KV head) so far
+        auto lookup = [&](unsigned& bad) {
+            int page = 0;
+            bad = 0;
+            if (p.c.paged) {
+                page = p.c.num_pages;                       // (out of range: filled with zeros)
+                const int blk = w.key0 / TILE + (lane & 7);
+                if (blk * TILE < w.ctx) {
+                    page = read_global(p.c.page_table + (long long)w.b * p.c.max_pages + blk);
+                    if ((unsigned)page >= (unsigned)p.c.num_pages) { page = p.c.num_pages; bad = 1; }
                 }
+            }
+            return page;
+        };
+        bool more = weight_tile(p, w);
+        unsigned bad = 0;
+        int page = more ? lookup(bad) : 0;
+        while (more && ok) {
+            const int b = w.b, key0 = w.key0, g0 = w.g0, g1 = w.q0 < w.q1 ? w.g1 : w.g0, here = page;
+            const unsigned skip = __ballot_sync(0xffffffffu, bad) & 0xffu;
+            if (skip && lane == 0) atomicOr(p.c.status, STATUS_BAD_PAGE);
+            w.tile += w.step;
+            more = weight_tile(p, w);
+            if (more) page = lookup(bad);
+            for (int g = g0; g < g1 && ok; ++g, ++tile) {
+                if ((tile & 1) != warp - 9) continue;
                 const int slot = KV8 ? tile % CH_RAW : tile % CW_RING;
                 if constexpr (KV8) { if (tile >= CH_RAW) ok = bar_wait(smem_u32(&sh.raw_empty[slot]), (tile / CH_RAW - 1) & 1, gave_up); }
                 else { if (tile >= CW_RING) ok = bar_wait(smem_u32(&sh.k_empty[slot]), (tile / CW_RING - 1) & 1, gave_up); }
@@ -247,7 +315,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                 if (!ok) break;
                 const uint32_t dst = KV8 ? raw + slot * CH_HALF : k_ring + slot * CH_MAT, bar = smem_u32(KV8 ? &sh.raw_full[slot] : &sh.k_full[slot]);
                 if (lane == 0) {
-                    sh.bad_pages[tile % CH_TAGS] = bad;
+                    sh.bad_pages[tile % CH_TAGS] = skip;
                     bar_expect(bar, KV8 ? CH_HALF : CH_MAT);
                 }
                 __syncwarp();
@@ -255,27 +323,38 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                 if (p.c.paged) {
                     if (lane < 8 * HALVES)
                         tma_load4(dst + (lane >> 3) * CH_HALF + (lane & 7) * 2048, &k_map, bar, (lane >> 3) * 64, 0, g * p.head_mul,
-                                  page * p.page_mul + (page == p.c.num_pages && !p.page_mul ? 1 : 0));
+                                  here * p.page_mul + (here == p.c.num_pages && !p.page_mul ? 1 : 0));
                 } else if (lane < HALVES) {
-                    tma_load4(dst + lane * CH_HALF, &k_map, bar, lane * 64, w.key0, g * p.head_mul, w.b * p.batch_mul);
+                    tma_load4(dst + lane * CH_HALF, &k_map, bar, lane * 64, key0, g * p.head_mul, b * p.batch_mul);
                 }
-                for (int q = w.q0; q < w.q1 && ok; ++q, ++step) {
-                    const int qs = step % QRING;
-                    if (step >= QRING) ok = bar_wait(smem_u32(&sh.q_empty[qs]), (step / QRING - 1) & 1, gave_up);
-                    ok = __all_sync(0xffffffffu, ok);
+            }
+        }
+    } else if (warp == 11) {
+        // ---- queries in, unless they are those of the product before ----
+        int n = 0;
+        long long there = -1;
+        for (; ok && weight_tile(p, w); w.tile += w.step)
+            for (int g = w.g0; g < w.g1 && ok; ++g)
+                for (int q = w.q0; q < w.q1 && ok; ++q) {
+                    const long long these = ((long long)w.b * p.c.Hkv + g) << 32 | q;
+                    if (these == there) continue;
+                    there = these;
+                    const int qs = n % QRING;
+                    if (n >= QRING) ok = bar_wait(smem_u32(&sh.q_empty[qs]), (n / QRING - 1) & 1, gave_up);
                     if (!ok) break;
-                    if (lane == 0) {
+                    if (elected()) {
                         bar_expect(smem_u32(&sh.q_full[qs]), 2 * G * tt * 128);
                         for (int h = 0; h < 2; ++h)
                             tma_load3(q_ring + qs * CH_MAT + h * CH_HALF, &q_map, smem_u32(&sh.q_full[qs]), h * 64, g * G, w.begin + w.t0 + q * tt);
                     }
+                    __syncwarp();
+                    ++n;
                 }
-            }
     } else if (KV8) {
         // ---- codes to bf16 ----
-        const int l = tid - 320;
+        const int l = tid - 384;
         int tile = 0;
-        for (; ok && weight_tile(p, w); w.at += gridDim.x)
+        for (; ok && weight_tile(p, w); w.tile += w.step)
             for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g, ++tile) {
                 const int rs = tile % CH_RAW, slot = tile % CW_RING;
                 ok = bar_wait(smem_u32(&sh.raw_full[rs]), (tile / CH_RAW) & 1, gave_up) &&

@@ -4,8 +4,8 @@
 //
 // A persistent CTA takes tiles of 128 positions one after the other: S^T = K Q^T into TMEM, positions as rows, so that a thread
 // owns a position and adds up along its row in registers; no atomics, the same sum in the same order every time. Keys are
-// read once. Two warpgroups take the products in turn (four accumulators in TMEM), so that the exponentials of one run beside the products and
-// loads of the next. Bound by memory where a sequence has few new tokens, by the exponentials (16 a clock and SM) where it has many.
+// read once. Two pairs of warpgroups take the tiles in turn, a pair's warpgroups its products (an accumulator in TMEM each), so that the
+// exponentials of four run beside the products and loads of the next. Bound by memory where a sequence has few new tokens, by the exponentials (16 a clock and SM) where it has many.
 #pragma once
 
 #include "chunk_kernels.cuh"
@@ -27,8 +27,7 @@ struct WeightParams {
     int strided;                                            // a CTA takes every gridDim.x-th tile instead of a run of them
 };
 
-constexpr int CW_POLY = 6;                          // of sixteen pairs of weights, those whose exponentials are polynomials (every other one of the first)
-constexpr int CW_THREADS = 384, CW_THREADS8 = 512, CW_RING = 3, CW_QRING = 3, CW_QRING8 = 2, CW_BUFS = 4;
+constexpr int CW_THREADS = 640, CW_THREADS8 = 768, CW_RING = 3, CW_QRING = 3, CW_QRING8 = 2, CW_BUFS = 4;
 constexpr size_t cw_smem(bool kv8) { return 1024 + (size_t)(CW_RING + (kv8 ? CW_QRING8 : CW_QRING)) * CH_MAT + (kv8 ? CH_RAW * CH_HALF : 0); }
 
 struct WeightShared {
@@ -36,9 +35,9 @@ struct WeightShared {
     uint32_t tmem;
     int gave_up;
     unsigned bad_pages[CH_TAGS];
-    alignas(16) float lse2[2][2][CH_TILE];                  // per warpgroup and turn: minus a row's log-sum-exp in base 2 (read four at a time), and what it sees
-    int2 sees[2][2][CH_TILE];
-    float sums[2][CH_TILE];
+    alignas(16) float lse2[4][2][CH_TILE];                  // per warpgroup and turn: minus a row's log-sum-exp in base 2 (read four at a time), and what it sees
+    int2 sees[4][2][CH_TILE];
+    float sums[2][2][CH_TILE];                              // per pair: the second warpgroup's part of a tile
 };
 
 // A walk over a CTA's tiles of positions. Where a tile is one product, a run of all sequences' and weight heads' tiles, so that it meets few
@@ -46,7 +45,7 @@ struct WeightShared {
 struct WeightWalk {
     long long left;                                         // tiles to come
     int step, b, ctx, tiles, first, begin, chunk;           // first: position of the first new token; begin: its row; chunk: new tokens
-    int head, tile, key0, g0, g1, t0, q0, q1;               // the tile; KV heads; first query, products that see the tile
+    int head, tile, key0, g0, g1, t0, q0, q1, all_q;        // the tile; KV heads; first query, products that see the tile, products of the sequence
 };
 
 __device__ __forceinline__ void weight_sequence(const WeightParams& p, WeightWalk& w, int b) {
@@ -115,6 +114,7 @@ __device__ __forceinline__ bool weight_tile(const WeightParams& p, WeightWalk& w
     const int from = w.first + w.t0, n = w.chunk - w.t0;     // position of the first query that counts, how many
     w.q0 = 0;
     w.q1 = n <= p.tile_tokens ? (n > 0) : (n + p.tile_tokens - 1) / p.tile_tokens;
+    w.all_q = w.q1;
     if (p.causal && w.key0 > from) w.q0 = (w.key0 - from) / p.tile_tokens;
     if (p.window > 0) {
         const long long last = (long long)w.key0 + CH_TILE - 1 + p.window - 1 - from;      // the last query whose window reaches the tile
@@ -158,21 +158,25 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
     WeightWalk w;
     weight_start(p, w, lane);
 
-    if (warp < 8) {
+    if (warp < 16) {
         // ---- sums ----
-        const int s = warp >> 2, row = tid & 127;
+        const int wg = warp >> 2, pair = wg >> 1, s = wg & 1, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        int step = 0, tile = 0, turn = 0, item = 0;          // products and key tiles so far, own fillings, joined tiles
+        int step = 0, tile = 0, turn = 0, item = 0, count = 0;           // the pair's products, key tiles of all, own fillings, the pair's joined tiles, tiles of positions
         long long filled = -1;                              // the queries whose sums are in shared memory
         for (; ok && weight_tile(p, w); w.tile += w.step) {
             const int key = w.key0 + row, steps = (w.q1 - w.q0) * (w.g1 - w.g0), first_step = step;
             float acc = 0.f;
+            if ((count++ & 1) != pair) {                    // the other pair's
+                tile += w.q1 > w.q0 ? w.g1 - w.g0 : 0;
+                continue;
+            }
             for (int g = w.g0; g < w.g1 && ok; ++g) {
                 float part = 0.f;
                 for (int q = w.q0; q < w.q1 && ok; ++q, ++step) {
                     if ((step & 1) != s) continue;
                     const int t = w.t0 + q * tt, rows = min(tt, w.chunk - t) * G;      // first token, rows that count
-                    const int buf = step % CW_BUFS, cols = (rows + 31) & ~31;
+                    const int buf = wg, cols = (rows + 31) & ~31;
                     const float scale = p.scale_log2 * (KV8 && p.k_scale ? read_global(p.k_scale + g) : 1.f);
                     const long long these = ((long long)w.b * p.c.Hkv + g) << 32 | q;
                     if (these != filled) {                  // (a run of tiles has the same queries)
@@ -180,13 +184,13 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                         ++turn;
                         const int pos = w.first + t + row / G;
                         const bool counts = row < rows;
-                        sh.lse2[s][turn & 1][row] = counts ? read_global(p.lse + (long long)(w.begin + t + row / G) * p.c.Hq + g * G + row % G) * -1.4426950408889634f : 0.f;
-                        sh.sees[s][turn & 1][row] = counts ? make_int2(p.window > 0 ? max(pos - p.window + 1, 0) : 0, p.causal ? min(pos + 1, w.ctx) : w.ctx) : make_int2(0, 0);
-                        asm volatile("bar.sync %0, 128;\n" ::"r"(1 + s) : "memory");
+                        sh.lse2[wg][turn & 1][row] = counts ? read_global(p.lse + (long long)(w.begin + t + row / G) * p.c.Hq + g * G + row % G) * -1.4426950408889634f : 0.f;
+                        sh.sees[wg][turn & 1][row] = counts ? make_int2(p.window > 0 ? max(pos - p.window + 1, 0) : 0, p.causal ? min(pos + 1, w.ctx) : w.ctx) : make_int2(0, 0);
+                        asm volatile("bar.sync %0, 128;\n" ::"r"(1 + wg) : "memory");
                     }
-                    const float* const lse2 = sh.lse2[s][turn & 1];
-                    const int2* const sees = sh.sees[s][turn & 1];
-                    ok = bar_wait(smem_u32(&sh.d_full[buf]), (step / CW_BUFS) & 1, gave_up);
+                    const float* const lse2 = sh.lse2[wg][turn & 1];
+                    const int2* const sees = sh.sees[wg][turn & 1];
+                    ok = bar_wait(smem_u32(&sh.d_full[buf]), (step >> 1) & 1, gave_up);
                     if (!ok) break;
                     tmem_fence_after();
                     const bool all = (!p.causal || w.key0 + CH_TILE - 1 <= w.first + t) && (p.window <= 0 || w.first + t + (rows - 1) / G - p.window < w.key0);
@@ -205,7 +209,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                                 const f32pair a = fma2(pair2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), scale2, pair2(l.x, l.y));
                                 const f32pair b = fma2(pair2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), scale2, pair2(l.z, l.w));
                                 sum0 = add2(sum0, pair2(fast_exp2(half2(a, 0)), fast_exp2(half2(a, 1))));
-                                sum1 = add2(sum1, j % 32 < CW_POLY * 4 ? exp2_by_polynomial<5>(b) : pair2(fast_exp2(half2(b, 0)), fast_exp2(half2(b, 1))));
+                                sum1 = add2(sum1, pair2(fast_exp2(half2(b, 0)), fast_exp2(half2(b, 1))));
                             }
                             sum0 = add2(sum0, sum1);
                             part += half2(sum0, 0) + half2(sum0, 1);
@@ -230,9 +234,18 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
             if (!ok) break;
             bool writes = steps == 0 ? s == 0 : (first_step & 1) == s;
             if (steps > 1) {
-                if (s == 1) sh.sums[item & 1][row] = acc;
-                asm volatile("bar.sync 3, 256;\n" ::: "memory");
-                if (s == 0) acc += sh.sums[item & 1][row];
+                // the second warpgroup leaves its part and goes on, the first adds it (barriers 5 + 4 pair: a part is there; two further on: its
+                // place is free again)
+                const int there = 5 + 4 * pair + (item & 1), free = there + 2;
+                if (s == 1) {
+                    if (item >= 2) asm volatile("bar.sync %0, 256;\n" ::"r"(free) : "memory");
+                    sh.sums[pair][item & 1][row] = acc;
+                    asm volatile("bar.arrive %0, 256;\n" ::"r"(there) : "memory");
+                } else {
+                    asm volatile("bar.sync %0, 256;\n" ::"r"(there) : "memory");
+                    acc += sh.sums[pair][item & 1][row];
+                    asm volatile("bar.arrive %0, 256;\n" ::"r"(free) : "memory");
+                }
                 writes = s == 0;
                 ++item;
             }
@@ -242,27 +255,31 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                 *to = acc;
             }
         }
-    } else if (warp == 8) {
+    } else if (warp == 16) {
         // ---- products: the whole warp walks, one lane issues (see chunk_attn_kernel) ----
         const uint32_t d = uniform(tmem);
-        int step = 0, tile = 0, ks = 0, kp = 0, qs = QRING - 1, qp = 1;
-        long long there = -1;                               // the queries in slot qs
-        for (; ok && weight_tile(p, w); w.tile += w.step)
-            for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g, ++tile) {
+        int steps[2] = {0, 0}, count = 0, ks = 0, kp = 0;
+        unsigned held = 0, qp = 0;                          // slots of queries that stay, parities of the slots' next fillings
+        long long group = -1;
+        for (; ok && weight_tile(p, w); w.tile += w.step) {
+            const int pair = count++ & 1;
+            for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g) {
+                if (const long long these = (long long)w.b * p.c.Hkv + g; these != group) {
+                    if (elected())
+                        for (int i = 0; i < QRING; ++i) if ((held >> i) & 1) mma_commit(smem_u32(&sh.q_empty[i]));
+                    __syncwarp();
+                    held = 0;
+                    group = these;
+                }
                 ok = bar_wait(smem_u32(&sh.k_full[ks]), kp, gave_up);
-                for (int q = w.q0; q < w.q1 && ok; ++q, ++step) {
-                    const int buf = step % CW_BUFS;
+                for (int q = w.q0; q < w.q1 && ok; ++q) {
+                    const int step = pair ? steps[1]++ : steps[0]++, buf = 2 * pair + (step & 1);
                     const int rows = min(tt, w.chunk - w.t0 - q * tt) * G, cols = (rows + 31) & ~31;
-                    const long long these = ((long long)w.b * p.c.Hkv + g) << 32 | q;
-                    const bool fresh = these != there;
-                    if (fresh) {
-                        if (there >= 0 && elected()) mma_commit(smem_u32(&sh.q_empty[qs]));
-                        __syncwarp();
-                        there = these;
-                        if (++qs == QRING) { qs = 0; qp ^= 1; }
-                    }
-                    ok = (!fresh || bar_wait(smem_u32(&sh.q_full[qs]), qp, gave_up)) &&
-                         (step < CW_BUFS || bar_wait(smem_u32(&sh.d_empty[buf]), (step / CW_BUFS - 1) & 1, gave_up));
+                    // Queries have the slot of their number; where a sequence and head has no more than there are slots they stay while it does.
+                    const int qs = q % QRING;
+                    const bool stay = w.all_q <= QRING, fresh = !((held >> qs) & 1);
+                    ok = (!fresh || bar_wait(smem_u32(&sh.q_full[qs]), (qp >> qs) & 1, gave_up)) &&
+                         (step < 2 || bar_wait(smem_u32(&sh.d_empty[buf]), ((step >> 1) - 1) & 1, gave_up));
                     if (!ok) break;
                     tmem_fence_after();
                     const uint64_t a = smem_matrix(k_ring + ks * CH_MAT, 16), b = smem_matrix(q_ring + qs * CH_MAT, 16);
@@ -274,13 +291,17 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                             mma_ss(d + buf * CH_TILE, a + off, b + off, shape, kk > 0);
                         }
                         mma_commit(smem_u32(&sh.d_full[buf]));
+                        if (!stay) mma_commit(smem_u32(&sh.q_empty[qs]));
                         if (q == w.q1 - 1) mma_commit(smem_u32(&sh.k_empty[ks]));
                     }
                     __syncwarp();
+                    if (fresh) qp ^= 1u << qs;
+                    if (stay) held |= 1u << qs;
                 }
                 if (++ks == CW_RING) { ks = 0; kp ^= 1; }
             }
-    } else if (warp == 9 || warp == 10) {
+        }
+    } else if (warp == 17 || warp == 18) {
         // ---- keys in: two warps, a tile each in turn; the pages of a warp's next tile are looked up before it waits for this one's place ----
         int tile = 0;                                       // of all (tile, KV head) so far
         auto lookup = [&](unsigned& bad) {
@@ -307,7 +328,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
             more = weight_tile(p, w);
             if (more) page = lookup(bad);
             for (int g = g0; g < g1 && ok; ++g, ++tile) {
-                if ((tile & 1) != warp - 9) continue;
+                if ((tile & 1) != warp - 17) continue;
                 const int slot = KV8 ? tile % CH_RAW : tile % CW_RING;
                 if constexpr (KV8) { if (tile >= CH_RAW) ok = bar_wait(smem_u32(&sh.raw_empty[slot]), (tile / CH_RAW - 1) & 1, gave_up); }
                 else { if (tile >= CW_RING) ok = bar_wait(smem_u32(&sh.k_empty[slot]), (tile / CW_RING - 1) & 1, gave_up); }
@@ -329,18 +350,20 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                 }
             }
         }
-    } else if (warp == 11) {
-        // ---- queries in, unless they are those of the product before ----
-        int n = 0;
-        long long there = -1;
+    } else if (warp == 19) {
+        // ---- queries in, unless they are there ----
+        unsigned held = 0, used = 0, parity = 0;
+        long long group = -1;
         for (; ok && weight_tile(p, w); w.tile += w.step)
-            for (int g = w.g0; g < w.g1 && ok; ++g)
+            for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g) {
+                if (const long long these = (long long)w.b * p.c.Hkv + g; these != group) { group = these; held = 0; }
                 for (int q = w.q0; q < w.q1 && ok; ++q) {
-                    const long long these = ((long long)w.b * p.c.Hkv + g) << 32 | q;
-                    if (these == there) continue;
-                    there = these;
-                    const int qs = n % QRING;
-                    if (n >= QRING) ok = bar_wait(smem_u32(&sh.q_empty[qs]), (n / QRING - 1) & 1, gave_up);
+                    const int qs = q % QRING;
+                    if ((held >> qs) & 1) continue;
+                    if ((used >> qs) & 1) {
+                        ok = bar_wait(smem_u32(&sh.q_empty[qs]), (parity >> qs) & 1, gave_up);
+                        parity ^= 1u << qs;
+                    }
                     if (!ok) break;
                     if (elected()) {
                         bar_expect(smem_u32(&sh.q_full[qs]), 2 * G * tt * 128);
@@ -348,11 +371,13 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                             tma_load3(q_ring + qs * CH_MAT + h * CH_HALF, &q_map, smem_u32(&sh.q_full[qs]), h * 64, g * G, w.begin + w.t0 + q * tt);
                     }
                     __syncwarp();
-                    ++n;
+                    used |= 1u << qs;
+                    if (w.all_q <= QRING) held |= 1u << qs;
                 }
+            }
     } else if (KV8) {
         // ---- codes to bf16 ----
-        const int l = tid - 384;
+        const int l = tid - 640;
         int tile = 0;
         for (; ok && weight_tile(p, w); w.tile += w.step)
             for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g, ++tile) {

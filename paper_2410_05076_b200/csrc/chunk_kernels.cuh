@@ -143,6 +143,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {         // no
 struct ChunkParams {
     BlockCache c;
     int page_mul, batch_mul, head_mul;                      // 0 where a coordinate has no stride
+    const __nv_bfloat16* q;
+    long long q_stride;
     const int* q_offsets;                                   // [batch + 1]
     int num_tokens, tile_tokens;                            // tokens per stream (128 / G)
     int q_tiles;                                            // bound of the CTA tiles of all sequences together
@@ -170,6 +172,7 @@ struct ChunkShared {
     unsigned long long q_full, full[5], empty[5], raw_full[2], raw_empty[2], s_full[2], p_most[2], p_full[2], o_done[2];
     uint32_t tmem;
     int gave_up, seq, tile;
+    int odd[2];                                             // per stream: a tile that not all rows see whole has values that are not finite
     unsigned bad_pages[CH_TAGS];                            // per tile, bit i: its i-th page is not one
 };
 // Partial results take the operands' place: 2 x 128 rows of 128 outputs, then their maxima and sums.
@@ -252,6 +255,93 @@ __device__ __forceinline__ void chunk_find(const ChunkParams& p, int want, int l
     }
 }
 
+// Whether eight 16-bit numbers are all finite.
+template <bool HALF>
+__device__ __forceinline__ bool all_finite(const uint32_t (&x)[4]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top |= (x[j] & (HALF ? 0x7c007c00u : 0x7f807f80u)) + (HALF ? 0x04000400u : 0x00800080u);       // a full exponent carries
+    return !(top & 0x80008000u);
+}
+
+// One row over a stream's tiles without matrix products: weights of zero times infinity do not come up where positions are masked. A warp together,
+// four channels per lane; (m, l, o) as the products give them. Slow (a row at a time), and for rows next to values that are not finite.
+template <bool KV8>
+__device__ __forceinline__ void chunk_row_plain(const ChunkParams& p, const ChunkWork& w, int s, int token, int head, int lane, float scale, float (&o)[4], float& m, float& l) {
+    constexpr int ESZ = KV8 ? 1 : 2;
+    auto four = [&](const uint8_t* at, float (&x)[4]) {     // four channels of a cached row
+        uint32_t a, b;
+        if constexpr (KV8) {
+            e4m3x4_to_f16x2x2(read_global(reinterpret_cast<const uint32_t*>(at + lane * 4)), a, b);
+            a = f16x2_to_bf16x2(a);
+            b = f16x2_to_bf16x2(b);
+        } else {
+            const uint2 y = read_global(reinterpret_cast<const uint2*>(at + lane * 8));
+            a = y.x; b = y.y;
+        }
+        x[0] = __uint_as_float(a << 16); x[1] = __uint_as_float(a & 0xffff0000u); x[2] = __uint_as_float(b << 16); x[3] = __uint_as_float(b & 0xffff0000u);
+    };
+    const uint2 y = read_global(reinterpret_cast<const uint2*>(p.q + (long long)(w.q_row + token - w.t0) * p.q_stride + head * HEAD_DIM + lane * 4));
+    const float q[4] = {__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xffff0000u), __uint_as_float(y.y << 16), __uint_as_float(y.y & 0xffff0000u)};
+    const int pos = w.first + token, hi = p.causal ? min(pos + 1, w.ctx) : w.ctx, lo = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
+    m = -INFINITY; l = 0.f;
+    o[0] = o[1] = o[2] = o[3] = 0.f;
+    for (int i = 0; i < w.stream_tiles[s]; ++i) {
+        const int key0 = (w.tile0 + w.at(s, i)) * CH_TILE;
+        for (int key = max(key0, lo); key < min(key0 + CH_TILE, hi); ++key) {
+            long long row = (long long)w.b * p.c.stride_b + key * p.c.stride_pos;
+            if (p.c.paged) {
+                const int page = read_global(p.c.page_table + (long long)w.b * p.c.max_pages + key / TILE);
+                if ((unsigned)page >= (unsigned)p.c.num_pages) continue;
+                row = page * p.c.stride_page + key % TILE * p.c.stride_pos;
+            }
+            row = (row + w.g * p.c.stride_head) * ESZ;
+            float k[4], v[4];
+            four(p.c.k + row, k);
+            four(p.c.v + row, v);
+            float t = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
+#pragma unroll
+            for (int sh = 16; sh; sh >>= 1) t += __shfl_xor_sync(0xffffffffu, t, sh);
+            t *= scale;
+            if (t == -INFINITY) continue;
+            const float up = fmaxf(m, t), f = m == up ? 1.f : fast_exp2(m - up), e = fast_exp2(t - up);
+            m = up;
+            l = fmaf(l, f, e);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] = fmaf(o[c], f, e * v[c]);
+        }
+    }
+}
+
+// All rows of a stream in that way, a quarter per warp: results, or partial results where they are joined.
+template <bool KV8>
+__device__ __forceinline__ void chunk_rows_again(const ChunkParams& p, const ChunkShared& sh, uint32_t base, int rank, int ranks, int g, int s, int quarter, int lane) {
+    ChunkWork w;
+    chunk_work(p, sh, rank, ranks, g, w);
+    const bool joined = ranks > 1 || w.twin;
+    const int G = p.c.G, tt = p.tile_tokens;
+    const float scale = p.scale_log2 * (KV8 && p.k_scale ? read_global(p.k_scale + w.g) : 1.f), vs = KV8 && p.v_scale ? read_global(p.v_scale + w.g) : 1.f;
+    for (int i = 0; i < 32; ++i) {
+        const int r = quarter * 32 + i, token = w.t0 + (w.twin ? 0 : s * tt) + r / G, head = w.g * G + r % G;
+        if (r >= tt * G || token >= w.new_tokens) break;
+        float o[4], m, l;
+        chunk_row_plain<KV8>(p, w, s, token, head, lane, scale, o, m, l);
+        if (joined) {
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(base + ((s * CH_TILE + r) * 32 + (lane ^ i)) * 16), "f"(o[0]), "f"(o[1]), "f"(o[2]), "f"(o[3]) : "memory");
+            if (lane == 0) {
+                asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(base + CH_PART_MAX + (s * CH_TILE + r) * 4), "f"(m) : "memory");
+                asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(base + CH_PART_SUM + (s * CH_TILE + r) * 4), "f"(l) : "memory");
+            }
+            continue;
+        }
+        const long long at = (long long)(w.q_row + token - w.t0) * p.c.Hq + head;
+        const float inv = l != 0.f ? vs / l : 0.f;
+        if (p.out_bf16) *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at * HEAD_DIM + lane * 4) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+        else *reinterpret_cast<float4*>(p.out + at * HEAD_DIM + lane * 4) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+        if (lane == 0 && p.lse) p.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
 template <bool KV8>
 __global__ void __launch_bounds__(KV8 ? CH_THREADS8 : CH_THREADS, 1)
 chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
@@ -279,7 +369,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             bar_init(smem_u32(&sh.s_full[i]), 1); bar_init(smem_u32(&sh.p_most[i]), 4); bar_init(smem_u32(&sh.p_full[i]), 4);
             bar_init(smem_u32(&sh.o_done[i]), 1);
         }
-        sh.gave_up = 0;
+        sh.gave_up = sh.odd[0] = sh.odd[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     pdl_wait();
@@ -309,7 +399,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
 
     // Registers: the softmax warpgroups hold a row of scores each, the others need few. The shares add up to what the launch has.
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(KV8 ? 200 : 216));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(KV8 ? 208 : 216));
         // ---- softmax ----
         const int s = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
@@ -373,6 +463,20 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
 #pragma unroll
                 for (int j = 0; j < CH_TILE; j += 2) top = max3(top, __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
                 m = top == top ? top : -INFINITY;
+            }
+            if (partly) {
+                // A weight of zero times a value that is not finite would spoil rows that do not see it: such tiles are worked out again, without products.
+                const int item = 2 * tile + 1, slot = item % RING;
+                if (!bar_wait(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up)) break;
+                bool finite = true;
+                for (int k = tid & 127; k < min(w.ctx - key0, CH_TILE) * 8; k += 128)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t v[4];
+                        lds128(ring + slot * CH_MAT + h * CH_HALF + k * 16, v);
+                        finite = finite && all_finite<KV8>(v);
+                    }
+                if (!finite) sh.odd[s] = 1;
             }
             // Weights by the maximum so far, while this tile's own is looked for: it is raised, and the weights are worked out again, only
             // where that leaves one above 2^8. Whole tiles take some of the exponentials from the polynomial; where positions are masked all come
@@ -439,7 +543,13 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         // ---- results ----
         if (n > 0 && bar_wait(smem_u32(&sh.o_done[s]), 0, gave_up)) tmem_fence_after();
         const float vs = KV8 && p.v_scale ? read_global(p.v_scale + w.g) : 1.f;
-        if (!joined) {
+        __syncwarp();
+        asm volatile("bar.sync %0, 128;\n" ::"r"(1 + s) : "memory");
+        const bool again = *(volatile int*)&sh.odd[s];
+        if (joined && w.stream_tiles[1 - s] > 0) bar_wait(smem_u32(&sh.o_done[1 - s]), 0, gave_up);    // (partial results take the operands' place)
+        if (again) {
+            // (all rows of the stream, further down)
+        } else if (!joined) {
             const bool some = l != 0.f;                     // (a sum that is not a number is some)
             const float inv = some ? vs / l : 0.f;
             const long long at = ((long long)(w.q_row + token - w.t0) * p.c.Hq + head);
@@ -469,8 +579,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 }
             }
         } else {
-            // partial results to shared memory: the operands' place is free once every product of the CTA is done
-            if (w.stream_tiles[1 - s] > 0) bar_wait(smem_u32(&sh.o_done[1 - s]), 0, gave_up);
+            // partial results to shared memory
             asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(base + CH_PART_MAX + (s * CH_TILE + row) * 4), "f"(m == -INFINITY ? m : m * scale) : "memory");
             asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(base + CH_PART_SUM + (s * CH_TILE + row) * 4), "f"(l) : "memory");
             if (n > 0 && __any_sync(0xffffffffu, valid)) {
@@ -490,7 +599,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(KV8 ? 56 : 72));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(KV8 ? 48 : 72));
     }
     if (warp == 8) {
         // ---- products: the whole warp walks, one lane issues ----
@@ -685,6 +794,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         }
     }
     __syncwarp();
+    if (warp < 8 && *(volatile int*)&sh.odd[warp >> 2]) chunk_rows_again<KV8>(p, sh, base, rank, ranks, g, warp >> 2, warp & 3, lane);
 
     if (joined) {
         // ---- partial results of the streams and of the cluster's CTAs ----

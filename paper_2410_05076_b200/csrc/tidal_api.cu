@@ -1058,7 +1058,7 @@ bool prepare_prompt_kernels(tidal_ctx* ctx) {
     // the softmax warpgroups raise their registers within what the launch holds
     cudaFuncAttributes a;
     if (cudaFuncGetAttributes(&a, chunk_attn_kernel<false>) != cudaSuccess || a.numRegs * CH_THREADS < 256 * 216 + 128 * 72) return false;
-    if (cudaFuncGetAttributes(&a, chunk_attn_kernel<true>) != cudaSuccess || a.numRegs * CH_THREADS8 < 256 * 200 + 256 * 56) return false;
+    if (cudaFuncGetAttributes(&a, chunk_attn_kernel<true>) != cudaSuccess || a.numRegs * CH_THREADS8 < 256 * 208 + 256 * 48) return false;
     count_clusters(chunk_attn_kernel<false>, CH_THREADS, ch_smem<false>(), ctx->chunk_clusters[0]);
     count_clusters(chunk_attn_kernel<true>, CH_THREADS8, ch_smem<true>(), ctx->chunk_clusters[1]);
     count_clusters(evict_select_kernel, EV_THREADS, EV_SMEM_MAX / 2, ctx->evict_clusters);
@@ -1884,6 +1884,7 @@ tidal_status_t tidal_chunk_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t 
     ChunkParams p;
     std::memset(&p, 0, sizeof p);
     fill_block_cache(p.c, ctx, kv, 0);
+    p.q = (const __nv_bfloat16*)q; p.q_stride = num_tokens > 1 ? q_stride : 0;
     p.q_offsets = q_offsets; p.num_tokens = num_tokens; p.tile_tokens = CH_TILE / p.c.G;
     p.causal = causal != 0; p.window = window;
     p.scale_log2 = (kv->sm_scale > 0.f ? kv->sm_scale : 1.0f / std::sqrt((float)kv->head_dim)) * 1.4426950408889634f;

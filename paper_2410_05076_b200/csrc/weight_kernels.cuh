@@ -5,7 +5,9 @@
 // A persistent CTA takes tiles of 128 positions one after the other: S^T = K Q^T into TMEM, positions as rows, so that a thread
 // owns a position and adds up along its row in registers; no atomics, the same sum in the same order every time. Keys are
 // read once. Two pairs of warpgroups take the tiles in turn, a pair's warpgroups its products (an accumulator in TMEM each), so that the
-// exponentials of four run beside the products and loads of the next. Bound by memory where a sequence has few new tokens, by the exponentials (16 a clock and SM) where it has many.
+// exponentials of four run beside the products and loads of the next. Single tokens (64 sequences of up to 16384 in
+// pages: 265 us, 4.1 TB/s) are bound by the copies of 16 rows of 128 bytes, of which an SM takes 27 bytes a clock, and by the walk from tile to tile; many
+// queries (64 of 131072: 106 us) by the exponential unit, 16 a clock and SM.
 #pragma once
 
 #include "chunk_kernels.cuh"

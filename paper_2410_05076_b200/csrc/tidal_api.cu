@@ -1880,13 +1880,13 @@ tidal_status_t tidal_chunk_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t 
     if (!dev.ok) return TIDAL_ERR_CUDA;
     // One token each: products of 128 rows would be empty but for one group of heads, and the cache streams at memory speed through
     // the decode kernels (64 sequences of up to 16384: 346 us, 600 as a chunk; one of 33 positions: 7.6 and 8.7).
-    if (max_new == 1 && window == 0) return run_tokens(ctx, kv, num_tokens, q, q_stride, q_offsets, causal != 0, out, lse, (cudaStream_t)stream);
+    if (max_new == 1 && (window == 0 || window >= MAX_CTX)) return run_tokens(ctx, kv, num_tokens, q, q_stride, q_offsets, causal != 0, out, lse, (cudaStream_t)stream);
     ChunkParams p;
     std::memset(&p, 0, sizeof p);
     fill_block_cache(p.c, ctx, kv, 0);
     p.q = (const __nv_bfloat16*)q; p.q_stride = num_tokens > 1 ? q_stride : 0;
     p.q_offsets = q_offsets; p.num_tokens = num_tokens; p.tile_tokens = CH_TILE / p.c.G;
-    p.causal = causal != 0; p.window = window;
+    p.causal = causal != 0; p.window = window < MAX_CTX ? window : 0;        // (a window of the longest context hides nothing)
     p.scale_log2 = (kv->sm_scale > 0.f ? kv->sm_scale : 1.0f / std::sqrt((float)kv->head_dim)) * 1.4426950408889634f;
     const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3;
     if (fp8) { p.k_scale = kv->k_scale; p.v_scale = kv->v_scale; }
@@ -1926,7 +1926,7 @@ tidal_status_t tidal_chunk_weights(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32
     int most = max_new > 0 ? std::min(max_new, num_tokens) : num_tokens;
     if (last > 0) most = std::min(most, last);
     p.tile_tokens = std::min(CH_TILE / p.c.G, most);
-    p.causal = causal != 0; p.window = window; p.last = last;
+    p.causal = causal != 0; p.window = window < MAX_CTX ? window : 0; p.last = last;     // (a window of the longest context hides nothing)
     p.scale_log2 = (kv->sm_scale > 0.f ? kv->sm_scale : 1.0f / std::sqrt((float)kv->head_dim)) * 1.4426950408889634f;
     const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3;
     if (fp8) p.k_scale = kv->k_scale;

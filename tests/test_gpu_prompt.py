@@ -352,6 +352,20 @@ def test_chunk_rows_that_see_nothing(td):
     assert ((out[5:15].double() - ref[0]).abs() <= ref[3]).all()
 
 
+@pytest.mark.parametrize("window", [262143, 262144, 2 ** 31 - 1])
+def test_windows_beyond_every_context(td, window):
+    """Rows before position 0 among them: nothing wraps."""
+    lay = make([10, 700], 4, 2, "hnd", seed=1)
+    q = randn(3, 320, 4, D)
+    off, lse = i32([0, 20, 320]), torch.zeros(320, 4, device=DEV)
+    want, w = td.chunk_attn(lay, q, off, lse=lse), torch.zeros(2, 2, 700, device=DEV)
+    assert torch.equal(td.chunk_attn(lay, q, off, window=window), want)
+    td.chunk_weights(lay, q, off, lse, w)
+    assert torch.equal(td.chunk_weights(lay, q, off, lse, torch.zeros_like(w), window=window), w)
+    one = td.chunk_attn(lay, q[:2], i32([0, 1, 2]), max_new=1, window=window)
+    assert float((one - td.chunk_attn(lay, q[:2], i32([0, 1, 2]), max_new=1)).abs().max()) <= 2.0 ** -8 * 6
+
+
 def test_chunk_offsets_out_of_order_are_cut_and_reported(td):
     lay = make([40, 40, 40], 2, 1, "paged")
     q = randn(3, 30, 2, D)

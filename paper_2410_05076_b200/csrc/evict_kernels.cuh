@@ -19,18 +19,17 @@ struct EvictParams {
     long long stride;
     const int* ctx_lens;
     int max_ctx, heads, m, keep_first, keep_last;
-    int slice_max;                                          // keys that a CTA has room for
     int* kept;                                              // [batch][heads][m]
     int* new_lens;                                          // [batch]
 };
 
-constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32, EV_BINS = 2048, EV_MAX_CLUSTER = 8, EV_BATCH = 8, EV_TLOG = 10;
+constexpr int EV_THREADS = 1024, EV_WARPS = EV_THREADS / 32, EV_BINS = 2048, EV_MAX_CLUSTER = 8, EV_BATCH = 4, EV_TLOG = 10;
 constexpr int EV_MERGE = EV_BINS / EV_THREADS;               // counts that a thread merges, bins that it scans
 constexpr size_t EV_SMEM_MAX = 160 * 1024;
 
 // Order-preserving: larger weight, larger key; -0 as 0; not-a-number below everything. Kept positions are above everything.
 __device__ __forceinline__ uint32_t evict_key(float w) {
-    if (!(w == w)) return 0u;
+    if (!(w == w)) return 1u;                               // (0: no position)
     const uint32_t b = __float_as_uint(w + 0.f);
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
@@ -44,7 +43,7 @@ __device__ __forceinline__ void st_cluster_int(uint32_t addr, int rank, int v) {
 }
 
 __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictParams p) {
-    extern __shared__ uint32_t ev_keys[];
+    extern __shared__ __align__(16) uint32_t ev_keys[];
     __shared__ int s_hist[EV_BINS], s_all[EV_BINS], s_part[EV_WARPS], s_found[2], s_mine[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int C, rank;
@@ -62,17 +61,43 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
         for (int i = rank * EV_THREADS + tid; i < n; i += C * EV_THREADS) kept[i] = i;
         return;                                             // (the whole cluster)
     }
-    const int slice = (n + C - 1) >> clog, lo = min(rank * slice, n), cnt = min(slice, n - lo);
+    const int slice = (((n + C - 1) >> clog) + 3) & ~3, lo = min(rank * slice, n), cnt = min(slice, n - lo);
     const float* const w = p.weights + (long long)row * p.stride + lo;
-    for (int i0 = tid; i0 < cnt; i0 += EV_BATCH * EV_THREADS) {
-        float x[EV_BATCH];
-#pragma unroll
-        for (int u = 0; u < EV_BATCH; ++u) x[u] = i0 + u * EV_THREADS < cnt ? read_global(w + i0 + u * EV_THREADS) : 0.f;
+    // four positions at a time, counted by their top digit on the way; behind the slice's end keys below every other
+    const int groups = (cnt + 3) >> 2;
+    uint4* const keys4 = reinterpret_cast<uint4*>(ev_keys);
+    const bool aligned = ((uintptr_t)w & 15) == 0;
+    for (int i = tid; i < EV_BINS; i += EV_THREADS) s_hist[i] = 0;
+    __syncthreads();
+    for (int i0 = tid; i0 < groups; i0 += EV_BATCH * EV_THREADS) {
+        float4 x[EV_BATCH];
 #pragma unroll
         for (int u = 0; u < EV_BATCH; ++u) {
-            const int i = i0 + u * EV_THREADS, pos = lo + i;
-            const bool keep = pos < p.keep_first || pos >= n - p.keep_last;
-            if (i < cnt) ev_keys[i] = keep ? 0xffffffffu : evict_key(x[u]);
+            const int i = 4 * (i0 + u * EV_THREADS);
+            x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (aligned && i + 4 <= cnt) {
+                x[u] = read_global(reinterpret_cast<const float4*>(w + i));
+            } else if (i < cnt) {
+                x[u].x = read_global(w + i);
+                if (i + 1 < cnt) x[u].y = read_global(w + i + 1);
+                if (i + 2 < cnt) x[u].z = read_global(w + i + 2);
+                if (i + 3 < cnt) x[u].w = read_global(w + i + 3);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < EV_BATCH; ++u) {
+            const int i = 4 * (i0 + u * EV_THREADS);
+            if (i >= cnt) break;
+            const float y[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+            uint32_t key[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int pos = lo + i + v;
+                const bool keep = pos < p.keep_first || pos >= n - p.keep_last;
+                key[v] = i + v >= cnt ? 0u : keep ? 0xffffffffu : evict_key(y[v]);
+                atomicAdd(&s_hist[key[v] >> 21], 1);        // (keys of no position are below what is looked for)
+            }
+            keys4[i >> 2] = make_uint4(key[0], key[1], key[2], key[3]);
         }
     }
     // the want-th largest key, digit by digit from the top
@@ -82,15 +107,16 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
 #pragma unroll 1
     for (int round = 0; round < 3; ++round) {
         const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048;
-        for (int i = tid; i < bins; i += EV_THREADS) s_hist[i] = 0;
-        __syncthreads();
-        for (int i0 = tid; i0 < cnt; i0 += EV_BATCH * EV_THREADS) {
-            uint32_t key[EV_BATCH];
+        if (round > 0) {
+            for (int i = tid; i < bins; i += EV_THREADS) s_hist[i] = 0;
+            __syncthreads();
+            for (int i = tid; i < groups; i += EV_THREADS) {
+                const uint4 k = keys4[i];
+                const uint32_t key[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
-            for (int u = 0; u < EV_BATCH; ++u) key[u] = i0 + u * EV_THREADS < cnt ? ev_keys[i0 + u * EV_THREADS] : 0u;
-#pragma unroll
-            for (int u = 0; u < EV_BATCH; ++u)
-                if (i0 + u * EV_THREADS < cnt && (key[u] & known) == prefix) atomicAdd(&s_hist[(key[u] >> shift) & (bins - 1)], 1);
+                for (int v = 0; v < 4; ++v)
+                    if ((key[v] & known) == prefix) atomicAdd(&s_hist[(key[v] >> shift) & (bins - 1)], 1);
+            }
         }
         if (C > 1) {
             cluster_arrive(); cluster_wait();
@@ -136,15 +162,20 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
         known |= (uint32_t)(bins - 1) << shift;
         left = s_found[1];
     }
-    // every warp a run of the slice: how much it keeps for certain, and how much shares the last key
-    const int run = ((cnt + EV_WARPS - 1) / EV_WARPS + 31) / 32 * 32;
-    const int from = min(warp * run, cnt), to = min(from + run, cnt);
-    int more = 0, same = 0;
-    for (int i = from; i < to; i += 32) {
-        const uint32_t key = i + lane < to ? ev_keys[i + lane] : 0u;
-        more += __popc(__ballot_sync(0xffffffffu, i + lane < to && key > prefix));
-        same += __popc(__ballot_sync(0xffffffffu, i + lane < to && key == prefix));
-    }
+    // every warp a run of the slice: how much it keeps for certain, and how much shares the last key (both in one word, 16 bits each)
+    const int run = ((groups + EV_WARPS - 1) / EV_WARPS + 31) & ~31, from = min(warp * run, groups), to = min(from + run, groups);
+    auto counts = [&](const uint4& k) {
+        int c = 0;
+        const uint32_t key[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) c += (key[v] > prefix ? 1 : 0) + (key[v] == prefix ? 0x10000 : 0);
+        return c;
+    };
+    int both = 0;
+    for (int i = from + lane; i < to; i += 32) both += counts(keys4[i]);
+    int more = both & 0xffff, same = both >> 16;
+#pragma unroll
+    for (int sh = 16; sh; sh >>= 1) { more += __shfl_xor_sync(0xffffffffu, more, sh); same += __shfl_xor_sync(0xffffffffu, same, sh); }
     __shared__ int s_more[EV_WARPS], s_same[EV_WARPS];
     if (lane == 0) { s_more[warp] = more; s_same[warp] = same; }
     __syncthreads();
@@ -168,14 +199,25 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(const EvictPar
         cluster_arrive();                                   // (waited for at the end: nobody leaves while it is read)
     }
     for (int i = from; i < to; i += 32) {
-        const uint32_t key = i + lane < to ? ev_keys[i + lane] : 0u;
-        const unsigned gt = __ballot_sync(0xffffffffu, i + lane < to && key > prefix), eq = __ballot_sync(0xffffffffu, i + lane < to && key == prefix);
-        const unsigned below = (1u << lane) - 1u;
-        const int e_at = same_at + __popc(eq & below);
-        const bool mine = ((gt >> lane) & 1) || (((eq >> lane) & 1) && e_at < left);
-        if (mine) kept[more_at + __popc(gt & below) + min(e_at, left)] = lo + i + lane;
-        more_at += __popc(gt);
-        same_at += __popc(eq);
+        const uint4 k = i + lane < to ? keys4[i + lane] : make_uint4(0, 0, 0, 0);
+        const int mine = counts(k);
+        int x = mine;
+#pragma unroll
+        for (int sh = 1; sh < 32; sh <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, sh); if (lane >= sh) x += y; }
+        if (mine) {
+            int m_at = more_at + ((x - mine) & 0xffff), e_at = same_at + ((x - mine) >> 16);
+            const uint32_t key[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const bool certain = key[v] > prefix, shares = key[v] == prefix;
+                if (certain || (shares && e_at < left)) kept[m_at + min(e_at, left)] = lo + 4 * (i + lane) + v;
+                m_at += certain;
+                e_at += shares;
+            }
+        }
+        const int all = __shfl_sync(0xffffffffu, x, 31);
+        more_at += all & 0xffff;
+        same_at += all >> 16;
     }
     if (C > 1) cluster_wait();
 }

@@ -1959,9 +1959,9 @@ tidal_status_t tidal_evict_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     int cluster = 1;
     while ((size_t)((kv->max_ctx_len + cluster - 1) / cluster) * 4 > EV_SMEM_MAX) cluster *= 2;
     while (cluster < EV_MAX_CLUSTER && kv->max_ctx_len > cluster * 4096 && rows * cluster * 2 <= ctx->sm_count && ctx->evict_clusters[cluster * 2] >= rows) cluster *= 2;
-    p.slice_max = (kv->max_ctx_len + cluster - 1) / cluster;
+    const int slice = ((kv->max_ctx_len + cluster - 1) / cluster + 3) / 4 * 4;
     if ((long long)rows * cluster > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
-    return launch_block(ctx, evict_select_kernel, p, rows * cluster, EV_THREADS, (size_t)p.slice_max * 4, cluster, (cudaStream_t)stream);
+    return launch_block(ctx, evict_select_kernel, p, rows * cluster, EV_THREADS, (size_t)slice * 4, cluster, (cudaStream_t)stream);
 }
 
 tidal_status_t tidal_kv_gather(tidal_ctx_t* ctx, const tidal_kv_t* kv, const tidal_kv_t* into, const int32_t* kept, const int32_t* counts,

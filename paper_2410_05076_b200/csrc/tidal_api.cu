@@ -1930,7 +1930,7 @@ tidal_status_t tidal_chunk_weights(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32
     p.scale_log2 = (kv->sm_scale > 0.f ? kv->sm_scale : 1.0f / std::sqrt((float)kv->head_dim)) * 1.4426950408889634f;
     const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3;
     if (fp8) p.k_scale = kv->k_scale;
-    p.strided = most > p.tile_tokens;
+    p.strided = most > p.tile_tokens && 8LL * most > kv->max_ctx_len;
     p.lse = lse; p.decay = decay; p.weights = weights; p.stride = stride; p.heads = num_weight_heads;
     CUtensorMap qm, km;
     if (!cache_maps(p, kv, &km, nullptr) || !query_map(&qm, q, num_tokens, kv->num_q_heads, q_stride, p.c.G, p.tile_tokens)) return TIDAL_ERR_CUDA;

@@ -42,12 +42,13 @@ struct WeightShared {
     float sums[2][2][CH_TILE];                              // per pair: the second warpgroup's part of a tile
 };
 
-// A walk over a CTA's tiles of positions. Where a tile is one product, a run of all sequences' and weight heads' tiles, so that it meets few
-// sequences; where new tokens are many and the tiles they see are not alike, every gridDim.x-th.
+// A walk over a CTA's tiles of positions. A run of all sequences' and weight heads' tiles, so that it meets few
+// sequences and their queries stay; where new tokens are a good part of the context, so that the tiles they see are not alike, every gridDim.x-th.
 struct WeightWalk {
     long long left;                                         // tiles to come
     int step, b, ctx, tiles, first, begin, chunk;           // first: position of the first new token; begin: its row; chunk: new tokens
     int head, tile, key0, g0, g1, t0, q0, q1, all_q;        // the tile; KV heads; first query, products that see the tile, products of the sequence
+    int alike;                                              // tiles of the head before this one differ in their place only: all queries see them, or the one product
 };
 
 __device__ __forceinline__ void weight_sequence(const WeightParams& p, WeightWalk& w, int b) {
@@ -100,12 +101,19 @@ __device__ __forceinline__ void weight_start(const WeightParams& p, WeightWalk& 
         if (over) break;
     }
     weight_sequence(p, w, b);
+    w.alike = 0;
     w.head = w.tiles > 0 ? (int)(at / w.tiles) : 0;
     w.tile = (int)(at - (long long)w.head * w.tiles);
 }
 // The next tile; false behind the last.
 __device__ __forceinline__ bool weight_tile(const WeightParams& p, WeightWalk& w) {
     if (w.left <= 0) return false;
+    if (w.tile < w.alike) {                                 // (few instructions: the issuing warp's turns are the bound)
+        --w.left;
+        w.key0 = w.tile * CH_TILE;
+        return true;
+    }
+    w.alike = 0;
     weight_settle(p, w);
     if (w.left <= 0) return false;
     --w.left;
@@ -123,6 +131,8 @@ __device__ __forceinline__ bool weight_tile(const WeightParams& p, WeightWalk& w
         w.q1 = last < 0 ? 0 : (int)min((long long)w.q1, last / p.tile_tokens + 1);
     }
     w.q0 = min(w.q0, w.q1);
+    // (a lone product's last query stands in the sequence's last tile; of several the first sees the tiles up to its own)
+    if (p.window <= 0 && w.q0 == 0) w.alike = w.all_q <= 1 || !p.causal ? w.tiles : min(w.tiles, max(from, 0) / CH_TILE + 1);
     return true;
 }
 

@@ -108,22 +108,6 @@ __device__ __forceinline__ void tmem_loaded32(uint32_t* x) {
 #undef R
 }
 
-// 2^t of two numbers in -126 .. 127, off by at most 2.7e-6 of the value: 2^n for the nearest whole n, added to the exponent, times the polynomial of
-// degree 4 with the least largest relative error over the rest in [-1/2, 1/2] (its mean error is 3e-9, so that long sums are good
-// to more). What is below -126 counts as that. Takes from the exponential unit, which has 16 results a clock and SM for 128 multiply-adds.
-__device__ __forceinline__ f32pair exp2_by_polynomial(f32pair t) {
-    float lo = fmaxf(half2(t, 0), -126.f), hi = fmaxf(half2(t, 1), -126.f);
-    t = pair2(lo, hi);
-    const f32pair whole = add2(t, pair2(12582912.f, 12582912.f));          // 1.5 x 2^23: the low bits are the nearest whole number
-    const f32pair rest = fma2(add2(whole, pair2(-12582912.f, -12582912.f)), pair2(-1.f, -1.f), t);
-    f32pair y = fma2(rest, pair2(0.009569674730300903f, 0.009569674730300903f), pair2(0.05591824650764465f, 0.05591824650764465f));
-    y = fma2(y, rest, pair2(0.2402476668357849f, 0.2402476668357849f));
-    y = fma2(y, rest, pair2(0.6931217312812805f, 0.6931217312812805f));
-    y = fma2(y, rest, pair2(0.9999992251396179f, 0.9999992251396179f));
-    lo = __int_as_float(__float_as_int(half2(y, 0)) + (__float_as_int(half2(whole, 0)) << 23));
-    hi = __int_as_float(__float_as_int(half2(y, 1)) + (__float_as_int(half2(whole, 1)) << 23));
-    return pair2(lo, hi);
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {         // not-a-number if one is
     float d;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -138,9 +122,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {         // no
 // take them, every other tile each. Long axes are cut over the CTAs of a cluster (and the two streams), whose partial results are joined
 // through shared memory.
 //
-// 4096 tokens at the end of 16384: 820 us, 1175 TFLOP/s, tensor pipe at 64 %; at the end of 131072 under the power limit 8.0 ms, 1080 TFLOP/s. Bound by
-// what lies between products: a stream's scores wait for its weights, the exponential unit (2048 clocks for a pair of tiles, as long as their products, less
-// a fifth by polynomial) and the issuing warp's turns beside the softmax warps. One warp issues for both streams in turn, which keeps one's softmax beside
+// 4096 tokens at the end of 16384: 817 us, 1175 TFLOP/s, tensor pipe at 64 %; at the end of 131072 under the power limit 8.0 ms, 1080 TFLOP/s. Bound by
+// what lies between products: a stream's scores wait for its weights, the exponential unit (2048 clocks for a pair of tiles, as long as their products) and the issuing warp's turns beside the softmax warps. One warp issues for both streams in turn, which keeps one's softmax beside
 // the other's products; a warp for each lets them fall into step (1090 us).
 //
 // Rounding: weights enter the second product as bf16 (fp16 over an 8-bit cache, whose codes are widened exactly); sums of weights, maxima and
@@ -166,7 +149,6 @@ constexpr int CH_TILE = 128;                                // positions per til
 constexpr int CH_HALF = CH_TILE * 128;                      // bytes of 64 channels of a tile's rows, 16 bits each
 constexpr int CH_MAT = 2 * CH_HALF;
 constexpr int CH_TAGS = 16;
-constexpr int CH_POLY = 3;                                  // of sixteen pairs of weights, those whose exponentials are polynomials (0: 884 us, 3: 820, 6: 847)
 constexpr int CH_THREADS = 384, CH_THREADS8 = 512;
 constexpr int CH_RING = 5, CH_RING8 = 4;                       // operand slots: keys and values of a tile take one each
 constexpr int CH_MOST = 6;                                  // of eight products of weights and values, those that begin before all weights are there
@@ -499,11 +481,10 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 if (!finite) sh.odd[s] = 1;
             }
             // Weights by the maximum so far, while this tile's own is looked for: it is raised, and the weights are worked out again, only
-            // where that leaves one above 2^8. Whole tiles take some of the exponentials from the polynomial; where positions are masked all come
-            // from the unit, whose 2^-infinity is 0.
+            // where that leaves one above 2^8.
             f32pair sum0, sum1;
             float top;
-            auto weights = [&](auto whole) -> bool {
+            auto weights = [&](auto) -> bool {
                 const float shift = m == -INFINITY ? 0.f : -m * scale;
                 const f32pair scale2 = pair2(scale, scale), shift2 = pair2(shift, shift);
                 sum0 = sum1 = pair2(0.f, 0.f);
@@ -520,7 +501,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                             other = max3(other, __uint_as_float(x[2 * at + 2]), __uint_as_float(x[2 * at + 3]));
                         }
                         const f32pair t = fma2(pair2(__uint_as_float(x[at]), __uint_as_float(x[at + 1])), scale2, shift2);
-                        const f32pair e = decltype(whole)::value && (j * CH_POLY) % 16 < CH_POLY ? exp2_by_polynomial(t) : pair2(fast_exp2(half2(t, 0)), fast_exp2(half2(t, 1)));
+                        const f32pair e = pair2(fast_exp2(half2(t, 0)), fast_exp2(half2(t, 1)));
                         if (j & 1) sum1 = add2(sum1, e); else sum0 = add2(sum0, e);
                         y[j] = KV8 ? pack_f16(half2(e, 0), half2(e, 1)) : pack_bf16(half2(e, 0), half2(e, 1));
                     }
@@ -536,6 +517,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 }
                 return true;
             };
+            // (two copies of the same code, one of them for whole tiles alone: the compiler schedules that one better when the masked tiles' paths do
+            // not lead into it, 817 against 844 us, over E4M3 975 against 1074)
             const bool whole = !(ragged || partly || bad);
             while (!(whole ? weights(std::true_type()) : weights(std::false_type()))) {
                 const float up = fmaxf(m, top), f = m == up ? 1.f : fast_exp2((m - up) * scale);

@@ -122,9 +122,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {         // no
 // take them, every other tile each. Long axes are cut over the CTAs of a cluster (and the two streams), whose partial results are joined
 // through shared memory.
 //
-// 4096 tokens at the end of 16384: 817 us, 1175 TFLOP/s, tensor pipe at 64 %; at the end of 131072 under the power limit 8.0 ms, 1080 TFLOP/s. Bound by
-// what lies between products: a stream's scores wait for its weights, the exponential unit (2048 clocks for a pair of tiles, as long as their products) and the issuing warp's turns beside the softmax warps. One warp issues for both streams in turn, which keeps one's softmax beside
-// the other's products; a warp for each lets them fall into step (1090 us).
+// 4096 tokens at the end of 16384: 817 us, 1175 TFLOP/s, tensor pipe at 64 %; at the end of 131072 under the power limit 7.8 ms, 1110 TFLOP/s. Bound by
+// what lies between products: a stream's scores wait for its weights, the exponential unit (2048 clocks for a pair of tiles, as long as their
+// products) and the issuing warp's turns beside the softmax warps. One warp issues for both streams in turn, which keeps one's softmax beside the
+// other's products; a warp for each lets them fall into step (1090 us).
 //
 // Rounding: weights enter the second product as bf16 (fp16 over an 8-bit cache, whose codes are widened exactly); sums of weights, maxima and
 // outputs are fp32.
@@ -213,7 +214,7 @@ __device__ __forceinline__ bool chunk_work(const ChunkParams& p, const ChunkShar
 
 // One CTA tile of a sequence: which of all of them it is. The last tokens of a sequence, which see most, first; up to 32 sequences by their
 // lengths, the longest first, so that no long tile begins when the others are nearly done (8 sequences of 8192 to 65536 with chunks of 1000 down
-// to 1, 8 bits: 1.93 -> 1.58 ms); more of them in order.
+// to 1, 8 bits: 1.93 -> 1.55 ms); more of them in order.
 __device__ __forceinline__ void chunk_find(const ChunkParams& p, int want, int lane, int& seq, int& tile, bool& damaged) {
     const int per = 2 * p.tile_tokens;
     int before = 0;

@@ -12,8 +12,8 @@ namespace tidal {
 // the positions that share it still belong to the set. In a round every CTA counts its slice, adds up its share of the
 // bins over all CTAs and hands the sums to all, so that each finds the bin for itself. Then each CTA counts what it
 // keeps and writes it behind what the CTAs before it keep, in ascending order; of equal weights the lower positions.
-// Bound by that chain of barriers and by the instructions of three counts, not by its 4 bytes a position: 8 rows of 131072 19.7 us in clusters of
-// eight (clusters of sixteen do not all find room at once: 20 to 31 us), 64 rows of up to 65536 26.5 us in clusters of two.
+// Bound by that chain of barriers and by the instructions of three counts, not by its 4 bytes a position: 8 rows of 131072 16.7 us in clusters of
+// eight (clusters of sixteen do not all find room at once: half as long again on some GPUs), 64 rows of up to 65536 20.9 us in clusters of two.
 struct EvictParams {
     const float* weights;                                   // [batch][heads][stride]
     long long stride;

@@ -13,7 +13,10 @@ namespace tidal {
 enum { STATUS_WAITED_OUT = 16 };          // a wait on a copy or a product ran out: results are invalid
 
 // ---- barriers, copies, products ------------------------------------------------------------------------------------
-constexpr int WAIT_TRIES = 1 << 22;       // each try sleeps for up to a microsecond or so
+#ifndef TIDAL_WAIT_TRIES
+#define TIDAL_WAIT_TRIES (1 << 22)
+#endif
+constexpr int WAIT_TRIES = TIDAL_WAIT_TRIES;       // each try sleeps for up to a microsecond or so
 
 __device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(bar) : "memory"); }
@@ -23,8 +26,19 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Waits for the phase of that parity to end. False once a wait of this CTA has run out: the caller then leaves its loop.
+// Waits for the phase of that parity to end; a whole warp together, with one answer for its lanes. False once a wait of this CTA has run out: the warp
+// then leaves its loop.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
+    if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    for (int i = 0; i < WAIT_TRIES && !__any_sync(0xffffffffu, *gave_up); ++i)
+        if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    *gave_up = 1;
+    return false;
+}
+// The same without the vote, which costs the attention kernel a tenth of its speed where its products and its softmax wait (4096 tokens after 131072: 7.39
+// and 8.12 ms). Lanes may then have different answers, so that no branch that the warp takes together may hang on one: what waits here goes
+// on through all its steps, with results that are none.
+__device__ __forceinline__ bool bar_pass(uint32_t bar, uint32_t parity, volatile int* gave_up) {
     if (bar_try(bar, parity)) return true;
     for (int i = 0; i < WAIT_TRIES && !*gave_up; ++i)
         if (bar_try(bar, parity)) return true;
@@ -416,7 +430,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         const int n = w.stream_tiles[s];
         float m = -INFINITY, l = 0.f;
         if constexpr (KV8) {                                // queries as fp16
-            if (busy && bar_wait(smem_u32(&sh.q_full), 0, gave_up)) {
+            if (busy) {
+                bar_pass(smem_u32(&sh.q_full), 0, gave_up);
                 for (int i = tid & 127; i < CH_MAT / 16; i += 128) {
                     const uint32_t a = q_smem + s * CH_MAT + i * 16;
                     uint32_t x[4];
@@ -432,7 +447,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         }
         for (int i = 0; i < n; ++i) {
             const int tile = w.at(s, i), key0 = (w.tile0 + tile) * CH_TILE;
-            if (!bar_wait(smem_u32(&sh.s_full[s]), i & 1, gave_up)) break;
+            bar_pass(smem_u32(&sh.s_full[s]), i & 1, gave_up);
             tmem_fence_after();
             uint32_t x[CH_TILE];
 #pragma unroll
@@ -452,7 +467,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 if (ragged) {
                     // what lies behind the sequence may be anything, and zero times infinity is not zero
                     const int item = 2 * tile + 1, slot = item % RING;
-                    if (!bar_wait(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up)) break;
+                    bar_pass(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up);
                     const int from = max(w.ctx - key0, 0);
                     for (int k = from * 8 + (tid & 127); k < CH_TILE * 8; k += 128)
 #pragma unroll
@@ -470,7 +485,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             if (partly) {
                 // A weight of zero times a value that is not finite would spoil rows that do not see it: such tiles are worked out again, without products.
                 const int item = 2 * tile + 1, slot = item % RING;
-                if (!bar_wait(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up)) break;
+                bar_pass(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up);
                 bool finite = true;
                 for (int k = tid & 127; k < min(w.ctx - key0, CH_TILE) * 8; k += 128)
 #pragma unroll
@@ -545,12 +560,13 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             if (lane == 0) bar_arrive(smem_u32(&sh.p_full[s]));
         }
         // ---- results ----
-        if (n > 0 && bar_wait(smem_u32(&sh.o_done[s]), 0, gave_up)) tmem_fence_after();
+        if (n > 0) bar_pass(smem_u32(&sh.o_done[s]), 0, gave_up);
+        tmem_fence_after();
         const float vs = KV8 && p.v_scale ? read_global(p.v_scale + w.g) : 1.f;
         __syncwarp();
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + s) : "memory");
         const bool again = *(volatile int*)&sh.odd[s];
-        if (joined && w.stream_tiles[1 - s] > 0) bar_wait(smem_u32(&sh.o_done[1 - s]), 0, gave_up);    // (partial results take the operands' place)
+        if (joined && w.stream_tiles[1 - s] > 0) bar_pass(smem_u32(&sh.o_done[1 - s]), 0, gave_up);    // (partial results take the operands' place)
         if (again) {
             // (all rows of the stream, further down)
         } else if (!joined) {
@@ -606,7 +622,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(KV8 ? 48 : 72));
     }
     if (warp == 8) {
-        // ---- products: the whole warp walks, one lane issues ----
+        // ---- products: the whole warp walks, one lane issues (nothing more once a wait of its own has run out) ----
         if (busy) {
             const uint32_t first = mma_shape(!KV8, CH_TILE, false), second = mma_shape(!KV8, HEAD_DIM, true);
             const uint32_t acc = uniform(tmem);
@@ -631,11 +647,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 for (int kk = k0; kk < k1; ++kk)
                     mma_ts(acc + 256 + s * CH_TILE, acc + s * CH_TILE + kk * 8, v + (kk * 2048 >> 4), second, add || kk > 0);
             };
-            bool ok = bar_wait(smem_u32(&sh.q_full), 0, gave_up);
-            if (KV8) for (int s = 0; s < 2 && ok; ++s) ok = bar_wait(p_full + 8 * s, 0, gave_up);
+            bool ok = bar_pass(smem_u32(&sh.q_full), 0, gave_up);
+            if (KV8) for (int s = 0; s < 2; ++s) ok = bar_pass(p_full + 8 * s, 0, gave_up) && ok;
             int slot = 0, parity = 0;                       // of the next ring item to be looked for
             auto next = [&]() {                             // waits for it; its slot
-                ok = ok && bar_wait(full + 8 * slot, parity, gave_up);
+                ok = bar_pass(full + 8 * slot, parity, gave_up) && ok;
                 const int at = slot;
                 if (++slot == RING) { slot = 0; parity ^= 1; }
                 return at;
@@ -644,7 +660,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             if (!twin) {
                 int k = next();
                 tmem_fence_after();
-                if (ok && elected()) {
+                if (elected() && ok) {
                     if (n0 > 0) scores(0, q, k);
                     scores(1, q + (CH_MAT >> 4), k);
                     mma_commit(empty + 8 * k);
@@ -652,28 +668,28 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 __syncwarp();
                 int v = next();
                 if (n1 > 1) k = next();
-                for (int i = 0; i < n1 && ok; ++i, turn ^= 1, most ^= 1) {
+                for (int i = 0; i < n1; ++i, turn ^= 1, most ^= 1) {
                     if (i < n0) {
-                        ok = bar_wait(p_most, most, gave_up);
+                        ok = bar_pass(p_most, most, gave_up) && ok;
                         tmem_fence_after();
-                        if (ok && elected()) values(0, v, i > 0, 0, CH_MOST);
+                        if (elected() && ok) values(0, v, i > 0, 0, CH_MOST);
                         __syncwarp();
-                        ok = ok && bar_wait(p_full, turn, gave_up);
+                        ok = bar_pass(p_full, turn, gave_up) && ok;
                         tmem_fence_after();
-                        if (ok && elected()) {
+                        if (elected() && ok) {
                             values(0, v, true, CH_MOST, 8);
                             if (i + 1 < n0) scores(0, q, k);
                             else mma_commit(o_done);
                         }
                         __syncwarp();
                     }
-                    ok = ok && bar_wait(p_most + 8, most, gave_up);
+                    ok = bar_pass(p_most + 8, most, gave_up) && ok;
                     tmem_fence_after();
-                    if (ok && elected()) values(1, v, i > 0, 0, CH_MOST);
+                    if (elected() && ok) values(1, v, i > 0, 0, CH_MOST);
                     __syncwarp();
-                    ok = ok && bar_wait(p_full + 8, turn, gave_up);
+                    ok = bar_pass(p_full + 8, turn, gave_up) && ok;
                     tmem_fence_after();
-                    if (ok && elected()) {
+                    if (elected() && ok) {
                         values(1, v, true, CH_MOST, 8);
                         mma_commit(empty + 8 * v);
                         if (i + 1 < n1) {
@@ -694,9 +710,9 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 auto on = [&](int& at, int& par) { at += 2; if (at >= RING) { at -= RING; par ^= 1; } };
                 const int tiles = n0 + n1;
                 auto keys = [&](int s) {
-                    ok = ok && bar_wait(full + 8 * ks, kp, gave_up);
+                    ok = bar_pass(full + 8 * ks, kp, gave_up) && ok;
                     tmem_fence_after();
-                    if (ok && elected()) {
+                    if (elected() && ok) {
                         scores(s, q, ks);
                         mma_commit(empty + 8 * ks);
                     }
@@ -704,11 +720,12 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     on(ks, kp);
                 };
                 for (int t = 0; t < min(tiles, 2); ++t) keys(t);
-                for (int t = 0; t < tiles && ok; ++t) {
+                for (int t = 0; t < tiles; ++t) {
                     const int s = t & 1;
-                    ok = bar_wait(full + 8 * vs, vp, gave_up) && bar_wait(p_full + 8 * s, turn, gave_up);
+                    ok = bar_pass(full + 8 * vs, vp, gave_up) && ok;
+                    ok = bar_pass(p_full + 8 * s, turn, gave_up) && ok;
                     tmem_fence_after();
-                    if (ok && elected()) {
+                    if (elected() && ok) {
                         values(s, vs, t > 1, 0, 8);
                         mma_commit(empty + 8 * vs);
                         if (t + 2 >= tiles) mma_commit(o_done + 8 * s);
@@ -759,7 +776,6 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                     if (item >= RING) ok = bar_wait(smem_u32(&sh.empty[slot]), (item / RING - 1) & 1, gave_up);
                     dst = ring + slot * CH_MAT; bar = smem_u32(&sh.full[slot]);
                 }
-                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (lane == 0) bar_expect(bar, KV8 ? CH_HALF : CH_MAT);
                 __syncwarp();

@@ -344,7 +344,6 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                 const int slot = KV8 ? tile % CH_RAW : tile % CW_RING;
                 if constexpr (KV8) { if (tile >= CH_RAW) ok = bar_wait(smem_u32(&sh.raw_empty[slot]), (tile / CH_RAW - 1) & 1, gave_up); }
                 else { if (tile >= CW_RING) ok = bar_wait(smem_u32(&sh.k_empty[slot]), (tile / CW_RING - 1) & 1, gave_up); }
-                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const uint32_t dst = KV8 ? raw + slot * CH_HALF : k_ring + slot * CH_MAT, bar = smem_u32(KV8 ? &sh.raw_full[slot] : &sh.k_full[slot]);
                 if (lane == 0) {

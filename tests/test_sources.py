@@ -30,3 +30,20 @@ def test_every_device_function_is_called():
     assert len(names) > 50
     unused = sorted({n for n in names if len(re.findall(r"\b%s\b" % n, text)) < 2})
     assert not unused, unused
+
+
+def test_no_warp_parts_over_a_wait():
+    """Loads of TMEM and the choice of an issuing lane want all lanes of a warp: if a wait runs out for some of them and not for others, the rest must not go
+    on without them. So the waits whose answer is a branch vote, the others' answers (bar_pass) decide no more than whether the chosen lane
+    issues, and nobody tries a barrier elsewhere."""
+    text = " ".join(code().values())
+    wait = re.search(r"bool bar_wait\(.*?\n\}\n", text, flags=re.S).group()
+    for t in ("if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;", "!__any_sync(0xffffffffu, *gave_up)"):
+        assert t in wait
+    assert wait.count("return true") == wait.count("bar_try(") == wait.count("__all_sync(0xffffffffu, bar_try(") == 2
+    assert len(re.findall(r"\bbar_try\(", text)) == 5                                            # its definition and the two waits
+    rest = re.sub(r"bool bar_pass\(.*?\n\}\n", "", text, flags=re.S)
+    for line in rest.splitlines():
+        if "bar_pass(" in line:
+            assert re.search(r"(^|;|\)|\{)\s*((bool )?ok = )?bar_pass\([^;]*\)( && ok)?;", line) and not re.search(r"(if|while) \(!?bar_pass|&& bar_pass|return bar_pass|\? bar_pass", line), line
+    assert not re.search(r"\bok && elected\(\)", text)

@@ -27,23 +27,42 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Waits for the phase of that parity to end; a whole warp together, with one answer for its lanes. False once a wait of this CTA has run out: the warp
-// then leaves its loop.
+// then leaves its loop. APART: the first try stands before the loop of the others, after which the compiler orders what follows differently; each kernel
+// takes what it is faster with (attention over 16 bits 7.33 ms with it and 7.40 without, weights of single tokens 215 and 207 us).
+template <bool APART>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-    if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
-    for (int i = 0; i < WAIT_TRIES && !__any_sync(0xffffffffu, *gave_up); ++i)
+    if (APART && __all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    for (int i = 0; i < WAIT_TRIES; ++i) {
+        if (APART && __any_sync(0xffffffffu, *gave_up)) break;
         if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+        if (!APART && __any_sync(0xffffffffu, *gave_up)) break;
+    }
     *gave_up = 1;
     return false;
 }
 // The same without the vote, which costs the attention kernel a tenth of its speed where its products and its softmax wait (4096 tokens after 131072: 7.39
 // and 8.12 ms). Lanes may then have different answers, so that no branch that the warp takes together may hang on one: what waits here goes
 // on through all its steps, with results that are none.
+template <bool APART>
 __device__ __forceinline__ bool bar_pass(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-    if (bar_try(bar, parity)) return true;
-    for (int i = 0; i < WAIT_TRIES && !*gave_up; ++i)
+    if (APART && bar_try(bar, parity)) return true;
+    for (int i = 0; i < WAIT_TRIES; ++i) {
+        if (APART && *gave_up) break;
         if (bar_try(bar, parity)) return true;
+        if (!APART && *gave_up) break;
+    }
     *gave_up = 1;
     return false;
+}
+// A millisecond after a wait has run out: copies and products that are still on their way land before the CTA gives its memory back.
+__device__ __noinline__ void let_land() {
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;\n" : "=l"(t0));
+    for (int i = 0; i < 100000; ++i) {
+        __nanosleep(10000);
+        asm volatile("mov.u64 %0, %%globaltimer;\n" : "=l"(t));
+        if (t - t0 >= 1000000) return;
+    }
 }
 __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n"
@@ -431,7 +450,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         float m = -INFINITY, l = 0.f;
         if constexpr (KV8) {                                // queries as fp16
             if (busy) {
-                bar_pass(smem_u32(&sh.q_full), 0, gave_up);
+                bar_pass<true>(smem_u32(&sh.q_full), 0, gave_up);
                 for (int i = tid & 127; i < CH_MAT / 16; i += 128) {
                     const uint32_t a = q_smem + s * CH_MAT + i * 16;
                     uint32_t x[4];
@@ -447,7 +466,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         }
         for (int i = 0; i < n; ++i) {
             const int tile = w.at(s, i), key0 = (w.tile0 + tile) * CH_TILE;
-            bar_pass(smem_u32(&sh.s_full[s]), i & 1, gave_up);
+            bar_pass<true>(smem_u32(&sh.s_full[s]), i & 1, gave_up);
             tmem_fence_after();
             uint32_t x[CH_TILE];
 #pragma unroll
@@ -467,7 +486,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 if (ragged) {
                     // what lies behind the sequence may be anything, and zero times infinity is not zero
                     const int item = 2 * tile + 1, slot = item % RING;
-                    bar_pass(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up);
+                    bar_pass<true>(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up);
                     const int from = max(w.ctx - key0, 0);
                     for (int k = from * 8 + (tid & 127); k < CH_TILE * 8; k += 128)
 #pragma unroll
@@ -485,7 +504,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             if (partly) {
                 // A weight of zero times a value that is not finite would spoil rows that do not see it: such tiles are worked out again, without products.
                 const int item = 2 * tile + 1, slot = item % RING;
-                bar_pass(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up);
+                bar_pass<true>(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up);
                 bool finite = true;
                 for (int k = tid & 127; k < min(w.ctx - key0, CH_TILE) * 8; k += 128)
 #pragma unroll
@@ -560,13 +579,13 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             if (lane == 0) bar_arrive(smem_u32(&sh.p_full[s]));
         }
         // ---- results ----
-        if (n > 0) bar_pass(smem_u32(&sh.o_done[s]), 0, gave_up);
+        if (n > 0) bar_pass<true>(smem_u32(&sh.o_done[s]), 0, gave_up);
         tmem_fence_after();
         const float vs = KV8 && p.v_scale ? read_global(p.v_scale + w.g) : 1.f;
         __syncwarp();
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + s) : "memory");
         const bool again = *(volatile int*)&sh.odd[s];
-        if (joined && w.stream_tiles[1 - s] > 0) bar_pass(smem_u32(&sh.o_done[1 - s]), 0, gave_up);    // (partial results take the operands' place)
+        if (joined && w.stream_tiles[1 - s] > 0) bar_pass<true>(smem_u32(&sh.o_done[1 - s]), 0, gave_up);    // (partial results take the operands' place)
         if (again) {
             // (all rows of the stream, further down)
         } else if (!joined) {
@@ -647,11 +666,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 for (int kk = k0; kk < k1; ++kk)
                     mma_ts(acc + 256 + s * CH_TILE, acc + s * CH_TILE + kk * 8, v + (kk * 2048 >> 4), second, add || kk > 0);
             };
-            bool ok = bar_pass(smem_u32(&sh.q_full), 0, gave_up);
-            if (KV8) for (int s = 0; s < 2; ++s) ok = bar_pass(p_full + 8 * s, 0, gave_up) && ok;
+            bool ok = bar_pass<!KV8>(smem_u32(&sh.q_full), 0, gave_up);
+            if (KV8) for (int s = 0; s < 2; ++s) ok = bar_pass<!KV8>(p_full + 8 * s, 0, gave_up) && ok;
             int slot = 0, parity = 0;                       // of the next ring item to be looked for
             auto next = [&]() {                             // waits for it; its slot
-                ok = bar_pass(full + 8 * slot, parity, gave_up) && ok;
+                ok = bar_pass<!KV8>(full + 8 * slot, parity, gave_up) && ok;
                 const int at = slot;
                 if (++slot == RING) { slot = 0; parity ^= 1; }
                 return at;
@@ -670,11 +689,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 if (n1 > 1) k = next();
                 for (int i = 0; i < n1; ++i, turn ^= 1, most ^= 1) {
                     if (i < n0) {
-                        ok = bar_pass(p_most, most, gave_up) && ok;
+                        ok = bar_pass<!KV8>(p_most, most, gave_up) && ok;
                         tmem_fence_after();
                         if (elected() && ok) values(0, v, i > 0, 0, CH_MOST);
                         __syncwarp();
-                        ok = bar_pass(p_full, turn, gave_up) && ok;
+                        ok = bar_pass<!KV8>(p_full, turn, gave_up) && ok;
                         tmem_fence_after();
                         if (elected() && ok) {
                             values(0, v, true, CH_MOST, 8);
@@ -683,11 +702,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                         }
                         __syncwarp();
                     }
-                    ok = bar_pass(p_most + 8, most, gave_up) && ok;
+                    ok = bar_pass<!KV8>(p_most + 8, most, gave_up) && ok;
                     tmem_fence_after();
                     if (elected() && ok) values(1, v, i > 0, 0, CH_MOST);
                     __syncwarp();
-                    ok = bar_pass(p_full + 8, turn, gave_up) && ok;
+                    ok = bar_pass<!KV8>(p_full + 8, turn, gave_up) && ok;
                     tmem_fence_after();
                     if (elected() && ok) {
                         values(1, v, true, CH_MOST, 8);
@@ -710,7 +729,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 auto on = [&](int& at, int& par) { at += 2; if (at >= RING) { at -= RING; par ^= 1; } };
                 const int tiles = n0 + n1;
                 auto keys = [&](int s) {
-                    ok = bar_pass(full + 8 * ks, kp, gave_up) && ok;
+                    ok = bar_pass<!KV8>(full + 8 * ks, kp, gave_up) && ok;
                     tmem_fence_after();
                     if (elected() && ok) {
                         scores(s, q, ks);
@@ -722,8 +741,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 for (int t = 0; t < min(tiles, 2); ++t) keys(t);
                 for (int t = 0; t < tiles; ++t) {
                     const int s = t & 1;
-                    ok = bar_pass(full + 8 * vs, vp, gave_up) && ok;
-                    ok = bar_pass(p_full + 8 * s, turn, gave_up) && ok;
+                    ok = bar_pass<!KV8>(full + 8 * vs, vp, gave_up) && ok;
+                    ok = bar_pass<!KV8>(p_full + 8 * s, turn, gave_up) && ok;
                     tmem_fence_after();
                     if (elected() && ok) {
                         values(s, vs, t > 1, 0, 8);
@@ -769,11 +788,11 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 uint32_t dst, bar;
                 if constexpr (KV8) {
                     const int slot = item % CH_RAW;
-                    if (item >= CH_RAW) ok = bar_wait(smem_u32(&sh.raw_empty[slot]), (item / CH_RAW - 1) & 1, gave_up);
+                    if (item >= CH_RAW) ok = bar_wait<!KV8>(smem_u32(&sh.raw_empty[slot]), (item / CH_RAW - 1) & 1, gave_up);
                     dst = raw + slot * CH_HALF; bar = smem_u32(&sh.raw_full[slot]);
                 } else {
                     const int slot = item % RING;
-                    if (item >= RING) ok = bar_wait(smem_u32(&sh.empty[slot]), (item / RING - 1) & 1, gave_up);
+                    if (item >= RING) ok = bar_wait<!KV8>(smem_u32(&sh.empty[slot]), (item / RING - 1) & 1, gave_up);
                     dst = ring + slot * CH_MAT; bar = smem_u32(&sh.full[slot]);
                 }
                 if (!ok) break;
@@ -794,8 +813,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         const int l = tid & 127;
         for (int item = 0; item < 2 * w.tiles; ++item) {
             const int rs = item % CH_RAW, slot = item % RING;
-            if (!bar_wait(smem_u32(&sh.raw_full[rs]), (item / CH_RAW) & 1, gave_up)) break;
-            if (item >= RING && !bar_wait(smem_u32(&sh.empty[slot]), (item / RING - 1) & 1, gave_up)) break;
+            if (!bar_wait<false>(smem_u32(&sh.raw_full[rs]), (item / CH_RAW) & 1, gave_up)) break;
+            if (item >= RING && !bar_wait<false>(smem_u32(&sh.empty[slot]), (item / RING - 1) & 1, gave_up)) break;
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const int k = u * 128 + l, r = k >> 3, c = k & 7;           // sixteen channels of a position
@@ -862,7 +881,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         }
         if (ranks > 1) { cluster_arrive(); cluster_wait(); }               // nobody leaves while its results are read
     }
-    if (sh.gave_up) for (int i = 0; i < 50; ++i) __nanosleep(20000);      // (copies that are still on their way land meanwhile)
+    if (sh.gave_up) let_land();
     tmem_fence_before();
     __syncthreads();
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem));

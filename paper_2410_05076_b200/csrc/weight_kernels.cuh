@@ -172,20 +172,21 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
 
     if (warp < 16) {
         // ---- sums ----
+        // (Nothing here hangs on how a wait ended: warps meet at named barriers, which know no limit, so all of them take all steps, whatever has run out.)
         const int wg = warp >> 2, pair = wg >> 1, s = wg & 1, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         int step = 0, tile = 0, turn = 0, item = 0, count = 0;           // the pair's products, key tiles of all, own fillings, the pair's joined tiles, tiles of positions
         long long filled = -1;                              // the queries whose sums are in shared memory
-        for (; ok && weight_tile(p, w); w.tile += w.step) {
+        for (; weight_tile(p, w); w.tile += w.step) {
             const int key = w.key0 + row, steps = (w.q1 - w.q0) * (w.g1 - w.g0), first_step = step;
             float acc = 0.f;
             if ((count++ & 1) != pair) {                    // the other pair's
                 tile += w.q1 > w.q0 ? w.g1 - w.g0 : 0;
                 continue;
             }
-            for (int g = w.g0; g < w.g1 && ok; ++g) {
+            for (int g = w.g0; g < w.g1; ++g) {
                 float part = 0.f;
-                for (int q = w.q0; q < w.q1 && ok; ++q, ++step) {
+                for (int q = w.q0; q < w.q1; ++q, ++step) {
                     if ((step & 1) != s) continue;
                     const int t = w.t0 + q * tt, rows = min(tt, w.chunk - t) * G;      // first token, rows that count
                     const int buf = wg, cols = (rows + 31) & ~31;
@@ -202,8 +203,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                     }
                     const float* const lse2 = sh.lse2[wg][turn & 1];
                     const int2* const sees = sh.sees[wg][turn & 1];
-                    ok = bar_wait(smem_u32(&sh.d_full[buf]), (step >> 1) & 1, gave_up);
-                    if (!ok) break;
+                    bar_pass<true>(smem_u32(&sh.d_full[buf]), (step >> 1) & 1, gave_up);
                     tmem_fence_after();
                     const bool all = (!p.causal || w.key0 + CH_TILE - 1 <= w.first + t) && (p.window <= 0 || w.first + t + (rows - 1) / G - p.window < w.key0);
                     const f32pair scale2 = pair2(scale, scale);
@@ -243,7 +243,6 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                 if (w.q1 > w.q0) ++tile;
                 acc += part;
             }
-            if (!ok) break;
             bool writes = steps == 0 ? s == 0 : (first_step & 1) == s;
             if (steps > 1) {
                 // the second warpgroup leaves its part and goes on, the first adds it (barriers 5 + 4 pair: a part is there; two further on: its
@@ -283,15 +282,15 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                     held = 0;
                     group = these;
                 }
-                ok = bar_wait(smem_u32(&sh.k_full[ks]), kp, gave_up);
+                ok = bar_wait<false>(smem_u32(&sh.k_full[ks]), kp, gave_up);
                 for (int q = w.q0; q < w.q1 && ok; ++q) {
                     const int step = pair ? steps[1]++ : steps[0]++, buf = 2 * pair + (step & 1);
                     const int rows = min(tt, w.chunk - w.t0 - q * tt) * G, cols = (rows + 31) & ~31;
                     // Queries have the slot of their number; where a sequence and head has no more than there are slots they stay while it does.
                     const int qs = q % QRING;
                     const bool stay = w.all_q <= QRING, fresh = !((held >> qs) & 1);
-                    ok = (!fresh || bar_wait(smem_u32(&sh.q_full[qs]), (qp >> qs) & 1, gave_up)) &&
-                         (step < 2 || bar_wait(smem_u32(&sh.d_empty[buf]), ((step >> 1) - 1) & 1, gave_up));
+                    ok = (!fresh || bar_wait<false>(smem_u32(&sh.q_full[qs]), (qp >> qs) & 1, gave_up)) &&
+                         (step < 2 || bar_wait<false>(smem_u32(&sh.d_empty[buf]), ((step >> 1) - 1) & 1, gave_up));
                     if (!ok) break;
                     tmem_fence_after();
                     const uint64_t a = smem_matrix(k_ring + ks * CH_MAT, 16), b = smem_matrix(q_ring + qs * CH_MAT, 16);
@@ -342,8 +341,8 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
             for (int g = g0; g < g1 && ok; ++g, ++tile) {
                 if ((tile & 1) != warp - 17) continue;
                 const int slot = KV8 ? tile % CH_RAW : tile % CW_RING;
-                if constexpr (KV8) { if (tile >= CH_RAW) ok = bar_wait(smem_u32(&sh.raw_empty[slot]), (tile / CH_RAW - 1) & 1, gave_up); }
-                else { if (tile >= CW_RING) ok = bar_wait(smem_u32(&sh.k_empty[slot]), (tile / CW_RING - 1) & 1, gave_up); }
+                if constexpr (KV8) { if (tile >= CH_RAW) ok = bar_wait<false>(smem_u32(&sh.raw_empty[slot]), (tile / CH_RAW - 1) & 1, gave_up); }
+                else { if (tile >= CW_RING) ok = bar_wait<false>(smem_u32(&sh.k_empty[slot]), (tile / CW_RING - 1) & 1, gave_up); }
                 if (!ok) break;
                 const uint32_t dst = KV8 ? raw + slot * CH_HALF : k_ring + slot * CH_MAT, bar = smem_u32(KV8 ? &sh.raw_full[slot] : &sh.k_full[slot]);
                 if (lane == 0) {
@@ -372,7 +371,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                     const int qs = q % QRING;
                     if ((held >> qs) & 1) continue;
                     if ((used >> qs) & 1) {
-                        ok = bar_wait(smem_u32(&sh.q_empty[qs]), (parity >> qs) & 1, gave_up);
+                        ok = bar_wait<false>(smem_u32(&sh.q_empty[qs]), (parity >> qs) & 1, gave_up);
                         parity ^= 1u << qs;
                     }
                     if (!ok) break;
@@ -393,8 +392,8 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
         for (; ok && weight_tile(p, w); w.tile += w.step)
             for (int g = w.g0; g < w.g1 && ok && w.q0 < w.q1; ++g, ++tile) {
                 const int rs = tile % CH_RAW, slot = tile % CW_RING;
-                ok = bar_wait(smem_u32(&sh.raw_full[rs]), (tile / CH_RAW) & 1, gave_up) &&
-                     (tile < CW_RING || bar_wait(smem_u32(&sh.k_empty[slot]), (tile / CW_RING - 1) & 1, gave_up));
+                ok = bar_wait<false>(smem_u32(&sh.raw_full[rs]), (tile / CH_RAW) & 1, gave_up) &&
+                     (tile < CW_RING || bar_wait<false>(smem_u32(&sh.k_empty[slot]), (tile / CW_RING - 1) & 1, gave_up));
                 if (!ok) break;
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
@@ -418,7 +417,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
             }
     }
     __syncwarp();
-    if (sh.gave_up) for (int i = 0; i < 50; ++i) __nanosleep(20000);      // (copies that are still on their way land meanwhile)
+    if (sh.gave_up) let_land();
     tmem_fence_before();
     __syncthreads();
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem));

@@ -38,12 +38,21 @@ def test_no_warp_parts_over_a_wait():
     issues, and nobody tries a barrier elsewhere."""
     text = " ".join(code().values())
     wait = re.search(r"bool bar_wait\(.*?\n\}\n", text, flags=re.S).group()
-    for t in ("if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;", "!__any_sync(0xffffffffu, *gave_up)"):
-        assert t in wait
     assert wait.count("return true") == wait.count("bar_try(") == wait.count("__all_sync(0xffffffffu, bar_try(") == 2
+    assert wait.count("*gave_up)") == wait.count("__any_sync(0xffffffffu, *gave_up)") == 2
     assert len(re.findall(r"\bbar_try\(", text)) == 5                                            # its definition and the two waits
     rest = re.sub(r"bool bar_pass\(.*?\n\}\n", "", text, flags=re.S)
     for line in rest.splitlines():
-        if "bar_pass(" in line:
-            assert re.search(r"(^|;|\)|\{)\s*((bool )?ok = )?bar_pass\([^;]*\)( && ok)?;", line) and not re.search(r"(if|while) \(!?bar_pass|&& bar_pass|return bar_pass|\? bar_pass", line), line
+        if "bar_pass<" in line:
+            assert re.search(r"(^|;|\)|\{)\s*((bool )?ok = )?bar_pass<!?\w+>\([^;]*\)( && ok)?;", line) and not re.search(r"(if|while) \(!?bar_pass|&& bar_pass|return bar_pass|\? bar_pass", line), line
     assert not re.search(r"\bok && elected\(\)", text)
+
+
+def test_attention_weights_meet_at_barriers_whatever_has_run_out():
+    """A warp that has given up a wait leaves its loop: it must not be one that others meet at a barrier without a limit."""
+    text = code()["weight_kernels.cuh"]
+    loops = text[text.index("chunk_weights_kernel("):]
+    loops = loops[loops.index("pdl_trigger"):loops.rindex("tmem_fence_before")]
+    sums, rest = loops[loops.index("if (warp < 16)"):loops.index("if (warp == 16)")], loops[loops.index("if (warp == 16)"):]
+    assert "bar.sync" in sums and "bar_pass<" in sums and not re.search(r"\bok\b|\bbreak\b|bar_wait|gave_up\)\s*(\)|&&)", sums)
+    assert "bar_wait<" in rest and not re.search(r"bar\.sync|bar\.arrive|barrier\.|__syncthreads|cluster_wait", rest)

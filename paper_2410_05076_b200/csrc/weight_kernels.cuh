@@ -36,6 +36,8 @@ struct WeightShared {
     unsigned long long k_full[CW_RING], k_empty[CW_RING], q_full[CW_QRING], q_empty[CW_QRING], d_full[CW_BUFS], d_empty[CW_BUFS], raw_full[CH_RAW], raw_empty[CH_RAW];
     uint32_t tmem;
     int gave_up;
+    // Per tile of positions with products, bit i: its i-th page is not one. Read before the warpgroup arrives for the last of its products with the tile: until
+    // then its pair's next-but-one product waits, so that tiles up to four further on are in work and five more on their way.
     unsigned bad_pages[CH_TAGS];
     alignas(16) float lse2[4][2][CH_TILE];                  // per warpgroup and turn: minus a row's log-sum-exp in base 2 (read four at a time), and what it sees
     int2 sees[4][2][CH_TILE];
@@ -175,17 +177,18 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
         // (Nothing here hangs on how a wait ended: warps meet at named barriers, which know no limit, so all of them take all steps, whatever has run out.)
         const int wg = warp >> 2, pair = wg >> 1, s = wg & 1, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        int step = 0, tile = 0, turn = 0, item = 0, count = 0;           // the pair's products, key tiles of all, own fillings, the pair's joined tiles, tiles of positions
+        int step = 0, tag = 0, turn = 0, item = 0, count = 0;           // the pair's products, tiles with products, own fillings, the pair's joined tiles, tiles of positions
         long long filled = -1;                              // the queries whose sums are in shared memory
         for (; weight_tile(p, w); w.tile += w.step) {
             const int key = w.key0 + row, steps = (w.q1 - w.q0) * (w.g1 - w.g0), first_step = step;
             float acc = 0.f;
             if ((count++ & 1) != pair) {                    // the other pair's
-                tile += w.q1 > w.q0 ? w.g1 - w.g0 : 0;
+                tag += w.q1 > w.q0;
                 continue;
             }
             for (int g = w.g0; g < w.g1; ++g) {
                 float part = 0.f;
+                unsigned skip = 0;
                 for (int q = w.q0; q < w.q1; ++q, ++step) {
                     if ((step & 1) != s) continue;
                     const int t = w.t0 + q * tt, rows = min(tt, w.chunk - t) * G;      // first token, rows that count
@@ -234,15 +237,16 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                             }
                         }
                     }
+                    skip = *(volatile unsigned*)&sh.bad_pages[tag % CH_TAGS];
                     tmem_fence_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive(smem_u32(&sh.d_empty[buf]));
                 }
                 // a page id outside the pool: its positions receive nothing
-                if (steps > 0 && ((sh.bad_pages[tile % CH_TAGS] >> (row / TILE)) & 1)) part = 0.f;
-                if (w.q1 > w.q0) ++tile;
+                if ((skip >> (row / TILE)) & 1) part = 0.f;
                 acc += part;
             }
+            tag += w.q1 > w.q0;
             bool writes = steps == 0 ? s == 0 : (first_step & 1) == s;
             if (steps > 1) {
                 // the second warpgroup leaves its part and goes on, the first adds it (barriers 5 + 4 pair: a part is there; two further on: its
@@ -314,7 +318,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
         }
     } else if (warp == 17 || warp == 18) {
         // ---- keys in: two warps, a tile each in turn; the pages of a warp's next tile are looked up before it waits for this one's place ----
-        int tile = 0;                                       // of all (tile, KV head) so far
+        int tile = 0, tag = 0;                              // of all (tile, KV head) so far; of tiles with products
         auto lookup = [&](unsigned& bad) {
             int page = 0;
             bad = 0;
@@ -346,7 +350,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                 if (!ok) break;
                 const uint32_t dst = KV8 ? raw + slot * CH_HALF : k_ring + slot * CH_MAT, bar = smem_u32(KV8 ? &sh.raw_full[slot] : &sh.k_full[slot]);
                 if (lane == 0) {
-                    sh.bad_pages[tile % CH_TAGS] = skip;
+                    sh.bad_pages[tag % CH_TAGS] = skip;
                     bar_expect(bar, KV8 ? CH_HALF : CH_MAT);
                 }
                 __syncwarp();
@@ -359,6 +363,7 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
                     tma_load4(dst + lane * CH_HALF, &k_map, bar, lane * 64, key0, g * p.head_mul, b * p.batch_mul);
                 }
             }
+            tag += g1 > g0;
         }
     } else if (warp == 19) {
         // ---- queries in, unless they are there ----

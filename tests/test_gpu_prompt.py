@@ -390,6 +390,25 @@ def test_chunk_bad_pages_are_skipped_and_reported(td, fp8):
     assert td.device_status() == binding.OK
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("hq,hkv,new", [(20, 20, 3), (32, 16, 200), (8, 1, 40)])
+@pytest.mark.parametrize("max_new", [0, 1])
+def test_weights_of_all_heads_together_next_to_bad_pages(td, fp8, hq, hkv, new, max_new):
+    """Every tile has other bad pages, and the tiles of many heads lie between one of a warpgroup's and its next."""
+    new = 1 if max_new else new
+    lay = make([6000], hq, hkv, "paged", fp8, seed=3)
+    bad = [pg for pg in range(375) if (pg * pg + pg // 8) % 7 == 3]
+    lay.page_table[0, bad] = lay.num_pages
+    q, off, lse, w, tol = check_chunk(td, lay, [new], skip=bad, max_new=0)
+    for heads, want, bound in ((hkv, w, tol), (1, w.sum(1, keepdim=True), tol.sum(1, keepdim=True) + 2.0 ** -20 * w.sum(1, keepdim=True))):
+        for _ in range(3):
+            got = td.chunk_weights(lay, q, off, lse, torch.full((1, heads, 6000), 5.0, device=DEV), decay=0.0, max_new=max_new)
+            assert ((got.double() - want).abs() <= bound).all()
+            blind = torch.isin(torch.arange(6000, device=DEV) // BLK, torch.tensor(bad, device=DEV))
+            assert (got[..., blind] == 0).all() and (got[..., : 6000 - new][..., ~blind[: 6000 - new]] > 0).all()
+    assert td.device_status() == binding.ERR_INDEX
+
+
 def test_chunk_attention_over_infinite_and_missing_numbers(td):
     """A logit that is not a number, or a value, spoils the rows that see it."""
     lay = make([260], 2, 1, "hnd", seed=7)

@@ -56,3 +56,10 @@ def test_attention_weights_meet_at_barriers_whatever_has_run_out():
     sums, rest = loops[loops.index("if (warp < 16)"):loops.index("if (warp == 16)")], loops[loops.index("if (warp == 16)"):]
     assert "bar.sync" in sums and "bar_pass<" in sums and not re.search(r"\bok\b|\bbreak\b|bar_wait|gave_up\)\s*(\)|&&)", sums)
     assert "bar_wait<" in rest and not re.search(r"bar\.sync|bar\.arrive|barrier\.|__syncthreads|cluster_wait", rest)
+
+
+def test_attention_weights_read_a_tiles_bad_pages_before_they_let_go_of_it():
+    """Behind the arrival nothing keeps the loading warps from the tag's place."""
+    text = code()["weight_kernels.cuh"]
+    sums = text[text.index("if (warp < 16)"):text.index("else if (warp == 16)")]
+    assert sums.count("bad_pages[") == 1 and sums.index("bad_pages[") < sums.index("bar_arrive(smem_u32(&sh.d_empty")

@@ -838,7 +838,10 @@ __global__ void __launch_bounds__(NW * 32, (MODE == MODE_SPARSE && KV8) ? 2 : 1)
                 const int pos0 = tile * TILE;
                 long long off;
                 bool ok = true;
-                if (p.paged) {
+                if (p.paged && TOKENS && pos0 >= total) {
+                    ok = false;                          // (an item has a tile at least: here of a token that sees nothing, or is none)
+                    off = 0;
+                } else if (p.paged) {
                     const int page = read_global(p.page_table + (long long)b * p.max_pages + tile);
                     ok = (unsigned)page < (unsigned)p.num_pages;
                     if (!ok && lane == 0) atomicOr(p.status, STATUS_BAD_PAGE);

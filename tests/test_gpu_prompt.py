@@ -469,6 +469,25 @@ def test_single_tokens_where_there_are_more(td):
     assert (got[[0, 2]] == 0).all() and (lse[[0, 2]] == -math.inf).all()
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lens,new", [([0, 5000], [0, 1]), ([0], [1]), ([0, 0, 700, 0] * 8, [1, 0, 1, 0] * 8), ([40, 20000], [0, 1])])
+def test_single_tokens_beside_idle_places(td, fp8, lens, new):
+    """Sequences without a token, or without a cached position, whose page tables hold nothing: their pages are nobody's business."""
+    lay = make(lens, 8, 2, "paged", fp8, seed=4)
+    idle = [b for b, (n, t) in enumerate(zip(lens, new)) if n == 0 or t == 0]
+    lay.page_table[idle] = -1
+    q, off = chunk_inputs(lay, new)
+    there = [t if n else 0 for n, t in zip(lens, new)]
+    full = torch.tensor([bool(n) for n, t in zip(lens, new) if t], device=DEV)       # of the tokens, in order
+    ref, ref_lse, _, tol, tol_l, _ = ref_chunk(lay, q[full], there)
+    for max_new in (1, 0):
+        lse = torch.zeros(q.shape[:2], device=DEV)
+        got = td.chunk_attn(lay, q, off, max_new=max_new, lse=lse)
+        assert td.device_status() == binding.OK
+        assert (got[~full] == 0).all() and (lse[~full] == -math.inf).all()
+        assert ((got[full].double() - ref).abs() <= tol).all() and ((lse[full].double() - ref_lse).abs() <= tol_l).all()
+
+
 def test_single_tokens_next_to_numbers_that_are_none(td):
     lay = make([40000], 4, 2, "hnd", seed=7)
     q, off = chunk_inputs(lay, [1])

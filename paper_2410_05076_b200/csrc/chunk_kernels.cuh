@@ -182,7 +182,7 @@ struct ChunkParams {
 constexpr int CH_TILE = 128;                                // positions per tile, rows per stream
 constexpr int CH_HALF = CH_TILE * 128;                      // bytes of 64 channels of a tile's rows, 16 bits each
 constexpr int CH_MAT = 2 * CH_HALF;
-constexpr int CH_TAGS = 16;
+constexpr int CH_TAGS = 16, CH_MAX_TILES = 2048;            // tiles of the longest context
 constexpr int CH_THREADS = 384, CH_THREADS8 = 512;
 constexpr int CH_RING = 5, CH_RING8 = 4;                       // operand slots: keys and values of a tile take one each
 constexpr int CH_MOST = 6;                                  // of eight products of weights and values, those that begin before all weights are there
@@ -193,7 +193,8 @@ struct ChunkShared {
     unsigned long long q_full, full[5], empty[5], raw_full[2], raw_empty[2], s_full[2], p_most[2], p_full[2], o_done[2];
     uint32_t tmem;
     int gave_up, seq, tile;
-    int odd[2];                                             // per stream: a tile that not all rows see whole has values that are not finite
+    int any_odd;                                            // a tile that not all rows of a stream see whole has values that are not finite:
+    unsigned odd[CH_MAX_TILES / 32];                        // bit i: the CTA's i-th
     unsigned bad_pages[CH_TAGS];                            // per tile, bit i: its i-th page is not one
 };
 // Partial results take the operands' place: 2 x 128 rows of 128 outputs, then their maxima and sums.
@@ -291,90 +292,83 @@ __device__ __forceinline__ void chunk_find(const ChunkParams& p, int want, int l
     }
 }
 
-// Whether eight 16-bit numbers are all finite.
+// Eight 16-bit numbers with zeros for those that are not finite; whether there were any.
 template <bool HALF>
-__device__ __forceinline__ bool all_finite(const uint32_t (&x)[4]) {
-    uint32_t top = 0;
+__device__ __forceinline__ bool drop_odd(uint32_t (&x)[4]) {
+    constexpr uint32_t EXP = HALF ? 0x7c007c00u : 0x7f807f80u, ONE = HALF ? 0x04000400u : 0x00800080u;
+    uint32_t any = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) top |= (x[j] & (HALF ? 0x7c007c00u : 0x7f807f80u)) + (HALF ? 0x04000400u : 0x00800080u);       // a full exponent carries
-    return !(top & 0x80008000u);
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t full = ((x[j] & EXP) + ONE) & 0x80008000u;          // a full exponent carries
+        any |= full;
+        x[j] &= ~((full >> 15) * 0xffffu);
+    }
+    return any != 0;
 }
 
-// One row over a stream's tiles without matrix products: weights of zero times infinity do not come up where positions are masked. A warp together,
-// four channels per lane; (m, l, o) as the products give them. Slow (a row at a time), and for rows next to values that are not finite.
+// What the values that were left out of a stream's products (see the kernel) add to its rows, a quarter of them per warp: infinities and not-a-numbers to the
+// channels of the rows that see their position, and that have a weight at all (`lives`), whatever is there already. Four channels per lane; into the partial results
+// where they are joined.
 template <bool KV8>
-__device__ __forceinline__ void chunk_row_plain(const ChunkParams& p, const ChunkWork& w, int s, int token, int head, int lane, float scale, float (&o)[4], float& m, float& l) {
-    constexpr int ESZ = KV8 ? 1 : 2;
-    auto four = [&](const uint8_t* at, float (&x)[4]) {     // four channels of a cached row
-        uint32_t a, b;
-        if constexpr (KV8) {
-            e4m3x4_to_f16x2x2(read_global(reinterpret_cast<const uint32_t*>(at + lane * 4)), a, b);
-            a = f16x2_to_bf16x2(a);
-            b = f16x2_to_bf16x2(b);
-        } else {
-            const uint2 y = read_global(reinterpret_cast<const uint2*>(at + lane * 8));
-            a = y.x; b = y.y;
-        }
-        x[0] = __uint_as_float(a << 16); x[1] = __uint_as_float(a & 0xffff0000u); x[2] = __uint_as_float(b << 16); x[3] = __uint_as_float(b & 0xffff0000u);
-    };
-    const uint2 y = read_global(reinterpret_cast<const uint2*>(p.q + (long long)(w.q_row + token - w.t0) * p.q_stride + head * HEAD_DIM + lane * 4));
-    const float q[4] = {__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xffff0000u), __uint_as_float(y.y << 16), __uint_as_float(y.y & 0xffff0000u)};
-    const int pos = w.first + token, hi = p.causal ? min(pos + 1, w.ctx) : w.ctx, lo = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
-    m = -INFINITY; l = 0.f;
-    o[0] = o[1] = o[2] = o[3] = 0.f;
-    for (int i = 0; i < w.stream_tiles[s]; ++i) {
-        const int key0 = (w.tile0 + w.at(s, i)) * CH_TILE;
-        for (int key = max(key0, lo); key < min(key0 + CH_TILE, hi); ++key) {
+__device__ __noinline__ void chunk_odd_values(const ChunkParams& p, const ChunkShared& sh, uint32_t base, int rank, int ranks, int g, int s, int quarter, int lane, unsigned lives) {
+    ChunkWork w;
+    chunk_work(p, sh, rank, ranks, g, w);
+    const bool joined = ranks > 1 || w.twin;
+    const int G = p.c.G, tt = p.tile_tokens;
+    for (int tile = 0; tile < w.tiles; ++tile) {
+        const unsigned word = sh.odd[tile >> 5];
+        if (!word) { tile |= 31; continue; }
+        if (!((word >> (tile & 31)) & 1) || (w.twin && (tile & 1) != s)) continue;
+        const int key0 = (w.tile0 + tile) * CH_TILE;
+        for (int key = key0; key < min(key0 + CH_TILE, w.ctx); ++key) {
             long long row = (long long)w.b * p.c.stride_b + key * p.c.stride_pos;
             if (p.c.paged) {
                 const int page = read_global(p.c.page_table + (long long)w.b * p.c.max_pages + key / TILE);
                 if ((unsigned)page >= (unsigned)p.c.num_pages) continue;
                 row = page * p.c.stride_page + key % TILE * p.c.stride_pos;
             }
-            row = (row + w.g * p.c.stride_head) * ESZ;
-            float k[4], v[4];
-            four(p.c.k + row, k);
-            four(p.c.v + row, v);
-            float t = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
-#pragma unroll
-            for (int sh = 16; sh; sh >>= 1) t += __shfl_xor_sync(0xffffffffu, t, sh);
-            t *= scale;
-            if (t == -INFINITY) continue;
-            const float up = fmaxf(m, t), f = m == up ? 1.f : fast_exp2(m - up), e = fast_exp2(t - up);
-            m = up;
-            l = fmaf(l, f, e);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) o[c] = fmaf(o[c], f, e * v[c]);
-        }
-    }
-}
-
-// All rows of a stream in that way, a quarter per warp: results, or partial results where they are joined.
-template <bool KV8>
-__device__ __forceinline__ void chunk_rows_again(const ChunkParams& p, const ChunkShared& sh, uint32_t base, int rank, int ranks, int g, int s, int quarter, int lane) {
-    ChunkWork w;
-    chunk_work(p, sh, rank, ranks, g, w);
-    const bool joined = ranks > 1 || w.twin;
-    const int G = p.c.G, tt = p.tile_tokens;
-    const float scale = p.scale_log2 * (KV8 && p.k_scale ? read_global(p.k_scale + w.g) : 1.f), vs = KV8 && p.v_scale ? read_global(p.v_scale + w.g) : 1.f;
-    for (int i = 0; i < 32; ++i) {
-        const int r = quarter * 32 + i, token = w.t0 + (w.twin ? 0 : s * tt) + r / G, head = w.g * G + r % G;
-        if (r >= tt * G || token >= w.new_tokens) break;
-        float o[4], m, l;
-        chunk_row_plain<KV8>(p, w, s, token, head, lane, scale, o, m, l);
-        if (joined) {
-            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(base + ((s * CH_TILE + r) * 32 + (lane ^ i)) * 16), "f"(o[0]), "f"(o[1]), "f"(o[2]), "f"(o[3]) : "memory");
-            if (lane == 0) {
-                asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(base + CH_PART_MAX + (s * CH_TILE + r) * 4), "f"(m) : "memory");
-                asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(base + CH_PART_SUM + (s * CH_TILE + r) * 4), "f"(l) : "memory");
+            row += w.g * p.c.stride_head + lane * 4;
+            uint32_t a, b;
+            if constexpr (KV8) {
+                e4m3x4_to_f16x2x2(read_global(reinterpret_cast<const uint32_t*>(p.c.v + row)), a, b);
+                a = f16x2_to_bf16x2(a);
+                b = f16x2_to_bf16x2(b);
+            } else {
+                const uint2 y = read_global(reinterpret_cast<const uint2*>(p.c.v + row * 2));
+                a = y.x; b = y.y;
             }
-            continue;
+            float v[4] = {__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
+            bool any = false;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (isfinite(v[c])) v[c] = 0.f;
+                else any = true;
+            }
+            if (!__any_sync(0xffffffffu, any)) continue;
+            for (int i = 0; i < 32; ++i) {
+                const int r = quarter * 32 + i, token = w.t0 + (w.twin ? 0 : s * tt) + r / G, head = w.g * G + r % G, pos = w.first + token;
+                if (!any || !((lives >> i) & 1) || key >= (p.causal ? min(pos + 1, w.ctx) : w.ctx) || (p.window > 0 && key <= pos - p.window)) continue;
+                const long long at = ((long long)(w.q_row + token - w.t0) * p.c.Hq + head) * HEAD_DIM + lane * 4;
+                if (joined) {
+                    const uint32_t to = base + ((s * CH_TILE + r) * 32 + (lane ^ i)) * 16;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float x;
+                        asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(x) : "r"(to + 4 * c) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(to + 4 * c), "f"(x + v[c]) : "memory");
+                    }
+                } else if (p.out_bf16) {
+                    uint2* const to = reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at);
+                    const uint2 x = read_global(to);
+                    *to = make_uint2(pack_bf16(__uint_as_float(x.x << 16) + v[0], __uint_as_float(x.x & 0xffff0000u) + v[1]),
+                                     pack_bf16(__uint_as_float(x.y << 16) + v[2], __uint_as_float(x.y & 0xffff0000u) + v[3]));
+                } else {
+                    float4* const to = reinterpret_cast<float4*>(p.out + at);
+                    const float4 x = read_global(to);
+                    *to = make_float4(x.x + v[0], x.y + v[1], x.z + v[2], x.w + v[3]);
+                }
+            }
         }
-        const long long at = (long long)(w.q_row + token - w.t0) * p.c.Hq + head;
-        const float inv = l != 0.f ? vs / l : 0.f;
-        if (p.out_bf16) *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at * HEAD_DIM + lane * 4) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-        else *reinterpret_cast<float4*>(p.out + at * HEAD_DIM + lane * 4) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-        if (lane == 0 && p.lse) p.lse[at] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
     }
 }
 
@@ -405,7 +399,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             bar_init(smem_u32(&sh.s_full[i]), 1); bar_init(smem_u32(&sh.p_most[i]), 4); bar_init(smem_u32(&sh.p_full[i]), 4);
             bar_init(smem_u32(&sh.o_done[i]), 1);
         }
-        sh.gave_up = sh.odd[0] = sh.odd[1] = 0;
+        sh.gave_up = sh.any_odd = 0;
+        for (unsigned& x : sh.odd) x = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     pdl_wait();
@@ -502,18 +497,26 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 m = top == top ? top : -INFINITY;
             }
             if (partly) {
-                // A weight of zero times a value that is not finite would spoil rows that do not see it: such tiles are worked out again, without products.
+                // A weight of zero times a value that is not finite would spoil rows that do not see it: such values are left out of the product and
+                // added at the end to the rows that do. (Every stream writes back what it has looked at, since its own product has to find it so; the other
+                // stream, whose rows may all see the tile, meets such a value or zero, and is given it at the end in both cases.)
                 const int item = 2 * tile + 1, slot = item % RING;
                 bar_pass<true>(smem_u32(&sh.full[slot]), (item / RING) & 1, gave_up);
-                bool finite = true;
+                bool odd = false;
                 for (int k = tid & 127; k < min(w.ctx - key0, CH_TILE) * 8; k += 128)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
+                        const uint32_t at = ring + slot * CH_MAT + h * CH_HALF + k * 16;
                         uint32_t v[4];
-                        lds128(ring + slot * CH_MAT + h * CH_HALF + k * 16, v);
-                        finite = finite && all_finite<KV8>(v);
+                        lds128(at, v);
+                        odd |= drop_odd<KV8>(v);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
                     }
-                if (!finite) sh.odd[s] = 1;
+                smem_to_async();
+                if (odd) {
+                    atomicOr(&sh.odd[tile >> 5], 1u << (tile & 31));
+                    sh.any_odd = 1;
+                }
             }
             // Weights by the maximum so far, while this tile's own is looked for: it is raised, and the weights are worked out again, only
             // where that leaves one above 2^8.
@@ -582,13 +585,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         if (n > 0) bar_pass<true>(smem_u32(&sh.o_done[s]), 0, gave_up);
         tmem_fence_after();
         const float vs = KV8 && p.v_scale ? read_global(p.v_scale + w.g) : 1.f;
-        __syncwarp();
-        asm volatile("bar.sync %0, 128;\n" ::"r"(1 + s) : "memory");
-        const bool again = *(volatile int*)&sh.odd[s];
         if (joined && w.stream_tiles[1 - s] > 0) bar_pass<true>(smem_u32(&sh.o_done[1 - s]), 0, gave_up);    // (partial results take the operands' place)
-        if (again) {
-            // (all rows of the stream, further down)
-        } else if (!joined) {
+        if (!joined) {
             const bool some = l != 0.f;                     // (a sum that is not a number is some)
             const float inv = some ? vs / l : 0.f;
             const long long at = ((long long)(w.q_row + token - w.t0) * p.c.Hq + head);
@@ -637,6 +635,9 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 }
             }
         }
+        const unsigned lives = __ballot_sync(0xffffffffu, valid && l != 0.f);
+        asm volatile("bar.sync 1, 256;\n" ::: "memory");    // both streams' results stand, and what they have left out is known
+        if (*(volatile int*)&sh.any_odd) chunk_odd_values<KV8>(p, sh, base, rank, ranks, g, s, warp & 3, lane, lives);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(KV8 ? 48 : 72));
     }
@@ -833,8 +834,6 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
         }
     }
     __syncwarp();
-    if (warp < 8 && *(volatile int*)&sh.odd[warp >> 2]) chunk_rows_again<KV8>(p, sh, base, rank, ranks, g, warp >> 2, warp & 3, lane);
-
     if (joined) {
         // ---- partial results of the streams and of the cluster's CTAs ----
         if (ranks > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();

@@ -943,6 +943,7 @@ EncodeTiled encode_tiled() {
 }
 
 constexpr int64_t TMA_STRIDE_LIMIT = 1LL << 40;
+static_assert(MAX_CTX <= CH_MAX_TILES * CH_TILE, "a bit per tile");
 
 // A tensor map of `rank` dimensions, element strides from the second on; the innermost box is 128 bytes, swizzled.
 bool tensor_map(CUtensorMap* map, bool bytes, const void* base, int rank, const uint64_t* dims, const int64_t* strides, const uint32_t* box) {

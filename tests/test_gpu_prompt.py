@@ -439,6 +439,87 @@ def test_a_value_spoils_only_the_rows_that_see_it(td, bad, fp8, lens, new, at, w
     assert (torch.isnan(got[hit]) if math.isnan(bad) else got[hit] == bad).all()
 
 
+def spoil_values(lay, spots):
+    """Values that are not finite at (sequence, KV head, position, channel): the cache's, and the plain copy's."""
+    for b, g, pos, c, bad in spots:
+        at = (lay.page_table[b, pos // BLK], g, pos % BLK) if lay.paged else (b, g, pos) if lay.stride_head > lay.stride_pos else (b, pos, g)
+        if lay.kv_dtype:
+            lay.v.view(torch.uint8)[at][c] = 0x7F
+        else:
+            lay.v[at][c] = bad
+        lay.dense[b][1][g, pos, c] = math.nan if lay.kv_dtype else bad
+
+
+def check_spoiled(td, lay, new, causal, window, bf16=False):
+    """Against 64 bits: numbers where a row sees finite values only, and what infinities and not-a-numbers add up to where it does not."""
+    q, off = chunk_inputs(lay, new)
+    lse = torch.zeros(q.shape[:2], device=DEV)
+    got = td.chunk_attn(lay, q, off, causal=causal, window=window, lse=lse).double()
+    finite = copy.copy(lay)
+    finite.dense = [(k, torch.where(torch.isfinite(v), v, 0.0)) for k, v in lay.dense]
+    out, ref_lse, _, tol, tol_l, _ = ref_chunk(finite, q, new, causal, window)
+    tol = tol + (2.0 ** -8 * (out.abs() + tol) if bf16 else 0)
+    G, at = lay.num_q_heads // lay.num_kv_heads, 0
+    for b, n in enumerate(new):
+        N = lay.dense[b][0].shape[1]
+        pos, j = N - n + torch.arange(n, device=DEV), torch.arange(N, device=DEV)
+        seen = torch.ones(n, N, dtype=torch.bool, device=DEV)
+        seen &= (j[None] <= pos[:, None]) | (not causal)
+        seen &= (j[None] > pos[:, None] - window) | (not window)
+        for g in range(lay.num_kv_heads):
+            v = lay.dense[b][1][g]
+            up, down, none = ((seen.double() @ x.double() > 0)[:, None].expand(n, G, D) for x in (v == math.inf, v == -math.inf, torch.isnan(v)))
+            o = got[at: at + n, g * G: (g + 1) * G]
+            none, hit = none | (up & down), none | up | down
+            assert torch.equal(torch.isnan(o), none) and (o[up & ~none] == math.inf).all() and (o[down & ~none] == -math.inf).all()
+            err = (o - out[at: at + n, g * G: (g + 1) * G]).abs()
+            assert ((err <= tol[at: at + n, g * G: (g + 1) * G]) | hit).all() and (~hit).any()
+        at += n
+    assert ((lse.double() - ref_lse).abs() <= tol_l).all()
+
+
+@pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 70), (True, 300), (False, 130)])
+@pytest.mark.parametrize("lens,new,hq,hkv", [([700], [500], 8, 2), ([300, 2000], [300, 30], 6, 2), ([900], [250], 3, 3), ([6000], [5], 8, 1), ([400, 260], [64, 130], 16, 2)])
+def test_values_that_are_not_finite(td, td16, layout, fp8, causal, window, lens, new, hq, hkv):
+    """Several of them: in tiles that all rows see, some or none, in both streams' tiles, on either side of a page's and of a tile's end, in one position and in many."""
+    r = torch.Generator().manual_seed(len(lens) + hq + window)
+    pick = lambda n: int(torch.randint(0, n, (1,), generator=r))  # noqa: E731
+    lay = make(lens, hq, hkv, layout, fp8, seed=hq)
+    spots = []
+    for b, n in enumerate(lens):
+        first = n - new[b]
+        for i in range(8):
+            pos = [n - 1, first, min(first + 1, n - 1), pick(n), pick(n), first + pick(new[b]), first + pick(new[b]), max(first - 1, 0)][i]
+            for c in range(1 + pick(3)):
+                spots.append((b, pick(hkv), pos, 8 * i + 64 * (c == 1) + pick(4), [math.nan, math.inf, -math.inf][pick(3)]))
+    spoil_values(lay, spots)
+    check_spoiled(td, lay, new, causal, window)
+    check_spoiled(td16, lay, new, causal, window, bf16=True)
+    assert td.device_status() == binding.OK
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_one_odd_value_does_not_hold_up_a_call(td, fp8):
+    """60000 positions, one not-a-number among the new tokens' values: about as long as without it."""
+    lay = make([60000], 8, 2, "paged", fp8, seed=1)
+    q, off = chunk_inputs(lay, [400])
+
+    def once():
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        td.chunk_attn(lay, q, off)
+        b.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(b)
+
+    once()
+    plain = min(once() for _ in range(5))
+    spoil_values(lay, [(0, 1, 59700, 7, math.inf)])
+    assert min(once() for _ in range(3)) <= 3 * plain + 0.5
+
+
 @pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("causal", [True, False])

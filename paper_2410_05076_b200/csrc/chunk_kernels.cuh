@@ -854,7 +854,8 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             float m = mi;
 #pragma unroll
             for (int sft = 16; sft; sft >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sft));
-            const float f = mi == -INFINITY && li == 0.f ? 0.f : (mi == m || li != li ? 1.f : fast_exp2(mi - m));
+            // (a part with weights counts for something however far it stands below the others: an infinity among its values is still one)
+            const float f = mi == -INFINITY && li == 0.f ? 0.f : (mi == m || li != li ? 1.f : fmaxf(fast_exp2(mi - m), 0x1p-120f));
             float l = f == 0.f ? 0.f : li * f;
 #pragma unroll
             for (int sft = 16; sft; sft >>= 1) l += __shfl_xor_sync(0xffffffffu, l, sft);

@@ -500,6 +500,20 @@ def test_values_that_are_not_finite(td, td16, layout, fp8, causal, window, lens,
     assert td.device_status() == binding.OK
 
 
+@pytest.mark.parametrize("max_new", [0, 1])
+@pytest.mark.parametrize("at,high", [(100, 2900), (2900, 100), (40, 60), (100, 200)])
+def test_an_infinity_far_below_the_largest_logit_is_not_lost(td, at, high, max_new):
+    """A weight of e^-300 times an infinity is an infinity, and in 32 bits not a number; whichever parts of the context the two positions lie in."""
+    lay = make([3000, 3000], 1, 1, "hnd", seed=3)
+    q, off = chunk_inputs(lay, [1, 1])
+    want = td.chunk_attn(lay, q, off, max_new=max_new)
+    lay.k[0, 0, high] = (q[0, 0].float() * (300 * math.sqrt(D) / float((q[0, 0].double() ** 2).sum()))).to(torch.bfloat16)
+    lay.v[0, 0, at, 5] = math.inf
+    got = td.chunk_attn(lay, q, off, max_new=max_new)
+    assert not math.isfinite(float(got[0, 0, 5])) and torch.isfinite(got[0, 0, :5]).all() and torch.isfinite(got[0, 0, 6:]).all()
+    assert float((got[1] - want[1]).abs().max()) <= 2.0 ** -8 * float(lay.dense[1][1].abs().max())
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 def test_one_odd_value_does_not_hold_up_a_call(td, fp8):
     """60000 positions, one not-a-number among the new tokens' values: about as long as without it."""

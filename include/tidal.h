@@ -472,7 +472,8 @@ tidal_status_t tidal_evict_select(tidal_ctx_t *ctx, const tidal_kv_t *kv, const 
  *             that receives the rows (same heads and element type; its ctx_lens is not read), of which no row is one that the lists name.
  *   weights   NULL, or float [batch, num_list_heads, stride] moved along to weights_out [.., stride_out], stride >= kv->max_ctx_len and
  *             stride_out >= min(m, the receiving max_ctx_len); within the cache weights_out may be weights, otherwise not.
- * -1 is skipped, another position outside [0, ctx_lens[b]) skipped and reported as TIDAL_ERR_INDEX, a page id outside the pool likewise.
+ * -1 is skipped, another position outside [0, ctx_lens[b]) skipped and reported as TIDAL_ERR_INDEX, a page id outside the pool likewise, and so are entries
+ * of a list from the receiving max_ctx_len on (within the cache: from ctx_lens[b] on).
  * ctx_lens holds the lengths before; the caller then takes new_lens (tidal_page_map gives the pages back), and key
  * bounds are computed anew. The cache is WRITTEN although the descriptor declares it const. */
 tidal_status_t tidal_kv_gather(tidal_ctx_t *ctx, const tidal_kv_t *kv, const tidal_kv_t *into, const int32_t *kept, const int32_t *counts,

@@ -278,7 +278,8 @@ __global__ void __launch_bounds__(GA_WARPS * 32) gather_copy_kernel(const Gather
     // (the list's entry is asked for together with the lengths that say which of them count)
     const long long row = (long long)b * p.heads + (p.heads > 1 ? g : 0);
     const int pos = j < p.m ? read_global(p.kept + row * p.m + j) : -1;
-    const int cnt = min(gather_count(p, b), p.max_ctx), n = cached_len(c, b);
+    const int all = gather_count(p, b), cnt = min(all, p.max_ctx), n = cached_len(c, b);
+    if (j >= cnt && j < all && pos != -1 && lane < GA_ROWS) atomicOr(c.status, STATUS_BAD_INDEX);        // (no place for it)
     if (j0 >= cnt) return;
     long long src = -1, dst = -1;
     if (j < cnt) {
@@ -344,7 +345,9 @@ __global__ void __launch_bounds__(GI_THREADS) gather_inplace_kernel(const Gather
     const int col = (int)(blockIdx.x % columns);
     const long long pair = blockIdx.x / columns;
     const int b = (int)(pair / c.Hkv), g = (int)(pair - (long long)b * c.Hkv);
-    const int n = cached_len(c, b), cnt = min(gather_count(p, b), n);       // (an ascending list has no more)
+    const int all = gather_count(p, b), n = cached_len(c, b), cnt = min(all, n);       // (an ascending list has no more)
+    if (col == 0)
+        for (int j = cnt + tid; j < all; j += GI_THREADS) gather_source(p, b, g, j, 0);    // (what it has all the same is reported)
     const int byte = col * GI_COLUMN + (tid % (GI_COLUMN / 16)) * 16;
     const bool value = byte >= p.row_bytes;
     uint8_t* const base = (value ? p.v : p.k) + (long long)g * c.stride_head * esz + (value ? byte - p.row_bytes : byte);

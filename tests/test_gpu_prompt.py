@@ -833,6 +833,43 @@ def test_kv_gather_reports_positions_and_pages_outside(td):
     assert td.device_status() == binding.OK
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("heads", [1, 2])
+@pytest.mark.parametrize("layout,room", [("hnd", 30), ("paged", 40), ("nhd", 1)])
+def test_kv_gather_reports_rows_that_find_no_room(td, fp8, heads, layout, room):
+    """Lists longer than the receiving cache: what fits is moved, the rest is reported; -1 entries there are nothing."""
+    lay = make([100, 100], 2, 2, "paged", fp8, seed=2)
+    into = make([room, room], 2, 2, layout, fp8, seed=5, max_len=room)
+    kept = torch.arange(0, 100, 2, dtype=torch.int32, device=DEV).expand(2, heads, 50).contiguous()
+    td.kv_gather(lay, kept, i32([room, 0]), into=into)
+    assert td.device_status() == binding.OK
+    want = [read_rows(into, b, room) for b in range(2)]
+    out = torch.full((2, heads, 50), 5.0, device=DEV)
+    again = make([room, room], 2, 2, layout, fp8, seed=5, max_len=room)
+    td.kv_gather(lay, kept, i32([50, 0]), into=again, weights=torch.ones(2, heads, 100, device=DEV), weights_out=out)
+    assert td.device_status() == binding.ERR_INDEX and td.device_status() == binding.OK
+    for b in range(2):
+        assert all(torch.equal(x, y) for x, y in zip(read_rows(again, b, room), want[b]))
+    assert (out[0, :, :room] == 1).all() and (out[0, :, room:] == 5).all() and (out[1] == 5).all()
+    assert torch.equal(again.keep[0].view(torch.uint8), into.keep[0].view(torch.uint8))
+    kept[:, :, room:] = -1
+    td.kv_gather(lay, kept, i32([50, 50]), into=again)
+    assert td.device_status() == binding.OK
+
+
+def test_kv_gather_in_place_reports_lists_longer_than_their_sequence(td):
+    lay = make([20, 40], 2, 2, "paged", seed=2)
+    kept = torch.full((2, 2, 40), -1, dtype=torch.int32, device=DEV)
+    kept[:, :, :10] = torch.arange(5, 15, device=DEV)
+    td.kv_gather(lay, kept, i32([40, 40]))
+    assert td.device_status() == binding.OK
+    before = lay.keep[0].clone()
+    kept[:] = torch.arange(40, device=DEV)
+    td.kv_gather(lay, kept, i32([40, 40]))
+    assert td.device_status() == binding.ERR_INDEX and td.device_status() == binding.OK
+    assert torch.equal(lay.keep[0].view(torch.int16), before.view(torch.int16))       # (NaN behind the sequences)
+
+
 def test_gather_takes_the_token_selection_lists(td):
     """A cache cut down to the positions that a selection layer keeps per KV head attends as the sparse layer does."""
     lay = make([3000], 8, 2, "hnd", seed=11)

@@ -449,7 +449,7 @@ tidal_status_t tidal_chunk_attn(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t 
  *            positions as if their weight before had been 0 (so nothing need be cleared when a sequence has become shorter and
  *            grows again), and with decay 0 all of them.
  *   last     > 0: only the last so many queries of each chunk count
- * With num_tokens 0 nothing is done. The sum's order does not change from call to call. No scratch memory. */
+ * Offsets and pages as there. With num_tokens 0 nothing is done. The sum's order does not change from call to call. No scratch memory. */
 tidal_status_t tidal_chunk_weights(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t num_tokens, const void *q, int64_t q_stride,
                                    const int32_t *q_offsets, int32_t max_new, int32_t causal, int32_t window, int32_t last,
                                    const float *lse, float decay, float *weights, int64_t stride, int32_t num_weight_heads, void *stream);

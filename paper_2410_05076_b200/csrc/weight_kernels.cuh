@@ -177,6 +177,11 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
         // (Nothing here hangs on how a wait ended: warps meet at named barriers, which know no limit, so all of them take all steps, whatever has run out.)
         const int wg = warp >> 2, pair = wg >> 1, s = wg & 1, row = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        if (blockIdx.x == 0)                                // offsets that are cut are reported
+            for (int b = tid; b < p.c.batch; b += 512) {
+                const int x = read_global(p.q_offsets + b), y = read_global(p.q_offsets + b + 1);
+                if (x < 0 || y < x || y > p.num_tokens) atomicOr(p.c.status, STATUS_BAD_INDEX);
+            }
         int step = 0, tag = 0, turn = 0, item = 0, count = 0;           // the pair's products, tiles with products, own fillings, the pair's joined tiles, tiles of positions
         long long filled = -1;                              // the queries whose sums are in shared memory
         for (; weight_tile(p, w); w.tile += w.step) {

@@ -375,6 +375,30 @@ def test_chunk_offsets_out_of_order_are_cut_and_reported(td):
     assert td.device_status() == binding.OK
 
 
+@pytest.mark.parametrize("heads", [1, 2])
+@pytest.mark.parametrize("off", [[0, 20, 10, 30], [0, 10, 20, 31], [-5, 10, 20, 30], [0, 40, 40, 40], [0, 0, 31, 30]])
+def test_weights_of_offsets_out_of_order_are_cut_and_reported(td, heads, off):
+    lay = make([40, 0, 40], 4, 2, "paged")
+    q, lse = randn(3, 30, 4, D), torch.zeros(30, 4, device=DEV)
+    got = td.chunk_weights(lay, q, i32(off), lse, torch.zeros(3, heads, 40, device=DEV))
+    assert td.device_status() == binding.ERR_INDEX and td.device_status() == binding.OK
+    assert torch.isfinite(got).all()
+    td.chunk_weights(lay, q, i32([0, 10, 20, 30]), lse, got)
+    assert td.device_status() == binding.OK
+
+
+def test_weights_report_the_offsets_of_the_last_of_many_sequences(td):
+    lay = make([1] * 700, 1, 1, "hnd")
+    q, lse = randn(3, 700, 1, D), torch.zeros(700, 1, device=DEV)
+    off = torch.arange(701, dtype=torch.int32, device=DEV)
+    w = torch.zeros(700, 1, 1, device=DEV)
+    td.chunk_weights(lay, q, off, lse, w)
+    assert td.device_status() == binding.OK
+    off[700] = 698
+    td.chunk_weights(lay, q, off, lse, w)
+    assert td.device_status() == binding.ERR_INDEX
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 def test_chunk_bad_pages_are_skipped_and_reported(td, fp8):
     lay = make([400], 4, 2, "paged", fp8, seed=2)

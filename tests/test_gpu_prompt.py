@@ -193,6 +193,52 @@ def test_rope_write(td, layout, fp8, T, hq, hkv, rotary, norm):
     assert all(torch.equal(x.view(torch.uint8), a) for x, a in zip(lay.keep, after))
 
 
+@pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("turn", [HALF, INTER])
+@pytest.mark.parametrize("T,hq,hkv,rotary,norm", [(1, 2, 1, 16, False), (9, 6, 3, 96, True), (200, 8, 2, 128, True), (64, 5, 5, 48, False), (2600, 4, 4, 64, True)])
+def test_rope_write_changes_its_rows_and_no_other_byte(td, layout, fp8, turn, T, hq, hkv, rotary, norm):
+    """Both layouts of the channels into every cache, rows with places all over it; bounds as in test_rope_write."""
+    rows = pages(T + 20) * BLK
+    lay = make([rows], hq, hkv, layout, fp8, seed=T)
+    q, k, v, pos = rope_inputs(T, hq, hkv, 262144, seed=T + 1)
+    qw, kw = (1 + 0.3 * randn(1, D), 1 - 0.3 * randn(2, D)) if norm else (None, None)
+    at = torch.randperm(rows, generator=gen(9), device=DEV)[:T]
+    slots = lay.page_table[0, at // BLK].long() * BLK + at % BLK if layout == "paged" else at
+    slots, pos = slots.clone(), pos.clone()
+    if T > 3:
+        slots[2::7], pos[3::5] = -1, -1
+    written = ((slots >= 0) & (pos >= 0)).nonzero()[:, 0]
+
+    def place(x):
+        a = at[written]
+        x = x.view(torch.uint8 if fp8 else torch.int16)
+        return (x, (lay.page_table[0, a // BLK].long(), slice(None), a % BLK)) if layout == "paged" else (x[0].transpose(0, 1) if layout == "hnd" else x[0], (a,))
+
+    before = [x.clone() for x in lay.keep]
+    (kx, ki), (vx, vi) = place(lay.k), place(lay.v)
+    old = kx[ki].clone(), vx[vi].clone()
+    plan = binding.rope_plan(rotary, base=500000.0, layout=turn)
+    qo = td.rope_write(lay, plan, q, k, v, pos, slots, qw, kw, 1e-6, torch.full((T, hq, D), 7.0, dtype=torch.bfloat16, device=DEV))
+    there = pos >= 0
+    ref = ref_rope(q, pos, frequencies(rotary, 500000.0), 1.0, turn, qw, 1e-6)
+    assert ((qo.double() - ref).abs() <= rope_bound(ref, 262144))[there].all() and (qo[~there] == 7).all()
+    ref = ref_rope(k, pos, frequencies(rotary, 500000.0), 1.0, turn, kw, 1e-6)[written]
+    if fp8:
+        x = ref / lay.k_scale.double()[:, None]
+        got = kx[ki].view(torch.float8_e4m3fn).double()
+        bound = ref_code(x) + 1.1 * (2.0 ** -19 + 2.0 ** -32) * x.abs().amax(-1, keepdim=True)
+        assert ((got - x.clamp(-448, 448)).abs() <= bound).all()
+        want = (v[written].float() / lay.v_scale[:, None]).clamp(-448, 448).to(torch.float8_e4m3fn)
+        assert torch.equal(vx[vi], want.view(torch.uint8))
+    else:
+        assert ((kx[ki].view(torch.bfloat16).double() - ref).abs() <= rope_bound(ref, 262144)).all()
+        assert torch.equal(vx[vi], v[written].contiguous().view(torch.int16))
+    kx[ki], vx[vi] = old
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(lay.keep, before))
+    assert td.device_status() == binding.OK
+
+
 def test_rope_write_equals_rope_and_kv_write(td):
     """16 bits: the same rows as in two calls; slots outside the cache are skipped and reported."""
     one, two = make([64], 8, 2, seed=1), make([64], 8, 2, seed=1)
@@ -571,6 +617,51 @@ def test_single_tokens_of_long_caches(td, layout, fp8, causal, lens, new, hq, hk
         q, off, lse, w, tol = check_chunk(td, lay, new, causal, max_new=1)
     got = td.chunk_weights(lay, q, off, lse, torch.zeros(len(lens), hkv, lay.max_ctx_len, device=DEV), max_new=1, causal=causal)
     assert ((got.double() - w).abs() <= tol).all()
+    assert td.device_status() == binding.OK
+
+
+def close_bound(lay, q, new):
+    """(out in 64 bits, bound per element, two results that are wrong). A weight is off by its logit's and exponential's error (2 e, see ref_chunk) and by its
+    rounding to bf16, 2^-8 (over an 8-bit cache to fp16, 2^-11, or 2^-25 in all where it is small): so much of sum p |v| in its channel. The product's
+    sums are rounded once per 16 positions, each by at most 2^-22 of that."""
+    hq, G, fp8, scale, T = lay.num_q_heads, lay.num_q_heads // lay.num_kv_heads, bool(lay.kv_dtype), lay.sm_scale, sum(new)
+    out, tol, wrong = torch.zeros(T, hq, D, dtype=torch.float64, device=DEV), torch.zeros(T, hq, D, dtype=torch.float64, device=DEV), []
+    swapped, half = torch.zeros_like(out), torch.zeros_like(out)
+    at = 0
+    for b, n in enumerate(new):
+        k, v = lay.dense[b]
+        N = k.shape[1]
+        for h in range(hq if n else 0):
+            kk, vv, qq = k[h // G], v[h // G], q[at: at + n, h].double()
+            t = qq @ kk.t() * scale
+            e = 2.0 ** -19 * (qq.abs() @ kk.abs().t()).amax(-1) * scale + 2.0 ** -22 * t.abs().amax(-1) + 2.0 ** -17 + (2.0 ** -25 * kk.abs().sum(-1).max() * scale if fp8 else 0)
+            p = torch.softmax(t, -1)
+            out[at: at + n, h] = p @ vv
+            tol[at: at + n, h] = (2 * e + 2.0 ** (-11 if fp8 else -8) + N * 2.0 ** -26)[:, None] * (p @ vv.abs()) + (2.0 ** -25 * vv.abs().sum(0) if fp8 else 0) + 2.0 ** -60
+            swapped[at: at + n, h] = p @ vv.roll(16, 0)                 # the next page's values
+            half[at: at + n, h] = torch.softmax(t[:, : (N + 1) // 2], -1) @ vv[: (N + 1) // 2]
+        at += n
+    return out, tol, (torch.zeros_like(out), swapped, half)
+
+
+@pytest.mark.parametrize("layout", ["paged", "hnd", "nhd"])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("scale", [0.088, 0.25])
+@pytest.mark.parametrize("lens,hq,hkv", [([40000], 8, 1), ([20000], 32, 8), ([9000, 20000, 33000], 6, 2), ([1500] * 40, 4, 2)])
+def test_single_tokens_of_long_caches_closely(td, layout, fp8, scale, lens, hq, hkv):
+    """Bounds that results without the values, with other positions' values, or of half the positions miss."""
+    lay = make(lens, hq, hkv, layout, fp8, seed=len(lens) + hq, sm_scale=scale)
+    new = [1] * len(lens)
+    q, off = chunk_inputs(lay, new)
+    out, tol, wrong = close_bound(lay, q, new)
+    for w in wrong:
+        assert float(((w - out).abs() > tol).double().mean()) > 0.5
+    for max_new in (1, 0):
+        got = td.chunk_attn(lay, q, off, max_new=max_new)
+        assert ((got.double() - out).abs() <= tol).all(), (max_new, float(((got.double() - out).abs() / tol).max()))
+    if not fp8:
+        got = td.full_attn(lay, q.contiguous())           # the decode step's
+        assert ((got.double() - out).abs() <= tol).all()
     assert td.device_status() == binding.OK
 
 

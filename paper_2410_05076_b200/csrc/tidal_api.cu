@@ -1800,7 +1800,8 @@ static bool rope_rows_ok(const void* x, int64_t stride, int heads, int32_t num_t
 
 static tidal_status_t run_rope(tidal_ctx_t* ctx, RopeParams& p, int mode, cudaStream_t st) {
     const int pairs = (p.Hq + 1) / 2 + (mode == ROPE_BACK ? 1 : 2) * ((p.Hkv + 1) / 2);
-    // A warp per token where there are tokens enough to fill the GPU; for fewer, several warps with a share of the rows each.
+    // A warp per token where there are tokens enough to fill the GPU; for fewer, several warps with a share of the rows each (32/8 heads, normed; 64 tokens: a
+    // warp each 6.5 us, as many as there are pairs 3.0; 256: 6.6, 5.4, and 4.3 as here; 4096: 16 and 40).
     const long long fill = 16LL * ctx->sm_count;
     p.parts = (int)std::max(1LL, std::min<long long>((pairs + 1) / 2, fill / std::max(p.num_tokens, 1)));
     const long long grid = ((long long)p.num_tokens * p.parts + RO_WARPS - 1) / RO_WARPS;
@@ -1899,10 +1900,11 @@ tidal_status_t tidal_chunk_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t 
     long long tiles = num_tokens / per + std::min(kv->batch, num_tokens);
     if (max_new > 0) tiles = std::min(tiles, kv->batch * ((max_new + per - 1) / per));
     const long long units = tiles * kv->num_kv_heads;
-    // Few rows: the cache is cut over the CTAs of a cluster, as long as all of them run at once and have two tiles of positions each.
+    // Few rows: the cache is cut over the CTAs of a cluster, as long as all of them run at once and there is a tile of positions for each (8 tokens after
+    // 992: 11.9 us, 16.8 with two tiles each, 23.2 uncut; 3 after 127 10.1 and 11.5 uncut; 8 of 16384 40 and 236; 32/8 heads).
     const int seen = window > 0 ? (int)std::min<long long>(kv->max_ctx_len, (long long)window + per) : kv->max_ctx_len;
     int ranks = 1;
-    while (ranks < 16 && units * ranks * 2 <= ctx->sm_count && seen >= ranks * 2 * 2 * CH_TILE && ctx->chunk_clusters[fp8][ranks * 2] >= units) ranks *= 2;
+    while (ranks < 16 && units * ranks * 2 <= ctx->sm_count && seen > ranks * CH_TILE && ctx->chunk_clusters[fp8][ranks * 2] >= units) ranks *= 2;
     if (units * ranks > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
     return fp8 ? launch_maps(ctx, chunk_attn_kernel<true>, (int)(units * ranks), CH_THREADS8, ch_smem<true>(), ranks, (cudaStream_t)stream, p, qm, km, vm)
                : launch_maps(ctx, chunk_attn_kernel<false>, (int)(units * ranks), CH_THREADS, ch_smem<false>(), ranks, (cudaStream_t)stream, p, qm, km, vm);
@@ -1931,6 +1933,9 @@ tidal_status_t tidal_chunk_weights(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32
     p.scale_log2 = (kv->sm_scale > 0.f ? kv->sm_scale : 1.0f / std::sqrt((float)kv->head_dim)) * 1.4426950408889634f;
     const bool fp8 = kv->kv_dtype == TIDAL_KV_FP8_E4M3;
     if (fp8) p.k_scale = kv->k_scale;
+    // New tokens that are a good part of the context see some tiles and not others: every gridDim.x-th tile evens that out (8192 tokens from the first on 731 us,
+    // as runs 973; 4096 of 16384 842 and 889; 8300 of 65536 6763 and 7120). Below that runs, which meet fewer sequences and
+    // queries, are as fast or faster (1024 of 16384 226 us, strided 228; 64 each of four of 16384 54 and 72).
     p.strided = most > p.tile_tokens && 8LL * most > kv->max_ctx_len;
     p.lse = lse; p.decay = decay; p.weights = weights; p.stride = stride; p.heads = num_weight_heads;
     CUtensorMap qm, km;
@@ -1956,10 +1961,11 @@ tidal_status_t tidal_evict_select(tidal_ctx_t* ctx, const tidal_kv_t* kv, const 
     p.weights = weights; p.stride = stride; p.ctx_lens = kv->ctx_lens; p.max_ctx = kv->max_ctx_len; p.heads = num_weight_heads;
     p.m = m; p.keep_first = keep_first; p.keep_last = keep_last; p.kept = kept; p.new_lens = new_lens;
     const int rows = kv->batch * num_weight_heads;
-    // a cluster holds a row; more CTAs than that needs as long as all run at once and have a few thousand keys each
+    // A cluster holds a row; more CTAs than that needs from 12288 positions on, as long as all run at once and have 4096 keys each: two more barriers of a cluster
+    // in every round cost 2 us (8 rows of 8192: one CTA 8.8 us, two 10.4; 13000: 11.7 and, of four, 10.7; 32768: 18.2 and, of eight, 12.5).
     int cluster = 1;
     while ((size_t)((kv->max_ctx_len + cluster - 1) / cluster) * 4 > EV_SMEM_MAX) cluster *= 2;
-    while (cluster < EV_MAX_CLUSTER && kv->max_ctx_len > cluster * 4096 && rows * cluster * 2 <= ctx->sm_count && ctx->evict_clusters[cluster * 2] >= rows) cluster *= 2;
+    while (cluster < EV_MAX_CLUSTER && kv->max_ctx_len > std::max(cluster * 4096, 12288) && rows * cluster * 2 <= ctx->sm_count && ctx->evict_clusters[cluster * 2] >= rows) cluster *= 2;
     const int slice = ((kv->max_ctx_len + cluster - 1) / cluster + 3) / 4 * 4;
     if ((long long)rows * cluster > 0x7fffffffLL) return TIDAL_ERR_UNSUPPORTED;
     return launch_block(ctx, evict_select_kernel, p, rows * cluster, EV_THREADS, (size_t)slice * 4, cluster, (cudaStream_t)stream);

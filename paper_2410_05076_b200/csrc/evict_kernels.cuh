@@ -279,11 +279,10 @@ __global__ void __launch_bounds__(GA_WARPS * 32) gather_copy_kernel(const Gather
     const long long row = (long long)b * p.heads + (p.heads > 1 ? g : 0);
     const int pos = j < p.m ? read_global(p.kept + row * p.m + j) : -1;
     const int all = gather_count(p, b), cnt = min(all, p.max_ctx), n = cached_len(c, b);
-    if (j >= cnt && j < all && pos != -1 && lane < GA_ROWS) atomicOr(c.status, STATUS_BAD_INDEX);        // (no place for it)
-    if (j0 >= cnt) return;
+    if (j0 >= all) return;
     long long src = -1, dst = -1;
-    if (j < cnt) {
-        if ((unsigned)pos >= (unsigned)n) {
+    if (j < all) {
+        if (j >= cnt || (unsigned)pos >= (unsigned)n) {     // (behind cnt there is no place for it)
             if (pos != -1 && lane < GA_ROWS) atomicOr(c.status, STATUS_BAD_INDEX);
         } else {
             if (p.weights && lane < GA_ROWS && (p.heads > 1 || g == 0)) p.weights_out[row * p.wo_stride + j] = read_global(p.weights + row * p.w_stride + pos);

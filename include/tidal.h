@@ -429,8 +429,8 @@ tidal_status_t tidal_rope_write(tidal_ctx_t *ctx, const tidal_rope_t *rope, cons
  * tokens in order, whose keys and values the cache holds already (ctx_lens counts them): row i is the token at position
  * p = ctx_lens[b] - n + i. It sees position j where j < ctx_lens[b], j <= p if causal != 0, and j > p - window if window > 0.
  *   q          device bf16, token t's rows [num_q_heads, 128] contiguous at t * q_stride elements (a multiple of 8; base 16-byte aligned)
- *   q_offsets  device int32 [batch + 1], ascending from 0 to at most num_tokens (tidal_page_map's token_offsets); others are cut to that and
- *              reported as TIDAL_ERR_INDEX. Sequences may bring no token, one, or all they have.
+ *   q_offsets  device int32 [batch + 1], ascending from 0 (or more: rows before the first are left as they were) to at most num_tokens (tidal_page_map's
+ *              token_offsets); others are cut to that and reported as TIDAL_ERR_INDEX. Sequences may bring no token, one, or all they have.
  *   max_new    host upper bound of the new tokens of a sequence (tokens beyond it may be left out); 0: not known
  *   out        [num_tokens, num_q_heads, 128] contiguous, type as set by tidal_set_output_dtype; lse: float [num_tokens, num_q_heads] or NULL,
  *              ln of the sum of exp(scaled logit) over what the row sees. Rows behind q_offsets[batch] are left as they were.

@@ -155,7 +155,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {         // no
 // take them, every other tile each. Long axes are cut over the CTAs of a cluster (and the two streams), whose partial results are joined
 // through shared memory.
 //
-// 4096 tokens at the end of 16384: 817 us, 1175 TFLOP/s, tensor pipe at 64 %; at the end of 131072 under the power limit 7.8 ms, 1110 TFLOP/s. Bound by
+// 4096 tokens at the end of 16384: 814 us, 1180 TFLOP/s, tensor pipe at 65 % (over E4M3 898 us, 57 %); at the end of 131072 under the power limit 7.0 to 7.9 ms. Bound by
 // what lies between products: a stream's scores wait for its weights, the exponential unit (2048 clocks for a pair of tiles, as long as their
 // products) and the issuing warp's turns beside the softmax warps. One warp issues for both streams in turn, which keeps one's softmax beside the
 // other's products; a warp for each lets them fall into step (1090 us).
@@ -556,7 +556,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 return true;
             };
             // (two copies of the same code, one of them for whole tiles alone: the compiler schedules that one better when the masked tiles' paths do
-            // not lead into it, 817 against 844 us, over E4M3 975 against 1074)
+            // not lead into it: 817 against 844 us, over E4M3 975 against 1074, when that was tried)
             const bool whole = !(ragged || partly || bad);
             while (!(whole ? weights(std::true_type()) : weights(std::false_type()))) {
                 const float up = fmaxf(m, top), f = m == up ? 1.f : fast_exp2((m - up) * scale);

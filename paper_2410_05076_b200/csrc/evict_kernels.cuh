@@ -13,7 +13,7 @@ namespace tidal {
 // bins over all CTAs and hands the sums to all, so that each finds the bin for itself. Then each CTA counts what it
 // keeps and writes it behind what the CTAs before it keep, in ascending order; of equal weights the lower positions.
 // Bound by that chain of barriers and by the instructions of three counts, not by its 4 bytes a position: 8 rows of 131072 16.7 us in clusters of
-// eight (clusters of sixteen do not all find room at once: half as long again on some GPUs), 64 rows of up to 65536 20.9 us in clusters of two.
+// eight (clusters of sixteen do not all find room at once: half as long again on some GPUs), 64 rows of up to 65536 21 us in clusters of two.
 struct EvictParams {
     const float* weights;                                   // [batch][heads][stride]
     long long stride;
@@ -315,8 +315,9 @@ __global__ void __launch_bounds__(GA_WARPS * 32) gather_copy_kernel(const Gather
 
 // Within a cache: the j-th listed position is never below j (the list is ascending), so a row may be written once all rows up to it
 // have been read. A CTA takes a column of 32 bytes of all rows of a sequence and KV head, so that this order is its own affair: it reads
-// GI_ROWS rows, waits for its threads, writes them. The last CTAs move the weights in the same way. 64 sequences of up to 2064 positions of eight heads that
-// lose 16 each: 71 us.
+// GI_ROWS rows, waits for its threads, writes them. The last CTAs move the weights in the same way. 64 sequences of eight heads that lose 1 to 16 of about 2056
+// positions, one list for all heads: 276 us for 461 MB that move (both ways 3.3 TB/s), over E4M3 144 us; where one of the 64 loses any, 77 us, of
+// which reading every list once per column is most.
 constexpr int GI_THREADS = 512, GI_COLUMN = 32, GI_UNROLL = 4;
 constexpr int GI_ROWS = GI_THREADS / (GI_COLUMN / 16) * GI_UNROLL;
 

@@ -1901,7 +1901,7 @@ tidal_status_t tidal_chunk_attn(tidal_ctx_t* ctx, const tidal_kv_t* kv, int32_t 
     if (max_new > 0) tiles = std::min(tiles, kv->batch * ((max_new + per - 1) / per));
     const long long units = tiles * kv->num_kv_heads;
     // Few rows: the cache is cut over the CTAs of a cluster, as long as all of them run at once and there is a tile of positions for each (8 tokens after
-    // 992: 11.9 us, 16.8 with two tiles each, 23.2 uncut; 3 after 127 10.1 and 11.5 uncut; 8 of 16384 40 and 236; 32/8 heads).
+    // 992: 11.9 us, 16.8 with two tiles each, 23.2 uncut; 3 after 127 10.2 and 11.0 uncut; 8 of 16384 40 and 236; 32/8 heads).
     const int seen = window > 0 ? (int)std::min<long long>(kv->max_ctx_len, (long long)window + per) : kv->max_ctx_len;
     int ranks = 1;
     while (ranks < 16 && units * ranks * 2 <= ctx->sm_count && seen > ranks * CH_TILE && ctx->chunk_clusters[fp8][ranks * 2] >= units) ranks *= 2;

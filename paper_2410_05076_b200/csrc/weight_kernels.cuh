@@ -6,8 +6,8 @@
 // owns a position and adds up along its row in registers; no atomics, the same sum in the same order every time. Keys are
 // read once. Two pairs of warpgroups take the tiles in turn, a pair's warpgroups its products (an accumulator in TMEM each), so that the
 // exponentials of four run beside the products and loads of the next. Single tokens (64 sequences of up to 16384 in
-// pages: 212 us, 5.1 TB/s) are bound by the copies of 16 rows of 128 bytes, of which an SM takes 27 bytes a clock, and by the issuing warp's turns; many
-// queries (64 of 131072: 94 us) by the exponential unit, 16 a clock and SM.
+// pages: 207 us, 5.3 TB/s) are bound by the copies of 16 rows of 128 bytes, of which an SM takes 27 bytes a clock, and by the issuing warp's turns; many
+// queries (64 of 131072: 92 us) by the exponential unit, 16 a clock and SM.
 #pragma once
 
 #include "chunk_kernels.cuh"

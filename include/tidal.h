@@ -435,7 +435,7 @@ tidal_status_t tidal_rope_write(tidal_ctx_t *ctx, const tidal_rope_t *rope, cons
  *   out        [num_tokens, num_q_heads, 128] contiguous, type as set by tidal_set_output_dtype; lse: float [num_tokens, num_q_heads] or NULL,
  *              ln of the sum of exp(scaled logit) over what the row sees. Rows behind q_offsets[batch] are left as they were.
  * A row that sees nothing (or nothing but pages that are skipped) gets zeros and -infinity. What lies behind a sequence in its last page or row block may be anything. Pages whose
- * id is outside the pool are skipped and reported; a value that is not finite reaches the rows that see it and no other. k_scale must be positive. Softmax weights enter the product with V as
+ * id is outside the pool are skipped and reported (not those that lie before the first new token's window whole, which may be gone); a value that is not finite reaches the rows that see it and no other. k_scale must be positive. Softmax weights enter the product with V as
  * bf16 (FP8 caches: fp16, and the query as fp16 too); maxima, sums and outputs are fp32. Scratch memory is of one size and
  * allocated with the context. */
 tidal_status_t tidal_chunk_attn(tidal_ctx_t *ctx, const tidal_kv_t *kv, int32_t num_tokens, const void *q, int64_t q_stride,

@@ -766,7 +766,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
                 for (int h = 0; h < 2; ++h)
                     tma_load3(q_smem + s * CH_MAT + h * CH_HALF, &q_map, smem_u32(&sh.q_full), h * 64, w.g * G, w.q_row + s * tt);
         }
-        const int hcoord = w.g * p.head_mul;
+        const int hcoord = w.g * p.head_mul, lo = p.window > 0 ? max(w.first + w.t0 - p.window + 1, 0) : 0;     // (pages before the first row's window are nobody's)
         for (int tile = 0; tile < w.tiles; ++tile) {
             const int key0 = (w.tile0 + tile) * CH_TILE;
             int page = 0;
@@ -774,7 +774,7 @@ chunk_attn_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__
             if (p.c.paged) {
                 page = p.c.num_pages;                       // (out of range: filled with zeros)
                 const int blk = key0 / TILE + (lane & 7);
-                if (blk * TILE < w.ctx) {
+                if (blk * TILE < w.ctx && blk * TILE + TILE > lo) {
                     page = read_global(p.c.page_table + (long long)w.b * p.c.max_pages + blk);
                     if ((unsigned)page >= (unsigned)p.c.num_pages) { page = p.c.num_pages; bad = 1; }
                 }

@@ -6,7 +6,7 @@
 // owns a position and adds up along its row in registers; no atomics, the same sum in the same order every time. Keys are
 // read once. Two pairs of warpgroups take the tiles in turn, a pair's warpgroups its products (an accumulator in TMEM each), so that the
 // exponentials of four run beside the products and loads of the next. Single tokens (64 sequences of up to 16384 in
-// pages: 207 us, 5.3 TB/s) are bound by the copies of 16 rows of 128 bytes, of which an SM takes 27 bytes a clock, and by the issuing warp's turns; many
+// pages: 209 us, 5.2 TB/s) are bound by the copies of 16 rows of 128 bytes, of which an SM takes 27 bytes a clock, and by the issuing warp's turns; many
 // queries (64 of 131072: 92 us) by the exponential unit, 16 a clock and SM.
 #pragma once
 
@@ -343,7 +343,10 @@ chunk_weights_kernel(const __grid_constant__ WeightParams p, const __grid_consta
         while (more && ok) {
             const int b = w.b, key0 = w.key0, g0 = w.g0, g1 = w.q0 < w.q1 ? w.g1 : w.g0, here = page;
             const unsigned skip = __ballot_sync(0xffffffffu, bad) & 0xffu;
-            if (skip && lane == 0) atomicOr(p.c.status, STATUS_BAD_PAGE);
+            if (skip && g1 > g0) {                          // pages before the first query's window are nobody's
+                const int before = p.window > 0 ? min(max((w.first + w.t0 - p.window + 1 - key0) / TILE, 0), 8) : 0;
+                if (lane == 0 && skip >> before) atomicOr(p.c.status, STATUS_BAD_PAGE);
+            }
             w.tile += w.step;
             more = weight_tile(p, w);
             if (more) page = lookup(bad);

@@ -479,6 +479,32 @@ def test_weights_of_all_heads_together_next_to_bad_pages(td, fp8, hq, hkv, new, 
     assert td.device_status() == binding.ERR_INDEX
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens,new,window,last", [([3000], [50], 200, 0), ([3000, 700, 90], [300, 1, 0], 33, 0), ([5000], [1], 1000, 0), ([900], [250], 17, 20), ([130], [1], 2, 0)])
+def test_pages_that_no_window_reaches_are_nobodys(td, fp8, causal, lens, new, window, last):
+    """Pages before the first new token's window, and those of a sequence without new tokens, may be gone; the first that is seen may not."""
+    lay = make(lens, 8, 2, "paged", fp8, seed=6)
+    q, off = chunk_inputs(lay, new)
+    lse = [torch.zeros(q.shape[:2], device=DEV) for _ in range(2)]
+    old = torch.rand(len(lens), 2, max(lens), generator=gen(1), device=DEV)
+    first = [max(n - t - window + 1, 0) // BLK for n, t in zip(lens, new)]
+    outs = []
+    for i in range(2):
+        outs.append((td.chunk_attn(lay, q, off, causal=causal, window=window, lse=lse[i]), lse[i],
+                     td.chunk_weights(lay, q, off, lse[i], old.clone(), decay=0.5, causal=causal, window=window, last=last)))
+        assert td.device_status() == binding.OK
+        for b, t in enumerate(new):
+            lay.page_table[b, : first[b] if t else pages(lens[b])] = -1
+    assert all(torch.equal(x, y) for x, y in zip(*outs))
+    lay.page_table[0, first[0]] = lay.num_pages
+    td.chunk_attn(lay, q, off, causal=causal, window=window)
+    assert td.device_status() == binding.ERR_INDEX
+    if not last:
+        td.chunk_weights(lay, q, off, lse[0], old.clone(), causal=causal, window=window)
+        assert td.device_status() == binding.ERR_INDEX
+
+
 def test_chunk_attention_over_infinite_and_missing_numbers(td):
     """A logit that is not a number, or a value, spoils the rows that see it."""
     lay = make([260], 2, 1, "hnd", seed=7)
